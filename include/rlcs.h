@@ -337,6 +337,103 @@ rlcs_status rlcs_elig_trace_vec(const void* x, const uint8_t* term, const uint8_
  * steps (rounded up); 0 for negative sizes or a size that overflows. */
 size_t rlcs_workspace_size_columns(int64_t columns, int64_t T);
 
+/* ---------------------------------------------------------------------------------------
+ * Around a group rollout: attention over a shared prompt, the sampling of the next token, and the
+ * policy loss of the tokens with its gradient. The conventions above hold (device pointers, dtype,
+ * checks on the host, streams, errors); rows of logits may lie a stride apart, and a size of 0 is a
+ * no-op.                                                                                   */
+
+/* Log-probability of the taken token and entropy of the policy, for M rows of V logits:
+ *   y = x / temperature,  logp = y_a - log sum_j e^{y_j},  ent = -sum_j p_j log p_j.
+ *   logits   [M, V] dtype, row m at m * ld (ld >= V); -inf masks an entry (p = 0). A row whose
+ *            logits are all -inf has logp = -inf and ent = 0
+ *   tokens   [M] int32. A token outside [0, V) leaves its row out: logp = ent = 0, no logit read
+ *   logp     [M] float32 out;  ent  [M] float32 out, optional
+ * temperature > 0, finite. Sums are float32, over at most 2^30 logits a row.               */
+rlcs_status rlcs_token_logp(const void* logits, const int32_t* tokens, float* logp, float* ent,
+                            int64_t M, int64_t V, int64_t ld, float temperature, rlcs_dtype dtype,
+                            rlcs_stream_t stream);
+
+/* The clipped policy loss of each token and its gradient by the logits. With logp and ent as above,
+ * rho = exp(logp - logp_old):
+ *   loss = weight * (-min(rho * adv, clamp(rho, 1 - clip_low, 1 + clip_high) * adv) - ent_coef * ent)
+ *   dlogits_j = 1/temperature * [g (1{j = a} - p_j) + weight * ent_coef * p_j (log p_j + ent)],
+ *   g = -weight * adv * rho where rho * adv <= the clamped product, else 0.
+ *   logp_old, adv  [M] float32, e.g. the sampling's logp and an estimator's advantages
+ *   weight   [M] float32, optional (NULL = 1): mask and normalisation of the mean. A row of weight 0
+ *            (or a token outside [0, V)) is left out: none of its inputs is read, loss, logp,
+ *            ent and its gradient are 0
+ *   loss     [M] float32 out;  logp, ent  [M] float32 out, optional
+ *   dlogits  [M, V] dtype out, optional, row m at m * ld_grad; may be `logits` itself (then
+ *            ld_grad = ld)
+ * clip_low in [0, 1], clip_high >= 0 (+infinity allowed), ent_coef finite.                  */
+rlcs_status rlcs_policy_loss(const void* logits, const int32_t* tokens, const float* logp_old,
+                             const float* adv, const float* weight, float* loss, void* dlogits,
+                             float* logp, float* ent, int64_t M, int64_t V, int64_t ld,
+                             int64_t ld_grad, float clip_low, float clip_high, float ent_coef,
+                             float temperature, rlcs_dtype dtype, rlcs_stream_t stream);
+
+/* One token per row, drawn from softmax(logits / temperature) cut down by, in this order,
+ *   top_k    the k largest logits (0 or less, or >= V: all),
+ *   top_p    of these, renormalised, the largest ones while the mass before them is < p (p >= 1:
+ *            all; the largest is always kept),
+ *   min_p    of these, the ones of at least min_p times the largest one's probability,
+ * equal logits in the order of their index. The draw is a race: the kept token of the largest
+ * y_j - log(noise_j), the lowest index among equal ones, which has the distribution above if the
+ * noise is exponential (rate 1) and independent.
+ *   logits   [M, V] dtype, row m at m * ld; -inf masks an entry; NaN counts as -inf
+ *   noise    [M, V] float32, row m at m * ld_noise, positive and finite, read at kept tokens only;
+ *            NULL = the largest logit
+ *   temperature, top_k, top_p, min_p  [M] of each row's own, or NULL: `all_...` for every row.
+ *            Temperature 0 (or less) takes the largest logit, with logp = 0.
+ *   tokens   [M] int32 out;  logp  [M] float32 out, optional: log-probability of the token under
+ *            the distribution it was drawn from. A row of masked logits only: token -1, logp -inf
+ *   ws       optional: rlcs_workspace_size_sample(M, V) bytes, 16-byte aligned, need not be cleared.
+ *            Calls of few rows and no filters use it to split a row over several workgroups.
+ * V <= 2^24. Masses of the filters are sums of multiples of 2^-38 of the largest weight, so the result
+ * does not depend on the order of addition.                                                  */
+rlcs_status rlcs_sample(const void* logits, const float* noise, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p,
+                        int32_t* tokens, float* logp, int64_t M, int64_t V, int64_t ld,
+                        int64_t ld_noise, float all_temperature, int32_t all_top_k,
+                        float all_top_p, float all_min_p, rlcs_dtype dtype, void* ws,
+                        size_t ws_bytes, rlcs_stream_t stream);
+size_t rlcs_workspace_size_sample(int64_t M, int64_t V);
+
+/* Attention of single-token queries over a prefix that a group shares and a suffix of their own: N
+ * groups (prompts) of G sequences (completions), Hq query heads on Hkv key heads (Hq a multiple
+ * of Hkv; query head h reads key head h / (Hq / Hkv)):
+ *   s_j = scale * q . k_j,  o = sum_j e^{s_j - m} v_j / sum_j e^{s_j - m},  lse = log sum_j e^{s_j}
+ * over the first prefix_len[n] keys of the group's prefix and the first suffix_len[n, g] of the
+ * sequence's suffix; without any key o = 0 and lse = -inf. The prefix is read once for the whole
+ * group.
+ *   q        [N, G, Hq, D] dtype;  o  [N, G, Hq, D] dtype out, contiguous
+ *   kp, vp   [N, P, Hkv, D] dtype;  ks, vs  [N, G, S, Hkv, D] dtype (NULL only if P, S is 0)
+ *   prefix_len [N], suffix_len [N, G] int32, optional (NULL = P, S): clamped to [0, P], [0, S].
+ *            Keys and values past the lengths may hold anything, NaN included
+ *   lse      [N, G, Hq] float32 out, optional
+ *   layout   strides in elements, NULL = contiguous. D is contiguous; strides are >= 0 and multiples
+ *            of 16 bytes, as are q, kp, vp, ks, vs and o
+ *   ws       rlcs_workspace_size_attn(...) bytes, 16-byte aligned, need not be cleared
+ * D a multiple of 8 up to 256; P and S up to 2^30. Scores, sums and the output's accumulator are
+ * float32; bfloat16 weights e^{s - m} are rounded to bfloat16 for the product with V.         */
+typedef struct {
+    int64_t q[3];  /* group, sequence, head */
+    int64_t kp[3]; /* group, token, head */
+    int64_t vp[3];
+    int64_t ks[4]; /* group, sequence, token, head */
+    int64_t vs[4];
+} rlcs_attn_layout;
+rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* vp, const void* ks,
+                                    const void* vs, const int32_t* prefix_len,
+                                    const int32_t* suffix_len, void* o, float* lse, int64_t N,
+                                    int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P,
+                                    int64_t S, const rlcs_attn_layout* layout, float scale,
+                                    rlcs_dtype dtype, void* ws, size_t ws_bytes,
+                                    rlcs_stream_t stream);
+size_t rlcs_workspace_size_attn(int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P,
+                                int64_t S);
+
 /* Static description of a status code. Never NULL. */
 const char* rlcs_status_string(rlcs_status status);
 

@@ -32,6 +32,8 @@ __all__ = [
     "rlcs_elig_trace_vec",
     "rlcs_workspace_size_columns", "make_workspace_columns", "rlcs_gae_masked",
     "rlcs_workspace_size_masked", "rlcs_gae_masked_noalloc",
+    "rlcs_token_logp", "rlcs_policy_loss", "rlcs_sample", "rlcs_workspace_size_sample",
+    "rlcs_shared_prefix_attn", "rlcs_workspace_size_attn",
 ]
 
 _fast = None  # the native functions, once loaded
@@ -643,3 +645,223 @@ def rlcs_gae_masked_noalloc(r, v, mask=None, term=None, trunc=None, bv=None, boo
               _ptr(bv), _ptr(boot), _ptr(adv), _ptr(ret), N, T, gamma, lam, 1 if normalize else 0,
               eps, _DTYPES[dt], _stream(dev))
     return adv, ret
+
+
+# ---------------------------------------------------------------- rows of logits
+# logits are [..., V] float32 / bfloat16: [M, V] with rows any stride apart, or contiguous with more
+# leading dimensions (an [N, T, V] batch). Everything per token has the leading shape.
+
+def _prep_logits(x):
+    if not isinstance(x, torch.Tensor) or x.dim() < 2:
+        raise ValueError("logits must be a [..., V] tensor of at least two dimensions")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"logits must be float32 or bfloat16, got {x.dtype}")
+    if x.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    return _rows("logits", x) + (tuple(x.shape[:-1]), x.dtype, x.device)
+
+
+def _rows(name, x):
+    """(M, V, ld) of a [..., V] tensor as rows of V elements, ld apart."""
+    V = int(x.shape[-1])
+    M = 1
+    for n in x.shape[:-1]:
+        M *= int(n)
+    if x.is_contiguous():
+        return M, V, V
+    ld = int(x.stride(0)) if M > 1 else V
+    if x.dim() != 2 or (V > 1 and x.stride(1) != 1) or ld < V:
+        raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows that do not overlap")
+    return M, V, ld
+
+
+def _check_lead(name, t, lead, dtype, device):
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if tuple(t.shape) != lead:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {lead}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on {device}")
+    return t
+
+
+def _out_lead(name, t, lead, dtype, device, want=True):
+    if t is None:
+        return torch.empty(lead, dtype=dtype, device=device) if want else None
+    return _check_lead(name, t, lead, dtype, device)
+
+
+def _required(**tensors):
+    for name, t in tensors.items():
+        if t is None:
+            raise TypeError(f"{name} must be a torch.Tensor")
+
+
+def rlcs_token_logp(logits, tokens, logp=None, ent=None, *, temperature: float = 1.0, want_ent: bool = True):
+    """(logp, ent): log-probability of each taken token and entropy of its policy,
+    softmax(logits / temperature). tokens int32; one outside [0, V) leaves its row out (0, 0)."""
+    done = (_fast or _load_fast()).token_logp(logits, tokens, logp, ent, temperature, want_ent)
+    if done is not NotImplemented:
+        return done
+    M, V, ld, lead, dt, dev = _prep_logits(logits)
+    _required(tokens=tokens)
+    _check_lead("tokens", tokens, lead, torch.int32, dev)
+    logp = _out_lead("logp", logp, lead, torch.float32, dev)
+    ent = _out_lead("ent", ent, lead, torch.float32, dev, want_ent)
+    with _on(dev):
+        _call("rlcs_token_logp", _ptr(logits), _ptr(tokens), _ptr(logp), _ptr(ent), M, V, ld, temperature,
+              _DTYPES[dt], _stream(dev))
+    return logp, ent
+
+
+def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlogits=None, logp=None, ent=None, *,
+                     clip_low: float, clip_high: float, ent_coef: float = 0.0, temperature: float = 1.0,
+                     want_grad: bool = True):
+    """(loss, dlogits, logp, ent): the clipped policy loss of each token with its weight, and the
+    gradient of their sum by the logits. logp_old, adv, weight are float32 of the leading shape; a
+    token of weight 0, or outside [0, V), is left out (all its outputs 0). `dlogits` may be `logits`."""
+    done = (_fast or _load_fast()).policy_loss(logits, tokens, logp_old, adv, weight, loss, dlogits, logp, ent,
+                                               clip_low, clip_high, ent_coef, temperature, want_grad)
+    if done is not NotImplemented:
+        return done
+    M, V, ld, lead, dt, dev = _prep_logits(logits)
+    _required(tokens=tokens, logp_old=logp_old, adv=adv)
+    _check_lead("tokens", tokens, lead, torch.int32, dev)
+    for name, t in (("logp_old", logp_old), ("adv", adv), ("weight", weight)):
+        _check_lead(name, t, lead, torch.float32, dev)
+    loss = _out_lead("loss", loss, lead, torch.float32, dev)
+    logp = _out_lead("logp", logp, lead, torch.float32, dev)
+    ent = _out_lead("ent", ent, lead, torch.float32, dev)
+    ldg = V
+    if dlogits is not None:
+        if not isinstance(dlogits, torch.Tensor) or dlogits.dtype != dt or dlogits.device != dev \
+                or tuple(dlogits.shape) != tuple(logits.shape):
+            raise ValueError(f"dlogits must be a {dt} tensor of the logits' shape on {dev}")
+        ldg = _rows("dlogits", dlogits)[2]
+    elif want_grad:
+        dlogits = torch.empty(lead + (V,), dtype=dt, device=dev)
+    with _on(dev):
+        _call("rlcs_policy_loss", _ptr(logits), _ptr(tokens), _ptr(logp_old), _ptr(adv), _ptr(weight), _ptr(loss),
+              _ptr(dlogits), _ptr(logp), _ptr(ent), M, V, ld, ldg, clip_low, clip_high, ent_coef, temperature,
+              _DTYPES[dt], _stream(dev))
+    return loss, dlogits, logp, ent
+
+
+def rlcs_workspace_size_sample(M: int, V: int) -> int:
+    return int(_native.load().rlcs_workspace_size_sample(int(M), int(V)))
+
+
+def _setting(name, value, lead, dtype, device):
+    """A sampling parameter as (pointer to each row's own, the value for all rows)."""
+    if isinstance(value, torch.Tensor):
+        return _check_lead(name, value, lead, dtype, device).data_ptr(), 0
+    return None, value
+
+
+def rlcs_sample(logits, noise=None, tokens=None, logp=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                want_logp: bool = True, ws=None):
+    """(tokens, logp): one token per row from softmax(logits / temperature) after top-k, top-p and
+    min-p, and its log-probability there. `noise`: float32 of the logits' shape, exponential numbers
+    (``torch.empty_like(...).exponential_()``); without it the most likely token. Each setting is a
+    number, or a tensor of the leading shape (float32; top_k int32)."""
+    done = (_fast or _load_fast()).sample(logits, noise, tokens, logp, temperature, top_k, top_p, min_p, want_logp, ws)
+    if done is not NotImplemented:
+        return done
+    M, V, ld, lead, dt, dev = _prep_logits(logits)
+    ldn = V
+    if noise is not None:
+        if not isinstance(noise, torch.Tensor) or noise.dtype != torch.float32 or noise.device != dev \
+                or tuple(noise.shape) != tuple(logits.shape):
+            raise ValueError(f"noise must be a float32 tensor of the logits' shape on {dev}")
+        ldn = _rows("noise", noise)[2]
+    tp, t = _setting("temperature", temperature, lead, torch.float32, dev)
+    kp, k = _setting("top_k", top_k, lead, torch.int32, dev)
+    pp, p = _setting("top_p", top_p, lead, torch.float32, dev)
+    mp, m = _setting("min_p", min_p, lead, torch.float32, dev)
+    k = max(-1, min(int(k), 2 ** 31 - 1))
+    tokens = _out_lead("tokens", tokens, lead, torch.int32, dev)
+    logp = _out_lead("logp", logp, lead, torch.float32, dev, want_logp)
+    if ws is None:
+        n = rlcs_workspace_size_sample(M, V)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    with _on(dev):
+        _call("rlcs_sample", _ptr(logits), _ptr(noise), tp, kp, pp, mp, _ptr(tokens), _ptr(logp), M, V, ld, ldn, t, k,
+              p, m, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+    return tokens, logp
+
+
+# ---------------------------------------------------------------- attention over a shared prefix
+
+def rlcs_workspace_size_attn(N: int, G: int, Hq: int, Hkv: int, D: int, P: int, S: int) -> int:
+    return int(_native.load().rlcs_workspace_size_attn(*(int(x) for x in (N, G, Hq, Hkv, D, P, S))))
+
+
+def _attn_operand(name, t, dims, dtype, device):
+    if not isinstance(t, torch.Tensor) or t.dim() != dims:
+        raise ValueError(f"{name} must be a {dims}-D tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype} like q")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _attn_strides(t):
+    # (the stride of a dimension of one element is never multiplied by anything but 0)
+    return [0 if n <= 1 else int(s) for n, s in zip(t.shape[:-1], t.stride()[:-1])]
+
+
+def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix_len=None, o=None, lse=None, *,
+                            scale: Optional[float] = None, ws=None, want_lse: bool = True):
+    """(o, lse): attention of one query token per sequence over its group's prefix and its own suffix.
+
+    q [N, G, Hq, D]; kp, vp [N, P, Hkv, D], shared by the G sequences of a group; ks, vs
+    [N, G, S, Hkv, D]. Any strides with D contiguous. prefix_len [N], suffix_len [N, G] int32: how many
+    keys of each count (default all). scale defaults to 1 / sqrt(D). o [N, G, Hq, D] of q's type,
+    lse float32 [N, G, Hq]."""
+    done = (_fast or _load_fast()).shared_prefix_attn(q, kp, vp, ks, vs, prefix_len, suffix_len, o, lse, scale,
+                                                      want_lse, ws)
+    if done is not NotImplemented:
+        return done
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a [N, G, Hq, D] tensor")
+    if q.dtype not in _DTYPES:
+        raise TypeError(f"q must be float32 or bfloat16, got {q.dtype}")
+    if q.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    N, G, Hq, D = (int(x) for x in q.shape)
+    dt, dev = q.dtype, q.device
+    _attn_operand("q", q, 4, dt, dev)
+    _attn_operand("kp", kp, 4, dt, dev); _attn_operand("vp", vp, 4, dt, dev)
+    P, Hkv = int(kp.shape[1]), int(kp.shape[2])
+    if tuple(kp.shape) != (N, P, Hkv, D) or tuple(vp.shape) != (N, P, Hkv, D):
+        raise ValueError(f"kp and vp have shapes {tuple(kp.shape)} and {tuple(vp.shape)}, expected [N, P, Hkv, D]")
+    if (ks is None) != (vs is None):
+        raise ValueError("ks and vs go together")
+    S = 0
+    if ks is not None:
+        _attn_operand("ks", ks, 5, dt, dev); _attn_operand("vs", vs, 5, dt, dev)
+        S = int(ks.shape[2])
+        if tuple(ks.shape) != (N, G, S, Hkv, D) or tuple(vs.shape) != (N, G, S, Hkv, D):
+            raise ValueError(f"ks and vs have shapes {tuple(ks.shape)} and {tuple(vs.shape)}, expected [N, G, S, Hkv, D]")
+    _check_lead("prefix_len", prefix_len, (N,), torch.int32, dev)
+    _check_lead("suffix_len", suffix_len, (N, G), torch.int32, dev)
+    o = _out_lead("o", o, (N, G, Hq, D), dt, dev)
+    lse = _out_lead("lse", lse, (N, G, Hq), torch.float32, dev, want_lse)
+    if ws is None:
+        n = rlcs_workspace_size_attn(N, G, Hq, Hkv, D, P, S)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    at = _native.AttnLayout()
+    for name, t in (("q", q), ("kp", kp), ("vp", vp), ("ks", ks), ("vs", vs)):
+        for i, x in enumerate(_attn_strides(t) if t is not None else ()):
+            getattr(at, name)[i] = x
+    with _on(dev):
+        _call("rlcs_shared_prefix_attn", _ptr(q), _ptr(kp), _ptr(vp), _ptr(ks), _ptr(vs), _ptr(prefix_len),
+              _ptr(suffix_len), _ptr(o), _ptr(lse), N, G, Hq, Hkv, D, P, S, _native.ctypes.addressof(at),
+              1.0 / D ** 0.5 if scale is None and D else scale or 0.0, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+    return o, lse

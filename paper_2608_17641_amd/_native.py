@@ -30,6 +30,13 @@ _I64 = ctypes.c_int64
 _F = ctypes.c_float
 _INT = ctypes.c_int
 _SZ = ctypes.c_size_t
+_I32 = ctypes.c_int32
+
+
+class AttnLayout(ctypes.Structure):
+    """rlcs_attn_layout: strides in elements."""
+    _fields_ = [("q", _I64 * 3), ("kp", _I64 * 3), ("vp", _I64 * 3), ("ks", _I64 * 4), ("vs", _I64 * 4)]
+
 
 # name -> argtypes, in the order of include/rlcs.h
 PROTOTYPES = {
@@ -65,13 +72,23 @@ PROTOTYPES = {
     "rlcs_workspace_size_masked": [_I64, _I64],
     "rlcs_gae_masked_noalloc": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _F, _F, _INT, _F,
                                 _INT, _P],
+    "rlcs_token_logp": [_P, _P, _P, _P, _I64, _I64, _I64, _F, _INT, _P],
+    "rlcs_policy_loss": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _F, _F, _F, _F,
+                         _INT, _P],
+    "rlcs_sample": [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _F, _I32, _F, _F, _INT,
+                    _P, _SZ, _P],
+    "rlcs_workspace_size_sample": [_I64, _I64],
+    "rlcs_shared_prefix_attn": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64,
+                                _I64, _P, _F, _INT, _P, _SZ, _P],
+    "rlcs_workspace_size_attn": [_I64, _I64, _I64, _I64, _I64, _I64, _I64],
     "rlcs_status_string": [_INT],
     "rlcs_version": [],
     "rlcs_testing_set_variant": [_INT],
     "rlcs_testing_set_whitening_wait": [_INT],
 }
 RESTYPES = {"rlcs_workspace_size": _SZ, "rlcs_workspace_size_columns": _SZ,
-            "rlcs_workspace_size_masked": _SZ,
+            "rlcs_workspace_size_masked": _SZ, "rlcs_workspace_size_sample": _SZ,
+            "rlcs_workspace_size_attn": _SZ,
             "rlcs_status_string": ctypes.c_char_p}
 
 _lib = None

@@ -21,6 +21,10 @@
 #include <torch/csrc/PyInterpreter.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+#include <initializer_list>
+#include <vector>
+
 #include "rlcs.h"
 
 namespace {
@@ -49,6 +53,12 @@ struct Library {
     decltype(&rlcs_elig_trace_vec) elig_trace_vec;
     decltype(&rlcs_gae_masked) gae_masked;
     decltype(&rlcs_gae_masked_noalloc) gae_masked_noalloc;
+    decltype(&rlcs_token_logp) token_logp;
+    decltype(&rlcs_policy_loss) policy_loss;
+    decltype(&rlcs_sample) sample;
+    decltype(&rlcs_workspace_size_sample) workspace_size_sample;
+    decltype(&rlcs_shared_prefix_attn) shared_prefix_attn;
+    decltype(&rlcs_workspace_size_attn) workspace_size_attn;
 } g_lib;
 bool g_bound = false;
 
@@ -481,6 +491,239 @@ PyObject* gae_masked(Argv x, Py_ssize_t nargs) {
     });
 }
 
+// ------------------------------------------------------------- rows of logits and attention
+
+// Rows of [..., V] logits (contiguous, or a matrix with its rows any stride apart) and what the calls
+// on them share.
+struct Rows {
+    int64_t M = 1, V = 0, ld = 0;
+    std::vector<int64_t> lead;
+
+    // False: not such rows.
+    bool of(const at::Tensor& t) {
+        const int64_t dims = t.dim();
+        if (dims < 2) return false;
+        V = t.size(dims - 1);
+        lead.assign(t.sizes().begin(), t.sizes().end() - 1);
+        for (const int64_t n : lead) M *= n;
+        ld = V;
+        if (t.is_contiguous()) return true;
+        if (dims != 2 || (V > 1 && t.stride(1) != 1)) return false;
+        if (M > 1) ld = t.stride(0);
+        return ld >= V;
+    }
+};
+
+void* rows_input(Call& c, PyObject* o, Rows& r) {
+    const at::Tensor* t = c.plain(o);
+    if (!t) {
+        c.ok = false;
+        return nullptr;
+    }
+    c.dtype = t->scalar_type();
+    c.device = t->device();
+    c.ok = c.ok && (c.dtype == at::kFloat || c.dtype == at::kBFloat16) && c.device.is_cuda() &&
+           c.device.index() == c10::hip::current_device() && r.of(*t);
+    return c.ok ? t->data_ptr() : nullptr;
+}
+
+// A matrix of the logits' shape with rows of its own stride.
+void* rows_beside(Call& c, PyObject* o, at::ScalarType type, const Rows& r, int64_t& ld) {
+    ld = r.V;
+    const at::Tensor* t = c.plain(o);
+    if (!t) return nullptr;
+    Rows own;
+    c.ok = c.ok && t->scalar_type() == type && t->device() == c.device && own.of(*t) && own.V == r.V && own.lead == r.lead;
+    ld = own.ld;
+    return c.ok ? t->data_ptr() : nullptr;
+}
+
+// An output of any shape and type: given by the caller, allocated by the call, or not wanted.
+struct Result {
+    PyObject* given = nullptr;
+    bool make = false;
+    at::ScalarType type;
+    std::vector<int64_t> shape;
+    at::Tensor made;
+    void* ptr = nullptr;
+
+    Result(Call& c, PyObject* o, bool want, at::ScalarType t, at::IntArrayRef sizes) : type(t), shape(sizes.vec()) {
+        if (o == Py_None) {
+            make = want;
+            return;
+        }
+        given = o;
+        ptr = c.checked(o, type, sizes, false);
+    }
+    void allocate(const Call& c) {
+        if (!make) return;
+        made = at::empty(shape, at::TensorOptions().dtype(type).device(c.device));
+        ptr = made.data_ptr();
+    }
+    PyObject* object() {
+        if (make) return THPVariable_Wrap(made);
+        PyObject* o = given ? given : Py_None;
+        Py_INCREF(o);
+        return o;
+    }
+    float* f32() const { return static_cast<float*>(ptr); }
+};
+
+// Allocates the results and `ws_bytes` of workspace, calls `fn(stream, workspace)` and returns the
+// results as a tuple.
+template <class Fn>
+PyObject* run_results(Call& c, const char* name, std::initializer_list<Result*> results, size_t ws_bytes, Fn&& fn) {
+    if (!c.ok) Py_RETURN_NOTIMPLEMENTED;
+    int code = 0;
+    try {
+        NoGil no_gil;
+        for (Result* r : results) r->allocate(c);
+        at::Tensor ws;
+        if (ws_bytes) ws = at::empty({int64_t(ws_bytes)}, at::TensorOptions().dtype(at::kByte).device(c.device));
+        code = fn(static_cast<rlcs_stream_t>(c10::hip::getCurrentHIPStream(c.device.index()).stream()),
+                  ws_bytes ? ws.data_ptr() : nullptr);
+    } catch (...) {  // an allocation that failed: the Python function meets it again and reports it
+        Py_RETURN_NOTIMPLEMENTED;
+    }
+    if (code != RLCS_OK) {
+        PyObject* e = PyObject_CallFunction(g_error, "si", name, code);
+        if (e) {
+            PyErr_SetObject(g_error, e);
+            Py_DECREF(e);
+        }
+        return nullptr;
+    }
+    PyObject* tuple = PyTuple_New(Py_ssize_t(results.size()));
+    Py_ssize_t i = 0;
+    for (Result* r : results) {
+        PyObject* o = tuple ? r->object() : nullptr;
+        if (!o) {
+            Py_XDECREF(tuple);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(tuple, i++, o);
+    }
+    return tuple;
+}
+
+// token_logp(logits, tokens, logp, ent, temperature, want_ent)
+PyObject* token_logp(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(6);
+    if (x[1] == Py_None) Py_RETURN_NOTIMPLEMENTED;
+    Call c(false);
+    Rows r;
+    void* logits = rows_input(c, x[0], r);
+    const int32_t* tokens = static_cast<int32_t*>(c.checked(x[1], at::kInt, r.lead, false));
+    Result logp(c, x[2], true, at::kFloat, r.lead), ent(c, x[3], c.truth(x[5]), at::kFloat, r.lead);
+    const float temperature = c.number(x[4]);
+    return run_results(c, "rlcs_token_logp", {&logp, &ent}, 0, [&](rlcs_stream_t s, void*) {
+        return g_lib.token_logp(logits, tokens, logp.f32(), ent.f32(), r.M, r.V, r.ld, temperature, c.type(), s);
+    });
+}
+
+// policy_loss(logits, tokens, logp_old, adv, weight, loss, dlogits, logp, ent, clip_low, clip_high, ent_coef,
+// temperature, want_grad)
+PyObject* policy_loss(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(14);
+    if (x[1] == Py_None || x[2] == Py_None || x[3] == Py_None) Py_RETURN_NOTIMPLEMENTED;
+    Call c(false);
+    Rows r;
+    void* logits = rows_input(c, x[0], r);
+    const int32_t* tokens = static_cast<int32_t*>(c.checked(x[1], at::kInt, r.lead, false));
+    auto per_token = [&](PyObject* o) { return static_cast<float*>(c.checked(o, at::kFloat, r.lead, false)); };
+    const float *old = per_token(x[2]), *adv = per_token(x[3]), *weight = per_token(x[4]);
+    Result loss(c, x[5], true, at::kFloat, r.lead);
+    std::vector<int64_t> full = r.lead;
+    full.push_back(r.V);
+    Result grad(c, Py_None, c.truth(x[13]), c.dtype, full);
+    int64_t ld_grad = r.V;
+    if (x[6] != Py_None) {  // rows of its own stride
+        grad.make = false;
+        grad.given = x[6];
+        grad.ptr = rows_beside(c, x[6], c.dtype, r, ld_grad);
+    }
+    Result logp(c, x[7], true, at::kFloat, r.lead), ent(c, x[8], true, at::kFloat, r.lead);
+    const float lo = c.number(x[9]), hi = c.number(x[10]), ec = c.number(x[11]), temperature = c.number(x[12]);
+    return run_results(c, "rlcs_policy_loss", {&loss, &grad, &logp, &ent}, 0, [&](rlcs_stream_t s, void*) {
+        return g_lib.policy_loss(logits, tokens, old, adv, weight, loss.f32(), grad.ptr, logp.f32(), ent.f32(), r.M, r.V, r.ld,
+                                 ld_grad, lo, hi, ec, temperature, c.type(), s);
+    });
+}
+
+// sample(logits, noise, tokens, logp, temperature, top_k, top_p, min_p, want_logp, ws)
+PyObject* sample(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(10);
+    Call c(false);
+    Rows r;
+    void* logits = rows_input(c, x[0], r);
+    int64_t ld_noise = 0;
+    const float* noise = static_cast<float*>(rows_beside(c, x[1], at::kFloat, r, ld_noise));
+    Result tokens(c, x[2], true, at::kInt, r.lead), logp(c, x[3], c.truth(x[8]), at::kFloat, r.lead);
+    // a setting: a number, or a tensor of each row's own
+    float all[3] = {0.f, 0.f, 0.f};
+    const float* own[3] = {nullptr, nullptr, nullptr};
+    const int at_arg[3] = {4, 6, 7};
+    for (int i = 0; i < 3; ++i) {
+        PyObject* o = x[at_arg[i]];
+        if (THPVariable_CheckExact(o)) own[i] = static_cast<float*>(c.checked(o, at::kFloat, r.lead, false));
+        else all[i] = c.number(o);
+    }
+    const int32_t* own_k = nullptr;
+    int32_t all_k = 0;
+    if (THPVariable_CheckExact(x[5])) {
+        own_k = static_cast<int32_t*>(c.checked(x[5], at::kInt, r.lead, false));
+    } else if (PyLong_CheckExact(x[5])) {
+        int over = 0;
+        const long long k = PyLong_AsLongLongAndOverflow(x[5], &over);
+        if (over || k > INT32_MAX || k < -1) Py_RETURN_NOTIMPLEMENTED;
+        all_k = int32_t(k);
+    } else {
+        Py_RETURN_NOTIMPLEMENTED;
+    }
+    size_t wb = 0;
+    void* ws = c.workspace(x[9], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_sample(r.M, r.V) : 0;
+    return run_results(c, "rlcs_sample", {&tokens, &logp}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.sample(logits, noise, own[0], own_k, own[1], own[2], static_cast<int32_t*>(tokens.ptr), logp.f32(), r.M, r.V,
+                            r.ld, ld_noise, all[0], all_k, all[1], all[2], c.type(), made ? made : ws, made ? make : wb, s);
+    });
+}
+
+// shared_prefix_attn(q, kp, vp, ks, vs, prefix_len, suffix_len, o, lse, scale, want_lse, ws)
+PyObject* shared_prefix_attn(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(12);
+    Call c(false);
+    const at::Tensor* q = c.plain(x[0]);
+    const at::Tensor *kp = c.plain(x[1]), *vp = c.plain(x[2]), *ks = c.plain(x[3]), *vs = c.plain(x[4]);
+    if (!c.ok || !q || !kp || !vp || q->dim() != 4 || kp->dim() != 4 || (ks == nullptr) != (vs == nullptr)) Py_RETURN_NOTIMPLEMENTED;
+    c.dtype = q->scalar_type();
+    c.device = q->device();
+    c.ok = (c.dtype == at::kFloat || c.dtype == at::kBFloat16) && c.device.is_cuda() && c.device.index() == c10::hip::current_device();
+    const int64_t N = q->size(0), G = q->size(1), Hq = q->size(2), D = q->size(3), P = kp->size(1), Hkv = kp->size(2);
+    const int64_t S = ks && ks->dim() == 5 ? ks->size(2) : 0;
+    rlcs_attn_layout at{};
+    auto operand = [&](const at::Tensor* t, at::IntArrayRef sizes, int64_t* strides) -> const void* {
+        if (!t) return nullptr;
+        c.ok = c.ok && t->scalar_type() == c.dtype && t->device() == c.device && t->sizes() == sizes && (D <= 1 || t->stride(-1) == 1);
+        if (!c.ok) return nullptr;
+        for (size_t i = 0; i + 1 < sizes.size(); ++i) strides[i] = sizes[i] <= 1 ? 0 : t->stride(int64_t(i));
+        return t->data_ptr();
+    };
+    const void *pq = operand(q, {N, G, Hq, D}, at.q), *pkp = operand(kp, {N, P, Hkv, D}, at.kp), *pvp = operand(vp, {N, P, Hkv, D}, at.vp);
+    const void *pks = operand(ks, {N, G, S, Hkv, D}, at.ks), *pvs = operand(vs, {N, G, S, Hkv, D}, at.vs);
+    const int32_t* pl = static_cast<int32_t*>(c.checked(x[5], at::kInt, {N}, false));
+    const int32_t* sl = static_cast<int32_t*>(c.checked(x[6], at::kInt, {N, G}, false));
+    Result o(c, x[7], true, c.dtype, {N, G, Hq, D}), lse(c, x[8], c.truth(x[10]), at::kFloat, {N, G, Hq});
+    const float scale = x[9] == Py_None ? (D > 0 ? float(1.0 / std::sqrt(double(D))) : 0.f) : c.number(x[9]);
+    size_t wb = 0;
+    void* ws = c.workspace(x[11], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_attn(N, G, Hq, Hkv, D, P, S) : 0;
+    return run_results(c, "rlcs_shared_prefix_attn", {&o, &lse}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.shared_prefix_attn(pq, pkp, pvp, pks, pvs, pl, sl, o.ptr, lse.f32(), N, G, Hq, Hkv, D, P, S, &at, scale, c.type(),
+                                        made ? made : ws, made ? make : wb, s);
+    });
+}
+
 // bind(handle, error, device): the dlopen handle of librlcs.so, the exception class of its status
 // codes and the class of torch's default-device mode
 PyObject* bind(PyObject*, PyObject* args) {
@@ -512,6 +755,12 @@ PyObject* bind(PyObject*, PyObject* args) {
     get(g_lib.elig_trace_vec, "rlcs_elig_trace_vec");
     get(g_lib.gae_masked, "rlcs_gae_masked");
     get(g_lib.gae_masked_noalloc, "rlcs_gae_masked_noalloc");
+    get(g_lib.token_logp, "rlcs_token_logp");
+    get(g_lib.policy_loss, "rlcs_policy_loss");
+    get(g_lib.sample, "rlcs_sample");
+    get(g_lib.workspace_size_sample, "rlcs_workspace_size_sample");
+    get(g_lib.shared_prefix_attn, "rlcs_shared_prefix_attn");
+    get(g_lib.workspace_size_attn, "rlcs_workspace_size_attn");
     if (!all) {
         PyErr_SetString(PyExc_RuntimeError, "librlcs.so lacks a function of the binding");
         return nullptr;
@@ -540,6 +789,8 @@ PyMethodDef g_methods[] = {
     fast<elig_trace<false>>("elig_trace"), fast<elig_trace<true>>("elig_trace_strided"),
     fast<episodic_prefix<false>>("episodic_prefix"), fast<episodic_prefix<true>>("episodic_prefix_strided"),
     fast<affine_scan>("affine_scan"), fast<elig_trace_vec>("elig_trace_vec"), fast<gae_masked>("gae_masked"),
+    fast<token_logp>("token_logp"), fast<policy_loss>("policy_loss"), fast<sample>("sample"),
+    fast<shared_prefix_attn>("shared_prefix_attn"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,71 @@
+// Entry points of the policy's log-probabilities, entropies and loss.
+#include "rlcs_dispatch.h"
+#include "rlcs_policy.h"
+
+#include <cmath>
+
+using namespace rlcs;
+using namespace rlcs::host;
+
+namespace {
+
+template <typename DT, bool LOSS>
+rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
+    hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, 4>), dim3(unsigned(p.M)), dim3(4 * kWave), 0, s, p);
+    return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
+}
+
+// Sizes, type and alignment of what both entry points share.
+rlcs_status check_rows(int64_t M, int64_t V, int64_t ld, float temperature, rlcs_dtype dtype, const void* logits,
+                       std::initializer_list<const void*> words) {
+    if (M < 0 || V < 0) return RLCS_ERR_INVALID_ARG;
+    if (dtype != RLCS_F32 && dtype != RLCS_BF16) return RLCS_ERR_DTYPE;
+    if (M > INT32_MAX || V > kMaxT || ld < V || (ld > 0 && M > INT64_MAX / 4 / ld)) return RLCS_ERR_INVALID_ARG;
+    if (!positive(temperature) || !std::isfinite(temperature) || !std::isfinite(kLog2e / temperature)) return RLCS_ERR_INVALID_ARG;
+    if (logits && !aligned(logits, dtype_size(dtype))) return RLCS_ERR_INVALID_ARG;
+    for (const void* p : words)
+        if (p && !aligned(p, 4)) return RLCS_ERR_INVALID_ARG;
+    return RLCS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+rlcs_status rlcs_token_logp(const void* logits, const int32_t* tokens, float* logp, float* ent,
+                            int64_t M, int64_t V, int64_t ld, float temperature, rlcs_dtype dtype,
+                            rlcs_stream_t stream) {
+    const rlcs_status st = check_rows(M, V, ld, temperature, dtype, logits, {tokens, logp, ent});
+    if (st != RLCS_OK) return st;
+    if (M == 0 || V == 0) return RLCS_OK;
+    if (!logits || !tokens || !logp) return RLCS_ERR_INVALID_ARG;
+    PolicyArgs p{};
+    p.logits = logits; p.tokens = tokens; p.logp = logp; p.ent = ent;
+    p.M = M; p.V = V; p.ld = ld; p.inv_temp = 1.f / temperature;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return dtype == RLCS_BF16 ? run_policy<bf16_t, false>(p, s) : run_policy<float, false>(p, s);
+}
+
+rlcs_status rlcs_policy_loss(const void* logits, const int32_t* tokens, const float* logp_old,
+                             const float* adv, const float* weight, float* loss, void* dlogits,
+                             float* logp, float* ent, int64_t M, int64_t V, int64_t ld,
+                             int64_t ld_grad, float clip_low, float clip_high, float ent_coef,
+                             float temperature, rlcs_dtype dtype, rlcs_stream_t stream) {
+    const rlcs_status st = check_rows(M, V, ld, temperature, dtype, logits, {tokens, logp_old, adv, weight, loss, logp, ent});
+    if (st != RLCS_OK) return st;
+    if (!unit_interval(clip_low) || !(clip_high >= 0.f) || !std::isfinite(ent_coef)) return RLCS_ERR_INVALID_ARG;
+    if (dlogits && (!aligned(dlogits, dtype_size(dtype)) || ld_grad < V || (ld_grad > 0 && M > INT64_MAX / 4 / ld_grad)))
+        return RLCS_ERR_INVALID_ARG;
+    if (dlogits && dlogits == logits && ld_grad != ld) return RLCS_ERR_INVALID_ARG;
+    if (M == 0 || V == 0) return RLCS_OK;
+    if (!logits || !tokens || !logp_old || !adv || !loss) return RLCS_ERR_INVALID_ARG;
+    PolicyArgs p{};
+    p.logits = logits; p.tokens = tokens; p.logp_old = logp_old; p.adv = adv; p.weight = weight;
+    p.loss = loss; p.logp = logp; p.ent = ent; p.grad = dlogits;
+    p.M = M; p.V = V; p.ld = ld; p.ld_grad = ld_grad;
+    p.low = 1.f - clip_low; p.high = 1.f + clip_high; p.ent_coef = ent_coef; p.inv_temp = 1.f / temperature;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return dtype == RLCS_BF16 ? run_policy<bf16_t, true>(p, s) : run_policy<float, true>(p, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,57 @@
+// Entry point of token sampling.
+#include "rlcs_dispatch.h"
+#include "rlcs_sample.h"
+
+using namespace rlcs;
+using namespace rlcs::host;
+
+namespace {
+
+template <typename DT>
+rlcs_status run_sample(const SampleArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL((sample_rows_kernel<DT, 4>), dim3(unsigned(a.M)), dim3(4 * kWave), 0, s, a);
+    return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rlcs_workspace_size_sample(int64_t M, int64_t V) {
+    (void)M;
+    (void)V;
+    return 0;
+}
+
+rlcs_status rlcs_sample(const void* logits, const float* noise, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p,
+                        int32_t* tokens, float* logp, int64_t M, int64_t V, int64_t ld,
+                        int64_t ld_noise, float all_temperature, int32_t all_top_k,
+                        float all_top_p, float all_min_p, rlcs_dtype dtype, void* ws,
+                        size_t ws_bytes, rlcs_stream_t stream) {
+    (void)ws;
+    (void)ws_bytes;
+    if (M < 0 || V < 0) return RLCS_ERR_INVALID_ARG;
+    if (dtype != RLCS_F32 && dtype != RLCS_BF16) return RLCS_ERR_DTYPE;
+    if (M > INT32_MAX || V > (int64_t(1) << 24) || ld < V || (ld > 0 && M > INT64_MAX / 4 / ld)) return RLCS_ERR_INVALID_ARG;
+    if (noise && (ld_noise < V || (ld_noise > 0 && M > INT64_MAX / 4 / ld_noise))) return RLCS_ERR_INVALID_ARG;
+    if (all_temperature != all_temperature || all_top_p != all_top_p || all_min_p != all_min_p) return RLCS_ERR_INVALID_ARG;
+    if (all_min_p > 1.f) return RLCS_ERR_INVALID_ARG;
+    if (logits && !aligned(logits, dtype_size(dtype))) return RLCS_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(noise), static_cast<const void*>(temperature), static_cast<const void*>(top_k),
+                          static_cast<const void*>(top_p), static_cast<const void*>(min_p), static_cast<const void*>(tokens),
+                          static_cast<const void*>(logp)})
+        if (p && !aligned(p, 4)) return RLCS_ERR_INVALID_ARG;
+    if (M == 0 || V == 0) return RLCS_OK;
+    if (!logits || !tokens) return RLCS_ERR_INVALID_ARG;
+    SampleArgs a{};
+    a.logits = logits; a.noise = noise;
+    a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+    a.tokens = tokens; a.logp = logp;
+    a.M = M; a.V = V; a.ld = ld; a.ld_noise = ld_noise;
+    a.all_temperature = all_temperature; a.all_top_k = all_top_k; a.all_top_p = all_top_p; a.all_min_p = all_min_p;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return dtype == RLCS_BF16 ? run_sample<bf16_t>(a, s) : run_sample<float>(a, s);
+}
+
+}  // extern "C"
