@@ -26,17 +26,111 @@ bool reachable(std::initializer_list<int64_t> sizes, const int64_t* strides) {
     return true;
 }
 
-template <typename DT>
-rlcs_status run_attn(const AttnArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((attn_heads_kernel<DT>), dim3(unsigned(a.Hq), unsigned(a.G), unsigned(a.N)), dim3(kWave), 0, s, a);
+// Keys of a part: no fewer than kMinChunk (a part of r rows costs r * D * 8 bytes written and read
+// again), and as many parts as give kWantItems workgroups.
+constexpr int64_t kMinChunk = 256;
+constexpr int64_t kWantItems = 1536;
+// Calls of at most this many keys run as one kernel in which each sequence takes its prefix itself.
+constexpr int64_t kWholeKeys = 512;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Query tiles of sixteen a workgroup of the prefix takes: as many as there are rows for, up to what
+// the registers hold.
+int prefix_query_tiles(int64_t rows, int64_t D, bool bf16) {
+    const int most = D > 128 ? 1 : bf16 ? 4 : 2;
+    return rows <= 16 || most == 1 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+}
+
+bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S, bool bf16) {
+    const int64_t r = Hq / Hkv;
+    p = AttnPlan{};
+    p.whole = P + S <= kWholeKeys || P == 0;
+    p.suffix_tiles = int32_t(ceil_div(r, kTileRows));
+    auto split = [](int64_t keys, int64_t base, int64_t& chunk, int32_t& parts) {
+        int64_t want = ceil_div(kWantItems, base), most = ceil_div(keys, kMinChunk);
+        if (want > most) want = most;
+        if (want < 1) want = 1;
+        chunk = keys > 0 ? ceil_div(ceil_div(keys, want), 32) * 32 : 1;
+        parts = int32_t(keys > 0 ? ceil_div(keys, chunk) : 1);
+    };
+    const int64_t suffix_base = N * G * Hkv * p.suffix_tiles;
+    p.suffix_chunk = 1;
+    p.prefix_chunk = 1;
+    if (p.whole && P > 0) {
+        p.suffix_parts = 1;
+        p.suffix_chunk = S > 0 ? S : 1;
+    } else if (S > 0 || P == 0) {
+        split(S, suffix_base, p.suffix_chunk, p.suffix_parts);
+    }
+    int64_t prefix_items = 0;
+    if (!p.whole) {
+        p.prefix_tiles = int32_t(ceil_div(G * r, kTileRows * prefix_query_tiles(G * r, D, bf16)));
+        const int64_t base = N * Hkv * p.prefix_tiles;
+        split(P, base, p.prefix_chunk, p.prefix_parts);
+        prefix_items = base * p.prefix_parts;
+    }
+    const int64_t items = prefix_items + suffix_base * p.suffix_parts;
+    if (items > INT32_MAX) return false;
+    p.prefix_items = int32_t(prefix_items);
+    p.items = int32_t(items);
+    return true;
+}
+
+size_t part_bytes(const AttnPlan& p, int64_t rows, int64_t D) {
+    const int64_t parts = p.prefix_parts + p.suffix_parts;
+    return parts > 1 ? size_t(parts * rows) * size_t(4 * D + 8) : 0;
+}
+
+template <typename DT, int ND, int QT>
+void launch_items(const AttnArgs& a, const AttnPlan& p, int first, int count, hipStream_t s) {
+    constexpr int W = ND > 8 ? 2 : 4;
+    if (count > 0) hipLaunchKernelGGL((attn_kernel<DT, ND, QT, W>), dim3(unsigned(count)), dim3(W * kWave), 0, s, a, p, first);
+}
+
+template <typename DT, int ND>
+rlcs_status run_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    const int qt = prefix_query_tiles(a.G * (a.Hq / a.Hkv), a.D, sizeof(DT) == 2);
+    int done = 0;
+    if (qt > 1) {
+        done = p.prefix_items;
+        if constexpr (ND <= 8) {
+            if constexpr (sizeof(DT) == 2) {
+                if (qt == 4) launch_items<DT, ND, 4>(a, p, 0, done, s);
+            }
+            if (qt == 2) launch_items<DT, ND, 2>(a, p, 0, done, s);
+        }
+    }
+    launch_items<DT, ND, 1>(a, p, done, p.items - done, s);
+    if (p.part_acc) {
+        const int64_t rows = a.N * a.G * a.Hq, per = 256 / (a.D / 4);
+        hipLaunchKernelGGL((attn_join_kernel<DT>), dim3(unsigned(ceil_div(rows, per))), dim3(256), 0, s, a, p);
+    }
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
+}
+
+template <typename DT>
+rlcs_status run_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    return a.D <= 64 ? run_attn<DT, 4>(a, p, s) : a.D <= 128 ? run_attn<DT, 8>(a, p, s) : run_attn<DT, 16>(a, p, s);
+}
+
+bool sizes_fit(int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S) {
+    if (N < 1 || G < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || P < 0 || S < 0) return false;
+    return N <= INT32_MAX && G <= INT32_MAX && Hq <= INT32_MAX && N <= INT32_MAX / G && N * G <= INT32_MAX / Hq && D >= 8 &&
+           D <= kMaxHeadDim && D % 8 == 0 && P <= kMaxT && S <= kMaxT;
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t rlcs_workspace_size_attn(int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t rlcs_workspace_size_attn(int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S) {
+    if (!sizes_fit(N, G, Hq, Hkv, D, P, S)) return 0;
+    AttnPlan b, f;
+    if (!make_plan(b, N, G, Hq, Hkv, D, P, S, true) || !make_plan(f, N, G, Hq, Hkv, D, P, S, false)) return 0;
+    const size_t x = part_bytes(b, N * G * Hq, D), y = part_bytes(f, N * G * Hq, D);
+    return x > y ? x : y;
+}
 
 rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* vp, const void* ks,
                                     const void* vs, const int32_t* prefix_len,
@@ -49,9 +143,7 @@ rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* v
     if (dtype != RLCS_F32 && dtype != RLCS_BF16) return RLCS_ERR_DTYPE;
     if (!std::isfinite(scale)) return RLCS_ERR_INVALID_ARG;
     if (N == 0 || G == 0 || Hq == 0 || D == 0) return RLCS_OK;
-    // grid dimensions and row counts that the kernels index with 32 bits
-    if (N > 65535 || G > 65535 || Hq > 65535 || Hkv < 1 || Hq % Hkv || N * G > INT32_MAX / Hq) return RLCS_ERR_INVALID_ARG;
-    if (D > kMaxHeadDim || D % 8 || P > kMaxT || S > kMaxT) return RLCS_ERR_INVALID_ARG;
+    if (!sizes_fit(N, G, Hq, Hkv, D, P, S)) return RLCS_ERR_INVALID_ARG;
     if (!q || !o || (P && (!kp || !vp)) || (S && (!ks || !vs))) return RLCS_ERR_INVALID_ARG;
     for (const void* p : {q, kp, vp, ks, vs, static_cast<const void*>(o)})
         if (!aligned(p, 16)) return RLCS_ERR_INVALID_ARG;
@@ -76,15 +168,23 @@ rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* v
     if (!reachable({N, G, Hq}, a.at.q) || !reachable({N, P, Hkv}, a.at.kp) || !reachable({N, P, Hkv}, a.at.vp) ||
         !reachable({N, G, S, Hkv}, a.at.ks) || !reachable({N, G, S, Hkv}, a.at.vs))
         return RLCS_ERR_INVALID_ARG;
-    if (ws_bytes < rlcs_workspace_size_attn(N, G, Hq, Hkv, D, P, S)) return RLCS_ERR_WORKSPACE;
-    (void)ws;
+    const bool bf16 = dtype == RLCS_BF16;
+    AttnPlan p;
+    if (!make_plan(p, N, G, Hq, Hkv, D, P, S, bf16)) return RLCS_ERR_INVALID_ARG;
+    if (const size_t need = part_bytes(p, N * G * Hq, D)) {
+        if (!ws || ws_bytes < need) return RLCS_ERR_WORKSPACE;
+        if (!aligned(ws, 16)) return RLCS_ERR_INVALID_ARG;
+        const int64_t slots = int64_t(p.prefix_parts + p.suffix_parts) * N * G * Hq;
+        p.part_acc = static_cast<float*>(ws);
+        p.part_ml = reinterpret_cast<float2*>(p.part_acc + slots * D);
+    }
     a.q = q; a.kp = kp; a.vp = vp; a.ks = ks; a.vs = vs;
     a.prefix_len = prefix_len; a.suffix_len = suffix_len;
     a.o = o; a.lse = lse;
     a.N = N; a.G = G; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.P = P; a.S = S;
     a.scale2 = scale * kLog2e;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    return dtype == RLCS_BF16 ? run_attn<bf16_t>(a, s) : run_attn<float>(a, s);
+    return bf16 ? run_attn<bf16_t>(a, p, s) : run_attn<float>(a, p, s);
 }
 
 }  // extern "C"
