@@ -413,7 +413,7 @@ size_t rlcs_workspace_size_sample(int64_t M, int64_t V);
  *            Keys and values past the lengths may hold anything, NaN included
  *   lse      [N, G, Hq] float32 out, optional
  *   layout   strides in elements, NULL = contiguous. D is contiguous; strides are >= 0 and multiples
- *            of 16 bytes, as are q, kp, vp, ks, vs and o
+ *            of 16 bytes, as are q, kp, vp, ks, vs and o; those of tokens are below 2^24
  *   ws       rlcs_workspace_size_attn(...) bytes, 16-byte aligned, need not be cleared
  * D a multiple of 8 up to 256; P and S up to 2^30. Scores, sums and the output's accumulator are
  * float32; bfloat16 weights e^{s - m} are rounded to bfloat16 for the product with V.         */

@@ -52,42 +52,74 @@ __device__ __forceinline__ int64_t clamp_len(const int32_t* p, int64_t i, int64_
 
 constexpr int kTileRows = 16;  // queries of a matrix product's columns
 
-// Keys of one block, as operands: of bfloat16 32 keys, of float32 16. ND: the head's dimensions in
-// sixteens.
-template <typename DT, int ND>
-struct KeyBlock;
+// One array of keys and values as a wave walks it: byte offsets of its lane's pieces of a block from
+// the block's first row (below 2^31: token strides are below 2^24 elements), and the rows' strides. A
+// piece past the head's dimensions reads the head's last one instead: its query is 0, its output
+// column is not stored. Rows past the end read the last row: their weights are 0, and it holds
+// ordinary numbers. So no load depends on a lane's condition.
+template <typename DT, int ND, bool EXACT>
+struct KeyBlock {
+    static constexpr bool kWide = sizeof(DT) == 4;
+    static constexpr int kKeys = kWide ? 16 : 32;
+    static constexpr int kRow = 16 * ND + 16;  // bfloat16: elements of a row of V in LDS, 32 bytes more than it
+                                               // has, so that the rows of half a wave's read lie in different banks
+    static constexpr int kVecs = 2 * ND;       // its 16-byte pieces
+    static constexpr int kKRows = kKeys / 16, kVRows = kWide ? 4 : ND;
+    // bfloat16: k[kt * ND / 2 + s] is key 16 kt + lane % 16, dimensions 32 s + 8 (lane / 16) ..., v rows
+    // of V, 16 bytes a lane. float32: k[t] is key lane % 16, dimensions 16 t + 4 (lane / 16) ..., v[t][i]
+    // is key 4 (lane / 16) + i, dimension 16 t + lane % 16.
+    u32x4 k[ND], v[ND];
+    uint32_t at_k[kKRows], at_v[kVRows];
 
-template <int ND>
-struct KeyBlock<bf16_t, ND> {
-    static constexpr int kKeys = 32;
-    static constexpr int kRow = 16 * ND + 16;  // elements of a row of V in LDS: 32 bytes more, so that
-                                               // the eight rows of half a wave's read lie in different banks
-    u32x4 k[ND];  // k[kt * ND / 2 + s]: key 16 kt + lane % 16, dimensions 32 s + 8 (lane / 16) ...
-    u32x4 v[ND];  // rows of V, 16 bytes a lane
-
-    __device__ __forceinline__ void load(const bf16_t* kb, const bf16_t* vb, int64_t sk, int64_t sv, int64_t j0, int64_t end,
-                                         int D, int lane) {
+    // `rows` of the block that exist
+    __device__ __forceinline__ void aim(int rows, int64_t sk, int64_t sv, int D, int lane) {
         const int c = lane & 15, g = lane >> 4;
-        const bool all = j0 + kKeys <= end;
+        auto row = [&](int j) { return uint32_t(j < rows ? j : rows - 1); };
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            int64_t j = j0 + 16 * kt + c;
-            if (!all) j = j < end ? j : end - 1;
-            const bf16_t* p = kb + j * sk + 8 * g;
+        for (int kt = 0; kt < kKRows; ++kt) at_k[kt] = (row(16 * kt + c) * uint32_t(sk)) * uint32_t(sizeof(DT)) + 16u * g;
 #pragma unroll
-            for (int s = 0; s < ND / 2; ++s)
-                k[kt * (ND / 2) + s] = 32 * s + 8 * g < D ? *reinterpret_cast<const u32x4*>(p + 32 * s) : u32x4{0, 0, 0, 0};
+        for (int i = 0; i < kVRows; ++i) {
+            if constexpr (kWide) {
+                at_v[i] = (row(4 * g + i) * uint32_t(sv) + c) * 4u;
+            } else {
+                const int at = lane + 64 * i, piece = at % kVecs;
+                at_v[i] = (row(at / kVecs) * uint32_t(sv) + 8u * (EXACT || 8 * piece < D ? piece : D / 8 - 1)) * 2u;
+            }
         }
-        constexpr int kVecs = 2 * ND;  // 16-byte pieces of a row
+    }
+    __device__ __forceinline__ void load_k(const char* base, int D, int lane) {
+        constexpr int kSteps = ND / kKRows;
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            const int at = lane + 64 * i, piece = at % kVecs;
-            const int64_t j = j0 + at / kVecs;
-            v[i] = (all || j < end) && 8 * piece < D ? *reinterpret_cast<const u32x4*>(vb + j * sv + 8 * piece) : u32x4{0, 0, 0, 0};
+        for (int kt = 0; kt < kKRows; ++kt)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                uint32_t at = at_k[kt] + 64u * s;
+                if constexpr (!EXACT) {  // (64 bytes a step, 16 a lane)
+                    const uint32_t d = 64u * s + 16u * (lane >> 4), last = uint32_t(D) * sizeof(DT) - 16u;
+                    if (d > last) at -= d - last;
+                }
+                k[kt * kSteps + s] = *reinterpret_cast<const u32x4*>(base + at);
+            }
+    }
+    __device__ __forceinline__ void load_v(const char* base, int D, int lane) {
+        if constexpr (kWide) {
+#pragma unroll
+            for (int t = 0; t < ND; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t at = at_v[i] + 64u * t;
+                    if constexpr (!EXACT) {
+                        const int d = 16 * t + (lane & 15);
+                        if (d >= D) at -= 4u * uint32_t(d - D + 1);
+                    }
+                    v[t][i] = *reinterpret_cast<const uint32_t*>(base + at);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < ND; ++i) v[i] = *reinterpret_cast<const u32x4*>(base + at_v[i]);
         }
     }
     __device__ __forceinline__ void stage(bf16_t* lds, int lane) const {
-        constexpr int kVecs = 2 * ND;
         wave_lds_sync();  // the block before has been read
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
@@ -98,40 +130,73 @@ struct KeyBlock<bf16_t, ND> {
     }
 };
 
-template <int ND>
-struct KeyBlock<float, ND> {
-    static constexpr int kKeys = 16;
-    f32x4 k[ND];     // key lane % 16, dimensions 16 j + 4 (lane / 16) ...
-    float v[ND][4];  // key 4 (lane / 16) + i, dimension 16 t + lane % 16
+// The largest over the four lanes that share lane % 16.
+__device__ __forceinline__ float max_of_four(float x) {
+    typedef unsigned u32x2v __attribute__((ext_vector_type(2)));
+    u32x2v p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
 
-    __device__ __forceinline__ void load(const float* kb, const float* vb, int64_t sk, int64_t sv, int64_t j0, int64_t end, int D,
-                                         int lane) {
-        const int c = lane & 15, g = lane >> 4;
-        const bool all = j0 + kKeys <= end;
-        int64_t j = j0 + c;
-        if (!all) j = j < end ? j : end - 1;
-        const float* p = kb + j * sk + 4 * g;
+// One softmax step of a query tile: scores of 16 * KT keys to weights (rounded to bfloat16 in `p`: to
+// nearest, for the product; the sums keep all bits), the running maximum, sum and outputs brought
+// to the new maximum.
+template <int KT, int ND>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[KT], float scale, float& m, float& l, f32x4 (&acc)[ND]) {
+    float top = kNegInf;
 #pragma unroll
-        for (int t = 0; t < ND; ++t)
-            k[t] = 16 * t + 4 * g < D ? *reinterpret_cast<const f32x4*>(p + 16 * t) : f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[kt][i]);
+    const float m1 = fmaxf(m, max_of_four(top) * scale);
+    if (__any(m1 > m)) {
+        const float keep = exp2_fast(m - m1);
+        l *= keep;
+#pragma unroll
+        for (int t = 0; t < ND; ++t) acc[t] *= keep;
+        m = m1;
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t jv = j0 + 4 * g + i;
-            const bool in = all || jv < end;
-            const float* pv = vb + (in ? jv : end - 1) * sv + c;
-#pragma unroll
-            for (int t = 0; t < ND; ++t) v[t][i] = in && 16 * t + c < D ? pv[16 * t] : 0.f;
+            s[kt][i] = exp2_fast(fmaf(s[kt][i], scale, -m));
+            l += s[kt][i];
         }
-    }
-};
+}
 
-// A wave's state: queries, running maxima, sums (of its lane's keys only) and outputs.
-template <typename DT, int ND, int QT>
+// Weights of 32 keys (two tiles of scores) as an operand.
+__device__ __forceinline__ bf16x8 weights_operand(f32x4 a, f32x4 b) {
+    bf16x8 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p[i] = static_cast<__bf16>(a[i]);
+        p[4 + i] = static_cast<__bf16>(b[i]);
+    }
+    return p;
+}
+
+// Values of 32 keys and 16 dimensions in LDS as an operand, keys in the order that scores come in:
+// `at` is the lane's place, row 4 (lane / 16) + lane % 16 / 4 and column 4 (lane % 4) of the block.
+__device__ __forceinline__ bf16x8 values_operand(const bf16_t* at, int row) {
+    union {
+        s16x4 half[2];
+        bf16x8 all;
+    } v;
+    v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+    v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 16 * row));
+    return v.all;
+}
+
+// A wave's state: queries, running maxima (base 2), sums (of its lane's keys only) and outputs.
+template <typename DT, int ND, int QT, bool EXACT>
 struct AttnWave {
-    static constexpr int kKeys = KeyBlock<DT, ND>::kKeys;
-    typedef typename std::conditional<sizeof(DT) == 2, u32x4, f32x4>::type QVec;
-    static constexpr int kQVecs = sizeof(DT) == 2 ? ND / 2 : ND;
-    QVec q[QT][kQVecs];
+    typedef KeyBlock<DT, ND, EXACT> Block;
+    static constexpr bool kWide = sizeof(DT) == 4;
+    static constexpr int kKeys = Block::kKeys;
+    static constexpr int kQVecs = kWide ? ND : ND / 2;
+    u32x4 q[QT][kQVecs];
     f32x4 acc[QT][ND];  // query lane % 16, dimensions 16 t + 4 (lane / 16) ...
     float m[QT], l[QT];
 
@@ -144,125 +209,205 @@ struct AttnWave {
             for (int t = 0; t < ND; ++t) acc[x][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // Query row of this lane's column of tile x, or null past the last.
-    __device__ __forceinline__ void load_query(int x, const DT* p, int D, int lane) {
+    // Query row of this lane's column of tile x, or null past the last; `sign` flips its elements' signs.
+    __device__ __forceinline__ void load_query(int x, const DT* p, int D, uint32_t sign, int lane) {
         const int g = lane >> 4;
         constexpr int kVec = 16 / sizeof(DT);
 #pragma unroll
         for (int s = 0; s < kQVecs; ++s) {
             const int d = 4 * kVec * s + kVec * g;
-            q[x][s] = p && d < D ? *reinterpret_cast<const QVec*>(p + d) : QVec{0, 0, 0, 0};
+            q[x][s] = p && d < D ? *reinterpret_cast<const u32x4*>(p + d) ^ sign : u32x4{0, 0, 0, 0};
         }
     }
 
-    // Scores of a block, its softmax step and its part of the outputs.
-    __device__ __forceinline__ void step(const KeyBlock<DT, ND>& b, bf16_t* lds, int64_t j0, int64_t end, float scale2, int lane) {
+    // Keys [from, end) of one array: blocks wave, wave + W, ... A block's values are on their way while
+    // the scores of the one before are worked out, its keys while those weigh their values. `scale` >= 0.
+    template <int W>
+    __device__ __forceinline__ void run(const DT* keys, const DT* values, int64_t sk, int64_t sv, int64_t from, int64_t end, int D,
+                                        float scale, bf16_t* lds, int wave, int lane) {
         const int c = lane & 15, g = lane >> 4;
         constexpr int KT = kKeys / 16;
-        f32x4 s[QT][KT];
+        int64_t j = from + wave * kKeys;
+        if (j >= end) return;
+        Block b;
+        const char* kb = reinterpret_cast<const char*>(keys + j * sk);
+        const char* vb = reinterpret_cast<const char*>(values + j * sv);
+        const int64_t hop_k = W * kKeys * sk * int64_t(sizeof(DT)), hop_v = W * kKeys * sv * int64_t(sizeof(DT));
+        b.aim(end - j < kKeys ? int(end - j) : kKeys, sk, sv, D, lane);
+        b.load_k(kb, D, lane);
+        b.load_v(vb, D, lane);
+        for (;;) {
+            const int rows = end - j < kKeys ? int(end - j) : kKeys;
+            j += W * kKeys;
+            const bool more = j < end;
+            kb += hop_k;
+            vb += hop_v;
+            if (end - j < kKeys && more) b.aim(int(end - j), sk, sv, D, lane);
+            u32x4 now[kWide ? ND : 1];
+            if constexpr (kWide) {
 #pragma unroll
-        for (int x = 0; x < QT; ++x)
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) s[x][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (sizeof(DT) == 2) {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int d = 0; d < ND / 2; ++d)
-#pragma unroll
-                    for (int x = 0; x < QT; ++x)
-                        s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b.k[kt * (ND / 2) + d]),
-                                                                          __builtin_bit_cast(bf16x8, q[x][d]), s[x][kt], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int x = 0; x < QT; ++x)
-                        s[x][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(b.k[d][i], q[x][d][i], s[x][0], 0, 0, 0);
-        }
-        const bool all = j0 + kKeys <= end;
-#pragma unroll
-        for (int x = 0; x < QT; ++x) {
-            float top = kNegInf;
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                s[x][kt] *= scale2;
-                if (!all) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (j0 + 16 * kt + 4 * g + i >= end) s[x][kt][i] = kNegInf;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[x][kt][i]);
+                for (int t = 0; t < ND; ++t) now[t] = b.v[t];
+            } else {
+                b.stage(lds, lane);
             }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m1 = fmaxf(m[x], top);
-            if (__any(m1 > m[x])) {
-                const float keep = exp2_fast(m[x] - m1);
-                l[x] *= keep;
-#pragma unroll
-                for (int t = 0; t < ND; ++t) acc[x][t] *= keep;
-                m[x] = m1;
-            }
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[x][kt][i] = exp2_fast(s[x][kt][i] - m[x]);
-                    l[x] += s[x][kt][i];
-                }
-        }
-        if constexpr (sizeof(DT) == 2) {
-            bf16x8 p[QT];  // rounded to nearest for the product; the sums keep all bits
+            if (more) b.load_v(vb, D, lane);
+
+            f32x4 s[QT][KT];
 #pragma unroll
             for (int x = 0; x < QT; ++x)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[x][i] = static_cast<__bf16>(s[x][i >> 2][i & 3]);
-            // rows 4 g ... of each sixteen keys, columns 16 t ...
-            const bf16_t* at = lds + (4 * g + (c >> 2)) * KeyBlock<DT, ND>::kRow + 4 * (c & 3);
+                for (int kt = 0; kt < KT; ++kt) s[x][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (!kWide) {
 #pragma unroll
-            for (int t = 0; t < ND; ++t) {
-                union {
-                    s16x4 half[2];
-                    bf16x8 all;
-                } v;
-                v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 16 * t));
-                v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(at + 16 * KeyBlock<DT, ND>::kRow + 16 * t));
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int x = 0; x < QT; ++x) acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.all, p[x], acc[x][t], 0, 0, 0);
+                    for (int d = 0; d < ND / 2; ++d)
+#pragma unroll
+                        for (int x = 0; x < QT; ++x)
+                            s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b.k[kt * (ND / 2) + d]),
+                                                                              __builtin_bit_cast(bf16x8, q[x][d]), s[x][kt], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int x = 0; x < QT; ++x)
+                            s[x][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.k[d][i]), __uint_as_float(q[x][d][i]),
+                                                                          s[x][0], 0, 0, 0);
             }
-        } else {
+            if (more) b.load_k(kb, D, lane);
+
+            if (rows < kKeys) {
 #pragma unroll
-            for (int t = 0; t < ND; ++t)
+                for (int x = 0; x < QT; ++x)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int x = 0; x < QT; ++x)
-                        acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(b.v[t][i], s[x][0][i], acc[x][t], 0, 0, 0);
+                        for (int i = 0; i < 4; ++i)
+                            if (16 * kt + 4 * g + i >= rows) s[x][kt][i] = kNegInf;
+            }
+#pragma unroll
+            for (int x = 0; x < QT; ++x) softmax_step<KT, ND>(s[x], scale, m[x], l[x], acc[x]);
+            if constexpr (!kWide) {
+                bf16x8 p[QT];
+#pragma unroll
+                for (int x = 0; x < QT; ++x) p[x] = weights_operand(s[x][0], s[x][1]);
+                const bf16_t* at = lds + (4 * g + (c >> 2)) * Block::kRow + 4 * (c & 3);
+#pragma unroll
+                for (int t = 0; t < ND; ++t) {
+                    const bf16x8 v = values_operand(at + 16 * t, Block::kRow);
+#pragma unroll
+                    for (int x = 0; x < QT; ++x) acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[x], acc[x][t], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < ND; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int x = 0; x < QT; ++x)
+                            acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(now[t][i]), s[x][0][i], acc[x][t], 0, 0, 0);
+            }
+            if (!more) return;
         }
     }
+};
 
-    // Keys [from, end) of one array: blocks wave, wave + W, ... The next block's loads are under way
-    // while one is worked on.
-    template <int W>
-    __device__ __forceinline__ void run(const DT* kb, const DT* vb, int64_t sk, int64_t sv, int64_t from, int64_t end, int D,
-                                        float scale2, bf16_t* lds, int wave, int lane) {
-        int64_t j = from + wave * kKeys;
-        if (j >= end) return;
-        KeyBlock<DT, ND> b;
-        b.load(kb, vb, sk, sv, j, end, D, lane);
-        for (;;) {
-            const int64_t next = j + W * kKeys;
-            KeyBlock<DT, ND> cur = b;
-            if constexpr (sizeof(DT) == 2) cur.stage(lds, lane);
-            if (next < end) b.load(kb, vb, sk, sv, next, end, D, lane);
-            step(cur, lds, j, end, scale2, lane);
-            if (next >= end) return;
-            j = next;
+// Keys [from, end) of one array for a workgroup whose waves have queries of their own (bfloat16): all of
+// its lanes bring a block of keys and values to LDS, every wave reads them from there. The next
+// block's loads are under way meanwhile.
+template <int ND, int QT, int W, bool EXACT>
+struct SharedKeys {
+    static constexpr int kKeys = ND > 8 ? 32 : 64;
+    static constexpr int kVecs = 2 * ND;  // 16-byte pieces of a row
+    static constexpr int kKRow = 16 * ND + 8;   // elements of a row in LDS: the sixteen rows of a key operand's read,
+    static constexpr int kVRow = 16 * ND + 16;  // and the eight of half a wave's of values, in different banks
+    static constexpr int kPieces = kKeys * kVecs / (W * kWave);
+    static constexpr size_t kLds = size_t(kKeys) * (kKRow + kVRow) * 2;
+
+    static __device__ __forceinline__ void run(AttnWave<bf16_t, ND, QT, EXACT>& w, const bf16_t* keys, const bf16_t* values, int64_t sk,
+                                               int64_t sv, int64_t from, int64_t end, int D, float scale, bf16_t* lds, int tid) {
+        const int lane = tid & 63, c = lane & 15, g = lane >> 4;
+        constexpr int KT = kKeys / 16;
+        bf16_t* lk = lds;
+        bf16_t* lv = lds + kKeys * kKRow;
+        u32x4 k[kPieces], v[kPieces];
+        uint32_t at_k[kPieces], at_v[kPieces];
+        auto aim = [&](int rows) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int at = tid + W * kWave * i, piece = at % kVecs;
+                const uint32_t row = at / kVecs < rows ? at / kVecs : rows - 1;
+                const uint32_t d = 8u * (EXACT || 8 * piece < D ? piece : D / 8 - 1);
+                at_k[i] = (row * uint32_t(sk) + d) * 2u;
+                at_v[i] = (row * uint32_t(sv) + d) * 2u;
+            }
+        };
+        auto load = [&](int64_t j) {
+            const char* kb = reinterpret_cast<const char*>(keys + j * sk);
+            const char* vb = reinterpret_cast<const char*>(values + j * sv);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) k[i] = *reinterpret_cast<const u32x4*>(kb + at_k[i]);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) v[i] = *reinterpret_cast<const u32x4*>(vb + at_v[i]);
+        };
+        if (from >= end) return;
+        aim(end - from < kKeys ? int(end - from) : kKeys);
+        load(from);
+        for (int64_t j = from; j < end; j += kKeys) {
+            const int rows = end - j < kKeys ? int(end - j) : kKeys;
+            const int64_t next = j + kKeys;
+            __syncthreads();  // the block before has been read
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int at = tid + W * kWave * i;
+                *reinterpret_cast<u32x4*>(lk + (at / kVecs) * kKRow + 8 * (at % kVecs)) = k[i];
+                *reinterpret_cast<u32x4*>(lv + (at / kVecs) * kVRow + 8 * (at % kVecs)) = v[i];
+            }
+            __syncthreads();
+            if (next < end) {
+                if (end - next < kKeys) aim(int(end - next));
+                load(next);
+            }
+            f32x4 s[QT][KT];
+#pragma unroll
+            for (int x = 0; x < QT; ++x)
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) s[x][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int d = 0; d < ND / 2; ++d) {
+                    const bf16x8 a = *reinterpret_cast<const bf16x8*>(lk + (16 * kt + c) * kKRow + 32 * d + 8 * g);
+#pragma unroll
+                    for (int x = 0; x < QT; ++x)
+                        s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, w.q[x][d]), s[x][kt], 0, 0, 0);
+                }
+            if (rows < kKeys) {
+#pragma unroll
+                for (int x = 0; x < QT; ++x)
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (16 * kt + 4 * g + i >= rows) s[x][kt][i] = kNegInf;
+            }
+#pragma unroll
+            for (int x = 0; x < QT; ++x) softmax_step<KT, ND>(s[x], scale, w.m[x], w.l[x], w.acc[x]);
+#pragma unroll
+            for (int h = 0; h < KT / 2; ++h) {
+                bf16x8 p[QT];
+#pragma unroll
+                for (int x = 0; x < QT; ++x) p[x] = weights_operand(s[x][2 * h], s[x][2 * h + 1]);
+                const bf16_t* at = lv + (32 * h + 4 * g + (c >> 2)) * kVRow + 4 * (c & 3);
+#pragma unroll
+                for (int t = 0; t < ND; ++t) {
+                    const bf16x8 b = values_operand(at + 16 * t, kVRow);
+#pragma unroll
+                    for (int x = 0; x < QT; ++x) w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, p[x], w.acc[x][t], 0, 0, 0);
+                }
+            }
         }
     }
 };
@@ -274,65 +419,115 @@ constexpr size_t attn_lds() {
     return join > v ? join : v;
 }
 
-template <typename DT, int ND, int QT, int W>
+// What a workgroup takes, and where its rows' results go.
+struct AttnItem {
+    bool prefix;
+    int tile, hk, part, own, rows;  // own: the sequence of a suffix; rows: query rows that share its keys
+    int64_t n, plen, from, end;
+    int r, Hq, G, slot;
+
+    // false: nothing to do (a part past the length, which the joining kernel does not look at)
+    __device__ __forceinline__ bool of(const AttnArgs& a, const AttnPlan& plan, int item) {
+        // (all of these are below 2^31, so 32-bit divisions do)
+        Hq = int(a.Hq);
+        G = int(a.G);
+        const int Hkv = int(a.Hkv);
+        r = Hq / Hkv;
+        prefix = item < plan.prefix_items;
+        if (!prefix) item -= plan.prefix_items;
+        const int tiles = prefix ? plan.prefix_tiles : plan.suffix_tiles;
+        const int parts = prefix ? plan.prefix_parts : plan.suffix_parts;
+        tile = item % tiles;
+        item /= tiles;
+        hk = item % Hkv;
+        item /= Hkv;
+        part = item % parts;
+        item /= parts;
+        n = prefix ? item : item / G;
+        own = prefix ? 0 : item % G;
+        rows = prefix ? G * r : r;
+        plen = clamp_len(a.prefix_len, n, a.P);
+        const int64_t chunk = prefix ? plan.prefix_chunk : plan.suffix_chunk;
+        from = part * chunk;
+        end = prefix ? plen : clamp_len(a.suffix_len, n * G + own, a.S);
+        if (end > from + chunk) end = from + chunk;
+        slot = prefix ? part : (plan.whole ? 0 : plan.prefix_parts) + part;
+        return !plan.part_acc || from < end;
+    }
+    // Row of the outputs that row i of the item is.
+    __device__ __forceinline__ int64_t out_row(int i) const {
+        const int g = prefix ? i / r : own, h = hk * r + (prefix ? i % r : i);
+        return (n * G + g) * Hq + h;
+    }
+    template <typename DT>
+    __device__ __forceinline__ const DT* query(const AttnArgs& a, int i) const {
+        if (i >= rows) return nullptr;
+        const int g = prefix ? i / r : own, h = hk * r + (prefix ? i % r : i);
+        return reinterpret_cast<const DT*>(a.q) + n * a.at.q[0] + g * a.at.q[1] + h * a.at.q[2];
+    }
+    // Four dimensions of a row: to the part, or finished.
+    template <typename DT>
+    __device__ __forceinline__ void store(const AttnArgs& a, const AttnPlan& plan, int i, int d, f32x4 o, float m, float z) const {
+        const int64_t out = out_row(i);
+        if (plan.part_acc) {
+            const int64_t at = int64_t(slot) * a.N * G * Hq + out;
+            *reinterpret_cast<f32x4*>(plan.part_acc + at * a.D + d) = o;
+            if (d == 0) plan.part_ml[at] = float2{m, z};
+        } else {
+            finish<DT>(a, out, d, o, m, z);
+        }
+    }
+    template <typename DT>
+    static __device__ __forceinline__ void finish(const AttnArgs& a, int64_t out, int d, f32x4 o, float m, float z) {
+        o = z > 0.f ? o / z : f32x4{0.f, 0.f, 0.f, 0.f};
+        DT* p = reinterpret_cast<DT*>(a.o) + out * a.D + d;
+        if constexpr (sizeof(DT) == 4) {
+            *reinterpret_cast<f32x4*>(p) = o;
+        } else {
+            bf16x4 b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = static_cast<__bf16>(o[e]);
+            *reinterpret_cast<bf16x4*>(p) = b;
+        }
+        if (d == 0 && a.lse) a.lse[out] = z > 0.f ? kLn2 * (m + log2_fast(z)) : kNegInf;
+    }
+};
+
+// A negative scale is its amount with the queries' signs flipped, so that maxima are taken before
+// scaling; and not 0, so that a masked score stays -inf.
+template <typename DT>
+__device__ __forceinline__ uint32_t query_sign(float scale2) {
+    return scale2 < 0.f ? (sizeof(DT) == 4 ? 0x80000000u : 0x80008000u) : 0u;
+}
+__device__ __forceinline__ float score_scale(float scale2) { return fmaxf(fabsf(scale2), 1e-30f); }
+
+// Waves of the workgroup on the same 16 * QT rows and keys of their own.
+template <typename DT, int ND, int QT, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) void attn_kernel(AttnArgs a, AttnPlan plan, int first_item) {
     __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, W>()];
     __shared__ float s_m[W][kTileRows], s_l[W][kTileRows];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g4 = lane >> 4;
-    const int D = int(a.D), r = int(a.Hq / a.Hkv);
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int D = EXACT ? 16 * ND : int(a.D);
     bf16_t* lds = reinterpret_cast<bf16_t*>(s_mem) + wave * 32 * (16 * ND + 16);
-
-    // what this workgroup takes
-    int item = first_item + int(blockIdx.x);
-    const bool prefix = item < plan.prefix_items;
-    if (!prefix) item -= plan.prefix_items;
-    const int tiles = prefix ? plan.prefix_tiles : plan.suffix_tiles;
-    const int parts = prefix ? plan.prefix_parts : plan.suffix_parts;
-    const int tile = item % tiles;
-    item /= tiles;
-    const int64_t hk = item % a.Hkv;
-    item /= int(a.Hkv);
-    const int part = item % parts;
-    item /= parts;
-    const int64_t n = prefix ? item : item / a.G, own = prefix ? 0 : item % a.G;
-    const int64_t rows = prefix ? a.G * r : r;
-    const int64_t row0 = int64_t(tile) * kTileRows * QT;
-
-    const int64_t plen = clamp_len(a.prefix_len, n, a.P), slen = prefix ? 0 : clamp_len(a.suffix_len, n * a.G + own, a.S);
-    const int64_t chunk = prefix ? plan.prefix_chunk : plan.suffix_chunk;
-    const int64_t from = part * chunk;
-    int64_t end = prefix ? plen : slen;
-    if (end > from + chunk) end = from + chunk;
-    const int slot = prefix ? part : (plan.whole ? 0 : plan.prefix_parts) + part;
-    // (a part past the length: the joining kernel knows, and does not look at it)
-    if (plan.part_acc && from >= end) return;
-
-    auto row_of = [&](int64_t i, int64_t& g, int64_t& h) {
-        g = prefix ? i / r : own;
-        h = hk * r + (prefix ? i % r : i);
-    };
-    AttnWave<DT, ND, QT> w;
+    AttnItem it;
+    if (!it.of(a, plan, first_item + int(blockIdx.x))) return;
+    const int row0 = it.tile * kTileRows * QT;
+    AttnWave<DT, ND, QT, EXACT> w;
     w.clear();
 #pragma unroll
-    for (int x = 0; x < QT; ++x) {
-        const int64_t i = row0 + x * kTileRows + c;
-        const DT* p = nullptr;
-        if (i < rows) {
-            int64_t g, h;
-            row_of(i, g, h);
-            p = reinterpret_cast<const DT*>(a.q) + n * a.at.q[0] + g * a.at.q[1] + h * a.at.q[2];
-        }
-        w.load_query(x, p, D, lane);
-    }
-    const DT* kp = reinterpret_cast<const DT*>(a.kp) + n * a.at.kp[0] + hk * a.at.kp[2];
-    const DT* vp = reinterpret_cast<const DT*>(a.vp) + n * a.at.vp[0] + hk * a.at.vp[2];
-    const DT* ks = reinterpret_cast<const DT*>(a.ks) + n * a.at.ks[0] + own * a.at.ks[1] + hk * a.at.ks[3];
-    const DT* vs = reinterpret_cast<const DT*>(a.vs) + n * a.at.vs[0] + own * a.at.vs[1] + hk * a.at.vs[3];
-    if (prefix) {
-        w.template run<W>(kp, vp, a.at.kp[1], a.at.vp[1], from, end, D, a.scale2, lds, wave, lane);
-    } else {
-        if (plan.whole) w.template run<W>(kp, vp, a.at.kp[1], a.at.vp[1], 0, plen, D, a.scale2, lds, wave, lane);
-        w.template run<W>(ks, vs, a.at.ks[2], a.at.vs[2], from, end, D, a.scale2, lds, wave, lane);
+    for (int x = 0; x < QT; ++x)
+        w.load_query(x, it.template query<DT>(a, row0 + x * kTileRows + c), D, query_sign<DT>(a.scale2), lane);
+    // the prefix (for a suffix tile only if it takes all), then the suffix
+    for (int pass = it.prefix || plan.whole ? 0 : 1; pass < (it.prefix ? 1 : 2); ++pass) {
+        const bool first = pass == 0;
+        const DT* k = first ? reinterpret_cast<const DT*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2]
+                            : reinterpret_cast<const DT*>(a.ks) + it.n * a.at.ks[0] + it.own * a.at.ks[1] + it.hk * a.at.ks[3];
+        const DT* v = first ? reinterpret_cast<const DT*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2]
+                            : reinterpret_cast<const DT*>(a.vs) + it.n * a.at.vs[0] + it.own * a.at.vs[1] + it.hk * a.at.vs[3];
+        const bool all = first && !it.prefix;
+        w.template run<W>(k, v, first ? a.at.kp[1] : a.at.ks[2], first ? a.at.vp[1] : a.at.vs[2], all ? 0 : it.from,
+                          all ? it.plen : it.end, D, score_scale(a.scale2), lds, wave, lane);
     }
 
     // the waves join, tile by tile
@@ -354,8 +549,8 @@ __global__ __launch_bounds__(W * kWave) void attn_kernel(AttnArgs a, AttnPlan pl
         __syncthreads();
         for (int at = tid; at < kTileRows * 4 * ND; at += W * kWave) {
             const int i = at / (4 * ND), d = 4 * (at % (4 * ND));
-            const int64_t row = row0 + x * kTileRows + i;
-            if (row >= rows || d >= D) continue;
+            const int row = row0 + x * kTileRows + i;
+            if (row >= it.rows || d >= D) continue;
             float m = kNegInf;
 #pragma unroll
             for (int v = 0; v < W; ++v) m = fmaxf(m, s_m[v][i]);
@@ -367,53 +562,78 @@ __global__ __launch_bounds__(W * kWave) void attn_kernel(AttnArgs a, AttnPlan pl
                 z = fmaf(keep, s_l[v][i], z);
                 o += keep * *reinterpret_cast<const f32x4*>(join + (v * kTileRows + i) * kJoinRow + d);
             }
-            int64_t g, h;
-            row_of(row, g, h);
-            const int64_t out = (n * a.G + g) * a.Hq + h;
-            if (plan.part_acc) {
-                const int64_t at_part = int64_t(slot) * a.N * a.G * a.Hq + out;
-                *reinterpret_cast<f32x4*>(plan.part_acc + at_part * D + d) = o;
-                if (d == 0) plan.part_ml[at_part] = float2{m, z};
-            } else {
-                o = z > 0.f ? o / z : f32x4{0.f, 0.f, 0.f, 0.f};
-                DT* po = reinterpret_cast<DT*>(a.o) + out * D + d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) po[e] = narrow(o[e], DT{});
-                if (d == 0 && a.lse) a.lse[out] = z > 0.f ? kLn2 * (m + log2_fast(z)) : kNegInf;
-            }
+            it.template store<DT>(a, plan, row, d, o, m, z);
         }
     }
 }
 
-// Joins the parts of every row: 4 dimensions a lane.
+// Waves of the workgroup on rows of their own, 16 * QT each, and the same keys: prefixes of many rows.
+template <int ND, int QT, int W, bool EXACT>
+__global__ __launch_bounds__(W * kWave) void attn_shared_kernel(AttnArgs a, AttnPlan plan, int first_item) {
+    typedef SharedKeys<ND, QT, W, EXACT> Keys;
+    __shared__ __attribute__((aligned(16))) char s_mem[Keys::kLds];
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
+    const int D = EXACT ? 16 * ND : int(a.D);
+    AttnItem it;
+    if (!it.of(a, plan, first_item + int(blockIdx.x))) return;
+    const int row0 = (it.tile * W + (tid >> 6)) * kTileRows * QT;
+    AttnWave<bf16_t, ND, QT, EXACT> w;
+    w.clear();
+#pragma unroll
+    for (int x = 0; x < QT; ++x)
+        w.load_query(x, it.template query<bf16_t>(a, row0 + x * kTileRows + c), D, query_sign<bf16_t>(a.scale2), lane);
+    Keys::run(w, reinterpret_cast<const bf16_t*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2],
+              reinterpret_cast<const bf16_t*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2], a.at.kp[1], a.at.vp[1], it.from, it.end, D,
+              score_scale(a.scale2), reinterpret_cast<bf16_t*>(s_mem), tid);
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+        float l = w.l[x];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        const int row = row0 + x * kTileRows + c;
+        if (row >= it.rows) continue;
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+            if (EXACT || 16 * t + 4 * g4 < D) it.template store<bf16_t>(a, plan, row, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l);
+    }
+}
+
+// Joins the parts of a row: one row a workgroup, `groups` of D / 4 lanes (four dimensions each) on
+// every groups-th part.
 template <typename DT>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan) {
-    const int lanes = int(a.D / 4);  // of a row
-    const int64_t rows = a.N * a.G * a.Hq;
-    const int64_t out = int64_t(blockIdx.x) * (256 / lanes) + threadIdx.x / lanes;
-    const int d = 4 * (int(threadIdx.x) % lanes);
-    if (int(threadIdx.x) >= 256 / lanes * lanes || out >= rows) return;
-    const int64_t seq = out / a.Hq;
-    const int64_t plen = plan.whole ? 0 : clamp_len(a.prefix_len, seq / a.G, a.P), slen = clamp_len(a.suffix_len, seq, a.S);
+    __shared__ f32x4 s_o[256];
+    __shared__ float s_z[256];
+    const int lanes = int(a.D / 4), groups = 256 / lanes;
+    const int64_t rows = a.N * a.G * a.Hq, out = blockIdx.x;
+    const int group = int(threadIdx.x) / lanes, d = 4 * (int(threadIdx.x) % lanes);
+    const int seq = int(out) / int(a.Hq);
+    const int64_t plen = plan.whole ? 0 : clamp_len(a.prefix_len, seq / int(a.G), a.P), slen = clamp_len(a.suffix_len, seq, a.S);
     // parts that hold keys
-    const int np = plen > 0 ? int((plen + plan.prefix_chunk - 1) / plan.prefix_chunk) : 0;
-    const int ns = slen > 0 ? int((slen + plan.suffix_chunk - 1) / plan.suffix_chunk) : 0;
+    const int np = int((plen + plan.prefix_chunk - 1) / plan.prefix_chunk), ns = int((slen + plan.suffix_chunk - 1) / plan.suffix_chunk);
+    auto slot = [&](int i) { return (i < np ? i : plan.prefix_parts + i - np) * rows + out; };
     float m = kNegInf;
-    for (int i = 0; i < np + ns; ++i) m = fmaxf(m, plan.part_ml[(i < np ? i : plan.prefix_parts + i - np) * rows + out].x);
+    for (int i = int(threadIdx.x) & 63; i < np + ns; i += kWave) m = fmaxf(m, plan.part_ml[slot(i)].x);
+    m = max_lanes(m);
     float z = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < np + ns; ++i) {
-        const int64_t at = (i < np ? i : plan.prefix_parts + i - np) * rows + out;
-        const float2 ml = plan.part_ml[at];
-        const float keep = exp2_fast(ml.x - m);
-        z = fmaf(keep, ml.y, z);
-        o += keep * *reinterpret_cast<const f32x4*>(plan.part_acc + at * a.D + d);
+    if (group < groups) {
+        for (int i = group; i < np + ns; i += groups) {
+            const float2 ml = plan.part_ml[slot(i)];
+            const float keep = exp2_fast(ml.x - m);
+            z = fmaf(keep, ml.y, z);
+            o += keep * *reinterpret_cast<const f32x4*>(plan.part_acc + slot(i) * a.D + d);
+        }
     }
-    o = z > 0.f ? o / z : f32x4{0.f, 0.f, 0.f, 0.f};
-    DT* po = reinterpret_cast<DT*>(a.o) + out * a.D + d;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) po[e] = narrow(o[e], DT{});
-    if (d == 0 && a.lse) a.lse[out] = z > 0.f ? kLn2 * (m + log2_fast(z)) : kNegInf;
+    s_o[threadIdx.x] = o;
+    s_z[threadIdx.x] = z;
+    __syncthreads();
+    if (group != 0) return;
+    for (int i = 1; i < groups; ++i) {
+        o += s_o[threadIdx.x + i * lanes];
+        z += s_z[threadIdx.x + i * lanes];
+    }
+    AttnItem::finish<DT>(a, out, d, o, m, z);
 }
 
 }  // namespace rlcs

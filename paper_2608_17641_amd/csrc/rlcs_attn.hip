@@ -10,6 +10,7 @@ using namespace rlcs::host;
 namespace {
 
 constexpr int64_t kMaxHeadDim = 256;
+constexpr int64_t kMaxTokenStride = int64_t(1) << 24;
 
 // Whether the elements that an array's strides reach have 63-bit offsets: the sum of
 // (size - 1) * stride over its dimensions.
@@ -29,17 +30,23 @@ bool reachable(std::initializer_list<int64_t> sizes, const int64_t* strides) {
 // Keys of a part: no fewer than kMinChunk (a part of r rows costs r * D * 8 bytes written and read
 // again), and as many parts as give kWantItems workgroups.
 constexpr int64_t kMinChunk = 256;
-constexpr int64_t kWantItems = 1536;
+constexpr int64_t kWantItems = 512, kWantSuffixItems = 1536;
 // Calls of at most this many keys run as one kernel in which each sequence takes its prefix itself.
 constexpr int64_t kWholeKeys = 512;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Query tiles of sixteen a workgroup of the prefix takes: as many as there are rows for, up to what
-// the registers hold.
-int prefix_query_tiles(int64_t rows, int64_t D, bool bf16) {
-    const int most = D > 128 ? 1 : bf16 ? 4 : 2;
-    return rows <= 16 || most == 1 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+// How a workgroup takes the prefix's rows: bfloat16 rows of more than one tile go to waves of their own,
+// one or two tiles each, that share the keys; others to waves that share the rows.
+struct PrefixTiles {
+    bool shared;
+    int qt, rows;  // tiles a wave, rows a workgroup
+};
+PrefixTiles prefix_tiles(int64_t rows, int64_t D, bool bf16) {
+    if (rows <= kTileRows) return {false, 1, kTileRows};
+    if (!bf16) return D <= 128 ? PrefixTiles{false, 2, 2 * kTileRows} : PrefixTiles{false, 1, kTileRows};
+    const int qt = rows <= 4 * kTileRows || D > 128 ? 1 : 2;
+    return {true, qt, 4 * qt * kTileRows};
 }
 
 bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S, bool bf16) {
@@ -47,11 +54,11 @@ bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64
     p = AttnPlan{};
     p.whole = P + S <= kWholeKeys || P == 0;
     p.suffix_tiles = int32_t(ceil_div(r, kTileRows));
-    auto split = [](int64_t keys, int64_t base, int64_t& chunk, int32_t& parts) {
-        int64_t want = ceil_div(kWantItems, base), most = ceil_div(keys, kMinChunk);
+    auto split = [](int64_t keys, int64_t base, int64_t items, int64_t& chunk, int32_t& parts) {
+        int64_t want = ceil_div(items, base), most = ceil_div(keys, kMinChunk);
         if (want > most) want = most;
         if (want < 1) want = 1;
-        chunk = keys > 0 ? ceil_div(ceil_div(keys, want), 32) * 32 : 1;
+        chunk = keys > 0 ? ceil_div(ceil_div(keys, want), 64) * 64 : 1;
         parts = int32_t(keys > 0 ? ceil_div(keys, chunk) : 1);
     };
     const int64_t suffix_base = N * G * Hkv * p.suffix_tiles;
@@ -61,13 +68,13 @@ bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64
         p.suffix_parts = 1;
         p.suffix_chunk = S > 0 ? S : 1;
     } else if (S > 0 || P == 0) {
-        split(S, suffix_base, p.suffix_chunk, p.suffix_parts);
+        split(S, suffix_base, kWantSuffixItems, p.suffix_chunk, p.suffix_parts);
     }
     int64_t prefix_items = 0;
     if (!p.whole) {
-        p.prefix_tiles = int32_t(ceil_div(G * r, kTileRows * prefix_query_tiles(G * r, D, bf16)));
+        p.prefix_tiles = int32_t(ceil_div(G * r, prefix_tiles(G * r, D, bf16).rows));
         const int64_t base = N * Hkv * p.prefix_tiles;
-        split(P, base, p.prefix_chunk, p.prefix_parts);
+        split(P, base, kWantItems, p.prefix_chunk, p.prefix_parts);
         prefix_items = base * p.prefix_parts;
     }
     const int64_t items = prefix_items + suffix_base * p.suffix_parts;
@@ -85,27 +92,41 @@ size_t part_bytes(const AttnPlan& p, int64_t rows, int64_t D) {
 template <typename DT, int ND, int QT>
 void launch_items(const AttnArgs& a, const AttnPlan& p, int first, int count, hipStream_t s) {
     constexpr int W = ND > 8 ? 2 : 4;
-    if (count > 0) hipLaunchKernelGGL((attn_kernel<DT, ND, QT, W>), dim3(unsigned(count)), dim3(W * kWave), 0, s, a, p, first);
+    if (count <= 0) return;
+    const dim3 grid(static_cast<unsigned>(count)), block(W * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a, p, first);
+    else hipLaunchKernelGGL((attn_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a, p, first);
+}
+
+template <int ND, int QT>
+void launch_shared(const AttnArgs& a, const AttnPlan& p, int count, hipStream_t s) {
+    if (count <= 0) return;
+    const dim3 grid(static_cast<unsigned>(count)), block(4 * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_shared_kernel<ND, QT, 4, true>), grid, block, 0, s, a, p, 0);
+    else hipLaunchKernelGGL((attn_shared_kernel<ND, QT, 4, false>), grid, block, 0, s, a, p, 0);
 }
 
 template <typename DT, int ND>
 rlcs_status run_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
-    const int qt = prefix_query_tiles(a.G * (a.Hq / a.Hkv), a.D, sizeof(DT) == 2);
+    const PrefixTiles t = prefix_tiles(a.G * (a.Hq / a.Hkv), a.D, sizeof(DT) == 2);
     int done = 0;
-    if (qt > 1) {
-        done = p.prefix_items;
-        if constexpr (ND <= 8) {
-            if constexpr (sizeof(DT) == 2) {
-                if (qt == 4) launch_items<DT, ND, 4>(a, p, 0, done, s);
+    if constexpr (sizeof(DT) == 2) {
+        if (t.shared) {
+            done = p.prefix_items;
+            if (t.qt == 1) launch_shared<ND, 1>(a, p, done, s);
+            if constexpr (ND <= 8) {
+                if (t.qt == 2) launch_shared<ND, 2>(a, p, done, s);
             }
-            if (qt == 2) launch_items<DT, ND, 2>(a, p, 0, done, s);
+        }
+    } else if constexpr (ND <= 8) {
+        if (t.qt == 2) {
+            done = p.prefix_items;
+            launch_items<DT, ND, 2>(a, p, 0, done, s);
         }
     }
     launch_items<DT, ND, 1>(a, p, done, p.items - done, s);
-    if (p.part_acc) {
-        const int64_t rows = a.N * a.G * a.Hq, per = 256 / (a.D / 4);
-        hipLaunchKernelGGL((attn_join_kernel<DT>), dim3(unsigned(ceil_div(rows, per))), dim3(256), 0, s, a, p);
-    }
+    if (p.part_acc)
+        hipLaunchKernelGGL((attn_join_kernel<DT>), dim3(unsigned(a.N * a.G * a.Hq)), dim3(256), 0, s, a, p);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
 
@@ -153,7 +174,7 @@ rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* v
     if (layout) {
         a.at = *layout;
     } else {
-        const int64_t t = Hkv * D;  // (at most 2^24; a group's suffixes may be more than 63 bits count)
+        const int64_t t = Hkv * D;  // (refused from 2^24; a group's suffixes may be more than 63 bits count)
         if (S > 0 && G > INT64_MAX / 8 / S / t) return RLCS_ERR_INVALID_ARG;
         a.at = rlcs_attn_layout{{G * Hq * D, Hq * D, D}, {P * t, t, D}, {P * t, t, D}, {G * S * t, S * t, t, D}, {G * S * t, S * t, t, D}};
     }
@@ -163,6 +184,9 @@ rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* v
             if (s[i] % vec) return false;
         return true;
     };
+    // a block's rows lie within 31 bits of bytes of each other
+    if (a.at.kp[1] >= kMaxTokenStride || a.at.vp[1] >= kMaxTokenStride || a.at.ks[2] >= kMaxTokenStride || a.at.vs[2] >= kMaxTokenStride)
+        return RLCS_ERR_INVALID_ARG;
     if (!whole(a.at.q, 3) || !whole(a.at.kp, 3) || !whole(a.at.vp, 3) || !whole(a.at.ks, 4) || !whole(a.at.vs, 4))
         return RLCS_ERR_INVALID_ARG;
     if (!reachable({N, G, Hq}, a.at.q) || !reachable({N, P, Hkv}, a.at.kp) || !reachable({N, P, Hkv}, a.at.vp) ||
