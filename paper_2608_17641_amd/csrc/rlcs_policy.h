@@ -25,13 +25,15 @@ struct PolicyArgs {
 struct PolicyRow {
     float logp, ent, loss;
     float a, b, d;  // gradient: p (a log2 p + b) + 1{taken} d
+    bool some;      // a logit is not masked
 };
 
 template <bool LOSS>
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, float z, float s, float u_taken,
                                                 float logp_old, float adv, float w) {
     PolicyRow r{};
-    const bool some = z > 0.f;  // a logit that is not masked
+    const bool some = z > 0.f;
+    r.some = some;
     const float l2z = some ? log2_fast(z) : 0.f;
     r.logp = some ? kLn2 * (u_taken - l2z) : kNegInf;
     r.ent = some ? kLn2 * (l2z - s / z) : 0.f;
@@ -48,71 +50,182 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, float z, fl
     return r;
 }
 
-// One row per workgroup of W waves, element by element: any alignment, any length.
+// The row's inputs beside its logits; false: the row is left out.
+template <bool LOSS>
+__device__ __forceinline__ bool policy_inputs(const PolicyArgs& p, int64_t row, int64_t& a, float& w, float& old, float& adv) {
+    a = p.tokens[row];
+    w = LOSS && p.weight ? p.weight[row] : 1.f;
+    old = adv = 0.f;
+    const bool part = a >= 0 && a < p.V && w != 0.f;
+    if (LOSS && part) {
+        old = p.logp_old[row];
+        adv = p.adv[row];
+    }
+    return part;
+}
+
+template <bool LOSS>
+__device__ __forceinline__ void policy_outputs(const PolicyArgs& p, int64_t row, const PolicyRow& r) {
+    if (p.logp) p.logp[row] = r.logp;
+    if (p.ent) p.ent[row] = r.ent;
+    if (LOSS) p.loss[row] = r.loss;
+}
+
+// The gradient by a logit that is not the taken one.
+__device__ __forceinline__ float policy_gradient(const PolicyRow& r, const Scale& sc, float l2z, float x) {
+    const float l = fmaxf(sc.log2_weight(x) - l2z, kLog2Zero);
+    return exp2_fast(l) * fmaf(r.a, l, r.b);
+}
+
+// Rows of up to L * E logits, L lanes a row, E logits a lane in registers.
+template <typename DT, bool LOSS, int L, int E>
+__global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
+    const int lane = threadIdx.x & 63, i = lane % L;
+    const int64_t row = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
+    if (row >= p.M) return;  // (a whole group of L lanes leaves together)
+    const DT* x = reinterpret_cast<const DT*>(p.logits) + row * p.ld;
+    int64_t a;
+    float w, old, adv, v[E];
+    const bool part = policy_inputs<LOSS>(p, row, a, w, old, adv);
+    PolicyRow r{};
+    Scale sc{};
+    float l2z = 0.f;
+    if (part) {
+        float top = kNegInf;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = i + L * e < p.V ? widen(x[i + L * e]) : kNegInf;
+            top = fmaxf(top, v[e]);
+        }
+        const float taken = widen(x[a]);
+        top = max_lanes<L>(top);
+        sc = scale_of(top, kLog2e * p.inv_temp);
+        float z = 0.f, s = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float u = fmaxf(sc.log2_weight(v[e]), kLog2Zero), q = exp2_fast(u);  // (NaN of an empty row: -150)
+            z += q;
+            s = fmaf(q, u, s);
+        }
+        z = sum_lanes<L>(z);
+        s = sum_lanes<L>(s);
+        r = policy_row<LOSS>(p, z, s, sc.log2_weight(taken), old, adv, w);
+        l2z = log2_fast(z);
+    }
+    if (LOSS && p.grad) {
+        DT* g = reinterpret_cast<DT*>(p.grad) + row * p.ld_grad;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int64_t j = i + L * e;
+            if (j >= p.V) continue;
+            float d = part && r.some ? policy_gradient(r, sc, l2z, v[e]) : 0.f;
+            if (part && j == a) d += r.d;
+            g[j] = narrow(d, DT{});
+        }
+    }
+    if (i == 0) policy_outputs<LOSS>(p, row, r);
+}
+
+// Longer rows, one per workgroup of W waves: one pass for the statistics, each lane relative to its own
+// running maximum, and one that writes the gradient, for which the row comes out of the caches.
 template <typename DT, bool LOSS, int W>
 __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
-    __shared__ float s_a[W], s_b[W], s_c[W];
+    __shared__ float s_m[W], s_z[W], s_s[W];
+    constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x;
     const DT* x = reinterpret_cast<const DT*>(p.logits) + row * p.ld;
-    DT* g = p.grad ? reinterpret_cast<DT*>(p.grad) + row * p.ld_grad : nullptr;
-    const int64_t a = p.tokens[row];
-    const float w = LOSS && p.weight ? p.weight[row] : 1.f;
-    const bool part = a >= 0 && a < p.V && w != 0.f;
-    if (!part) {
-        if (tid == 0) {
-            if (p.logp) p.logp[row] = 0.f;
-            if (p.ent) p.ent[row] = 0.f;
-            if (LOSS) p.loss[row] = 0.f;
+    DT* g = LOSS && p.grad ? reinterpret_cast<DT*>(p.grad) + row * p.ld_grad : nullptr;
+    const int64_t vecs = (p.V + K - 1) / K;
+    int64_t a;
+    float w, old, adv;
+    if (!policy_inputs<LOSS>(p, row, a, w, old, adv)) {
+        if (tid == 0) policy_outputs<LOSS>(p, row, PolicyRow{});
+        if (g) {
+            const float zero[K] = {};
+            for (int64_t i = tid; i < vecs; i += kLanes) store_row_vec<DT>(g, i, p.V, zero);
         }
-        if (LOSS && g)
-            for (int64_t j = tid; j < p.V; j += W * kWave) g[j] = narrow(0.f, DT{});
         return;
     }
-    float top = kNegInf;
-    for (int64_t j = tid; j < p.V; j += W * kWave) top = fmaxf(top, widen(x[j]));
-    top = max_lanes(top);
-    if ((tid & 63) == 0) s_a[tid >> 6] = top;
-    __syncthreads();
+    const float c = kLog2e * p.inv_temp;
+    const float taken = widen(x[a]);
+    float top = kNegInf, z = 0.f, s = 0.f;
+    for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
+        RowVec<DT> v[U];
 #pragma unroll
-    for (int i = 0; i < W; ++i) top = fmaxf(top, s_a[i]);
-    const Scale sc = scale_of(top, kLog2e * p.inv_temp);
-    float z = 0.f, s = 0.f;
-    for (int64_t j = tid; j < p.V; j += W * kWave) {
-        const float u = sc.log2_weight(widen(x[j])), e = exp2_fast(u);
-        if (e > 0.f) {
-            z += e;
-            s = fmaf(e, u, s);
+        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, p.V);  // (past the end: -inf)
+        float t = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
+        if (t > top) {  // what there is so far, relative to the new maximum
+            const float d = fmaxf((top - t) * c, kLog2Zero), f = exp2_fast(d);
+            s = f * fmaf(d, z, s);
+            z *= f;
+            top = t;
         }
+        const Scale sc = scale_of(top, c);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const float l = fmaxf(sc.log2_weight(v[u].at(k)), kLog2Zero), e = exp2_fast(l);
+                z += e;
+                s = fmaf(e, l, s);
+            }
     }
+    // over the wave, then the workgroup: every lane's sums relative to one maximum
+    auto rebase = [&](float m) {
+        const float d = top == m ? 0.f : fmaxf((top - m) * c, kLog2Zero), f = exp2_fast(d);
+        s = f * fmaf(d, z, s);
+        z *= f;
+        top = m;
+    };
+    rebase(max_lanes(top));
     z = sum_lanes(z);
     s = sum_lanes(s);
     if ((tid & 63) == 0) {
-        s_b[tid >> 6] = z;
-        s_c[tid >> 6] = s;
+        s_m[tid >> 6] = top;
+        s_z[tid >> 6] = z;
+        s_s[tid >> 6] = s;
     }
-    const float u_taken = sc.log2_weight(widen(x[a]));
     __syncthreads();  // (and everyone has read the taken logit, which the gradient may overwrite)
-    z = s = 0.f;
+    float m = s_m[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) m = fmaxf(m, s_m[i]);
+    float z1 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        z += s_b[i];
-        s += s_c[i];
+        top = s_m[i];
+        z = s_z[i];
+        s = s_s[i];
+        rebase(m);
+        z1 += z;
+        s1 += s;
     }
-    const PolicyRow r = policy_row<LOSS>(p, z, s, u_taken, LOSS ? p.logp_old[row] : 0.f, LOSS ? p.adv[row] : 0.f, w);
-    if (LOSS && g) {
-        const float l2z = log2_fast(z);
-        for (int64_t j = tid; j < p.V; j += W * kWave) {
-            const float l = sc.log2_weight(widen(x[j])) - l2z, q = exp2_fast(l);
-            float v = q > 0.f ? q * fmaf(r.a, l, r.b) : 0.f;
-            if (j == a) v += r.d;
-            g[j] = narrow(v, DT{});
+    const Scale sc = scale_of(m, c);
+    const PolicyRow r = policy_row<LOSS>(p, z1, s1, sc.log2_weight(taken), old, adv, w);
+    if (tid == 0) policy_outputs<LOSS>(p, row, r);
+    if (!g) return;
+    const float l2z = log2_fast(z1);
+    for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
+        RowVec<DT> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, p.V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * kLanes;
+            float d[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) d[k] = r.some ? policy_gradient(r, sc, l2z, v[u].at(k)) : 0.f;
+            if (i == a / K) {
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+                    if (k == a % K) d[k] += r.d;
+            }
+            if (i < vecs) store_row_vec<DT>(g, i, p.V, d);
         }
-    }
-    if (tid == 0) {
-        if (p.logp) p.logp[row] = r.logp;
-        if (p.ent) p.ent[row] = r.ent;
-        if (LOSS) p.loss[row] = r.loss;
     }
 }
 

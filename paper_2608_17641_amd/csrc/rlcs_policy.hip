@@ -9,9 +9,21 @@ using namespace rlcs::host;
 
 namespace {
 
+template <typename DT, bool LOSS, int L, int E>
+void launch_small(const PolicyArgs& p, hipStream_t s) {
+    const int64_t rows = 4 * (kWave / L);
+    hipLaunchKernelGGL((policy_small_kernel<DT, LOSS, L, E>), dim3(unsigned((p.M + rows - 1) / rows)), dim3(4 * kWave), 0, s, p);
+}
+
 template <typename DT, bool LOSS>
 rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
-    hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, 4>), dim3(unsigned(p.M)), dim3(4 * kWave), 0, s, p);
+    if (p.V <= 32) launch_small<DT, LOSS, 8, 4>(p, s);
+    else if (p.V <= 64) launch_small<DT, LOSS, 16, 4>(p, s);
+    else if (p.V <= 128) launch_small<DT, LOSS, 32, 4>(p, s);
+    else if (p.V <= 256) launch_small<DT, LOSS, 64, 4>(p, s);
+    else if (p.V <= 512) launch_small<DT, LOSS, 64, 8>(p, s);
+    else if (p.V <= 1024) launch_small<DT, LOSS, 64, 16>(p, s);
+    else hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, 8>), dim3(unsigned(p.M)), dim3(8 * kWave), 0, s, p);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
 

@@ -38,15 +38,77 @@ __device__ __forceinline__ Scale scale_of(float top, float c) {
     return Scale{p, top * p};
 }
 
+// Over each group of L lanes, every lane with the result; the tree is fixed, so the sums are too.
+template <int L = kWave>
 __device__ __forceinline__ float sum_lanes(float v) {
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d);
+    for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
+template <int L = kWave>
 __device__ __forceinline__ float max_lanes(float v) {
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
+    for (int d = 1; d < L; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
     return v;
+}
+
+// Logarithms of weights are kept from -inf, whose product with a weight of 0 is NaN: 2^-150 is 0.
+constexpr float kLog2Zero = -150.f;
+
+// 16 bytes of a row at any element address (elements before `from` read nothing: `fill`).
+template <typename DT>
+struct RowVec {
+    static constexpr int K = 16 / sizeof(DT);
+    typedef typename std::conditional<sizeof(DT) == 4, u32x4_any, u32x4_any2>::type Any;
+    u32x4 w;
+    // Vector i of a row of V elements: whole, or the row's end with -inf after it.
+    __device__ __forceinline__ void load(const DT* x, int64_t i, int64_t V) {
+        if ((i + 1) * K <= V) {
+            w = *reinterpret_cast<const Any*>(x + i * K);
+        } else {
+            const uint32_t inf = sizeof(DT) == 4 ? 0xff800000u : 0xff80ff80u;
+            w = u32x4{inf, inf, inf, inf};
+            for (int k = 0; i * K + k < V; ++k) {
+                if constexpr (sizeof(DT) == 4) {
+                    const uint32_t e = reinterpret_cast<const uint32_t*>(x)[i * K + k];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) w[q] = k == q ? e : w[q];
+                } else {
+                    const uint32_t e = reinterpret_cast<const uint16_t*>(x)[i * K + k];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (k >> 1 == q) w[q] = (k & 1) ? (w[q] & 0xffffu) | (e << 16) : (w[q] & 0xffff0000u) | e;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int k) const {
+        if constexpr (sizeof(DT) == 4) return __uint_as_float(w[k]);
+        else return __uint_as_float((k & 1) ? (w[k >> 1] & 0xffff0000u) : (w[k >> 1] << 16));
+    }
+};
+
+// Writes vector i of a row of V elements.
+template <typename DT>
+__device__ __forceinline__ void store_row_vec(DT* x, int64_t i, int64_t V, const float (&v)[16 / sizeof(DT)]) {
+    constexpr int K = 16 / sizeof(DT);
+    u32x4 w;
+    if constexpr (sizeof(DT) == 4) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(v[k]);
+    } else {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            w[k] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(v[2 * k]), static_cast<__bf16>(v[2 * k + 1])});
+    }
+    if ((i + 1) * K <= V) {
+        __builtin_nontemporal_store(w, reinterpret_cast<typename RowVec<DT>::Any*>(x + i * K));
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (i * K + k < V) x[i * K + k] = narrow(v[k], DT{});
+    }
 }
 
 // Floats as unsigned keys in the same order (-0 as +0; NaN as -inf).
