@@ -6,10 +6,17 @@
 // normalisation nor the order of addition can move it.
 //
 // What top-k and top-p keep are the elements above a threshold in the order (logit falling, index
-// rising). The general way to it is a descent through the 32-bit keys of the logits, eight bits a
-// level: a histogram of the elements that share the prefix, by count for top-k, by mass for top-p,
-// names the next eight bits. Masses are integers (multiples of 2^-38 of the largest weight), so
-// that LDS atomics add them in any order to the same sum.
+// rising). Each row takes the shortest way to it:
+//   no filter    one pass: the race and the sum of weights.
+//   few kept     (a top-k of at most kFewest) the k-th largest of the lanes' maxima is a lower bound of the
+//                k-th logit; the elements from there on, little more than k, are ranked by comparing
+//                each with each.
+//   a mass       (top-p without top-k) a histogram of masses over 1/64 of an octave each; its
+//                crossing bin is ranked the same way, everything above it is kept.
+//   otherwise    a descent through the 32-bit keys of the logits, eight bits a level, by histograms of
+//                counts or masses.
+// Masses in histograms are integers (multiples of 2^-38 of the largest weight), so that LDS atomics
+// add them in any order to the same sum.
 #pragma once
 
 #include "rlcs_softmax.h"
@@ -54,9 +61,10 @@ __device__ __forceinline__ uint64_t race_entry(uint32_t key, uint32_t index) {
 }
 __device__ __forceinline__ uint32_t race_index(uint64_t e) { return ~uint32_t(e); }
 
+template <int L = kWave>
 __device__ __forceinline__ uint64_t max_lanes(uint64_t v) {
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
+    for (int d = 1; d < L; d <<= 1) {
         const uint64_t o = __shfl_xor(v, d);
         v = o > v ? o : v;
     }
@@ -121,6 +129,15 @@ __device__ __forceinline__ Crossing find_crossing(const uint64_t* bins, uint64_t
     return Crossing{kDigits - 1 - __shfl(at, first), __shfl(above, first), __shfl(own, first)};
 }
 
+__device__ __forceinline__ void sample_outputs(const SampleArgs& a, int64_t row, uint32_t token, float log2_p) {
+    a.tokens[row] = int32_t(token);
+    if (a.logp) a.logp[row] = kLn2 * log2_p;
+}
+__device__ __forceinline__ void sample_none(const SampleArgs& a, int64_t row) {  // every logit is masked
+    a.tokens[row] = -1;
+    if (a.logp) a.logp[row] = kNegInf;
+}
+
 // What of a row is kept: keys above `key`, and the first `quota` of those equal to it. `cut`: there
 // are more equal ones than that.
 struct Threshold {
@@ -141,9 +158,15 @@ struct RowView {
     }
     __device__ __forceinline__ float log2_weight(float v) const { return scale.log2_weight(v); }
     __device__ __forceinline__ uint64_t mass(float v) const {
-        return uint64_t(double(exp2_fast(log2_weight(v))) * kMassUnit);
+        return uint64_t(exp2_fast(log2_weight(v)) * float(kMassUnit));
     }
 };
+
+// The weight that min-p asks for (the largest logit always has it).
+template <typename DT>
+__device__ __forceinline__ float least_weight(const SampleRow& s, const RowView<DT>& r, float top) {
+    return s.min_p > 0.f ? fminf(s.min_p, 1.f) * exp2_fast(r.log2_weight(top)) : 0.f;
+}
 
 // The k-th largest logit (k < V).
 template <typename DT, int W>
@@ -212,41 +235,16 @@ __device__ Threshold descend_mass(const RowView<DT>& r, Threshold t, float p, ui
     return Threshold{prefix, quota, quota < count || (prefix == t.key && t.cut)};
 }
 
-// One row per workgroup of W waves, element by element: any alignment, length and settings.
+// The general way: one row, any settings, by a workgroup of W waves.
 template <typename DT, int W>
-__global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
-    __shared__ uint64_t s_bins[kDigits];
-    __shared__ uint64_t s_slots[W];
+__device__ void sample_general(const SampleArgs& a, const SampleRow& s, RowView<DT> r, const float* noise, float top, int64_t row,
+                               uint64_t* bins, uint64_t* slots) {
     constexpr int kLanes = W * kWave;
-    const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
-    const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
-
-    uint64_t best = 0;
-    for (int64_t j = tid; j < a.V; j += kLanes) {
-        const uint64_t e = race_entry(order_key(r.logit(j)), uint32_t(j));
-        best = e > best ? e : best;
-    }
-    best = max_group<W>(best, s_slots);
-    const float top = r.logit(race_index(best));
-    const SampleRow s = sample_row(a, row);
-    const float c = kLog2e / s.temperature;
-    const bool greedy = !(s.temperature > 0.f) || !(c < __builtin_inff());
-    r.scale = scale_of(top, c);
-    if (top == kNegInf || greedy) {
-        if (tid == 0) {
-            a.tokens[row] = top == kNegInf ? -1 : int32_t(race_index(best));
-            if (a.logp) a.logp[row] = top == kNegInf ? kNegInf : 0.f;
-        }
-        return;
-    }
     Threshold t{0u, ~0ull, false};
-    if (s.top_k < a.V) t = descend_count<DT, W>(r, uint64_t(s.top_k), s_bins);
-    if (s.top_p < 1.f) t = descend_mass<DT, W>(r, t, s.top_p, s_bins);
-    // (the largest logit is always kept)
-    const float least = s.min_p > 0.f ? fminf(s.min_p, 1.f) * exp2_fast(r.log2_weight(top)) : 0.f;
-
+    if (s.top_k < a.V) t = descend_count<DT, W>(r, uint64_t(s.top_k), bins);
+    if (s.top_p < 1.f) t = descend_mass<DT, W>(r, t, s.top_p, bins);
+    const float least = least_weight(s, r, top);
     float z = 0.f;
     uint64_t winner = 0, ties = 0;
     for (int64_t j0 = 0; j0 < a.V; j0 += kLanes) {
@@ -258,13 +256,13 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
             const bool tie = keep && key == t.key;
             const uint64_t votes = __ballot(tie);
             __syncthreads();
-            if (lane == 0) s_slots[wave] = __popcll(votes);
+            if (lane == 0) slots[wave] = __popcll(votes);
             __syncthreads();
             uint64_t before = ties + __popcll(votes & ((1ull << lane) - 1));
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                if (i < wave) before += s_slots[i];
-                ties += s_slots[i];
+                if (i < wave) before += slots[i];
+                ties += slots[i];
             }
             keep = keep && (!tie || before < t.quota);
         }
@@ -276,13 +274,445 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
         const uint64_t e = race_entry(order_key(score), uint32_t(j));
         winner = e > winner ? e : winner;
     }
-    winner = max_group<W>(winner, s_slots);
-    z = sum_group<W>(z, s_slots);
-    if (tid == 0) {
-        const uint32_t token = race_index(winner);
-        a.tokens[row] = int32_t(token);
-        if (a.logp) a.logp[row] = kLn2 * (r.log2_weight(r.logit(token)) - log2_fast(z));
+    winner = max_group<W>(winner, slots);
+    z = sum_group<W>(z, slots);
+    if (tid == 0) sample_outputs(a, row, race_index(winner), r.log2_weight(r.logit(race_index(winner))) - log2_fast(z));
+}
+
+constexpr int kList = 512;       // elements that can be ranked
+constexpr int kFewest = 256;     // top-k that goes by lanes' maxima
+constexpr int kMassBins = 2048;  // 64 an octave of weight: down to 2^-32 of the largest
+constexpr float kBinsPerOctave = 64.f;
+
+// f(value, index) for every element of a row, four vectors a lane under way.
+template <typename DT, int W, class F>
+__device__ __forceinline__ void each_element(const DT* x, int64_t V, F&& f) {
+    constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
+    const int64_t vecs = (V + K - 1) / K;
+    for (int64_t i0 = threadIdx.x; i0 < vecs; i0 += U * kLanes) {
+        RowVec<DT> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, V);  // (past the end: -inf)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) f(fmaxf(v[u].at(k), kNegInf), uint32_t((i0 + u * kLanes) * K + k));  // (NaN as -inf)
     }
+}
+
+template <int W>
+struct SampleShared {
+    union {
+        uint64_t bins[kMassBins];
+        float maxima[W * kWave];
+    };
+    uint64_t list[kList], sorted[kList];
+    uint64_t slots[W];
+    float slots_f[2 * W];
+    uint32_t count, pivot;
+    float top;
+};
+
+template <int W>
+__device__ __forceinline__ float max_group_f(float v, float* slots) {
+    v = max_lanes(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = slots[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v = fmaxf(v, slots[i]);
+    return v;
+}
+
+// list[0, n) into `sorted`, largest first.
+template <int W>
+__device__ __forceinline__ void rank_list(const uint64_t* list, uint64_t* sorted, int n) {
+    for (int i = threadIdx.x; i < n; i += W * kWave) {
+        const uint64_t e = list[i];
+        int rank = 0;
+        int j = 0;
+        for (; j + 4 <= n; j += 4)
+            rank += int(list[j] > e) + int(list[j + 1] > e) + int(list[j + 2] > e) + int(list[j + 3] > e);
+        for (; j < n; ++j) rank += int(list[j] > e);
+        sorted[rank] = e;
+    }
+    __syncthreads();
+}
+
+// What a wave finds among sorted elements: of the first `most`, in their order, those before which the
+// weights' sum (from `above` on) is below `target` and that weigh `least`.
+struct Drawn {
+    uint64_t winner;
+    float z;
+};
+template <typename DT>
+__device__ __forceinline__ Drawn draw_sorted(const uint64_t* sorted, int most, const RowView<DT>& r, const float* noise, float above,
+                                             float target, float least, bool first_kept) {
+    const int lane = threadIdx.x & 63;
+    Drawn d{0, 0.f};
+    for (int i0 = 0; i0 < most; i0 += kWave) {
+        const int i = i0 + lane;
+        const bool in = i < most;
+        const uint64_t e = in ? sorted[i] : 0;
+        const uint32_t j = race_index(e);
+        const float v = key_value(uint32_t(e >> 32)), u = in ? r.log2_weight(v) : kNegInf, w = in ? exp2_fast(u) : 0.f;
+        float upto = w;  // inclusive
+#pragma unroll
+        for (int step = 1; step < kWave; step <<= 1) {
+            const float o = __shfl_up(upto, step);
+            if (lane >= step) upto += o;
+        }
+        float before = __shfl_up(upto, 1);
+        before = above + (lane == 0 ? 0.f : before);
+        const bool keep = in && (before < target || (first_kept && i == 0)) && w >= least;
+        if (keep) {
+            d.z += w;
+            const float score = noise ? u - log2_fast(noise[j]) : v;
+            const uint64_t x = race_entry(order_key(score), j);
+            d.winner = x > d.winner ? x : d.winner;
+        }
+        above += __shfl(upto, kWave - 1);
+        if (!(above < target)) break;
+    }
+    d.winner = max_lanes(d.winner);
+    d.z = sum_lanes(d.z);
+    return d;
+}
+
+// One row per workgroup of W waves.
+template <typename DT, int W>
+__global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
+    __shared__ SampleShared<W> sh;
+    constexpr int kLanes = W * kWave;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
+    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
+    const SampleRow s = sample_row(a, row);
+    const float c = kLog2e / s.temperature;
+    const bool greedy = !(s.temperature > 0.f) || !(c < __builtin_inff());
+    const bool by_k = s.top_k < a.V, by_p = s.top_p < 1.f, by_min = s.min_p > 0.f;
+
+    if (greedy || (!by_k && !by_p && !by_min)) {
+        // one pass: the race, and the sum of weights relative to the lane's running maximum
+        float top = kNegInf, z = 0.f, best = kNegInf;
+        uint32_t at = ~0u;  // (none)
+        constexpr int K = RowVec<DT>::K, U = 4;
+        const bool race = noise && !greedy;
+        const int64_t vecs = (a.V + K - 1) / K;
+        for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
+            RowVec<DT> v[U];
+            RowVec<float> e[U][K / 4];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                v[u].load(r.x, i0 + u * kLanes, a.V);  // (past the end: -inf)
+                if (race)
+#pragma unroll
+                    for (int q = 0; q < K / 4; ++q) e[u][q].load(noise, (i0 + u * kLanes) * (K / 4) + q, a.V);
+            }
+            float t = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
+            if (t > top) {
+                z *= exp2_fast((top - t) * c);
+                top = t;
+            }
+            const Scale sc = scale_of(top, c);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const float x = fmaxf(v[u].at(k), kNegInf);  // (NaN as -inf)
+                    z += fmaxf(exp2_fast(sc.log2_weight(x)), 0.f);  // (NaN while all is -inf: 0)
+                    const float score = race ? fmaxf(fmaf(x, c, -log2_fast(e[u][k / 4].at(k % 4))), kNegInf) : x;
+                    if (x > kNegInf && (score > best || at == ~0u)) {
+                        best = score;
+                        at = uint32_t((i0 + u * kLanes) * K + k);
+                    }
+                }
+        }
+        const float all_top = max_group_f<W>(top, sh.slots_f);
+        if (all_top == kNegInf) {
+            if (tid == 0) sample_none(a, row);
+            return;
+        }
+        r.scale = scale_of(all_top, c);
+        if (greedy || r.scale.c == c) {
+            z = top == kNegInf ? 0.f : z * exp2_fast((top - all_top) * c);
+            z = sum_group<W>(z, sh.slots);
+            const uint64_t winner = max_group<W>(at == ~0u ? 0 : race_entry(order_key(best), at), sh.slots);
+            if (tid == 0) {
+                const uint32_t j = race_index(winner);
+                sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(z));
+            }
+            return;
+        }
+        // (scores overflowed: logits beyond 10^38 / c. The general way takes them relative to the largest.)
+        sample_general<DT, W>(a, s, r, noise, all_top, row, sh.bins, sh.slots);
+        return;
+    }
+
+    if (by_k && s.top_k <= kFewest) {
+        float top = kNegInf;
+        each_element<DT, W>(r.x, a.V, [&](float v, uint32_t) { top = fmaxf(top, v); });
+        sh.maxima[tid] = top;
+        if (tid == 0) sh.count = 0;
+        __syncthreads();
+        if (tid < kWave) {
+            // the largest 16-bit prefix of a key that k lanes' maxima reach; of fours of lanes while there
+            // are plenty (fewer to compare, hardly more elements)
+            constexpr int E = W;
+            uint32_t key[E];
+            float all = kNegInf;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float m = sh.maxima[lane + kWave * i];
+                all = fmaxf(all, m);
+                key[i] = m > kNegInf ? order_key(m) >> 16 : 0u;
+            }
+            int used = E;
+            if constexpr (E % 4 == 0) {
+                if (s.top_k <= kLanes / 8) {
+#pragma unroll
+                    for (int i = 0; i < E / 4; ++i) {
+                        const uint32_t x = key[4 * i] > key[4 * i + 1] ? key[4 * i] : key[4 * i + 1];
+                        const uint32_t y = key[4 * i + 2] > key[4 * i + 3] ? key[4 * i + 2] : key[4 * i + 3];
+                        key[i] = x > y ? x : y;
+                    }
+                    used = E / 4;
+                }
+            }
+            uint32_t prefix = 0;
+            for (int bit = 15; bit >= 0; --bit) {
+                const uint32_t tried = prefix | (1u << bit);
+                int reached = 0;
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (i < used) reached += __popcll(__ballot(key[i] >= tried));
+                if (reached >= s.top_k) prefix = tried;
+            }
+            all = max_lanes(all);
+            if (lane == 0) {
+                sh.pivot = prefix << 16;
+                sh.top = all;
+            }
+        }
+        __syncthreads();
+        top = sh.top;
+        if (top == kNegInf) {
+            if (tid == 0) sample_none(a, row);
+            return;
+        }
+        r.scale = scale_of(top, c);
+        const float from = sh.pivot > order_key(kNegInf) ? key_value(sh.pivot) : kNegInf;
+        each_element<DT, W>(r.x, a.V, [&](float v, uint32_t j) {
+            if (v >= from && v > kNegInf) {
+                const uint32_t i = atomicAdd(&sh.count, 1u);
+                if (i < kList) sh.list[i] = race_entry(order_key(v), j);
+            }
+        });
+        __syncthreads();
+        const int n = int(sh.count);
+        if (n > kList) {
+            sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
+            return;
+        }
+        rank_list<W>(sh.list, sh.sorted, n);
+        if (tid >= kWave) return;
+        const int most = n < s.top_k ? n : int(s.top_k);
+        float target = __builtin_inff();
+        if (by_p) {
+            float sum = 0.f;
+            for (int i = lane; i < most; i += kWave) sum += exp2_fast(r.log2_weight(key_value(uint32_t(sh.sorted[i] >> 32))));
+            target = s.top_p * sum_lanes(sum);
+        }
+        const Drawn d = draw_sorted(sh.sorted, most, r, noise, 0.f, target, least_weight(s, r, top), true);
+        if (lane == 0) sample_outputs(a, row, race_index(d.winner), r.log2_weight(r.logit(race_index(d.winner))) - log2_fast(d.z));
+        return;
+    }
+
+    // the largest logit and the sum of weights
+    float top = kNegInf, z = 0.f;
+    {
+        constexpr int K = RowVec<DT>::K, U = 4;
+        const int64_t vecs = (a.V + K - 1) / K;
+        for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
+            RowVec<DT> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u].load(r.x, i0 + u * kLanes, a.V);
+            float t = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
+            if (t > top) {
+                z *= exp2_fast((top - t) * c);
+                top = t;
+            }
+            const Scale sc = scale_of(top, c);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) z += fmaxf(exp2_fast(sc.log2_weight(v[u].at(k))), 0.f);
+        }
+    }
+    const float own_top = top;
+    top = max_group_f<W>(top, sh.slots_f);
+    if (top == kNegInf) {
+        if (tid == 0) sample_none(a, row);
+        return;
+    }
+    r.scale = scale_of(top, c);
+    const float least = least_weight(s, r, top);
+    if (by_k || r.scale.c != c) {
+        sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
+        return;
+    }
+    z = own_top == kNegInf ? 0.f : z * exp2_fast((own_top - top) * c);
+    z = sum_group<W>(z, sh.slots);
+
+    // without top-p everything is above the crossing bin
+    int cross = kMassBins;
+    float above = 0.f;
+    const float target = by_p ? s.top_p * z : __builtin_inff();
+    if (by_p) {
+        // the smallest elements, of less than 1 - p in all, cannot be in: at most V of them below this
+        const float low = log2_fast(0.99f * (1.f - s.top_p) * z / float(a.V));
+        for (int i = tid; i < kMassBins; i += kLanes) sh.bins[i] = 0;
+        if (tid == 0) sh.count = 0;
+        __syncthreads();
+        each_element<DT, W>(r.x, a.V, [&](float v, uint32_t) {
+            const float u = r.log2_weight(v);
+            const int bin = int(-u * kBinsPerOctave);
+            if (u >= low && bin < kMassBins)
+                atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[bin < 0 ? 0 : bin]), (unsigned long long)(r.mass(v)));
+        });
+        __syncthreads();
+        // its first bin at which the sum reaches p of the mass (at least the largest element's)
+        const uint64_t want0 = uint64_t(ceil(double(target) * kMassUnit)), want = want0 < 1 ? 1 : want0;
+        {
+            constexpr int kEach = kMassBins / kLanes;  // bins a lane, in order
+            uint64_t bin[kEach], sum = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                bin[i] = sh.bins[tid * kEach + i];
+                sum += bin[i];
+            }
+            uint64_t upto = sum;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const uint64_t o = __shfl_up(upto, d);
+                if (lane >= d) upto += o;
+            }
+            if (lane == kWave - 1) sh.slots[tid >> 6] = upto;
+            if (tid == 0) sh.pivot = kMassBins;
+            __syncthreads();
+            uint64_t before = upto - sum;
+#pragma unroll
+            for (int i = 0; i < W; ++i) before += i < (tid >> 6) ? sh.slots[i] : 0;
+            if (before < want && before + sum >= want) {  // one lane's
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    if (found) continue;
+                    if (before + bin[i] >= want) {
+                        found = true;
+                        sh.pivot = uint32_t(tid * kEach + i);
+                        sh.top = float(double(before) / kMassUnit);
+                    }
+                    before += bin[i];
+                }
+            }
+        }
+        __syncthreads();
+        cross = int(sh.pivot);
+        above = sh.top;
+        if (cross == kMassBins) {  // (so flat that the cut lies below 2^-32)
+            sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
+            return;
+        }
+    }
+    float zk = 0.f;
+    uint64_t winner = 0;
+    each_element<DT, W>(r.x, a.V, [&](float v, uint32_t j) {
+        const float u = r.log2_weight(v), w = exp2_fast(u);
+        if (!(w >= least) || !(v > kNegInf)) return;
+        const int bin = by_p ? int(fminf(fmaxf(-u * kBinsPerOctave, 0.f), float(kMassBins))) : 0;
+        if (bin > cross) return;
+        if (bin == cross) {
+            const uint32_t i = atomicAdd(&sh.count, 1u);
+            if (i < kList) sh.list[i] = race_entry(order_key(v), j);
+            return;
+        }
+        zk += w;
+        const float score = noise ? u - log2_fast(noise[j]) : v;
+        const uint64_t e = race_entry(order_key(score), j);
+        winner = e > winner ? e : winner;
+    });
+    zk = sum_group<W>(zk, sh.slots);
+    winner = max_group<W>(winner, sh.slots);
+    if (by_p) {
+        __syncthreads();
+        const int n = int(sh.count);
+        if (n > kList) {
+            sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
+            return;
+        }
+        rank_list<W>(sh.list, sh.sorted, n);
+        if (tid >= kWave) return;
+        const Drawn d = draw_sorted(sh.sorted, n, r, noise, above, target, least, true);
+        zk += d.z;
+        winner = d.winner > winner ? d.winner : winner;
+    }
+    if (tid == 0) sample_outputs(a, row, race_index(winner), r.log2_weight(r.logit(race_index(winner))) - log2_fast(zk));
+}
+
+// Rows of up to L * E logits, L lanes a row, no filters.
+template <typename DT, int L, int E>
+__global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
+    const int lane = threadIdx.x & 63, i = lane % L;
+    const int64_t row = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
+    if (row >= a.M) return;  // (a whole group of L lanes leaves together)
+    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
+    const SampleRow s = sample_row(a, row);
+    const float c = kLog2e / s.temperature;
+    const bool greedy = !(s.temperature > 0.f) || !(c < __builtin_inff());
+    float v[E], n[E], top = kNegInf;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const bool in = i + L * e < a.V;
+        v[e] = in ? r.logit(i + L * e) : kNegInf;
+        n[e] = in && noise && !greedy ? noise[i + L * e] : 1.f;
+        top = fmaxf(top, v[e]);
+    }
+    top = max_lanes<L>(top);
+    if (top == kNegInf) {
+        if (i == 0) sample_none(a, row);
+        return;
+    }
+    r.scale = scale_of(top, c);
+    float z = 0.f;
+    uint64_t winner = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float u = r.log2_weight(v[e]);
+        z += exp2_fast(u);
+        const float score = noise && !greedy ? u - log2_fast(n[e]) : v[e];
+        const uint64_t x = v[e] > kNegInf ? race_entry(order_key(score), uint32_t(i + L * e)) : 0;
+        winner = x > winner ? x : winner;
+    }
+    z = sum_lanes<L>(z);
+    winner = max_lanes<L>(winner);
+    const uint32_t j = race_index(winner);
+    float won = kNegInf;  // the winner's logit, from the lane that has it
+#pragma unroll
+    for (int e = 0; e < E; ++e) won = uint32_t(i + L * e) == j ? v[e] : won;
+    won = max_lanes<L>(won);
+    if (i == 0) sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(won) - log2_fast(z));
 }
 
 }  // namespace rlcs

@@ -7,9 +7,30 @@ using namespace rlcs::host;
 
 namespace {
 
+template <typename DT, int L, int E>
+void launch_small(const SampleArgs& a, hipStream_t s) {
+    const int64_t rows = 4 * (kWave / L);
+    hipLaunchKernelGGL((sample_small_kernel<DT, L, E>), dim3(unsigned((a.M + rows - 1) / rows)), dim3(4 * kWave), 0, s, a);
+}
+
 template <typename DT>
 rlcs_status run_sample(const SampleArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((sample_rows_kernel<DT, 4>), dim3(unsigned(a.M)), dim3(4 * kWave), 0, s, a);
+    // no row has a filter, as far as the host can tell
+    const bool open = !a.top_k && !a.top_p && !a.min_p && (a.all_top_k <= 0 || a.all_top_k >= a.V) && a.all_top_p >= 1.f &&
+                      !(a.all_min_p > 0.f);
+    if (open && a.V <= 1024) {
+        if (a.V <= 32) launch_small<DT, 8, 4>(a, s);
+        else if (a.V <= 64) launch_small<DT, 16, 4>(a, s);
+        else if (a.V <= 128) launch_small<DT, 32, 4>(a, s);
+        else if (a.V <= 256) launch_small<DT, 64, 4>(a, s);
+        else launch_small<DT, 64, 16>(a, s);
+    } else if (a.V <= 256) {
+        hipLaunchKernelGGL((sample_rows_kernel<DT, 1>), dim3(unsigned(a.M)), dim3(kWave), 0, s, a);
+    } else if (a.V <= 8192) {
+        hipLaunchKernelGGL((sample_rows_kernel<DT, 4>), dim3(unsigned(a.M)), dim3(4 * kWave), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((sample_rows_kernel<DT, 16>), dim3(unsigned(a.M)), dim3(16 * kWave), 0, s, a);
+    }
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
 
