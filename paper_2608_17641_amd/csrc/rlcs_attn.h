@@ -614,7 +614,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
     auto slot = [&](int i) { return (i < np ? i : plan.prefix_parts + i - np) * rows + out; };
     float m = kNegInf;
     for (int i = int(threadIdx.x) & 63; i < np + ns; i += kWave) m = fmaxf(m, plan.part_ml[slot(i)].x);
-    m = max_lanes(m);
+    m = max_wave(m);
     float z = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     if (group < groups) {

@@ -182,9 +182,9 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
         z *= f;
         top = m;
     };
-    rebase(max_lanes(top));
-    z = sum_lanes(z);
-    s = sum_lanes(s);
+    rebase(max_wave(top));
+    z = sum_wave(z);
+    s = sum_wave(s);
     if ((tid & 63) == 0) {
         s_m[tid >> 6] = top;
         s_z[tid >> 6] = z;

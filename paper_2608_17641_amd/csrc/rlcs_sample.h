@@ -45,6 +45,11 @@ struct SampleRow {
     int64_t top_k;  // >= V: all
 };
 
+// log2(e) / temperature, or infinity for a temperature of 0 (or none, or too small to divide by).
+__device__ __forceinline__ float sample_scale(const SampleRow& s) {
+    return s.temperature > 0.f ? kLog2e / s.temperature : __builtin_inff();
+}
+
 __device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, int64_t row) {
     SampleRow r;
     r.temperature = a.temperature ? a.temperature[row] : a.all_temperature;
@@ -61,7 +66,7 @@ __device__ __forceinline__ uint64_t race_entry(uint32_t key, uint32_t index) {
 }
 __device__ __forceinline__ uint32_t race_index(uint64_t e) { return ~uint32_t(e); }
 
-template <int L = kWave>
+template <int L>
 __device__ __forceinline__ uint64_t max_lanes(uint64_t v) {
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) {
@@ -73,7 +78,7 @@ __device__ __forceinline__ uint64_t max_lanes(uint64_t v) {
 // Over the workgroup; every lane has the result. `slots`: one word a wave.
 template <int W>
 __device__ __forceinline__ uint64_t max_group(uint64_t v, uint64_t* slots) {
-    v = max_lanes(v);
+    v = max_wave(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -84,7 +89,7 @@ __device__ __forceinline__ uint64_t max_group(uint64_t v, uint64_t* slots) {
 }
 template <int W>
 __device__ __forceinline__ float sum_group(float v, uint64_t* slots) {
-    v = sum_lanes(v);
+    v = sum_wave(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = __float_as_uint(v);
     __syncthreads();
@@ -237,7 +242,7 @@ __device__ Threshold descend_mass(const RowView<DT>& r, Threshold t, float p, ui
 
 // The general way: one row, any settings, by a workgroup of W waves.
 template <typename DT, int W>
-__device__ void sample_general(const SampleArgs& a, const SampleRow& s, RowView<DT> r, const float* noise, float top, int64_t row,
+__device__ __forceinline__ void sample_general(const SampleArgs& a, const SampleRow& s, RowView<DT> r, const float* noise, float top, int64_t row,
                                uint64_t* bins, uint64_t* slots) {
     constexpr int kLanes = W * kWave;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -284,21 +289,68 @@ constexpr int kFewest = 256;     // top-k that goes by lanes' maxima
 constexpr int kMassBins = 2048;  // 64 an octave of weight: down to 2^-32 of the largest
 constexpr float kBinsPerOctave = 64.f;
 
-// f(value, index) for every element of a row, four vectors a lane under way.
-template <typename DT, int W, class F>
-__device__ __forceinline__ void each_element(const DT* x, int64_t V, F&& f) {
-    constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
-    const int64_t vecs = (V + K - 1) / K;
-    for (int64_t i0 = threadIdx.x; i0 < vecs; i0 += U * kLanes) {
-        RowVec<DT> v[U];
+// A row as its workgroup walks it, U vectors a lane at a time: f(vectors, index of the first; the
+// others follow kLanes vectors apart). Past the row's end vectors are -inf. With ONE the row is no longer
+// than that, and stays in registers.
+template <typename DT, int W, int U, bool ONE>
+struct RowWalk {
+    static constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
+    const DT* x;
+    int64_t V;
+    RowVec<DT> kept[ONE ? U : 1];
+
+    __device__ __forceinline__ void read(RowVec<DT> (&v)[U], int64_t i0) const {
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, V);  // (past the end: -inf)
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int k = 0; k < K; ++k) f(fmaxf(v[u].at(k), kNegInf), uint32_t((i0 + u * kLanes) * K + k));  // (NaN as -inf)
+        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, V);
     }
-}
+    __device__ __forceinline__ RowWalk(const DT* row, int64_t n) : x(row), V(n) {
+        if constexpr (ONE) read(kept, threadIdx.x);
+    }
+    template <class F>
+    __device__ __forceinline__ void chunks(F&& f) const {
+        if constexpr (ONE) {
+            f(kept, int64_t(threadIdx.x));
+        } else {
+            const int64_t vecs = (V + K - 1) / K;
+            for (int64_t i0 = threadIdx.x; i0 < vecs; i0 += U * kLanes) {
+                RowVec<DT> v[U];
+                read(v, i0);
+                f(v, i0);
+            }
+        }
+    }
+    // f(value, index) for every element, NaN as -inf
+    template <class F>
+    __device__ __forceinline__ void each(F&& f) const {
+        chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) f(fmaxf(v[u].at(k), kNegInf), uint32_t((i0 + u * kLanes) * K + k));
+        });
+    }
+    // The lane's largest element, and the sum of its weights relative to that. NaN as -inf.
+    __device__ __forceinline__ void statistics(float c, float& top, float& z) const {
+        top = kNegInf;
+        z = 0.f;
+        chunks([&](const RowVec<DT>(&v)[U], int64_t) {
+            float t = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
+            if (t > top) {
+                z *= exp2_fast((top - t) * c);
+                top = t;
+            }
+            const Scale sc = scale_of(top, c);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) z += fmaxf(exp2_fast(sc.log2_weight(v[u].at(k))), 0.f);
+        });
+    }
+};
 
 template <int W>
 struct SampleShared {
@@ -315,7 +367,7 @@ struct SampleShared {
 
 template <int W>
 __device__ __forceinline__ float max_group_f(float v, float* slots) {
-    v = max_lanes(v);
+    v = max_wave(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -375,225 +427,218 @@ __device__ __forceinline__ Drawn draw_sorted(const uint64_t* sorted, int most, c
         above += __shfl(upto, kWave - 1);
         if (!(above < target)) break;
     }
-    d.winner = max_lanes(d.winner);
-    d.z = sum_lanes(d.z);
+    d.winner = max_wave(d.winner);
+    d.z = sum_wave(d.z);
     return d;
 }
 
-// One row per workgroup of W waves.
-template <typename DT, int W>
+// A row without filters: the race and the sum of weights in one pass. False: the scores overflow
+// (logits beyond 10^38 / c), and the general way has to take them relative to the largest.
+template <typename DT, int W, int U, bool ONE>
+__device__ __forceinline__ bool sample_open(const SampleArgs& a, const RowWalk<DT, W, U, ONE>& walk, RowView<DT>& r, const float* noise,
+                                            float c, int64_t row, uint64_t* slots, float* slots_f, float& all_top) {
+    constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
+    const bool greedy = !(c < __builtin_inff());  // (temperature 0)
+    const bool race = noise && !greedy;
+    float top = kNegInf, z = 0.f, best = kNegInf;
+    uint32_t at = 0;
+    walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
+        RowVec<float> e[U][K / 4];
+        if (race) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int q = 0; q < K / 4; ++q) e[u][q].load(noise, (i0 + u * kLanes) * (K / 4) + q, a.V);
+        }
+        float t = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
+        if (t > top) {
+            z *= exp2_fast((top - t) * c);
+            top = t;
+        }
+        const Scale sc = scale_of(top, c);
+        int where = -1;  // in this chunk
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const float x = v[u].at(k);
+                z += fmaxf(exp2_fast(sc.log2_weight(x)), 0.f);  // (NaN, of a NaN or while all is -inf: 0)
+                const float score = race ? fmaf(x, c, -log2_fast(e[u][k / 4].at(k % 4))) : x;
+                if (score > best) {  // (never of NaN or of a masked logit)
+                    best = score;
+                    where = u * K + k;
+                }
+            }
+        if (where >= 0) at = uint32_t((i0 + where / K * kLanes) * K + where % K);
+    });
+    all_top = max_group_f<W>(top, slots_f);
+    if (all_top == kNegInf) {
+        if (threadIdx.x == 0) sample_none(a, row);
+        return true;
+    }
+    r.scale = scale_of(all_top, c);
+    const uint64_t winner = max_group<W>(best == kNegInf ? 0 : race_entry(order_key(best), at), slots);
+    if (!greedy && (r.scale.c != c || winner == 0)) return false;  // (no score above -inf: noise out of its range)
+    z = top == kNegInf || greedy ? 0.f : z * exp2_fast((top - all_top) * c);
+    z = sum_group<W>(z, slots);
+    if (threadIdx.x == 0) {
+        const uint32_t j = race_index(winner);
+        sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(z));
+    }
+    return true;
+}
+
+template <typename DT, int W, int U, bool ONE>
+__global__ __launch_bounds__(W * kWave) void sample_open_kernel(SampleArgs a) {
+    __shared__ uint64_t s_bins[kDigits], s_slots[W];
+    __shared__ float s_slots_f[W];
+    const int64_t row = blockIdx.x;
+    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
+    const SampleRow s = sample_row(a, row);
+    const RowWalk<DT, W, U, ONE> walk(r.x, a.V);
+    float top;
+    if (!sample_open<DT, W, U, ONE>(a, walk, r, noise, sample_scale(s), row, s_slots, s_slots_f, top))
+        sample_general<DT, W>(a, s, r, noise, top, row, s_bins, s_slots);
+}
+
+// One row per workgroup of W waves, with its filters. The cases that the quicker ways leave end in
+// the general one, at the end (one place, so that it is compiled into the kernel, not called).
+template <typename DT, int W, int U, bool ONE>
 __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
     __shared__ SampleShared<W> sh;
-    constexpr int kLanes = W * kWave;
+    constexpr int kLanes = W * kWave, K = RowVec<DT>::K;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63;
     RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
-    const float c = kLog2e / s.temperature;
-    const bool greedy = !(s.temperature > 0.f) || !(c < __builtin_inff());
+    const RowWalk<DT, W, U, ONE> walk(r.x, a.V);
+    const float c = sample_scale(s);
     const bool by_k = s.top_k < a.V, by_p = s.top_p < 1.f, by_min = s.min_p > 0.f;
+    float top = kNegInf;
 
-    if (greedy || (!by_k && !by_p && !by_min)) {
-        // one pass: the race, and the sum of weights relative to the lane's running maximum
-        float top = kNegInf, z = 0.f, best = kNegInf;
-        uint32_t at = ~0u;  // (none)
-        constexpr int K = RowVec<DT>::K, U = 4;
-        const bool race = noise && !greedy;
-        const int64_t vecs = (a.V + K - 1) / K;
-        for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
-            RowVec<DT> v[U];
-            RowVec<float> e[U][K / 4];
+    auto quick = [&]() -> bool {
+        if (!(c < __builtin_inff()) || (!by_k && !by_p && !by_min))
+            return sample_open<DT, W, U, ONE>(a, walk, r, noise, c, row, sh.slots, sh.slots_f, top);
+
+        if (by_k && s.top_k <= kFewest) {
+            walk.chunks([&](const RowVec<DT>(&v)[U], int64_t) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                v[u].load(r.x, i0 + u * kLanes, a.V);  // (past the end: -inf)
-                if (race)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int q = 0; q < K / 4; ++q) e[u][q].load(noise, (i0 + u * kLanes) * (K / 4) + q, a.V);
-            }
-            float t = top;
+                    for (int k = 0; k < K; ++k) top = fmaxf(top, v[u].at(k));
+            });
+            sh.maxima[tid] = top;
+            if (tid == 0) sh.count = 0;
+            __syncthreads();
+            if (tid < kWave) {
+                // the largest 16-bit prefix of a key that k lanes' maxima reach; of fours of lanes while
+                // there are plenty (fewer to compare, hardly more elements)
+                constexpr int E = W;
+                uint32_t key[E];
+                float all = kNegInf;
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+                for (int i = 0; i < E; ++i) {
+                    const float m = sh.maxima[lane + kWave * i];
+                    all = fmaxf(all, m);
+                    key[i] = m > kNegInf ? order_key(m) >> 16 : 0u;
+                }
+                int used = E;
+                if constexpr (E % 4 == 0) {
+                    if (s.top_k <= kLanes / 8) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
-            if (t > top) {
-                z *= exp2_fast((top - t) * c);
-                top = t;
-            }
-            const Scale sc = scale_of(top, c);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const float x = fmaxf(v[u].at(k), kNegInf);  // (NaN as -inf)
-                    z += fmaxf(exp2_fast(sc.log2_weight(x)), 0.f);  // (NaN while all is -inf: 0)
-                    const float score = race ? fmaxf(fmaf(x, c, -log2_fast(e[u][k / 4].at(k % 4))), kNegInf) : x;
-                    if (x > kNegInf && (score > best || at == ~0u)) {
-                        best = score;
-                        at = uint32_t((i0 + u * kLanes) * K + k);
+                        for (int i = 0; i < E / 4; ++i) {
+                            const uint32_t x = key[4 * i] > key[4 * i + 1] ? key[4 * i] : key[4 * i + 1];
+                            const uint32_t y = key[4 * i + 2] > key[4 * i + 3] ? key[4 * i + 2] : key[4 * i + 3];
+                            key[i] = x > y ? x : y;
+                        }
+                        used = E / 4;
                     }
                 }
-        }
-        const float all_top = max_group_f<W>(top, sh.slots_f);
-        if (all_top == kNegInf) {
-            if (tid == 0) sample_none(a, row);
-            return;
-        }
-        r.scale = scale_of(all_top, c);
-        if (greedy || r.scale.c == c) {
-            z = top == kNegInf ? 0.f : z * exp2_fast((top - all_top) * c);
-            z = sum_group<W>(z, sh.slots);
-            const uint64_t winner = max_group<W>(at == ~0u ? 0 : race_entry(order_key(best), at), sh.slots);
-            if (tid == 0) {
-                const uint32_t j = race_index(winner);
-                sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(z));
-            }
-            return;
-        }
-        // (scores overflowed: logits beyond 10^38 / c. The general way takes them relative to the largest.)
-        sample_general<DT, W>(a, s, r, noise, all_top, row, sh.bins, sh.slots);
-        return;
-    }
-
-    if (by_k && s.top_k <= kFewest) {
-        float top = kNegInf;
-        each_element<DT, W>(r.x, a.V, [&](float v, uint32_t) { top = fmaxf(top, v); });
-        sh.maxima[tid] = top;
-        if (tid == 0) sh.count = 0;
-        __syncthreads();
-        if (tid < kWave) {
-            // the largest 16-bit prefix of a key that k lanes' maxima reach; of fours of lanes while there
-            // are plenty (fewer to compare, hardly more elements)
-            constexpr int E = W;
-            uint32_t key[E];
-            float all = kNegInf;
+                uint32_t prefix = 0;
+                for (int bit = 15; bit >= 0; --bit) {
+                    const uint32_t tried = prefix | (1u << bit);
+                    int reached = 0;
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float m = sh.maxima[lane + kWave * i];
-                all = fmaxf(all, m);
-                key[i] = m > kNegInf ? order_key(m) >> 16 : 0u;
-            }
-            int used = E;
-            if constexpr (E % 4 == 0) {
-                if (s.top_k <= kLanes / 8) {
-#pragma unroll
-                    for (int i = 0; i < E / 4; ++i) {
-                        const uint32_t x = key[4 * i] > key[4 * i + 1] ? key[4 * i] : key[4 * i + 1];
-                        const uint32_t y = key[4 * i + 2] > key[4 * i + 3] ? key[4 * i + 2] : key[4 * i + 3];
-                        key[i] = x > y ? x : y;
-                    }
-                    used = E / 4;
+                    for (int i = 0; i < E; ++i)
+                        if (i < used) reached += __popcll(__ballot(key[i] >= tried));
+                    if (reached >= s.top_k) prefix = tried;
+                }
+                all = max_wave(all);
+                if (lane == 0) {
+                    sh.pivot = prefix << 16;
+                    sh.top = all;
                 }
             }
-            uint32_t prefix = 0;
-            for (int bit = 15; bit >= 0; --bit) {
-                const uint32_t tried = prefix | (1u << bit);
-                int reached = 0;
-#pragma unroll
-                for (int i = 0; i < E; ++i)
-                    if (i < used) reached += __popcll(__ballot(key[i] >= tried));
-                if (reached >= s.top_k) prefix = tried;
+            __syncthreads();
+            top = sh.top;
+            if (top == kNegInf) {
+                if (tid == 0) sample_none(a, row);
+                return true;
             }
-            all = max_lanes(all);
-            if (lane == 0) {
-                sh.pivot = prefix << 16;
-                sh.top = all;
+            r.scale = scale_of(top, c);
+            const float from = sh.pivot > order_key(kNegInf) ? key_value(sh.pivot) : kNegInf;
+            walk.each([&](float v, uint32_t j) {
+                if (v >= from && v > kNegInf) {
+                    const uint32_t i = atomicAdd(&sh.count, 1u);
+                    if (i < kList) sh.list[i] = race_entry(order_key(v), j);
+                }
+            });
+            __syncthreads();
+            const int n = int(sh.count);
+            if (n > kList) return false;
+            rank_list<W>(sh.list, sh.sorted, n);
+            if (tid >= kWave) return true;
+            const int most = n < s.top_k ? n : int(s.top_k);
+            float target = __builtin_inff();
+            if (by_p) {
+                float sum = 0.f;
+                for (int i = lane; i < most; i += kWave) sum += exp2_fast(r.log2_weight(key_value(uint32_t(sh.sorted[i] >> 32))));
+                target = s.top_p * sum_wave(sum);
             }
+            const Drawn d = draw_sorted(sh.sorted, most, r, noise, 0.f, target, least_weight(s, r, top), true);
+            if (lane == 0) sample_outputs(a, row, race_index(d.winner), r.log2_weight(r.logit(race_index(d.winner))) - log2_fast(d.z));
+            return true;
         }
-        __syncthreads();
-        top = sh.top;
+
+        // the largest logit and the sum of weights
+        float own_top, z;
+        walk.statistics(c, own_top, z);
+        top = max_group_f<W>(own_top, sh.slots_f);
         if (top == kNegInf) {
             if (tid == 0) sample_none(a, row);
-            return;
+            return true;
         }
         r.scale = scale_of(top, c);
-        const float from = sh.pivot > order_key(kNegInf) ? key_value(sh.pivot) : kNegInf;
-        each_element<DT, W>(r.x, a.V, [&](float v, uint32_t j) {
-            if (v >= from && v > kNegInf) {
-                const uint32_t i = atomicAdd(&sh.count, 1u);
-                if (i < kList) sh.list[i] = race_entry(order_key(v), j);
-            }
-        });
-        __syncthreads();
-        const int n = int(sh.count);
-        if (n > kList) {
-            sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
-            return;
-        }
-        rank_list<W>(sh.list, sh.sorted, n);
-        if (tid >= kWave) return;
-        const int most = n < s.top_k ? n : int(s.top_k);
-        float target = __builtin_inff();
+        if (by_k || r.scale.c != c) return false;
+        const float least = least_weight(s, r, top);
+        z = own_top == kNegInf ? 0.f : z * exp2_fast((own_top - top) * c);
+        z = sum_group<W>(z, sh.slots);
+
+        // without top-p everything is above the crossing bin
+        int cross = kMassBins;
+        float above = 0.f;
+        const float target = by_p ? s.top_p * z : __builtin_inff();
         if (by_p) {
-            float sum = 0.f;
-            for (int i = lane; i < most; i += kWave) sum += exp2_fast(r.log2_weight(key_value(uint32_t(sh.sorted[i] >> 32))));
-            target = s.top_p * sum_lanes(sum);
-        }
-        const Drawn d = draw_sorted(sh.sorted, most, r, noise, 0.f, target, least_weight(s, r, top), true);
-        if (lane == 0) sample_outputs(a, row, race_index(d.winner), r.log2_weight(r.logit(race_index(d.winner))) - log2_fast(d.z));
-        return;
-    }
-
-    // the largest logit and the sum of weights
-    float top = kNegInf, z = 0.f;
-    {
-        constexpr int K = RowVec<DT>::K, U = 4;
-        const int64_t vecs = (a.V + K - 1) / K;
-        for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
-            RowVec<DT> v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u].load(r.x, i0 + u * kLanes, a.V);
-            float t = top;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
-            if (t > top) {
-                z *= exp2_fast((top - t) * c);
-                top = t;
-            }
-            const Scale sc = scale_of(top, c);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int k = 0; k < K; ++k) z += fmaxf(exp2_fast(sc.log2_weight(v[u].at(k))), 0.f);
-        }
-    }
-    const float own_top = top;
-    top = max_group_f<W>(top, sh.slots_f);
-    if (top == kNegInf) {
-        if (tid == 0) sample_none(a, row);
-        return;
-    }
-    r.scale = scale_of(top, c);
-    const float least = least_weight(s, r, top);
-    if (by_k || r.scale.c != c) {
-        sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
-        return;
-    }
-    z = own_top == kNegInf ? 0.f : z * exp2_fast((own_top - top) * c);
-    z = sum_group<W>(z, sh.slots);
-
-    // without top-p everything is above the crossing bin
-    int cross = kMassBins;
-    float above = 0.f;
-    const float target = by_p ? s.top_p * z : __builtin_inff();
-    if (by_p) {
-        // the smallest elements, of less than 1 - p in all, cannot be in: at most V of them below this
-        const float low = log2_fast(0.99f * (1.f - s.top_p) * z / float(a.V));
-        for (int i = tid; i < kMassBins; i += kLanes) sh.bins[i] = 0;
-        if (tid == 0) sh.count = 0;
-        __syncthreads();
-        each_element<DT, W>(r.x, a.V, [&](float v, uint32_t) {
-            const float u = r.log2_weight(v);
-            const int bin = int(-u * kBinsPerOctave);
-            if (u >= low && bin < kMassBins)
-                atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[bin < 0 ? 0 : bin]), (unsigned long long)(r.mass(v)));
-        });
-        __syncthreads();
-        // its first bin at which the sum reaches p of the mass (at least the largest element's)
-        const uint64_t want0 = uint64_t(ceil(double(target) * kMassUnit)), want = want0 < 1 ? 1 : want0;
-        {
+            // the smallest elements, of less than 1 - p in all, cannot be in: at most V of them below this
+            const float low = log2_fast(0.99f * (1.f - s.top_p) * z / float(a.V));
+            for (int i = tid; i < kMassBins; i += kLanes) sh.bins[i] = 0;
+            if (tid == 0) sh.count = 0;
+            __syncthreads();
+            walk.each([&](float v, uint32_t) {
+                const float u = r.log2_weight(v);
+                const int bin = int(-u * kBinsPerOctave);
+                if (u >= low && bin < kMassBins)
+                    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[bin < 0 ? 0 : bin]), (unsigned long long)(r.mass(v)));
+            });
+            __syncthreads();
+            // the first bin at which the sum reaches p of the mass (at least the largest element's)
+            const uint64_t want0 = uint64_t(ceil(double(target) * kMassUnit)), want = want0 < 1 ? 1 : want0;
             constexpr int kEach = kMassBins / kLanes;  // bins a lane, in order
             uint64_t bin[kEach], sum = 0;
 #pragma unroll
@@ -626,48 +671,69 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
                     before += bin[i];
                 }
             }
+            __syncthreads();
+            cross = int(sh.pivot);
+            above = sh.top;
+            if (cross == kMassBins) return false;  // (so flat that the cut lies below 2^-32)
         }
-        __syncthreads();
-        cross = int(sh.pivot);
-        above = sh.top;
-        if (cross == kMassBins) {  // (so flat that the cut lies below 2^-32)
-            sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
-            return;
+        float zk = 0.f;
+        uint64_t winner = 0;
+        walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
+            // which are kept; then the noise of those alone, all of its loads before the first use
+            float e[U][K];
+            uint64_t keep = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const float x = fmaxf(v[u].at(k), kNegInf), l = r.log2_weight(x), w = exp2_fast(l);
+                    const uint32_t j = uint32_t((i0 + u * kLanes) * K + k);
+                    bool in = w >= least && x > kNegInf;
+                    if (by_p) {
+                        const int at = int(fminf(fmaxf(-l * kBinsPerOctave, 0.f), float(kMassBins)));
+                        if (in && at == cross) {
+                            const uint32_t i = atomicAdd(&sh.count, 1u);
+                            if (i < kList) sh.list[i] = race_entry(order_key(x), j);
+                        }
+                        in = in && at < cross;
+                    }
+                    if (in) keep |= 1ull << (u * K + k);
+                    zk += in ? w : 0.f;
+                    e[u][k] = 1.f;
+                }
+            if (noise) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+                        if ((keep >> (u * K + k)) & 1) e[u][k] = noise[(i0 + u * kLanes) * K + k];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    if (!((keep >> (u * K + k)) & 1)) continue;
+                    const float x = v[u].at(k), score = noise ? r.log2_weight(x) - log2_fast(e[u][k]) : x;
+                    const uint64_t y = race_entry(order_key(score), uint32_t((i0 + u * kLanes) * K + k));
+                    winner = y > winner ? y : winner;
+                }
+        });
+        zk = sum_group<W>(zk, sh.slots);
+        winner = max_group<W>(winner, sh.slots);
+        if (by_p) {
+            __syncthreads();
+            const int n = int(sh.count);
+            if (n > kList) return false;
+            rank_list<W>(sh.list, sh.sorted, n);
+            if (tid >= kWave) return true;
+            const Drawn d = draw_sorted(sh.sorted, n, r, noise, above, target, least, true);
+            zk += d.z;
+            winner = d.winner > winner ? d.winner : winner;
         }
-    }
-    float zk = 0.f;
-    uint64_t winner = 0;
-    each_element<DT, W>(r.x, a.V, [&](float v, uint32_t j) {
-        const float u = r.log2_weight(v), w = exp2_fast(u);
-        if (!(w >= least) || !(v > kNegInf)) return;
-        const int bin = by_p ? int(fminf(fmaxf(-u * kBinsPerOctave, 0.f), float(kMassBins))) : 0;
-        if (bin > cross) return;
-        if (bin == cross) {
-            const uint32_t i = atomicAdd(&sh.count, 1u);
-            if (i < kList) sh.list[i] = race_entry(order_key(v), j);
-            return;
-        }
-        zk += w;
-        const float score = noise ? u - log2_fast(noise[j]) : v;
-        const uint64_t e = race_entry(order_key(score), j);
-        winner = e > winner ? e : winner;
-    });
-    zk = sum_group<W>(zk, sh.slots);
-    winner = max_group<W>(winner, sh.slots);
-    if (by_p) {
-        __syncthreads();
-        const int n = int(sh.count);
-        if (n > kList) {
-            sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
-            return;
-        }
-        rank_list<W>(sh.list, sh.sorted, n);
-        if (tid >= kWave) return;
-        const Drawn d = draw_sorted(sh.sorted, n, r, noise, above, target, least, true);
-        zk += d.z;
-        winner = d.winner > winner ? d.winner : winner;
-    }
-    if (tid == 0) sample_outputs(a, row, race_index(winner), r.log2_weight(r.logit(race_index(winner))) - log2_fast(zk));
+        if (tid == 0) sample_outputs(a, row, race_index(winner), r.log2_weight(r.logit(race_index(winner))) - log2_fast(zk));
+        return true;
+    };
+    if (!quick()) sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
 }
 
 // Rows of up to L * E logits, L lanes a row, no filters.

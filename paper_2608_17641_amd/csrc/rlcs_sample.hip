@@ -13,8 +13,16 @@ void launch_small(const SampleArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((sample_small_kernel<DT, L, E>), dim3(unsigned((a.M + rows - 1) / rows)), dim3(4 * kWave), 0, s, a);
 }
 
+template <typename DT, int W, int U, bool ONE>
+void launch_rows(const SampleArgs& a, bool open, hipStream_t s) {
+    const dim3 grid(static_cast<unsigned>(a.M)), block(W * kWave);
+    if (open) hipLaunchKernelGGL((sample_open_kernel<DT, W, U, ONE>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((sample_rows_kernel<DT, W, U, ONE>), grid, block, 0, s, a);
+}
+
 template <typename DT>
 rlcs_status run_sample(const SampleArgs& a, hipStream_t s) {
+    constexpr int kVec = 16 / sizeof(DT);
     // no row has a filter, as far as the host can tell
     const bool open = !a.top_k && !a.top_p && !a.min_p && (a.all_top_k <= 0 || a.all_top_k >= a.V) && a.all_top_p >= 1.f &&
                       !(a.all_min_p > 0.f);
@@ -24,12 +32,14 @@ rlcs_status run_sample(const SampleArgs& a, hipStream_t s) {
         else if (a.V <= 128) launch_small<DT, 32, 4>(a, s);
         else if (a.V <= 256) launch_small<DT, 64, 4>(a, s);
         else launch_small<DT, 64, 16>(a, s);
-    } else if (a.V <= 256) {
-        hipLaunchKernelGGL((sample_rows_kernel<DT, 1>), dim3(unsigned(a.M)), dim3(kWave), 0, s, a);
-    } else if (a.V <= 8192) {
-        hipLaunchKernelGGL((sample_rows_kernel<DT, 4>), dim3(unsigned(a.M)), dim3(4 * kWave), 0, s, a);
+    } else if (a.V <= 256) {  // (a vector a lane)
+        launch_rows<DT, 1, 4, true>(a, open, s);
+    } else if (a.V <= 4 * 256 * kVec) {
+        launch_rows<DT, 4, 4, true>(a, open, s);
+    } else if (a.V <= 4 * 1024 * kVec) {
+        launch_rows<DT, 16, 4, true>(a, open, s);
     } else {
-        hipLaunchKernelGGL((sample_rows_kernel<DT, 16>), dim3(unsigned(a.M)), dim3(16 * kWave), 0, s, a);
+        launch_rows<DT, 16, 4, false>(a, open, s);
     }
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }

@@ -39,17 +39,55 @@ __device__ __forceinline__ Scale scale_of(float top, float c) {
 }
 
 // Over each group of L lanes, every lane with the result; the tree is fixed, so the sums are too.
-template <int L = kWave>
+template <int L>
 __device__ __forceinline__ float sum_lanes(float v) {
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
-template <int L = kWave>
+template <int L>
 __device__ __forceinline__ float max_lanes(float v) {
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
     return v;
+}
+
+// Over the whole wave: within rows of 16 lanes by row shifts, across them by two broadcasts (DPP moves of
+// the vector unit, a few clocks each, where a shuffle goes through LDS); lane 63 has the result,
+// which a lane read hands to all. f(a, b) with `id` its neutral element.
+template <class T, class F>
+__device__ __forceinline__ T fold_wave(T v, T id, F&& f) {
+    constexpr int kWords = sizeof(T) / 4;
+    struct Words {
+        int w[kWords];
+    };
+    auto step = [&](auto ctrl, auto rows) {
+        const Words x = __builtin_bit_cast(Words, v), n = __builtin_bit_cast(Words, id);
+        Words o;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            o.w[i] = __builtin_amdgcn_update_dpp(n.w[i], x.w[i], decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        v = f(v, __builtin_bit_cast(T, o));
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});  // row_shr:1
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // row_bcast:15
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // row_bcast:31
+    Words x = __builtin_bit_cast(Words, v);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) x.w[i] = __builtin_amdgcn_readlane(x.w[i], 63);
+    return __builtin_bit_cast(T, x);
+}
+__device__ __forceinline__ float sum_wave(float v) {
+    return fold_wave(v, 0.f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float max_wave(float v) {
+    return fold_wave(v, kNegInf, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ uint64_t max_wave(uint64_t v) {
+    return fold_wave(v, uint64_t(0), [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
 
 // Logarithms of weights are kept from -inf, whose product with a weight of 0 is NaN: 2^-150 is 0.

@@ -45,29 +45,27 @@ def sample_row(x, noise, T, k, p, min_p):
     if not T > 0:
         return int(torch.argmax(x)), 0.0, math.inf
     y = (x - x.max()) / T
-    order = torch.sort(x, descending=True, stable=True).indices.tolist()
-    order = [j for j in order if x[j] > -math.inf]
+    order = torch.sort(x, descending=True, stable=True).indices
+    order = order[x[order] > -math.inf]
     if 0 < k < V:
         order = order[:k]
     if p < 1:
-        w = torch.exp(y[order] - y[order[0]])
-        z, before, kept = float(w.sum()), 0.0, []
-        for j, wj in zip(order, w.tolist()):
-            if kept and before >= p * z:
-                break
-            kept.append(j)
-            before += wj
-        order = kept
+        w = torch.exp(y[order])
+        before = torch.cumsum(w, 0) - w
+        kept = before < p * w.sum()
+        kept[0] = True
+        order = order[kept]
     if min_p > 0:
-        w = torch.exp(y[order] - y[order[0]])
-        order = [j for i, j in enumerate(order) if i == 0 or float(w[i]) >= min(min_p, 1.0)]
-    order.sort()
+        kept = torch.exp(y[order] - y[order[0]]) >= min(min_p, 1.0)
+        kept[0] = True
+        order = order[kept]
+    order = torch.sort(order).values
     yk = y[order]
     score = yk - torch.log(noise[order]) if noise is not None else yk
     best = int(torch.argmax(score))
     rest = torch.cat([score[:best], score[best + 1:]])
     margin = float(score[best] - rest.max()) if rest.numel() and noise is not None else math.inf
-    return order[best], float(yk[best] - torch.logsumexp(yk, 0)), margin
+    return int(order[best]), float(yk[best] - torch.logsumexp(yk, 0)), margin
 
 
 def attention(q, kp, vp, ks, vs, plen, slen, scale):
