@@ -39,6 +39,7 @@ struct AttnPlan {
     int64_t prefix_chunk, suffix_chunk;
     int32_t prefix_parts, suffix_parts, prefix_tiles, suffix_tiles;
     int32_t prefix_items, items;  // workgroups of the prefix, and all
+    int32_t prefix_groups, groups;  // the same in groups of kGroup, as they are dealt
     bool whole;
     float* part_acc;  // [part][row][D]: outputs relative to the part's own maximum
     float2* part_ml;  // [part][row]: maximum (base 2) and sum
@@ -49,6 +50,10 @@ __device__ __forceinline__ int64_t clamp_len(const int32_t* p, int64_t i, int64_
     const int64_t n = p[i];
     return n < 0 ? 0 : n > most ? most : n;
 }
+
+// The prefix's workgroups, which compute, and the suffix's, which wait for memory, are dealt in turn,
+// kGroup of each kind at a time in proportion to their numbers, so that a CU has both.
+constexpr int kGroup = 16;
 
 constexpr int kTileRows = 16;  // queries of a matrix product's columns
 
@@ -315,8 +320,8 @@ struct AttnWave {
 };
 
 // Keys [from, end) of one array for a workgroup whose waves have queries of their own (bfloat16): all of
-// its lanes bring a block of keys and values to LDS, every wave reads them from there. The next
-// block's loads are under way meanwhile.
+// its lanes bring blocks of keys and values to LDS, every wave reads them from there. While one
+// block is worked on, the next is in the other half of LDS and the one after it on its way.
 template <int ND, int QT, int W, bool EXACT>
 struct SharedKeys {
     static constexpr int kKeys = ND > 8 ? 32 : 64;
@@ -324,14 +329,13 @@ struct SharedKeys {
     static constexpr int kKRow = 16 * ND + 8;   // elements of a row in LDS: the sixteen rows of a key operand's read,
     static constexpr int kVRow = 16 * ND + 16;  // and the eight of half a wave's of values, in different banks
     static constexpr int kPieces = kKeys * kVecs / (W * kWave);
-    static constexpr size_t kLds = size_t(kKeys) * (kKRow + kVRow) * 2;
+    static constexpr int kHalf = kKeys * (kKRow + kVRow);  // elements
+    static constexpr size_t kLds = size_t(2 * kHalf) * 2;
 
     static __device__ __forceinline__ void run(AttnWave<bf16_t, ND, QT, EXACT>& w, const bf16_t* keys, const bf16_t* values, int64_t sk,
                                                int64_t sv, int64_t from, int64_t end, int D, float scale, bf16_t* lds, int tid) {
         const int lane = tid & 63, c = lane & 15, g = lane >> 4;
         constexpr int KT = kKeys / 16;
-        bf16_t* lk = lds;
-        bf16_t* lv = lds + kKeys * kKRow;
         u32x4 k[kPieces], v[kPieces];
         uint32_t at_k[kPieces], at_v[kPieces];
         auto aim = [&](int rows) {
@@ -345,6 +349,7 @@ struct SharedKeys {
             }
         };
         auto load = [&](int64_t j) {
+            if (end - j < kKeys) aim(int(end - j));
             const char* kb = reinterpret_cast<const char*>(keys + j * sk);
             const char* vb = reinterpret_cast<const char*>(values + j * sv);
 #pragma unroll
@@ -352,24 +357,28 @@ struct SharedKeys {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) v[i] = *reinterpret_cast<const u32x4*>(vb + at_v[i]);
         };
-        if (from >= end) return;
-        aim(end - from < kKeys ? int(end - from) : kKeys);
-        load(from);
-        for (int64_t j = from; j < end; j += kKeys) {
-            const int rows = end - j < kKeys ? int(end - j) : kKeys;
-            const int64_t next = j + kKeys;
-            __syncthreads();  // the block before has been read
+        auto put = [&](bf16_t* half) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int at = tid + W * kWave * i;
-                *reinterpret_cast<u32x4*>(lk + (at / kVecs) * kKRow + 8 * (at % kVecs)) = k[i];
-                *reinterpret_cast<u32x4*>(lv + (at / kVecs) * kVRow + 8 * (at % kVecs)) = v[i];
+                *reinterpret_cast<u32x4*>(half + (at / kVecs) * kKRow + 8 * (at % kVecs)) = k[i];
+                *reinterpret_cast<u32x4*>(half + kKeys * kKRow + (at / kVecs) * kVRow + 8 * (at % kVecs)) = v[i];
             }
-            __syncthreads();
-            if (next < end) {
-                if (end - next < kKeys) aim(int(end - next));
-                load(next);
-            }
+        };
+        if (from >= end) return;
+        aim(kKeys);
+        load(from);
+        put(lds);
+        if (from + kKeys < end) load(from + kKeys);
+        int turn = 0;
+        for (int64_t j = from; j < end; j += kKeys) {
+            const int rows = end - j < kKeys ? int(end - j) : kKeys;
+            const bf16_t* lk = lds + turn * kHalf;
+            const bf16_t* lv = lk + kKeys * kKRow;
+            turn ^= 1;
+            __syncthreads();  // this block is there, and the one before has been read
+            if (j + kKeys < end) put(lds + turn * kHalf);
+            if (j + 2 * kKeys < end) load(j + 2 * kKeys);
             f32x4 s[QT][KT];
 #pragma unroll
             for (int x = 0; x < QT; ++x)
@@ -426,15 +435,21 @@ struct AttnItem {
     int64_t n, plen, from, end;
     int r, Hq, G, slot;
 
-    // false: nothing to do (a part past the length, which the joining kernel does not look at)
-    __device__ __forceinline__ bool of(const AttnArgs& a, const AttnPlan& plan, int item) {
+    // false: nothing to do (past the last item, or a part past the length, which the joining kernel
+    // does not look at)
+    __device__ __forceinline__ bool of(const AttnArgs& a, const AttnPlan& plan, int block) {
+        const int group = block / kGroup;
+        const int before = int(int64_t(group) * plan.prefix_groups / plan.groups);
+        prefix = int64_t(group + 1) * plan.prefix_groups / plan.groups > before;
+        // workgroups that run on one XCD are eight apart: there, two tiles of a prefix read the same keys
+        const int within = (block % 8) * (kGroup / 8) + block % kGroup / 8;
+        int item = (prefix ? before : group - before) * kGroup + within;
+        if (item >= (prefix ? plan.prefix_items : plan.items - plan.prefix_items)) return false;
         // (all of these are below 2^31, so 32-bit divisions do)
         Hq = int(a.Hq);
         G = int(a.G);
         const int Hkv = int(a.Hkv);
         r = Hq / Hkv;
-        prefix = item < plan.prefix_items;
-        if (!prefix) item -= plan.prefix_items;
         const int tiles = prefix ? plan.prefix_tiles : plan.suffix_tiles;
         const int parts = prefix ? plan.prefix_parts : plan.suffix_parts;
         tile = item % tiles;
@@ -503,15 +518,12 @@ __device__ __forceinline__ float score_scale(float scale2) { return fmaxf(fabsf(
 
 // Waves of the workgroup on the same 16 * QT rows and keys of their own.
 template <typename DT, int ND, int QT, int W, bool EXACT>
-__global__ __launch_bounds__(W * kWave) void attn_kernel(AttnArgs a, AttnPlan plan, int first_item) {
-    __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, W>()];
-    __shared__ float s_m[W][kTileRows], s_l[W][kTileRows];
+__device__ __forceinline__ void attn_split_keys(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem,
+                                                float (*s_m)[kTileRows], float (*s_l)[kTileRows]) {
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = EXACT ? 16 * ND : int(a.D);
-    bf16_t* lds = reinterpret_cast<bf16_t*>(s_mem) + wave * 32 * (16 * ND + 16);
-    AttnItem it;
-    if (!it.of(a, plan, first_item + int(blockIdx.x))) return;
+    bf16_t* lds = reinterpret_cast<bf16_t*>(mem) + wave * 32 * (16 * ND + 16);
     const int row0 = it.tile * kTileRows * QT;
     AttnWave<DT, ND, QT, EXACT> w;
     w.clear();
@@ -531,7 +543,7 @@ __global__ __launch_bounds__(W * kWave) void attn_kernel(AttnArgs a, AttnPlan pl
     }
 
     // the waves join, tile by tile
-    float* join = reinterpret_cast<float*>(s_mem);
+    float* join = reinterpret_cast<float*>(mem);
     constexpr int kJoinRow = 16 * ND + 4;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
@@ -569,22 +581,18 @@ __global__ __launch_bounds__(W * kWave) void attn_kernel(AttnArgs a, AttnPlan pl
 
 // Waves of the workgroup on rows of their own, 16 * QT each, and the same keys: prefixes of many rows.
 template <int ND, int QT, int W, bool EXACT>
-__global__ __launch_bounds__(W * kWave) void attn_shared_kernel(AttnArgs a, AttnPlan plan, int first_item) {
-    typedef SharedKeys<ND, QT, W, EXACT> Keys;
-    __shared__ __attribute__((aligned(16))) char s_mem[Keys::kLds];
+__device__ __forceinline__ void attn_share_keys(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem) {
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
     const int D = EXACT ? 16 * ND : int(a.D);
-    AttnItem it;
-    if (!it.of(a, plan, first_item + int(blockIdx.x))) return;
     const int row0 = (it.tile * W + (tid >> 6)) * kTileRows * QT;
     AttnWave<bf16_t, ND, QT, EXACT> w;
     w.clear();
 #pragma unroll
     for (int x = 0; x < QT; ++x)
         w.load_query(x, it.template query<bf16_t>(a, row0 + x * kTileRows + c), D, query_sign<bf16_t>(a.scale2), lane);
-    Keys::run(w, reinterpret_cast<const bf16_t*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2],
-              reinterpret_cast<const bf16_t*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2], a.at.kp[1], a.at.vp[1], it.from, it.end, D,
-              score_scale(a.scale2), reinterpret_cast<bf16_t*>(s_mem), tid);
+    SharedKeys<ND, QT, W, EXACT>::run(w, reinterpret_cast<const bf16_t*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2],
+                                      reinterpret_cast<const bf16_t*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2], a.at.kp[1],
+                                      a.at.vp[1], it.from, it.end, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(mem), tid);
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
         float l = w.l[x];
@@ -596,6 +604,42 @@ __global__ __launch_bounds__(W * kWave) void attn_shared_kernel(AttnArgs a, Attn
         for (int t = 0; t < ND; ++t)
             if (EXACT || 16 * t + 4 * g4 < D) it.template store<bf16_t>(a, plan, row, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l);
     }
+}
+
+constexpr int kAttnWaves = 4;
+
+// How the rows of a prefix are taken: like a suffix's, or two tiles at a time; or (bfloat16) by waves of
+// their own, four of one tile, or, in a kernel of its own, four or eight of two.
+enum PrefixRows { kPrefixOne, kPrefixTwo, kPrefixShared64, kPrefixShared128, kPrefixShared256 };
+
+template <typename DT, int ND, PrefixRows PR, bool EXACT>
+constexpr size_t attn_mem() {
+    size_t n = attn_lds<DT, ND, kAttnWaves>();
+    if constexpr (PR == kPrefixShared64) n = n > SharedKeys<ND, 1, kAttnWaves, EXACT>::kLds ? n : SharedKeys<ND, 1, kAttnWaves, EXACT>::kLds;
+    return n;
+}
+
+template <typename DT, int ND, PrefixRows PR, bool EXACT>
+__global__ __launch_bounds__(kAttnWaves * kWave) void attn_kernel(AttnArgs a, AttnPlan plan) {
+    __shared__ __attribute__((aligned(16))) char s_mem[attn_mem<DT, ND, PR, EXACT>()];
+    __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
+    AttnItem it;
+    if (!it.of(a, plan, int(blockIdx.x))) return;
+    if (PR != kPrefixOne && it.prefix) {
+        if constexpr (PR == kPrefixTwo) attn_split_keys<DT, ND, 2, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
+        if constexpr (PR == kPrefixShared64) attn_share_keys<ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem);
+    } else {
+        attn_split_keys<DT, ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
+    }
+}
+
+// The prefix alone: its registers (two tiles a wave) would halve the suffix's waves on a CU.
+template <int ND, int W, bool EXACT>
+__global__ __launch_bounds__(W * kWave) void attn_prefix_kernel(AttnArgs a, AttnPlan plan) {
+    __shared__ __attribute__((aligned(16))) char s_mem[SharedKeys<ND, 2, W, EXACT>::kLds];
+    AttnItem it;
+    if (!it.of(a, plan, int(blockIdx.x))) return;
+    attn_share_keys<ND, 2, W, EXACT>(a, plan, it, s_mem);
 }
 
 // Joins the parts of a row: one row a workgroup, `groups` of D / 4 lanes (four dimensions each) on

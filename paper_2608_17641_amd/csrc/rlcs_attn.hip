@@ -36,17 +36,19 @@ constexpr int64_t kWholeKeys = 512;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a workgroup takes the prefix's rows: bfloat16 rows of more than one tile go to waves of their own,
-// one or two tiles each, that share the keys; others to waves that share the rows.
-struct PrefixTiles {
-    bool shared;
-    int qt, rows;  // tiles a wave, rows a workgroup
-};
-PrefixTiles prefix_tiles(int64_t rows, int64_t D, bool bf16) {
-    if (rows <= kTileRows) return {false, 1, kTileRows};
-    if (!bf16) return D <= 128 ? PrefixTiles{false, 2, 2 * kTileRows} : PrefixTiles{false, 1, kTileRows};
-    const int qt = rows <= 4 * kTileRows || D > 128 ? 1 : 2;
-    return {true, qt, 4 * qt * kTileRows};
+PrefixRows prefix_rows(int64_t rows, int64_t D, bool bf16) {
+    if (rows <= kTileRows) return kPrefixOne;
+    if (!bf16) return D <= 128 ? kPrefixTwo : kPrefixOne;
+    return rows <= 64 || D > 128 ? kPrefixShared64 : rows <= 128 ? kPrefixShared128 : kPrefixShared256;
+}
+int64_t rows_of(PrefixRows p) {  // of a workgroup
+    switch (p) {
+        case kPrefixTwo: return 32;
+        case kPrefixShared64: return 64;
+        case kPrefixShared128: return 128;
+        case kPrefixShared256: return 256;
+        default: return kTileRows;
+    }
 }
 
 bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S, bool bf16) {
@@ -72,13 +74,16 @@ bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64
     }
     int64_t prefix_items = 0;
     if (!p.whole) {
-        p.prefix_tiles = int32_t(ceil_div(G * r, prefix_tiles(G * r, D, bf16).rows));
+        const PrefixRows pr = prefix_rows(G * r, D, bf16);
+        p.prefix_tiles = int32_t(ceil_div(G * r, rows_of(pr)));
         const int64_t base = N * Hkv * p.prefix_tiles;
-        split(P, base, kWantItems, p.prefix_chunk, p.prefix_parts);
+        split(P, base, pr == kPrefixShared256 ? kWantItems / 2 : kWantItems, p.prefix_chunk, p.prefix_parts);
         prefix_items = base * p.prefix_parts;
     }
     const int64_t items = prefix_items + suffix_base * p.suffix_parts;
-    if (items > INT32_MAX) return false;
+    if (items > INT32_MAX - 2 * kGroup) return false;
+    p.prefix_groups = int32_t(ceil_div(prefix_items, kGroup));
+    p.groups = p.prefix_groups + int32_t(ceil_div(items - prefix_items, kGroup));
     p.prefix_items = int32_t(prefix_items);
     p.items = int32_t(items);
     return true;
@@ -89,42 +94,48 @@ size_t part_bytes(const AttnPlan& p, int64_t rows, int64_t D) {
     return parts > 1 ? size_t(parts * rows) * size_t(4 * D + 8) : 0;
 }
 
-template <typename DT, int ND, int QT>
-void launch_items(const AttnArgs& a, const AttnPlan& p, int first, int count, hipStream_t s) {
-    constexpr int W = ND > 8 ? 2 : 4;
-    if (count <= 0) return;
-    const dim3 grid(static_cast<unsigned>(count)), block(W * kWave);
-    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a, p, first);
-    else hipLaunchKernelGGL((attn_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a, p, first);
+// The items of the prefix alone, or of the suffix alone, of a plan that has both.
+AttnPlan only(AttnPlan p, bool prefix) {
+    if (prefix) {
+        p.items = p.prefix_items;
+        p.groups = p.prefix_groups;
+    } else {
+        p.items -= p.prefix_items;
+        p.groups -= p.prefix_groups;
+        p.prefix_items = p.prefix_groups = 0;
+    }
+    return p;
 }
 
-template <int ND, int QT>
-void launch_shared(const AttnArgs& a, const AttnPlan& p, int count, hipStream_t s) {
-    if (count <= 0) return;
-    const dim3 grid(static_cast<unsigned>(count)), block(4 * kWave);
-    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_shared_kernel<ND, QT, 4, true>), grid, block, 0, s, a, p, 0);
-    else hipLaunchKernelGGL((attn_shared_kernel<ND, QT, 4, false>), grid, block, 0, s, a, p, 0);
+template <typename DT, int ND, PrefixRows PR>
+void launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    if (p.groups == 0) return;
+    const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(kAttnWaves * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_kernel<DT, ND, PR, true>), grid, block, 0, s, a, p);
+    else hipLaunchKernelGGL((attn_kernel<DT, ND, PR, false>), grid, block, 0, s, a, p);
+}
+
+template <int ND, int W>
+void launch_prefix(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(W * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_prefix_kernel<ND, W, true>), grid, block, 0, s, a, p);
+    else hipLaunchKernelGGL((attn_prefix_kernel<ND, W, false>), grid, block, 0, s, a, p);
 }
 
 template <typename DT, int ND>
 rlcs_status run_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
-    const PrefixTiles t = prefix_tiles(a.G * (a.Hq / a.Hkv), a.D, sizeof(DT) == 2);
-    int done = 0;
+    const PrefixRows pr = p.prefix_items ? prefix_rows(a.G * (a.Hq / a.Hkv), a.D, sizeof(DT) == 2) : kPrefixOne;
+    if (pr == kPrefixOne) launch_attn<DT, ND, kPrefixOne>(a, p, s);
     if constexpr (sizeof(DT) == 2) {
-        if (t.shared) {
-            done = p.prefix_items;
-            if (t.qt == 1) launch_shared<ND, 1>(a, p, done, s);
-            if constexpr (ND <= 8) {
-                if (t.qt == 2) launch_shared<ND, 2>(a, p, done, s);
-            }
+        if (pr == kPrefixShared64) launch_attn<DT, ND, kPrefixShared64>(a, p, s);
+        if constexpr (ND <= 8) {
+            if (pr == kPrefixShared128) launch_prefix<ND, 4>(a, only(p, true), s);
+            if (pr == kPrefixShared256) launch_prefix<ND, 8>(a, only(p, true), s);
+            if (pr == kPrefixShared128 || pr == kPrefixShared256) launch_attn<DT, ND, kPrefixOne>(a, only(p, false), s);
         }
     } else if constexpr (ND <= 8) {
-        if (t.qt == 2) {
-            done = p.prefix_items;
-            launch_items<DT, ND, 2>(a, p, 0, done, s);
-        }
+        if (pr == kPrefixTwo) launch_attn<DT, ND, kPrefixTwo>(a, p, s);
     }
-    launch_items<DT, ND, 1>(a, p, done, p.items - done, s);
     if (p.part_acc)
         hipLaunchKernelGGL((attn_join_kernel<DT>), dim3(unsigned(a.N * a.G * a.Hq)), dim3(256), 0, s, a, p);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
