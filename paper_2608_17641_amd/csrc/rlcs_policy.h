@@ -126,6 +126,88 @@ __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     if (i == 0) policy_outputs<LOSS>(p, row, r);
 }
 
+// Rows of up to U vectors a lane of W waves, which stay in registers: the maximum, the sums, the
+// gradient. With W = 1 the four waves of a workgroup take a row each.
+template <typename DT, bool LOSS, int W, int U>
+__global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void policy_vec_kernel(PolicyArgs p) {
+    __shared__ float s_m[W], s_z[W], s_s[W];
+    constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
+    const int tid = W == 1 ? int(threadIdx.x) & 63 : int(threadIdx.x), wave = tid >> 6;
+    const int64_t row = W == 1 ? int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : int64_t(blockIdx.x);
+    if (row >= p.M) return;
+    const DT* x = reinterpret_cast<const DT*>(p.logits) + row * p.ld;
+    DT* g = LOSS && p.grad ? reinterpret_cast<DT*>(p.grad) + row * p.ld_grad : nullptr;
+    const int64_t vecs = (p.V + K - 1) / K;
+    int64_t a;
+    float w, old, adv;
+    if (!policy_inputs<LOSS>(p, row, a, w, old, adv)) {
+        if (tid == 0) policy_outputs<LOSS>(p, row, PolicyRow{});
+        if (g) {
+            const float zero[K] = {};
+            for (int64_t i = tid; i < vecs; i += kLanes) store_row_vec<DT>(g, i, p.V, zero);
+        }
+        return;
+    }
+    RowVec<DT> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u].load(x, tid + u * kLanes, p.V);  // (past the end: -inf)
+    const float taken = widen(x[a]);
+    float top = kNegInf;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < K; ++k) top = fmaxf(top, v[u].at(k));
+    top = max_wave(top);
+    if constexpr (W > 1) {
+        if ((tid & 63) == 0) s_m[wave] = top;
+        __syncthreads();  // (and everyone has read the taken logit, which the gradient may overwrite)
+#pragma unroll
+        for (int i = 0; i < W; ++i) top = fmaxf(top, s_m[i]);
+    }
+    const Scale sc = scale_of(top, kLog2e * p.inv_temp);
+    float z = 0.f, s = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const float l = fmaxf(sc.log2_weight(v[u].at(k)), kLog2Zero), e = exp2_fast(l);
+            z += e;
+            s = fmaf(e, l, s);
+        }
+    z = sum_wave(z);
+    s = sum_wave(s);
+    if constexpr (W > 1) {
+        if ((tid & 63) == 0) {
+            s_z[wave] = z;
+            s_s[wave] = s;
+        }
+        __syncthreads();
+        z = s = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            z += s_z[i];
+            s += s_s[i];
+        }
+    }
+    const PolicyRow r = policy_row<LOSS>(p, z, s, sc.log2_weight(taken), old, adv, w);
+    if (tid == 0) policy_outputs<LOSS>(p, row, r);
+    if (!g) return;
+    const float l2z = log2_fast(z);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = tid + u * kLanes;
+        float d[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) d[k] = r.some ? policy_gradient(r, sc, l2z, v[u].at(k)) : 0.f;
+        if (i == a / K) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (k == a % K) d[k] += r.d;
+        }
+        if (i < vecs) store_row_vec<DT>(g, i, p.V, d);
+    }
+}
+
 // Longer rows, one per workgroup of W waves: one pass for the statistics, each lane relative to its own
 // running maximum, and one that writes the gradient, for which the row comes out of the caches.
 template <typename DT, bool LOSS, int W>

@@ -15,14 +15,31 @@ void launch_small(const PolicyArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((policy_small_kernel<DT, LOSS, L, E>), dim3(unsigned((p.M + rows - 1) / rows)), dim3(4 * kWave), 0, s, p);
 }
 
+template <typename DT, bool LOSS, int W, int U>
+void launch_vec(const PolicyArgs& p, hipStream_t s) {
+    const int64_t rows = W == 1 ? 4 : 1;
+    hipLaunchKernelGGL((policy_vec_kernel<DT, LOSS, W, U>), dim3(unsigned((p.M + rows - 1) / rows)), dim3((W == 1 ? 4 : W) * kWave), 0, s, p);
+}
+
 template <typename DT, bool LOSS>
 rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
-    if (p.V <= 32) launch_small<DT, LOSS, 8, 4>(p, s);
-    else if (p.V <= 64) launch_small<DT, LOSS, 16, 4>(p, s);
-    else if (p.V <= 128) launch_small<DT, LOSS, 32, 4>(p, s);
-    else if (p.V <= 256) launch_small<DT, LOSS, 64, 4>(p, s);
-    else if (p.V <= 512) launch_small<DT, LOSS, 64, 8>(p, s);
-    else if (p.V <= 1024) launch_small<DT, LOSS, 64, 16>(p, s);
+    constexpr int64_t kVec = 16 / sizeof(DT);
+    if (p.V <= 8) launch_small<DT, LOSS, 4, 2>(p, s);
+    else if (p.V <= 16) launch_small<DT, LOSS, 4, 4>(p, s);
+    else if (p.V <= 24) launch_small<DT, LOSS, 4, 6>(p, s);
+    else if (p.V <= 32) launch_small<DT, LOSS, 4, 8>(p, s);
+    else if (p.V <= 64) launch_small<DT, LOSS, 8, 8>(p, s);
+    else if (p.V <= 128) launch_small<DT, LOSS, 16, 8>(p, s);
+    else if (p.V <= 256) launch_small<DT, LOSS, 32, 8>(p, s);
+    else if (sizeof(DT) == 4 && p.V <= 512) launch_small<DT, LOSS, 64, 8>(p, s);
+    else if (sizeof(DT) == 4 && p.V <= 1024) launch_small<DT, LOSS, 64, 16>(p, s);
+    else if (p.V <= 64 * kVec) launch_vec<DT, LOSS, 1, 1>(p, s);
+    else if (p.V <= 64 * 2 * kVec) launch_vec<DT, LOSS, 1, 2>(p, s);
+    else if (p.V <= 64 * 4 * kVec) launch_vec<DT, LOSS, 1, 4>(p, s);
+    else if (p.V <= 64 * 8 * kVec) launch_vec<DT, LOSS, 1, 8>(p, s);
+    else if (p.V <= 256 * 4 * kVec) launch_vec<DT, LOSS, 4, 4>(p, s);
+    else if (p.V <= 256 * 8 * kVec) launch_vec<DT, LOSS, 4, 8>(p, s);
+    else if (p.V <= 512 * 8 * kVec) launch_vec<DT, LOSS, 8, 8>(p, s);
     else hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, 8>), dim3(unsigned(p.M)), dim3(8 * kWave), 0, s, p);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
