@@ -21,6 +21,18 @@ void launch_vec(const PolicyArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((policy_vec_kernel<DT, LOSS, W, U>), dim3(unsigned((p.M + rows - 1) / rows)), dim3((W == 1 ? 4 : W) * kWave), 0, s, p);
 }
 
+// Rows that do not fit the registers of eight waves (with sixteen, one workgroup would have the CU to
+// itself and nothing to do while it waits: 4096 x 40000 bfloat16 196 us against 148) take sixteen waves where few rows leave CUs to them (64 x 128000
+// bfloat16 27 -> 23 us), and from this length on, where eight waves have twice as many rows in the
+// caches between their two readings (2048 x 128000 float32 594 -> 460 us, x 40000 280 either way);
+// otherwise eight (8192 x 20000 float32 272 us against 330).
+constexpr int64_t kFewRows = 256, kLongRow = 320 << 10;
+
+template <typename DT, bool LOSS, int W>
+void launch_rows(const PolicyArgs& p, hipStream_t s) {
+    hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, W>), dim3(unsigned(p.M)), dim3(W * kWave), 0, s, p);
+}
+
 template <typename DT, bool LOSS>
 rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
     constexpr int64_t kVec = 16 / sizeof(DT);
@@ -40,7 +52,8 @@ rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
     else if (p.V <= 256 * 4 * kVec) launch_vec<DT, LOSS, 4, 4>(p, s);
     else if (p.V <= 256 * 8 * kVec) launch_vec<DT, LOSS, 4, 8>(p, s);
     else if (p.V <= 512 * 8 * kVec) launch_vec<DT, LOSS, 8, 8>(p, s);
-    else hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, 8>), dim3(unsigned(p.M)), dim3(8 * kWave), 0, s, p);
+    else if (p.M <= kFewRows || p.V * int64_t(sizeof(DT)) >= kLongRow) launch_rows<DT, LOSS, 16>(p, s);
+    else launch_rows<DT, LOSS, 8>(p, s);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
 
