@@ -390,8 +390,9 @@ rlcs_status rlcs_policy_loss(const void* logits, const int32_t* tokens, const fl
  *            the distribution it was drawn from. A row of masked logits only: token -1, logp -inf
  *   ws       optional: rlcs_workspace_size_sample(M, V) bytes, 16-byte aligned, need not be cleared.
  *            Calls of few rows and no filters use it to split a row over several workgroups.
- * V <= 2^24. Masses of the filters are sums of multiples of 2^-38 of the largest weight, so the result
- * does not depend on the order of addition.                                                  */
+ * V <= 2^24. Masses are added in an order fixed by the sizes, or as integers (multiples of 2^-38 of the
+ * largest weight), so results repeat bit for bit; a cut by mass that lies within their rounding
+ * of a token may fall on either side of it.                                                  */
 rlcs_status rlcs_sample(const void* logits, const float* noise, const float* temperature,
                         const int32_t* top_k, const float* top_p, const float* min_p,
                         int32_t* tokens, float* logp, int64_t M, int64_t V, int64_t ld,

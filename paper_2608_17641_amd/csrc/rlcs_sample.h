@@ -8,6 +8,7 @@
 // What top-k and top-p keep are the elements above a threshold in the order (logit falling, index
 // rising). Each row takes the shortest way to it:
 //   no filter    one pass: the race and the sum of weights.
+//   short rows   one wave a row: halving the range of keys, in registers.
 //   few kept     (a top-k of at most kFewest) the k-th largest of the lanes' maxima is a lower bound of the
 //                k-th logit; the elements from there on, little more than k, are ranked by comparing
 //                each with each.
@@ -432,11 +433,18 @@ __device__ __forceinline__ Drawn draw_sorted(const uint64_t* sorted, int most, c
     return d;
 }
 
-// A row without filters: the race and the sum of weights in one pass. False: the scores overflow
-// (logits beyond 10^38 / c), and the general way has to take them relative to the largest.
+// What a part of a row without filters comes to: its race's winner, its largest logit, the sum of weights
+// relative to that.
+struct OpenPart {
+    uint64_t winner;
+    float top, z;
+};
+
+// Part of a row without filters: the race and the sum of weights in one pass. `first`: index of the
+// part's first element.
 template <typename DT, int W, int U, bool ONE>
-__device__ __forceinline__ bool sample_open(const SampleArgs& a, const RowWalk<DT, W, U, ONE>& walk, RowView<DT>& r, const float* noise,
-                                            float c, int64_t row, uint64_t* slots, float* slots_f, float& all_top) {
+__device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk, const float* noise, float c, uint32_t first,
+                                              uint64_t* slots, float* slots_f) {
     constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
     const bool greedy = !(c < __builtin_inff());  // (temperature 0)
     const bool race = noise && !greedy;
@@ -448,7 +456,7 @@ __device__ __forceinline__ bool sample_open(const SampleArgs& a, const RowWalk<D
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int q = 0; q < K / 4; ++q) e[u][q].load(noise, (i0 + u * kLanes) * (K / 4) + q, a.V);
+                for (int q = 0; q < K / 4; ++q) e[u][q].load(noise, (i0 + u * kLanes) * (K / 4) + q, walk.V);
         }
         float t = top;
 #pragma unroll
@@ -475,19 +483,27 @@ __device__ __forceinline__ bool sample_open(const SampleArgs& a, const RowWalk<D
             }
         if (where >= 0) at = uint32_t((i0 + where / K * kLanes) * K + where % K);
     });
-    all_top = max_group_f<W>(top, slots_f);
-    if (all_top == kNegInf) {
+    OpenPart p;
+    p.top = max_group_f<W>(top, slots_f);
+    p.winner = max_group<W>(best == kNegInf ? 0 : race_entry(order_key(best), first + at), slots);
+    p.z = sum_group<W>(top == kNegInf || greedy ? 0.f : z * exp2_fast((top - p.top) * c), slots);
+    return p;
+}
+
+// The row's outputs from its whole part. False: the scores overflow (logits beyond 10^38 / c), or none is
+// above -inf (noise out of its range), and the general way has to take the row.
+template <typename DT>
+__device__ __forceinline__ bool open_finish(const SampleArgs& a, const OpenPart& p, RowView<DT>& r, float c, int64_t row) {
+    if (p.top == kNegInf) {
         if (threadIdx.x == 0) sample_none(a, row);
         return true;
     }
-    r.scale = scale_of(all_top, c);
-    const uint64_t winner = max_group<W>(best == kNegInf ? 0 : race_entry(order_key(best), at), slots);
-    if (!greedy && (r.scale.c != c || winner == 0)) return false;  // (no score above -inf: noise out of its range)
-    z = top == kNegInf || greedy ? 0.f : z * exp2_fast((top - all_top) * c);
-    z = sum_group<W>(z, slots);
+    const bool greedy = !(c < __builtin_inff());
+    r.scale = scale_of(p.top, c);
+    if (!greedy && (r.scale.c != c || p.winner == 0)) return false;
     if (threadIdx.x == 0) {
-        const uint32_t j = race_index(winner);
-        sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(z));
+        const uint32_t j = race_index(p.winner);
+        sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(p.z));
     }
     return true;
 }
@@ -500,10 +516,40 @@ __global__ __launch_bounds__(W * kWave) void sample_open_kernel(SampleArgs a) {
     RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
-    const RowWalk<DT, W, U, ONE> walk(r.x, a.V);
-    float top;
-    if (!sample_open<DT, W, U, ONE>(a, walk, r, noise, sample_scale(s), row, s_slots, s_slots_f, top))
-        sample_general<DT, W>(a, s, r, noise, top, row, s_bins, s_slots);
+    const float c = sample_scale(s);
+    const OpenPart p = open_part<DT, W, U, ONE>(RowWalk<DT, W, U, ONE>(r.x, a.V), noise, c, 0u, s_slots, s_slots_f);
+    if (!open_finish<DT>(a, p, r, c, row)) sample_general<DT, W>(a, s, r, noise, p.top, row, s_bins, s_slots);
+}
+
+// Few long rows: parts of `length` elements (a multiple of a vector) on workgroups of their own,
+template <typename DT, int W, int U>
+__global__ __launch_bounds__(W * kWave) void sample_parts_kernel(SampleArgs a, OpenPart* parts, int64_t length) {
+    __shared__ uint64_t s_slots[W];
+    __shared__ float s_slots_f[W];
+    const int64_t row = blockIdx.y, first = int64_t(blockIdx.x) * length;
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld + first;
+    const float* noise = a.noise ? a.noise + row * a.ld_noise + first : nullptr;
+    const RowWalk<DT, W, U, false> walk(x, a.V - first < length ? a.V - first : length);
+    const OpenPart p = open_part<DT, W, U, false>(walk, noise, sample_scale(sample_row(a, row)), uint32_t(first), s_slots, s_slots_f);
+    if (threadIdx.x == 0) parts[row * gridDim.x + blockIdx.x] = p;
+}
+
+// and their join, four waves a row (one does, unless the general way has to take it).
+template <typename DT>
+__global__ __launch_bounds__(4 * kWave) void sample_join_kernel(SampleArgs a, const OpenPart* parts, int count) {
+    __shared__ uint64_t s_bins[kDigits], s_slots[4];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const SampleRow s = sample_row(a, row);
+    const float c = sample_scale(s);
+    const OpenPart mine = lane < count ? parts[row * count + lane] : OpenPart{0, kNegInf, 0.f};
+    OpenPart p;
+    p.top = max_wave(mine.top);
+    p.winner = max_wave(mine.winner);
+    p.z = sum_wave(mine.top == kNegInf ? 0.f : mine.z * exp2_fast(mine.top == p.top ? 0.f : (mine.top - p.top) * c));
+    if (!open_finish<DT>(a, p, r, c, row))
+        sample_general<DT, 4>(a, s, r, a.noise ? a.noise + row * a.ld_noise : nullptr, p.top, row, s_bins, s_slots);
 }
 
 // One row per workgroup of W waves, with its filters. The cases that the quicker ways leave end in
@@ -524,7 +570,11 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
 
     auto quick = [&]() -> bool {
         if (!(c < __builtin_inff()) || (!by_k && !by_p && !by_min))
-            return sample_open<DT, W, U, ONE>(a, walk, r, noise, c, row, sh.slots, sh.slots_f, top);
+        {
+            const OpenPart p = open_part<DT, W, U, ONE>(walk, noise, c, 0u, sh.slots, sh.slots_f);
+            top = p.top;
+            return open_finish<DT>(a, p, r, c, row);
+        }
 
         if (by_k && s.top_k <= kFewest) {
             walk.chunks([&](const RowVec<DT>(&v)[U], int64_t) {
@@ -734,6 +784,130 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
         return true;
     };
     if (!quick()) sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
+}
+
+// Rows of up to 64 * E logits with filters, one per wave, logits and keys in registers (lane i has
+// elements i, 64 + i, ...). A threshold is searched for by halving the range of keys: each step counts,
+// or weighs, what lies above the middle, and the search ends when the cut falls between two elements
+// (12 to 14 steps on random logits) or at equal ones, of which the first by index stay.
+template <typename DT, int E>
+__global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= a.M) return;
+    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
+    const SampleRow s = sample_row(a, row);
+    const float c = sample_scale(s);
+    const bool greedy = !(c < __builtin_inff());
+    constexpr uint32_t kOut = 0u, kLowest = 0x00800000u;  // keys: of a dropped element; of the lowest finite number
+    float v[E], n[E], top = kNegInf;
+    uint32_t key[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int j = lane + kWave * e;
+        v[e] = j < a.V ? r.logit(j) : kNegInf;
+        n[e] = j < a.V && noise && !greedy ? noise[j] : 1.f;
+        key[e] = v[e] > kNegInf ? order_key(v[e]) : kOut;
+        top = fmaxf(top, v[e]);
+    }
+    top = max_wave(top);
+    if (top == kNegInf) {
+        if (lane == 0) sample_none(a, row);
+        return;
+    }
+    r.scale = scale_of(top, c);
+    auto count = [&](uint32_t from) {
+        int x = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x += __popcll(__ballot(key[e] >= from));
+        return x;
+    };
+    // Drops what lies below `from`, and of the elements equal to it all but the first `quota`.
+    auto drop = [&](uint32_t from, int quota) {
+        int before = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint64_t ties = __ballot(key[e] == from);
+            const int rank = before + __popcll(ties & ((1ull << lane) - 1));
+            before += __popcll(ties);
+            if (key[e] < from || (key[e] == from && rank >= quota)) key[e] = kOut;
+        }
+    };
+    if (!greedy) {
+        if (s.top_k < a.V) {
+            const int k = int(s.top_k);
+            uint32_t lo = kLowest, hi = order_key(top) + 1;
+            int above_lo = count(lo), above_hi = 0;
+            if (above_lo > k) {
+                while (hi - lo > 1 && above_lo > k) {
+                    const uint32_t mid = lo + (hi - lo) / 2;
+                    const int x = count(mid);
+                    if (x >= k) {
+                        lo = mid;
+                        above_lo = x;
+                    } else {
+                        hi = mid;
+                        above_hi = x;
+                    }
+                }
+                drop(lo, above_lo > k ? k - above_hi : kWave * E);
+            }
+        }
+        if (s.top_p < 1.f) {
+            float w[E], z = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                w[e] = key[e] != kOut ? exp2_fast(r.log2_weight(v[e])) : 0.f;
+                z += w[e];
+            }
+            const float target = fmaxf(s.top_p * sum_wave(z), 1e-30f);
+            uint32_t lo = kLowest, hi = order_key(top) + 1;
+            int above_lo = count(lo), above_hi = 0;
+            float mass_hi = 0.f;
+            while (hi - lo > 1 && above_lo - above_hi > 1) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                float m = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) m += key[e] >= mid ? w[e] : 0.f;
+                m = sum_wave(m);
+                if (m >= target) {
+                    lo = mid;
+                    above_lo = count(mid);
+                } else {
+                    hi = mid;
+                    above_hi = count(mid);
+                    mass_hi = m;
+                }
+            }
+            int quota = kWave * E;
+            if (above_lo - above_hi > 1) {  // equal ones: as many as begin below the target
+                const float one = exp2_fast(r.log2_weight(key_value(lo)));
+                quota = one > 0.f ? int(fminf(fmaxf(ceilf((target - mass_hi) / one), 1.f), float(kWave * E))) : 1;
+            }
+            drop(lo, quota);
+        }
+        if (s.min_p > 0.f) {
+            const float least = least_weight(s, r, top);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (!(exp2_fast(r.log2_weight(v[e])) >= least)) key[e] = kOut;
+        }
+    }
+    float z = 0.f;
+    uint64_t winner = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (key[e] == kOut) continue;
+        const float u = r.log2_weight(v[e]);
+        z += exp2_fast(u);
+        const uint64_t x = race_entry(noise && !greedy ? order_key(u - log2_fast(n[e])) : key[e], uint32_t(lane + kWave * e));
+        winner = x > winner ? x : winner;
+    }
+    z = sum_wave(z);
+    winner = max_wave(winner);
+    const uint32_t j = race_index(winner);
+    if (lane == 0) sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(z));
 }
 
 // Rows of up to L * E logits, L lanes a row, no filters.
