@@ -36,6 +36,10 @@ int64_t open_parts(int64_t M, int64_t V) {
     return parts > 64 ? 64 : parts;
 }
 
+// Waves a row: sixteen where a row has a CU to itself, four where there are rows enough to fill the
+// CUs with small workgroups, whose waves spend less time at barriers and behind the one that ranks
+// and draws (1024 x 30000 bfloat16 top-k 45 us with sixteen, 26 with four; top-p 107 and 86; 512 x 30000
+// 24 with sixteen, 18 with eight; 64 x 32000 11 with sixteen).
 template <typename DT>
 rlcs_status run_sample(const SampleArgs& a, void* ws, size_t ws_bytes, hipStream_t s) {
     constexpr int kVec = 16 / sizeof(DT);
@@ -63,8 +67,12 @@ rlcs_status run_sample(const SampleArgs& a, void* ws, size_t ws_bytes, hipStream
         launch_wave<DT, 8>(a, s);
     } else if (a.V <= 1024) {
         launch_wave<DT, 16>(a, s);
-    } else if (a.V <= 4 * 256 * kVec) {
-        launch_rows<DT, 4, 4, true>(a, open, s);
+    } else if (a.V <= 2 * 256 * kVec) {  // rows that four waves hold in registers, two vectors a lane
+        launch_rows<DT, 4, 2, true>(a, open, s);
+    } else if (a.M >= 1024) {
+        launch_rows<DT, 4, 2, false>(a, open, s);
+    } else if (a.M > 256) {
+        launch_rows<DT, 8, 2, false>(a, open, s);
     } else if (a.V <= 4 * 1024 * kVec) {
         launch_rows<DT, 16, 4, true>(a, open, s);
     } else {
