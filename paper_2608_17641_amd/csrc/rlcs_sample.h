@@ -163,9 +163,12 @@ struct RowView {
         return v == v ? v : kNegInf;
     }
     __device__ __forceinline__ float log2_weight(float v) const { return scale.log2_weight(v); }
-    __device__ __forceinline__ uint64_t mass(float v) const {
-        return uint64_t(exp2_fast(log2_weight(v)) * float(kMassUnit));
+    // A weight (at most a little over 1) as an integer: its 2^-6 and 2^-38 parts, exact in float32.
+    static __device__ __forceinline__ uint64_t mass_of(float w) {
+        const float x = w * 64.f;
+        return (uint64_t(uint32_t(x)) << 32) | uint32_t(__builtin_amdgcn_fractf(x) * 4294967296.f);
     }
+    __device__ __forceinline__ uint64_t mass(float v) const { return mass_of(exp2_fast(log2_weight(v))); }
 };
 
 // The weight that min-p asks for (the largest logit always has it).
@@ -289,6 +292,7 @@ constexpr int kList = 512;       // elements that can be ranked
 constexpr int kFewest = 256;     // top-k that goes by lanes' maxima
 constexpr int kMassBins = 2048;  // 64 an octave of weight: down to 2^-32 of the largest
 constexpr float kBinsPerOctave = 64.f;
+constexpr int kBatch = 256;  // kept elements a wave draws from at a time
 
 // A row as its workgroup walks it, U vectors a lane at a time: f(vectors, index of the first; the
 // others follow kLanes vectors apart). Past the row's end vectors are -inf. With ONE the row is no longer
@@ -312,11 +316,12 @@ struct RowWalk {
         if constexpr (ONE) {
             f(kept, int64_t(threadIdx.x));
         } else {
-            const int64_t vecs = (V + K - 1) / K;
-            for (int64_t i0 = threadIdx.x; i0 < vecs; i0 += U * kLanes) {
+            // (a wave's lanes all make the same rounds, some of them past the end: f may vote)
+            const int64_t vecs = (V + K - 1) / K, lane = threadIdx.x & 63;
+            for (int64_t i0 = threadIdx.x & ~63u; i0 < vecs; i0 += U * kLanes) {
                 RowVec<DT> v[U];
-                read(v, i0);
-                f(v, i0);
+                read(v, i0 + lane);
+                f(v, i0 + lane);
             }
         }
     }
@@ -358,6 +363,10 @@ struct SampleShared {
     union {
         uint64_t bins[kMassBins];
         float maxima[W * kWave];
+        struct {
+            float v[W][kBatch * 2];
+            uint32_t j[W][kBatch * 2];
+        } kept;
     };
     uint64_t list[kList], sorted[kList];
     uint64_t slots[W];
@@ -680,11 +689,17 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
             for (int i = tid; i < kMassBins; i += kLanes) sh.bins[i] = 0;
             if (tid == 0) sh.count = 0;
             __syncthreads();
-            walk.each([&](float v, uint32_t) {
-                const float u = r.log2_weight(v);
-                const int bin = int(-u * kBinsPerOctave);
-                if (u >= low && bin < kMassBins)
-                    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[bin < 0 ? 0 : bin]), (unsigned long long)(r.mass(v)));
+            const float from = fmaxf(low, -float(kMassBins) / kBinsPerOctave * 0.9999f);  // (in the last bin still)
+            walk.chunks([&](const RowVec<DT>(&v)[U], int64_t) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        const float l = r.log2_weight(v[u].at(k));
+                        if (l >= from)  // (not of NaN)
+                            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[uint32_t(fmaxf(l * -kBinsPerOctave, 0.f))]),
+                                      (unsigned long long)(r.mass_of(exp2_fast(l))));
+                    }
             });
             __syncthreads();
             // the first bin at which the sum reaches p of the mass (at least the largest element's)
@@ -726,48 +741,80 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
             above = sh.top;
             if (cross == kMassBins) return false;  // (so flat that the cut lies below 2^-32)
         }
+        // Above `sure` everything is kept, between the two edges lies the crossing bin. What passes goes
+        // through a buffer of the wave's own, so that the few kept ones of many are weighed, and their
+        // noise fetched, by full waves.
+        // (the first bin takes logarithms that rounding leaves above 0, too)
+        const float sure = !by_p ? kNegInf : cross > 0 ? -float(cross) / kBinsPerOctave : __builtin_inff();
+        const float edge = by_p ? -float(cross + 1) / kBinsPerOctave : kNegInf;
+        __syncthreads();  // (the bins' memory)
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        float* kept_v = sh.kept.v[wave];
+        uint32_t* kept_j = sh.kept.j[wave];
         float zk = 0.f;
         uint64_t winner = 0;
-        walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
-            // which are kept; then the noise of those alone, all of its loads before the first use
-            float e[U][K];
-            uint64_t keep = 0;
+        auto draw = [&](int n) {  // the buffer's first n (at most kBatch)
+            float x[kBatch / kWave], e[kBatch / kWave];
+            uint32_t j[kBatch / kWave];
+            wave_lds_sync();
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const float x = fmaxf(v[u].at(k), kNegInf), l = r.log2_weight(x), w = exp2_fast(l);
-                    const uint32_t j = uint32_t((i0 + u * kLanes) * K + k);
-                    bool in = w >= least && x > kNegInf;
-                    if (by_p) {
-                        const int at = int(fminf(fmaxf(-l * kBinsPerOctave, 0.f), float(kMassBins)));
-                        if (in && at == cross) {
-                            const uint32_t i = atomicAdd(&sh.count, 1u);
-                            if (i < kList) sh.list[i] = race_entry(order_key(x), j);
-                        }
-                        in = in && at < cross;
-                    }
-                    if (in) keep |= 1ull << (u * K + k);
-                    zk += in ? w : 0.f;
-                    e[u][k] = 1.f;
-                }
-            if (noise) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-                        if ((keep >> (u * K + k)) & 1) e[u][k] = noise[(i0 + u * kLanes) * K + k];
+            for (int q = 0; q < kBatch / kWave; ++q) {
+                const int i = q * kWave + lane;
+                x[q] = i < n ? kept_v[i] : kNegInf;
+                j[q] = i < n ? kept_j[i] : 0u;
+                e[q] = noise ? noise[j[q]] : 1.f;
             }
 #pragma unroll
+            for (int q = 0; q < kBatch / kWave; ++q) {
+                if (!(x[q] > kNegInf)) continue;
+                const float l = r.log2_weight(x[q]), w = exp2_fast(l);
+                if (!(w >= least)) continue;
+                if (l <= sure) {
+                    const uint32_t i = atomicAdd(&sh.count, 1u);
+                    if (i < kList) sh.list[i] = race_entry(order_key(x[q]), j[q]);
+                    continue;
+                }
+                zk += w;
+                const uint64_t y = race_entry(order_key(noise ? l - log2_fast(e[q]) : x[q]), j[q]);
+                winner = y > winner ? y : winner;
+            }
+        };
+        int held = 0;
+        walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
+#pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    if (!((keep >> (u * K + k)) & 1)) continue;
-                    const float x = v[u].at(k), score = noise ? r.log2_weight(x) - log2_fast(e[u][k]) : x;
-                    const uint64_t y = race_entry(order_key(score), uint32_t((i0 + u * kLanes) * K + k));
-                    winner = y > winner ? y : winner;
+                    const float x = v[u].at(k);
+                    const bool in = r.log2_weight(x) > edge;  // (not of NaN, nor of a masked logit)
+                    const uint64_t passed = __ballot(in);
+                    if (in) {
+                        const int i = held + __popcll(passed & ((1ull << lane) - 1));
+                        kept_v[i] = x;
+                        kept_j[i] = uint32_t((i0 + u * kLanes) * K + k);
+                    }
+                    held += __popcll(passed);
+                    if (k % 4 == 3 && held >= kBatch) {  // (at most kBatch + 4 * 63 by then)
+                        draw(kBatch);
+                        held -= kBatch;
+                        wave_lds_sync();
+                        float xs[kBatch / kWave];
+                        uint32_t js[kBatch / kWave];
+#pragma unroll
+                        for (int q = 0; q < kBatch / kWave; ++q) {
+                            xs[q] = kept_v[kBatch + q * kWave + lane];
+                            js[q] = kept_j[kBatch + q * kWave + lane];
+                        }
+                        wave_lds_sync();
+#pragma unroll
+                        for (int q = 0; q < kBatch / kWave; ++q) {
+                            kept_v[q * kWave + lane] = xs[q];
+                            kept_j[q * kWave + lane] = js[q];
+                        }
+                    }
                 }
         });
+        if (held) draw(held);
         zk = sum_group<W>(zk, sh.slots);
         winner = max_group<W>(winner, sh.slots);
         if (by_p) {
