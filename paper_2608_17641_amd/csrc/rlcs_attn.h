@@ -27,33 +27,35 @@ struct AttnArgs {
     const int32_t *prefix_len, *suffix_len;
     void* o;
     float* lse;
-    int64_t N, G, Hq, Hkv, D, P, S;
+    int32_t N, G, Hq, Hkv, D, P, S;  // (N * G * Hq below 2^31, P and S up to 2^30)
     rlcs_attn_layout at;
     float scale2;  // scale * log2(e): scores in base 2
 };
 
-// How a call is cut into workgroups: `prefix_parts` pieces of `prefix_chunk` keys of every prefix tile
+// How a call is cut into items, each a workgroup's, or with `solo` a wave's (but a prefix that waves
+// share): `prefix_parts` pieces of `prefix_chunk` keys of every prefix tile
 // (`prefix_tiles` a key head), then the suffix's. With `whole` a suffix tile takes the prefix too. With
 // one part in all (`part_acc` null) results go straight to the outputs.
 struct AttnPlan {
-    int64_t prefix_chunk, suffix_chunk;
-    int32_t prefix_parts, suffix_parts, prefix_tiles, suffix_tiles;
-    int32_t prefix_items, items;  // workgroups of the prefix, and all
-    int32_t prefix_groups, groups;  // the same in groups of kGroup, as they are dealt
-    bool whole;
+    int32_t prefix_chunk, suffix_chunk, prefix_parts, suffix_parts, prefix_tiles, suffix_tiles;
+    int32_t prefix_items, suffix_items;
+    int32_t prefix_groups, groups;  // workgroups of the prefix, and all, in groups of kGroup, as they are dealt
+    bool whole, solo;
     float* part_acc;  // [part][row][D]: outputs relative to the part's own maximum
     float2* part_ml;  // [part][row]: maximum (base 2) and sum
 };
 
-__device__ __forceinline__ int64_t clamp_len(const int32_t* p, int64_t i, int64_t most) {
+__device__ __forceinline__ int clamp_len(const int32_t* p, int64_t i, int most) {
     if (!p) return most;
-    const int64_t n = p[i];
+    const int n = p[i];
     return n < 0 ? 0 : n > most ? most : n;
 }
 
 // The prefix's workgroups, which compute, and the suffix's, which wait for memory, are dealt in turn,
 // kGroup of each kind at a time in proportion to their numbers, so that a CU has both.
 constexpr int kGroup = 16;
+
+constexpr int kAttnWaves = 4;
 
 constexpr int kTileRows = 16;  // queries of a matrix product's columns
 
@@ -228,11 +230,11 @@ struct AttnWave {
     // Keys [from, end) of one array: blocks wave, wave + W, ... A block's values are on their way while
     // the scores of the one before are worked out, its keys while those weigh their values. `scale` >= 0.
     template <int W>
-    __device__ __forceinline__ void run(const DT* keys, const DT* values, int64_t sk, int64_t sv, int64_t from, int64_t end, int D,
+    __device__ __forceinline__ void run(const DT* keys, const DT* values, int64_t sk, int64_t sv, int from, int end, int D,
                                         float scale, bf16_t* lds, int wave, int lane) {
         const int c = lane & 15, g = lane >> 4;
         constexpr int KT = kKeys / 16;
-        int64_t j = from + wave * kKeys;
+        int j = from + wave * kKeys;
         if (j >= end) return;
         Block b;
         const char* kb = reinterpret_cast<const char*>(keys + j * sk);
@@ -333,7 +335,7 @@ struct SharedKeys {
     static constexpr size_t kLds = size_t(2 * kHalf) * 2;
 
     static __device__ __forceinline__ void run(AttnWave<bf16_t, ND, QT, EXACT>& w, const bf16_t* keys, const bf16_t* values, int64_t sk,
-                                               int64_t sv, int64_t from, int64_t end, int D, float scale, bf16_t* lds, int tid) {
+                                               int64_t sv, int from, int end, int D, float scale, bf16_t* lds, int tid) {
         const int lane = tid & 63, c = lane & 15, g = lane >> 4;
         constexpr int KT = kKeys / 16;
         u32x4 k[kPieces], v[kPieces];
@@ -348,7 +350,7 @@ struct SharedKeys {
                 at_v[i] = (row * uint32_t(sv) + d) * 2u;
             }
         };
-        auto load = [&](int64_t j) {
+        auto load = [&](int j) {
             if (end - j < kKeys) aim(int(end - j));
             const char* kb = reinterpret_cast<const char*>(keys + j * sk);
             const char* vb = reinterpret_cast<const char*>(values + j * sv);
@@ -371,7 +373,7 @@ struct SharedKeys {
         put(lds);
         if (from + kKeys < end) load(from + kKeys);
         int turn = 0;
-        for (int64_t j = from; j < end; j += kKeys) {
+        for (int j = from; j < end; j += kKeys) {
             const int rows = end - j < kKeys ? int(end - j) : kKeys;
             const bf16_t* lk = lds + turn * kHalf;
             const bf16_t* lv = lk + kKeys * kKRow;
@@ -432,26 +434,30 @@ constexpr size_t attn_lds() {
 struct AttnItem {
     bool prefix;
     int tile, hk, part, own, rows;  // own: the sequence of a suffix; rows: query rows that share its keys
-    int64_t n, plen, from, end;
-    int r, Hq, G, slot;
+    int64_t n;
+    int plen, from, end, r, Hq, G, slot;
 
     // false: nothing to do (past the last item, or a part past the length, which the joining kernel
     // does not look at)
-    __device__ __forceinline__ bool of(const AttnArgs& a, const AttnPlan& plan, int block) {
+    // `solo_prefix`, `solo_suffix`: the wave, where waves have items of their own, else -1.
+    __device__ __forceinline__ bool of(const AttnArgs& a, const AttnPlan& plan, int block, int solo_prefix, int solo_suffix) {
         const int group = block / kGroup;
         const int before = int(int64_t(group) * plan.prefix_groups / plan.groups);
         prefix = int64_t(group + 1) * plan.prefix_groups / plan.groups > before;
-        // workgroups that run on one XCD are eight apart: there, two tiles of a prefix read the same keys
-        const int within = (block % 8) * (kGroup / 8) + block % kGroup / 8;
+        // Workgroups that run on one XCD are eight apart: there, two tiles of a prefix read the same keys.
+        // The XCDs take turns at a group's places, which else could be the same part of every
+        // sequence (with eight parts and suffixes half their longest, half of the XCDs had no work).
+        const int within = ((block + group) % 8) * (kGroup / 8) + block % kGroup / 8;
         int item = (prefix ? before : group - before) * kGroup + within;
-        if (item >= (prefix ? plan.prefix_items : plan.items - plan.prefix_items)) return false;
+        if ((prefix ? solo_prefix : solo_suffix) >= 0) item = item * kAttnWaves + (prefix ? solo_prefix : solo_suffix);
+        if (item >= (prefix ? +plan.prefix_items : +plan.suffix_items)) return false;
         // (all of these are below 2^31, so 32-bit divisions do)
-        Hq = int(a.Hq);
-        G = int(a.G);
-        const int Hkv = int(a.Hkv);
+        Hq = a.Hq;
+        G = a.G;
+        const int Hkv = a.Hkv;
         r = Hq / Hkv;
-        const int tiles = prefix ? plan.prefix_tiles : plan.suffix_tiles;
-        const int parts = prefix ? plan.prefix_parts : plan.suffix_parts;
+        const int tiles = prefix ? +plan.prefix_tiles : +plan.suffix_tiles;
+        const int parts = prefix ? +plan.prefix_parts : +plan.suffix_parts;
         tile = item % tiles;
         item /= tiles;
         hk = item % Hkv;
@@ -462,10 +468,10 @@ struct AttnItem {
         own = prefix ? 0 : item % G;
         rows = prefix ? G * r : r;
         plen = clamp_len(a.prefix_len, n, a.P);
-        const int64_t chunk = prefix ? plan.prefix_chunk : plan.suffix_chunk;
-        from = part * chunk;
+        const int chunk = prefix ? +plan.prefix_chunk : +plan.suffix_chunk;
+        from = part * chunk;  // (parts reach past 2^30 by less than a chunk)
         end = prefix ? plen : clamp_len(a.suffix_len, n * G + own, a.S);
-        if (end > from + chunk) end = from + chunk;
+        if (end - from > chunk) end = from + chunk;
         slot = prefix ? part : (plan.whole ? 0 : plan.prefix_parts) + part;
         return !plan.part_acc || from < end;
     }
@@ -485,7 +491,7 @@ struct AttnItem {
     __device__ __forceinline__ void store(const AttnArgs& a, const AttnPlan& plan, int i, int d, f32x4 o, float m, float z) const {
         const int64_t out = out_row(i);
         if (plan.part_acc) {
-            const int64_t at = int64_t(slot) * a.N * G * Hq + out;
+            const int64_t at = int64_t(slot) * (a.N * G * Hq) + out;
             *reinterpret_cast<f32x4*>(plan.part_acc + at * a.D + d) = o;
             if (d == 0) plan.part_ml[at] = float2{m, z};
         } else {
@@ -516,6 +522,33 @@ __device__ __forceinline__ uint32_t query_sign(float scale2) {
 }
 __device__ __forceinline__ float score_scale(float scale2) { return fmaxf(fabsf(scale2), 1e-30f); }
 
+// The prefix's or the suffix's keys and values of an item.
+template <typename DT>
+struct ItemKeys {
+    const DT *k, *v;
+    int64_t sk, sv;
+    __device__ __forceinline__ ItemKeys(const AttnArgs& a, const AttnItem& it, bool prefix) {
+        int64_t ak, av;
+        if (prefix) {
+            k = reinterpret_cast<const DT*>(a.kp);
+            v = reinterpret_cast<const DT*>(a.vp);
+            ak = it.n * a.at.kp[0] + it.hk * a.at.kp[2];
+            av = it.n * a.at.vp[0] + it.hk * a.at.vp[2];
+            sk = a.at.kp[1];
+            sv = a.at.vp[1];
+        } else {
+            k = reinterpret_cast<const DT*>(a.ks);
+            v = reinterpret_cast<const DT*>(a.vs);
+            ak = it.n * a.at.ks[0] + it.own * a.at.ks[1] + it.hk * a.at.ks[3];
+            av = it.n * a.at.vs[0] + it.own * a.at.vs[1] + it.hk * a.at.vs[3];
+            sk = a.at.ks[2];
+            sv = a.at.vs[2];
+        }
+        k += ak;
+        v += av;
+    }
+};
+
 // Waves of the workgroup on the same 16 * QT rows and keys of their own.
 template <typename DT, int ND, int QT, int W, bool EXACT>
 __device__ __forceinline__ void attn_split_keys(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem,
@@ -532,14 +565,9 @@ __device__ __forceinline__ void attn_split_keys(const AttnArgs& a, const AttnPla
         w.load_query(x, it.template query<DT>(a, row0 + x * kTileRows + c), D, query_sign<DT>(a.scale2), lane);
     // the prefix (for a suffix tile only if it takes all), then the suffix
     for (int pass = it.prefix || plan.whole ? 0 : 1; pass < (it.prefix ? 1 : 2); ++pass) {
-        const bool first = pass == 0;
-        const DT* k = first ? reinterpret_cast<const DT*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2]
-                            : reinterpret_cast<const DT*>(a.ks) + it.n * a.at.ks[0] + it.own * a.at.ks[1] + it.hk * a.at.ks[3];
-        const DT* v = first ? reinterpret_cast<const DT*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2]
-                            : reinterpret_cast<const DT*>(a.vs) + it.n * a.at.vs[0] + it.own * a.at.vs[1] + it.hk * a.at.vs[3];
-        const bool all = first && !it.prefix;
-        w.template run<W>(k, v, first ? a.at.kp[1] : a.at.ks[2], first ? a.at.vp[1] : a.at.vs[2], all ? 0 : it.from,
-                          all ? it.plen : it.end, D, score_scale(a.scale2), lds, wave, lane);
+        const bool all = pass == 0 && !it.prefix;
+        const ItemKeys<DT> x(a, it, pass == 0);
+        w.template run<W>(x.k, x.v, x.sk, x.sv, all ? 0 : it.from, all ? it.plen : it.end, D, score_scale(a.scale2), lds, wave, lane);
     }
 
     // the waves join, tile by tile
@@ -579,10 +607,46 @@ __device__ __forceinline__ void attn_split_keys(const AttnArgs& a, const AttnPla
     }
 }
 
+// The rows of a wave that has worked out all of their keys.
+template <typename DT, int ND, int QT, bool EXACT>
+__device__ __forceinline__ void attn_store_wave(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, int row0,
+                                                const AttnWave<DT, ND, QT, EXACT>& w) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g4 = lane >> 4;
+    const int D = EXACT ? 16 * ND : int(a.D);
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+        float l = w.l[x];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        const int row = row0 + x * kTileRows + c;
+        if (row >= it.rows) continue;
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+            if (EXACT || 16 * t + 4 * g4 < D) it.template store<DT>(a, plan, row, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l);
+    }
+}
+
+// A wave on rows and keys of its own: no barrier, nothing to join. (Prefix or suffix is a matter of
+// compilation: a choice between members of the arguments at run time kept those in memory.)
+template <typename DT, int ND, bool PREFIX, bool EXACT>
+__device__ __forceinline__ void attn_solo(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem) {
+    const int lane = threadIdx.x & 63, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int D = EXACT ? 16 * ND : int(a.D);
+    bf16_t* lds = reinterpret_cast<bf16_t*>(mem) + wave * 32 * (16 * ND + 16);
+    const int row0 = it.tile * kTileRows;
+    AttnWave<DT, ND, 1, EXACT> w;
+    w.clear();
+    w.load_query(0, it.template query<DT>(a, row0 + c), D, query_sign<DT>(a.scale2), lane);
+    const ItemKeys<DT> x(a, it, PREFIX);
+    w.template run<1>(x.k, x.v, x.sk, x.sv, it.from, it.end, D, score_scale(a.scale2), lds, 0, lane);
+    attn_store_wave<DT, ND, 1, EXACT>(a, plan, it, row0, w);
+}
+
 // Waves of the workgroup on rows of their own, 16 * QT each, and the same keys: prefixes of many rows.
 template <int ND, int QT, int W, bool EXACT>
 __device__ __forceinline__ void attn_share_keys(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem) {
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
     const int D = EXACT ? 16 * ND : int(a.D);
     const int row0 = (it.tile * W + (tid >> 6)) * kTileRows * QT;
     AttnWave<bf16_t, ND, QT, EXACT> w;
@@ -593,20 +657,8 @@ __device__ __forceinline__ void attn_share_keys(const AttnArgs& a, const AttnPla
     SharedKeys<ND, QT, W, EXACT>::run(w, reinterpret_cast<const bf16_t*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2],
                                       reinterpret_cast<const bf16_t*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2], a.at.kp[1],
                                       a.at.vp[1], it.from, it.end, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(mem), tid);
-#pragma unroll
-    for (int x = 0; x < QT; ++x) {
-        float l = w.l[x];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        const int row = row0 + x * kTileRows + c;
-        if (row >= it.rows) continue;
-#pragma unroll
-        for (int t = 0; t < ND; ++t)
-            if (EXACT || 16 * t + 4 * g4 < D) it.template store<bf16_t>(a, plan, row, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l);
-    }
+    attn_store_wave<bf16_t, ND, QT, EXACT>(a, plan, it, row0, w);
 }
-
-constexpr int kAttnWaves = 4;
 
 // How the rows of a prefix are taken: like a suffix's, or two tiles at a time; or (bfloat16) by waves of
 // their own, four of one tile, or, in a kernel of its own, four or eight of two.
@@ -619,17 +671,30 @@ constexpr size_t attn_mem() {
     return n;
 }
 
-template <typename DT, int ND, PrefixRows PR, bool EXACT>
+template <typename DT, int ND, PrefixRows PR, bool SOLO, bool EXACT>
 __global__ __launch_bounds__(kAttnWaves * kWave) void attn_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ __attribute__((aligned(16))) char s_mem[attn_mem<DT, ND, PR, EXACT>()];
-    __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
+    const int wave = SOLO ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : -1;
     AttnItem it;
-    if (!it.of(a, plan, int(blockIdx.x))) return;
-    if (PR != kPrefixOne && it.prefix) {
-        if constexpr (PR == kPrefixTwo) attn_split_keys<DT, ND, 2, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
-        if constexpr (PR == kPrefixShared64) attn_share_keys<ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem);
+    if (!it.of(a, plan, int(blockIdx.x), PR == kPrefixOne ? wave : -1, wave)) return;
+    if constexpr (PR == kPrefixShared64) {
+        if (it.prefix) {
+            attn_share_keys<ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem);
+            return;
+        }
+    }
+    if constexpr (SOLO && PR != kPrefixTwo) {
+        if (PR == kPrefixOne && it.prefix) attn_solo<DT, ND, true, EXACT>(a, plan, it, s_mem);
+        else attn_solo<DT, ND, false, EXACT>(a, plan, it, s_mem);
     } else {
-        attn_split_keys<DT, ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
+        __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
+        if (PR == kPrefixTwo && it.prefix) {
+            attn_split_keys<DT, ND, 2, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
+        } else if constexpr (SOLO) {
+            attn_solo<DT, ND, false, EXACT>(a, plan, it, s_mem);
+        } else {
+            attn_split_keys<DT, ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
+        }
     }
 }
 
@@ -638,7 +703,7 @@ template <int ND, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) void attn_prefix_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ __attribute__((aligned(16))) char s_mem[SharedKeys<ND, 2, W, EXACT>::kLds];
     AttnItem it;
-    if (!it.of(a, plan, int(blockIdx.x))) return;
+    if (!it.of(a, plan, int(blockIdx.x), -1, -1)) return;
     attn_share_keys<ND, 2, W, EXACT>(a, plan, it, s_mem);
 }
 
@@ -648,13 +713,13 @@ template <typename DT>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ f32x4 s_o[256];
     __shared__ float s_z[256];
-    const int lanes = int(a.D / 4), groups = 256 / lanes;
+    const int lanes = a.D / 4, groups = 256 / lanes;
     const int64_t rows = a.N * a.G * a.Hq, out = blockIdx.x;
     const int group = int(threadIdx.x) / lanes, d = 4 * (int(threadIdx.x) % lanes);
-    const int seq = int(out) / int(a.Hq);
-    const int64_t plen = plan.whole ? 0 : clamp_len(a.prefix_len, seq / int(a.G), a.P), slen = clamp_len(a.suffix_len, seq, a.S);
+    const int seq = int(out) / a.Hq;
+    const int plen = plan.whole ? 0 : clamp_len(a.prefix_len, seq / a.G, a.P), slen = clamp_len(a.suffix_len, seq, a.S);
     // parts that hold keys
-    const int np = int((plen + plan.prefix_chunk - 1) / plan.prefix_chunk), ns = int((slen + plan.suffix_chunk - 1) / plan.suffix_chunk);
+    const int np = (plen + plan.prefix_chunk - 1) / plan.prefix_chunk, ns = (slen + plan.suffix_chunk - 1) / plan.suffix_chunk;
     auto slot = [&](int i) { return (i < np ? i : plan.prefix_parts + i - np) * rows + out; };
     float m = kNegInf;
     for (int i = int(threadIdx.x) & 63; i < np + ns; i += kWave) m = fmaxf(m, plan.part_ml[slot(i)].x);

@@ -28,9 +28,12 @@ bool reachable(std::initializer_list<int64_t> sizes, const int64_t* strides) {
 }
 
 // Keys of a part: no fewer than kMinChunk (a part of r rows costs r * D * 8 bytes written and read
-// again), and as many parts as give kWantItems workgroups.
+// again), and as many parts as give the workgroups, or waves, wanted.
 constexpr int64_t kMinChunk = 256;
-constexpr int64_t kWantItems = 512, kWantSuffixItems = 1536;
+constexpr int64_t kWantPrefix = 512, kWantSuffix = 1536, kWantSolo = 4096;
+// From this many pieces of kMinChunk keys (two for each SIMD) every wave takes items of its own, which
+// needs no join in the workgroup; with fewer the waves of a workgroup split an item's keys.
+constexpr int64_t kSoloFrom = 2048;
 // Calls of at most this many keys run as one kernel in which each sequence takes its prefix itself.
 constexpr int64_t kWholeKeys = 512;
 
@@ -53,39 +56,43 @@ int64_t rows_of(PrefixRows p) {  // of a workgroup
 
 bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S, bool bf16) {
     const int64_t r = Hq / Hkv;
+    const PrefixRows pr = prefix_rows(G * r, D, bf16);
     p = AttnPlan{};
     p.whole = P + S <= kWholeKeys || P == 0;
     p.suffix_tiles = int32_t(ceil_div(r, kTileRows));
-    auto split = [](int64_t keys, int64_t base, int64_t items, int64_t& chunk, int32_t& parts) {
+    p.prefix_tiles = int32_t(ceil_div(G * r, rows_of(pr)));
+    const int64_t suffix_base = N * G * Hkv * p.suffix_tiles, prefix_base = N * Hkv * p.prefix_tiles;
+    p.solo = !(p.whole && P > 0) &&
+             suffix_base * ceil_div(S, kMinChunk) + (pr == kPrefixOne ? prefix_base * ceil_div(P, kMinChunk) : 0) >= kSoloFrom;
+    auto split = [](int64_t keys, int64_t base, int64_t items, int32_t& chunk, int32_t& parts) {
         int64_t want = ceil_div(items, base), most = ceil_div(keys, kMinChunk);
         if (want > most) want = most;
         if (want < 1) want = 1;
-        chunk = keys > 0 ? ceil_div(ceil_div(keys, want), 64) * 64 : 1;
+        chunk = int32_t(keys > 0 ? ceil_div(ceil_div(keys, want), 64) * 64 : 1);
         parts = int32_t(keys > 0 ? ceil_div(keys, chunk) : 1);
     };
-    const int64_t suffix_base = N * G * Hkv * p.suffix_tiles;
     p.suffix_chunk = 1;
     p.prefix_chunk = 1;
     if (p.whole && P > 0) {
         p.suffix_parts = 1;
-        p.suffix_chunk = S > 0 ? S : 1;
+        p.suffix_chunk = int32_t(S > 0 ? S : 1);
     } else if (S > 0 || P == 0) {
-        split(S, suffix_base, kWantSuffixItems, p.suffix_chunk, p.suffix_parts);
+        split(S, suffix_base, p.solo ? kWantSolo : kWantSuffix, p.suffix_chunk, p.suffix_parts);
     }
+    const int64_t suffix_items = suffix_base * p.suffix_parts;
     int64_t prefix_items = 0;
+    const bool prefix_solo = p.solo && pr == kPrefixOne;
     if (!p.whole) {
-        const PrefixRows pr = prefix_rows(G * r, D, bf16);
-        p.prefix_tiles = int32_t(ceil_div(G * r, rows_of(pr)));
-        const int64_t base = N * Hkv * p.prefix_tiles;
-        split(P, base, pr == kPrefixShared256 ? kWantItems / 2 : kWantItems, p.prefix_chunk, p.prefix_parts);
-        prefix_items = base * p.prefix_parts;
+        split(P, prefix_base, prefix_solo ? kWantSolo : pr == kPrefixShared256 ? kWantPrefix / 2 : kWantPrefix, p.prefix_chunk, p.prefix_parts);
+        prefix_items = prefix_base * p.prefix_parts;
     }
-    const int64_t items = prefix_items + suffix_base * p.suffix_parts;
-    if (items > INT32_MAX - 2 * kGroup) return false;
-    p.prefix_groups = int32_t(ceil_div(prefix_items, kGroup));
-    p.groups = p.prefix_groups + int32_t(ceil_div(items - prefix_items, kGroup));
+    const int64_t prefix_groups = ceil_div(prefix_items, kGroup * (prefix_solo ? kAttnWaves : 1));
+    const int64_t groups = prefix_groups + ceil_div(suffix_items, kGroup * (p.solo ? kAttnWaves : 1));
+    if (prefix_items + suffix_items > INT32_MAX - 4 * kGroup * kAttnWaves || groups > INT32_MAX / kGroup) return false;
     p.prefix_items = int32_t(prefix_items);
-    p.items = int32_t(items);
+    p.suffix_items = int32_t(suffix_items);
+    p.prefix_groups = int32_t(prefix_groups);
+    p.groups = int32_t(groups);
     return true;
 }
 
@@ -94,25 +101,28 @@ size_t part_bytes(const AttnPlan& p, int64_t rows, int64_t D) {
     return parts > 1 ? size_t(parts * rows) * size_t(4 * D + 8) : 0;
 }
 
-// The items of the prefix alone, or of the suffix alone, of a plan that has both.
+// The workgroups of the prefix alone, or of the suffix alone, of a plan that has both.
 AttnPlan only(AttnPlan p, bool prefix) {
     if (prefix) {
-        p.items = p.prefix_items;
         p.groups = p.prefix_groups;
     } else {
-        p.items -= p.prefix_items;
         p.groups -= p.prefix_groups;
-        p.prefix_items = p.prefix_groups = 0;
+        p.prefix_groups = 0;
     }
     return p;
 }
 
+template <typename DT, int ND, PrefixRows PR, bool SOLO>
+void launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(kAttnWaves * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_kernel<DT, ND, PR, SOLO, true>), grid, block, 0, s, a, p);
+    else hipLaunchKernelGGL((attn_kernel<DT, ND, PR, SOLO, false>), grid, block, 0, s, a, p);
+}
 template <typename DT, int ND, PrefixRows PR>
 void launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     if (p.groups == 0) return;
-    const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(kAttnWaves * kWave);
-    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_kernel<DT, ND, PR, true>), grid, block, 0, s, a, p);
-    else hipLaunchKernelGGL((attn_kernel<DT, ND, PR, false>), grid, block, 0, s, a, p);
+    if (p.solo) launch_attn<DT, ND, PR, true>(a, p, s);
+    else launch_attn<DT, ND, PR, false>(a, p, s);
 }
 
 template <int ND, int W>
@@ -216,7 +226,8 @@ rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* v
     a.q = q; a.kp = kp; a.vp = vp; a.ks = ks; a.vs = vs;
     a.prefix_len = prefix_len; a.suffix_len = suffix_len;
     a.o = o; a.lse = lse;
-    a.N = N; a.G = G; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.P = P; a.S = S;
+    a.N = int32_t(N); a.G = int32_t(G); a.Hq = int32_t(Hq); a.Hkv = int32_t(Hkv); a.D = int32_t(D);
+    a.P = int32_t(P); a.S = int32_t(S);
     a.scale2 = scale * kLog2e;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return bf16 ? run_attn<bf16_t>(a, p, s) : run_attn<float>(a, p, s);
