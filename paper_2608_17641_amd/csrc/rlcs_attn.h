@@ -321,21 +321,25 @@ struct AttnWave {
     }
 };
 
-// Keys [from, end) of one array for a workgroup whose waves have queries of their own (bfloat16): all of
+// Keys [from, end) of one array for a workgroup whose waves have queries of their own: all of
 // its lanes bring blocks of keys and values to LDS, every wave reads them from there. While one
 // block is worked on, the next is in the other half of LDS and the one after it on its way.
-template <int ND, int QT, int W, bool EXACT>
+template <typename DT, int ND, int QT, int W, bool EXACT>
 struct SharedKeys {
-    static constexpr int kKeys = ND > 8 ? 32 : 64;
-    static constexpr int kVecs = 2 * ND;  // 16-byte pieces of a row
-    static constexpr int kKRow = 16 * ND + 8;   // elements of a row in LDS: the sixteen rows of a key operand's read,
-    static constexpr int kVRow = 16 * ND + 16;  // and the eight of half a wave's of values, in different banks
+    static constexpr bool kWide = sizeof(DT) == 4;
+    static constexpr int kKeys = (ND > 8 ? 32 : 64) / (kWide ? 2 : 1);
+    static constexpr int kVecs = ND * int(sizeof(DT));  // 16-byte pieces of a row
+    static constexpr int kVec = 16 / int(sizeof(DT));
+    // elements of a row in LDS: the sixteen rows of a key operand's read, and the eight of half a wave's
+    // of bfloat16 values, or the four of a wave's of float32 ones, in different banks
+    static constexpr int kKRow = 16 * ND + kVec;
+    static constexpr int kVRow = 16 * ND + (kWide ? 4 : 16);
     static constexpr int kPieces = kKeys * kVecs / (W * kWave);
     static constexpr int kHalf = kKeys * (kKRow + kVRow);  // elements
-    static constexpr size_t kLds = size_t(2 * kHalf) * 2;
+    static constexpr size_t kLds = size_t(2 * kHalf) * sizeof(DT);
 
-    static __device__ __forceinline__ void run(AttnWave<bf16_t, ND, QT, EXACT>& w, const bf16_t* keys, const bf16_t* values, int64_t sk,
-                                               int64_t sv, int from, int end, int D, float scale, bf16_t* lds, int tid) {
+    static __device__ __forceinline__ void run(AttnWave<DT, ND, QT, EXACT>& w, const DT* keys, const DT* values, int64_t sk, int64_t sv,
+                                               int from, int end, int D, float scale, DT* lds, int tid) {
         const int lane = tid & 63, c = lane & 15, g = lane >> 4;
         constexpr int KT = kKeys / 16;
         u32x4 k[kPieces], v[kPieces];
@@ -345,9 +349,9 @@ struct SharedKeys {
             for (int i = 0; i < kPieces; ++i) {
                 const int at = tid + W * kWave * i, piece = at % kVecs;
                 const uint32_t row = at / kVecs < rows ? at / kVecs : rows - 1;
-                const uint32_t d = 8u * (EXACT || 8 * piece < D ? piece : D / 8 - 1);
-                at_k[i] = (row * uint32_t(sk) + d) * 2u;
-                at_v[i] = (row * uint32_t(sv) + d) * 2u;
+                const uint32_t d = uint32_t(kVec) * (EXACT || kVec * piece < D ? piece : D / kVec - 1);
+                at_k[i] = (row * uint32_t(sk) + d) * uint32_t(sizeof(DT));
+                at_v[i] = (row * uint32_t(sv) + d) * uint32_t(sizeof(DT));
             }
         };
         auto load = [&](int j) {
@@ -359,12 +363,12 @@ struct SharedKeys {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) v[i] = *reinterpret_cast<const u32x4*>(vb + at_v[i]);
         };
-        auto put = [&](bf16_t* half) {
+        auto put = [&](DT* half) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int at = tid + W * kWave * i;
-                *reinterpret_cast<u32x4*>(half + (at / kVecs) * kKRow + 8 * (at % kVecs)) = k[i];
-                *reinterpret_cast<u32x4*>(half + kKeys * kKRow + (at / kVecs) * kVRow + 8 * (at % kVecs)) = v[i];
+                *reinterpret_cast<u32x4*>(half + (at / kVecs) * kKRow + kVec * (at % kVecs)) = k[i];
+                *reinterpret_cast<u32x4*>(half + kKeys * kKRow + (at / kVecs) * kVRow + kVec * (at % kVecs)) = v[i];
             }
         };
         if (from >= end) return;
@@ -375,8 +379,8 @@ struct SharedKeys {
         int turn = 0;
         for (int j = from; j < end; j += kKeys) {
             const int rows = end - j < kKeys ? int(end - j) : kKeys;
-            const bf16_t* lk = lds + turn * kHalf;
-            const bf16_t* lv = lk + kKeys * kKRow;
+            const DT* lk = lds + turn * kHalf;
+            const DT* lv = lk + kKeys * kKRow;
             turn ^= 1;
             __syncthreads();  // this block is there, and the one before has been read
             if (j + kKeys < end) put(lds + turn * kHalf);
@@ -386,15 +390,29 @@ struct SharedKeys {
             for (int x = 0; x < QT; ++x)
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) s[x][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (kWide) {
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int d = 0; d < ND / 2; ++d) {
-                    const bf16x8 a = *reinterpret_cast<const bf16x8*>(lk + (16 * kt + c) * kKRow + 32 * d + 8 * g);
+                    for (int t = 0; t < ND; ++t) {
+                        const f32x4 k4 = *reinterpret_cast<const f32x4*>(lk + (16 * kt + c) * kKRow + 16 * t + 4 * g);
 #pragma unroll
-                    for (int x = 0; x < QT; ++x)
-                        s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, w.q[x][d]), s[x][kt], 0, 0, 0);
-                }
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int x = 0; x < QT; ++x)
+                                s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[i], __uint_as_float(w.q[x][t][i]), s[x][kt], 0, 0, 0);
+                    }
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int d = 0; d < ND / 2; ++d) {
+                        const bf16x8 k8 = *reinterpret_cast<const bf16x8*>(lk + (16 * kt + c) * kKRow + 32 * d + 8 * g);
+#pragma unroll
+                        for (int x = 0; x < QT; ++x)
+                            s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(bf16x8, w.q[x][d]), s[x][kt], 0, 0, 0);
+                    }
+            }
             if (rows < kKeys) {
 #pragma unroll
                 for (int x = 0; x < QT; ++x)
@@ -406,17 +424,32 @@ struct SharedKeys {
             }
 #pragma unroll
             for (int x = 0; x < QT; ++x) softmax_step<KT, ND>(s[x], scale, w.m[x], w.l[x], w.acc[x]);
+            if constexpr (kWide) {
 #pragma unroll
-            for (int h = 0; h < KT / 2; ++h) {
-                bf16x8 p[QT];
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int x = 0; x < QT; ++x) p[x] = weights_operand(s[x][2 * h], s[x][2 * h + 1]);
-                const bf16_t* at = lv + (32 * h + 4 * g + (c >> 2)) * kVRow + 4 * (c & 3);
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int t = 0; t < ND; ++t) {
-                    const bf16x8 b = values_operand(at + 16 * t, kVRow);
+                        for (int t = 0; t < ND; ++t) {
+                            const float v1 = lv[(16 * kt + 4 * g + i) * kVRow + 16 * t + c];
 #pragma unroll
-                    for (int x = 0; x < QT; ++x) w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, p[x], w.acc[x][t], 0, 0, 0);
+                            for (int x = 0; x < QT; ++x)
+                                w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v1, s[x][kt][i], w.acc[x][t], 0, 0, 0);
+                        }
+            } else {
+#pragma unroll
+                for (int h = 0; h < KT / 2; ++h) {
+                    bf16x8 p[QT];
+#pragma unroll
+                    for (int x = 0; x < QT; ++x) p[x] = weights_operand(s[x][2 * h], s[x][2 * h + 1]);
+                    const DT* at = lv + (32 * h + 4 * g + (c >> 2)) * kVRow + 4 * (c & 3);
+#pragma unroll
+                    for (int t = 0; t < ND; ++t) {
+                        const bf16x8 b = values_operand(reinterpret_cast<const bf16_t*>(at + 16 * t), kVRow);
+#pragma unroll
+                        for (int x = 0; x < QT; ++x)
+                            w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, p[x], w.acc[x][t], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -549,20 +582,18 @@ struct ItemKeys {
     }
 };
 
-// Waves of the workgroup on the same 16 * QT rows and keys of their own.
-template <typename DT, int ND, int QT, int W, bool EXACT>
+// Waves of the workgroup on the same sixteen rows and keys of their own.
+template <typename DT, int ND, int W, bool EXACT>
 __device__ __forceinline__ void attn_split_keys(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem,
                                                 float (*s_m)[kTileRows], float (*s_l)[kTileRows]) {
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = EXACT ? 16 * ND : int(a.D);
     bf16_t* lds = reinterpret_cast<bf16_t*>(mem) + wave * 32 * (16 * ND + 16);
-    const int row0 = it.tile * kTileRows * QT;
-    AttnWave<DT, ND, QT, EXACT> w;
+    const int row0 = it.tile * kTileRows;
+    AttnWave<DT, ND, 1, EXACT> w;
     w.clear();
-#pragma unroll
-    for (int x = 0; x < QT; ++x)
-        w.load_query(x, it.template query<DT>(a, row0 + x * kTileRows + c), D, query_sign<DT>(a.scale2), lane);
+    w.load_query(0, it.template query<DT>(a, row0 + c), D, query_sign<DT>(a.scale2), lane);
     // the prefix (for a suffix tile only if it takes all), then the suffix
     for (int pass = it.prefix || plan.whole ? 0 : 1; pass < (it.prefix ? 1 : 2); ++pass) {
         const bool all = pass == 0 && !it.prefix;
@@ -570,40 +601,37 @@ __device__ __forceinline__ void attn_split_keys(const AttnArgs& a, const AttnPla
         w.template run<W>(x.k, x.v, x.sk, x.sv, all ? 0 : it.from, all ? it.plen : it.end, D, score_scale(a.scale2), lds, wave, lane);
     }
 
-    // the waves join, tile by tile
+    // the waves join
     float* join = reinterpret_cast<float*>(mem);
     constexpr int kJoinRow = 16 * ND + 4;
+    float l = w.l[0];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();
+    if (g4 == 0) {
+        s_m[wave][c] = w.m[0];
+        s_l[wave][c] = l;
+    }
 #pragma unroll
-    for (int x = 0; x < QT; ++x) {
-        float l = w.l[x];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        __syncthreads();
-        if (g4 == 0) {
-            s_m[wave][c] = w.m[x];
-            s_l[wave][c] = l;
+    for (int t = 0; t < ND; ++t)
+        *reinterpret_cast<f32x4*>(join + (wave * kTileRows + c) * kJoinRow + 16 * t + 4 * g4) = w.acc[0][t];
+    __syncthreads();
+    for (int at = tid; at < kTileRows * 4 * ND; at += W * kWave) {
+        const int i = at / (4 * ND), d = 4 * (at % (4 * ND));
+        const int row = row0 + i;
+        if (row >= it.rows || d >= D) continue;
+        float m = kNegInf;
+#pragma unroll
+        for (int v = 0; v < W; ++v) m = fmaxf(m, s_m[v][i]);
+        float z = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < W; ++v) {
+            const float keep = s_m[v][i] == kNegInf ? 0.f : exp2_fast(s_m[v][i] - m);
+            z = fmaf(keep, s_l[v][i], z);
+            o += keep * *reinterpret_cast<const f32x4*>(join + (v * kTileRows + i) * kJoinRow + d);
         }
-#pragma unroll
-        for (int t = 0; t < ND; ++t)
-            *reinterpret_cast<f32x4*>(join + (wave * kTileRows + c) * kJoinRow + 16 * t + 4 * g4) = w.acc[x][t];
-        __syncthreads();
-        for (int at = tid; at < kTileRows * 4 * ND; at += W * kWave) {
-            const int i = at / (4 * ND), d = 4 * (at % (4 * ND));
-            const int row = row0 + x * kTileRows + i;
-            if (row >= it.rows || d >= D) continue;
-            float m = kNegInf;
-#pragma unroll
-            for (int v = 0; v < W; ++v) m = fmaxf(m, s_m[v][i]);
-            float z = 0.f;
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int v = 0; v < W; ++v) {
-                const float keep = s_m[v][i] == kNegInf ? 0.f : exp2_fast(s_m[v][i] - m);
-                z = fmaf(keep, s_l[v][i], z);
-                o += keep * *reinterpret_cast<const f32x4*>(join + (v * kTileRows + i) * kJoinRow + d);
-            }
-            it.template store<DT>(a, plan, row, d, o, m, z);
-        }
+        it.template store<DT>(a, plan, row, d, o, m, z);
     }
 }
 
@@ -644,31 +672,29 @@ __device__ __forceinline__ void attn_solo(const AttnArgs& a, const AttnPlan& pla
 }
 
 // Waves of the workgroup on rows of their own, 16 * QT each, and the same keys: prefixes of many rows.
-template <int ND, int QT, int W, bool EXACT>
+template <typename DT, int ND, int QT, int W, bool EXACT>
 __device__ __forceinline__ void attn_share_keys(const AttnArgs& a, const AttnPlan& plan, const AttnItem& it, char* mem) {
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
     const int D = EXACT ? 16 * ND : int(a.D);
     const int row0 = (it.tile * W + (tid >> 6)) * kTileRows * QT;
-    AttnWave<bf16_t, ND, QT, EXACT> w;
+    AttnWave<DT, ND, QT, EXACT> w;
     w.clear();
 #pragma unroll
     for (int x = 0; x < QT; ++x)
-        w.load_query(x, it.template query<bf16_t>(a, row0 + x * kTileRows + c), D, query_sign<bf16_t>(a.scale2), lane);
-    SharedKeys<ND, QT, W, EXACT>::run(w, reinterpret_cast<const bf16_t*>(a.kp) + it.n * a.at.kp[0] + it.hk * a.at.kp[2],
-                                      reinterpret_cast<const bf16_t*>(a.vp) + it.n * a.at.vp[0] + it.hk * a.at.vp[2], a.at.kp[1],
-                                      a.at.vp[1], it.from, it.end, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(mem), tid);
-    attn_store_wave<bf16_t, ND, QT, EXACT>(a, plan, it, row0, w);
+        w.load_query(x, it.template query<DT>(a, row0 + x * kTileRows + c), D, query_sign<DT>(a.scale2), lane);
+    const ItemKeys<DT> x(a, it, true);
+    SharedKeys<DT, ND, QT, W, EXACT>::run(w, x.k, x.v, x.sk, x.sv, it.from, it.end, D, score_scale(a.scale2), reinterpret_cast<DT*>(mem), tid);
+    attn_store_wave<DT, ND, QT, EXACT>(a, plan, it, row0, w);
 }
 
-// How the rows of a prefix are taken: like a suffix's, or two tiles at a time; or (bfloat16) by waves of
-// their own, four of one tile, or, in a kernel of its own, four or eight of two.
-enum PrefixRows { kPrefixOne, kPrefixTwo, kPrefixShared64, kPrefixShared128, kPrefixShared256 };
+// How the rows of a prefix are taken: like a suffix's; by waves of their own, four of one tile; or, in a
+// kernel of its own, by more rows: bfloat16 four or eight waves of two tiles, float32 eight of one.
+enum PrefixRows { kPrefixOne, kPrefixShared64, kPrefixShared128, kPrefixShared256 };
 
 template <typename DT, int ND, PrefixRows PR, bool EXACT>
 constexpr size_t attn_mem() {
-    size_t n = attn_lds<DT, ND, kAttnWaves>();
-    if constexpr (PR == kPrefixShared64) n = n > SharedKeys<ND, 1, kAttnWaves, EXACT>::kLds ? n : SharedKeys<ND, 1, kAttnWaves, EXACT>::kLds;
-    return n;
+    const size_t n = attn_lds<DT, ND, kAttnWaves>(), k = SharedKeys<DT, ND, 1, kAttnWaves, EXACT>::kLds;
+    return PR == kPrefixShared64 && k > n ? k : n;
 }
 
 template <typename DT, int ND, PrefixRows PR, bool SOLO, bool EXACT>
@@ -679,32 +705,26 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void attn_kernel(AttnArgs a, At
     if (!it.of(a, plan, int(blockIdx.x), PR == kPrefixOne ? wave : -1, wave)) return;
     if constexpr (PR == kPrefixShared64) {
         if (it.prefix) {
-            attn_share_keys<ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem);
+            attn_share_keys<DT, ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem);
             return;
         }
     }
-    if constexpr (SOLO && PR != kPrefixTwo) {
+    if constexpr (SOLO) {
         if (PR == kPrefixOne && it.prefix) attn_solo<DT, ND, true, EXACT>(a, plan, it, s_mem);
         else attn_solo<DT, ND, false, EXACT>(a, plan, it, s_mem);
     } else {
         __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
-        if (PR == kPrefixTwo && it.prefix) {
-            attn_split_keys<DT, ND, 2, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
-        } else if constexpr (SOLO) {
-            attn_solo<DT, ND, false, EXACT>(a, plan, it, s_mem);
-        } else {
-            attn_split_keys<DT, ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
-        }
+        attn_split_keys<DT, ND, kAttnWaves, EXACT>(a, plan, it, s_mem, s_m, s_l);
     }
 }
 
 // The prefix alone: its registers (two tiles a wave) would halve the suffix's waves on a CU.
-template <int ND, int W, bool EXACT>
+template <typename DT, int ND, int QT, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) void attn_prefix_kernel(AttnArgs a, AttnPlan plan) {
-    __shared__ __attribute__((aligned(16))) char s_mem[SharedKeys<ND, 2, W, EXACT>::kLds];
+    __shared__ __attribute__((aligned(16))) char s_mem[SharedKeys<DT, ND, QT, W, EXACT>::kLds];
     AttnItem it;
     if (!it.of(a, plan, int(blockIdx.x), -1, -1)) return;
-    attn_share_keys<ND, 2, W, EXACT>(a, plan, it, s_mem);
+    attn_share_keys<DT, ND, QT, W, EXACT>(a, plan, it, s_mem);
 }
 
 // Joins the parts of a row: one row a workgroup, `groups` of D / 4 lanes (four dimensions each) on

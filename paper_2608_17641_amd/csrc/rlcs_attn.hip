@@ -41,17 +41,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 PrefixRows prefix_rows(int64_t rows, int64_t D, bool bf16) {
     if (rows <= kTileRows) return kPrefixOne;
-    if (!bf16) return D <= 128 ? kPrefixTwo : kPrefixOne;
-    return rows <= 64 || D > 128 ? kPrefixShared64 : rows <= 128 ? kPrefixShared128 : kPrefixShared256;
+    if (rows <= 64 || D > 128) return kPrefixShared64;
+    return rows <= 128 || !bf16 ? kPrefixShared128 : kPrefixShared256;
 }
 int64_t rows_of(PrefixRows p) {  // of a workgroup
-    switch (p) {
-        case kPrefixTwo: return 32;
-        case kPrefixShared64: return 64;
-        case kPrefixShared128: return 128;
-        case kPrefixShared256: return 256;
-        default: return kTileRows;
-    }
+    return p == kPrefixOne ? kTileRows : p == kPrefixShared64 ? 64 : p == kPrefixShared128 ? 128 : 256;
 }
 
 bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P, int64_t S, bool bf16) {
@@ -125,26 +119,28 @@ void launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     else launch_attn<DT, ND, PR, false>(a, p, s);
 }
 
-template <int ND, int W>
+template <typename DT, int ND, int QT, int W>
 void launch_prefix(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(W * kWave);
-    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_prefix_kernel<ND, W, true>), grid, block, 0, s, a, p);
-    else hipLaunchKernelGGL((attn_prefix_kernel<ND, W, false>), grid, block, 0, s, a, p);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((attn_prefix_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a, p);
+    else hipLaunchKernelGGL((attn_prefix_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a, p);
 }
 
 template <typename DT, int ND>
 rlcs_status run_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     const PrefixRows pr = p.prefix_items ? prefix_rows(a.G * (a.Hq / a.Hkv), a.D, sizeof(DT) == 2) : kPrefixOne;
     if (pr == kPrefixOne) launch_attn<DT, ND, kPrefixOne>(a, p, s);
-    if constexpr (sizeof(DT) == 2) {
-        if (pr == kPrefixShared64) launch_attn<DT, ND, kPrefixShared64>(a, p, s);
-        if constexpr (ND <= 8) {
-            if (pr == kPrefixShared128) launch_prefix<ND, 4>(a, only(p, true), s);
-            if (pr == kPrefixShared256) launch_prefix<ND, 8>(a, only(p, true), s);
-            if (pr == kPrefixShared128 || pr == kPrefixShared256) launch_attn<DT, ND, kPrefixOne>(a, only(p, false), s);
+    if (pr == kPrefixShared64) launch_attn<DT, ND, kPrefixShared64>(a, p, s);
+    if constexpr (ND <= 8) {
+        if (pr == kPrefixShared128 || pr == kPrefixShared256) {
+            if constexpr (sizeof(DT) == 4) {
+                launch_prefix<DT, ND, 1, 8>(a, only(p, true), s);
+            } else {
+                if (pr == kPrefixShared128) launch_prefix<DT, ND, 2, 4>(a, only(p, true), s);
+                else launch_prefix<DT, ND, 2, 8>(a, only(p, true), s);
+            }
+            launch_attn<DT, ND, kPrefixOne>(a, only(p, false), s);
         }
-    } else if constexpr (ND <= 8) {
-        if (pr == kPrefixTwo) launch_attn<DT, ND, kPrefixTwo>(a, p, s);
     }
     if (p.part_acc)
         hipLaunchKernelGGL((attn_join_kernel<DT>), dim3(unsigned(a.N * a.G * a.Hq)), dim3(256), 0, s, a, p);
