@@ -81,6 +81,32 @@ def test_against_definition(shape, dtype, ragged):
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
+MANY = [  # enough sequences that waves take items of their own, with every way of taking the prefix's rows
+    (128, 1, 32, 16, 64, 600, 20), (8, 32, 8, 8, 64, 530, 40), (4, 64, 16, 8, 72, 600, 300), (1, 260, 16, 8, 128, 700, 33),
+    (2, 130, 8, 8, 128, 515, 1), (1, 2, 600, 2, 64, 1030, 17), (1, 128, 16, 16, 8, 900, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", MANY)
+def test_many_items(shape, dtype):
+    N, G, Hq, Hkv, D, P, S = shape
+    q, kp, vp, ks, vs, pl, sl = inputs(*shape, dtype, sum(shape))
+    pl[0] = P
+    spoil(kp, pl, 1); spoil(vp, pl, 1)
+    for t in (ks, vs):
+        for n in range(N):
+            spoil(t[n], sl[n], 1)
+    got = rl.rlcs_shared_prefix_attn(*(t.cuda() for t in (q, kp, vp, ks, vs, pl, sl)))
+    # a sample of the sequences, the first and last among them
+    some = sorted({0, G - 1} | set(range(0, G, max(1, G // 3))))
+    groups = sorted({0, N - 1} | set(range(0, N, max(1, N // 3))))
+    at = torch.tensor(some)
+    for n in groups:
+        check(q[n:n + 1, at], kp[n:n + 1], vp[n:n + 1], ks[n:n + 1, at], vs[n:n + 1, at], pl[n:n + 1], sl[n:n + 1, at],
+              1 / math.sqrt(D), (got[0][n:n + 1, at.cuda()], got[1][n:n + 1, at.cuda()]))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("scale", [3.0, -0.2, 0.0])
 def test_large_scores(dtype, scale):
@@ -144,6 +170,30 @@ def test_far_offsets():
     pl = torch.tensor([7], dtype=torch.int32)
     got = rl.rlcs_shared_prefix_attn(q.cuda(), short.cuda(), short.cuda(), kv, kv, pl.cuda(), sl.cuda())
     check(q, short, short, tail, tail, pl, sl, 1 / math.sqrt(D), got)
+
+
+def test_far_tokens():
+    """Tokens so far apart that offsets within one sequence pass 2^31 elements."""
+    N, G, Hq, Hkv, D, n, far = 1, 2, 4, 1, 64, 300, 1 << 23
+    g = torch.Generator().manual_seed(4)
+    k = torch.randn((1, n, 1, D), generator=g).to(torch.bfloat16)
+    v = torch.randn((1, n, 1, D), generator=g).to(torch.bfloat16)
+    q = torch.randn((N, G, Hq, D), generator=g).to(torch.bfloat16)
+    room = torch.empty(n * far, dtype=torch.bfloat16, device="cuda")  # 5 GB
+    kd = room.as_strided((1, n, 1, D), (0, far, 0, 1))
+    vd = room[far // 2:].as_strided((1, n, 1, D), (0, far, 0, 1))
+    kd.copy_(k)
+    vd.copy_(v)
+    for prefix in (True, False):
+        if prefix:
+            got = rl.rlcs_shared_prefix_attn(q.cuda(), kd, vd)
+            check(q, k, v, None, None, torch.tensor([n]), None, 1 / math.sqrt(D), got)
+        else:
+            none = torch.empty((1, 0, 1, D), dtype=torch.bfloat16, device="cuda")
+            got = rl.rlcs_shared_prefix_attn(q.cuda(), none, none, kd[:, None].expand(1, G, n, 1, D), vd[:, None].expand(1, G, n, 1, D))
+            check(q, k, v, None, None, torch.tensor([n]), None, 1 / math.sqrt(D), got)
+    with pytest.raises(rl.RlcsError, match="INVALID_ARG"):
+        rl.rlcs_shared_prefix_attn(q.cuda(), room.as_strided((1, 2, 1, D), (0, 1 << 24, 0, 1)), kd[:, :2])
 
 
 def test_other_stream():
