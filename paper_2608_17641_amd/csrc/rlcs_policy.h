@@ -291,7 +291,8 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
     if (tid == 0) policy_outputs<LOSS>(p, row, r);
     if (!g) return;
     const float l2z = log2_fast(z1);
-    for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
+    // backwards: what the first pass read last is nearest in the caches
+    for (int64_t i0 = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid; i0 >= 0; i0 -= U * kLanes) {
         RowVec<DT> v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, p.V);

@@ -22,11 +22,12 @@ void launch_vec(const PolicyArgs& p, hipStream_t s) {
 }
 
 // Rows that do not fit the registers of eight waves (with sixteen, one workgroup would have the CU to
-// itself and nothing to do while it waits: 4096 x 40000 bfloat16 196 us against 148) take sixteen waves where few rows leave CUs to them (64 x 128000
-// bfloat16 27 -> 23 us), and from this length on, where eight waves have twice as many rows in the
-// caches between their two readings (2048 x 128000 float32 594 -> 460 us, x 40000 280 either way);
-// otherwise eight (8192 x 20000 float32 272 us against 330).
-constexpr int64_t kFewRows = 256, kLongRow = 320 << 10;
+// itself and nothing to do while it waits: 4096 x 40000 bfloat16 196 us against 148) take sixteen
+// waves where few rows leave CUs to them (64 x 128000 bfloat16 27 -> 24 us), and from this length
+// on, where eight waves have twice as many rows in the caches between their two readings (2048 rows of
+// 208 KB 195 -> 185 us, 256 KB 237 -> 215 float32 and 254 -> 230 bfloat16, 512 KB 594 -> 460); otherwise eight
+// (8192 x 20000 float32 272 us against 330).
+constexpr int64_t kFewRows = 256, kLongRow = 200 << 10;
 
 template <typename DT, bool LOSS, int W>
 void launch_rows(const PolicyArgs& p, hipStream_t s) {
