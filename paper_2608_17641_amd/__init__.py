@@ -11,6 +11,9 @@ Tensors: data inputs are ``[N, T]`` contiguous float32 or bfloat16 (all of one c
 dtype), flags are ``[N, T]`` uint8 or bool, ``boot`` / ``carry`` are ``[N]`` of the data dtype,
 outputs are float32 ``[N, T]`` (allocated when not given). All tensors must live on the same
 GPU. ``ws`` is an optional zero-initialised uint8 workspace (see ``make_workspace``).
+
+The operators around a group rollout (``rlcs_shared_prefix_attn``, ``rlcs_sample``,
+``rlcs_token_logp``, ``rlcs_policy_loss``) document their own shapes.
 """
 from __future__ import annotations
 
