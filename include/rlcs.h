@@ -346,7 +346,7 @@ size_t rlcs_workspace_size_columns(int64_t columns, int64_t T);
 /* Log-probability of the taken token and entropy of the policy, for M rows of V logits:
  *   y = x / temperature,  logp = y_a - log sum_j e^{y_j},  ent = -sum_j p_j log p_j.
  *   logits   [M, V] dtype, row m at m * ld (ld >= V); -inf masks an entry (p = 0). A row whose
- *            logits are all -inf has logp = -inf and ent = 0
+ *            logits are all -inf has logp = -inf and ent = 0, one with a NaN or +inf has NaN
  *   tokens   [M] int32. A token outside [0, V) leaves its row out: logp = ent = 0, no logit read
  *   logp     [M] float32 out;  ent  [M] float32 out, optional
  * temperature > 0, finite. Sums are float32, over at most 2^30 logits a row.               */
@@ -381,11 +381,13 @@ rlcs_status rlcs_policy_loss(const void* logits, const int32_t* tokens, const fl
  * equal logits in the order of their index. The draw is a race: the kept token of the largest
  * y_j - log(noise_j), the lowest index among equal ones, which has the distribution above if the
  * noise is exponential (rate 1) and independent.
- *   logits   [M, V] dtype, row m at m * ld; -inf masks an entry; NaN counts as -inf
+ *   logits   [M, V] dtype, row m at m * ld; -inf masks an entry; NaN counts as -inf, +inf as the
+ *            largest float
  *   noise    [M, V] float32, row m at m * ld_noise, positive and finite, used at kept tokens only;
  *            NULL = the largest logit
  *   temperature, top_k, top_p, min_p  [M] of each row's own, or NULL: `all_...` for every row.
- *            Temperature 0 (or less) takes the largest logit, with logp = 0.
+ *            Temperature 0 (or less) takes the largest logit, with logp = 0; +inf weighs
+ *            all alike.
  *   tokens   [M] int32 out;  logp  [M] float32 out, optional: log-probability of the token under
  *            the distribution it was drawn from. A row of masked logits only: token -1, logp -inf
  *   ws       optional: rlcs_workspace_size_sample(M, V) bytes, 16-byte aligned, need not be cleared.

@@ -21,6 +21,9 @@ struct PolicyArgs {
     float ent_coef, inv_temp;
 };
 
+// At least kLog2Zero, or NaN: a NaN or +inf among the logits makes all of the row's outputs NaN.
+__device__ __forceinline__ float clamp_log2(float x) { return __builtin_elementwise_maximum(x, kLog2Zero); }
+
 // What the gradient of a row needs, from its statistics.
 struct PolicyRow {
     float logp, ent, loss;
@@ -32,7 +35,7 @@ template <bool LOSS>
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, float z, float s, float u_taken,
                                                 float logp_old, float adv, float w) {
     PolicyRow r{};
-    const bool some = z > 0.f;
+    const bool some = !(z == 0.f);  // (NaN is some)
     r.some = some;
     const float l2z = some ? log2_fast(z) : 0.f;
     r.logp = some ? kLn2 * (u_taken - l2z) : kNegInf;
@@ -72,8 +75,8 @@ __device__ __forceinline__ void policy_outputs(const PolicyArgs& p, int64_t row,
 }
 
 // The gradient by a logit that is not the taken one.
-__device__ __forceinline__ float policy_gradient(const PolicyRow& r, const Scale& sc, float l2z, float x) {
-    const float l = fmaxf(sc.log2_weight(x) - l2z, kLog2Zero);
+__device__ __forceinline__ float policy_gradient(const PolicyRow& r, const Above& sc, float l2z, float x) {
+    const float l = clamp_log2(fmaf(x - sc.top, sc.c, -l2z));
     return exp2_fast(l) * fmaf(r.a, l, r.b);
 }
 
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     float w, old, adv, v[E];
     const bool part = policy_inputs<LOSS>(p, row, a, w, old, adv);
     PolicyRow r{};
-    Scale sc{};
+    Above sc{};
     float l2z = 0.f;
     if (part) {
         float top = kNegInf;
@@ -99,11 +102,11 @@ __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
         }
         const float taken = widen(x[a]);
         top = max_lanes<L>(top);
-        sc = scale_of(top, kLog2e * p.inv_temp);
+        sc = above(top, kLog2e * p.inv_temp);
         float z = 0.f, s = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float u = fmaxf(sc.log2_weight(v[e]), kLog2Zero), q = exp2_fast(u);  // (NaN of an empty row: -150)
+            const float u = clamp_log2(sc.log2_weight(v[e])), q = exp2_fast(u);
             z += q;
             s = fmaf(q, u, s);
         }
@@ -164,13 +167,13 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void policy_vec_kernel(Po
 #pragma unroll
         for (int i = 0; i < W; ++i) top = fmaxf(top, s_m[i]);
     }
-    const Scale sc = scale_of(top, kLog2e * p.inv_temp);
+    const Above sc = above(top, kLog2e * p.inv_temp);
     float z = 0.f, s = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const float l = fmaxf(sc.log2_weight(v[u].at(k)), kLog2Zero), e = exp2_fast(l);
+            const float l = clamp_log2(sc.log2_weight(v[u].at(k))), e = exp2_fast(l);
             z += e;
             s = fmaf(e, l, s);
         }
@@ -232,6 +235,12 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
     const float c = kLog2e * p.inv_temp;
     const float taken = widen(x[a]);
     float top = kNegInf, z = 0.f, s = 0.f;
+    auto rebase = [&](float t) {  // the sums so far, relative to a new maximum
+        const float d = top == t ? 0.f : fmaxf((top - t) * c, kLog2Zero), f = exp2_fast(d);
+        s = f * fmaf(d, z, s);
+        z *= f;
+        top = t;
+    };
     for (int64_t i0 = tid; i0 < vecs; i0 += U * kLanes) {
         RowVec<DT> v[U];
 #pragma unroll
@@ -241,29 +250,18 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
-        if (t > top) {  // what there is so far, relative to the new maximum
-            const float d = fmaxf((top - t) * c, kLog2Zero), f = exp2_fast(d);
-            s = f * fmaf(d, z, s);
-            z *= f;
-            top = t;
-        }
-        const Scale sc = scale_of(top, c);
+        if (t > top) rebase(t);
+        const Above sc = above(top, c);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const float l = fmaxf(sc.log2_weight(v[u].at(k)), kLog2Zero), e = exp2_fast(l);
+                const float l = clamp_log2(sc.log2_weight(v[u].at(k))), e = exp2_fast(l);
                 z += e;
                 s = fmaf(e, l, s);
             }
     }
     // over the wave, then the workgroup: every lane's sums relative to one maximum
-    auto rebase = [&](float m) {
-        const float d = top == m ? 0.f : fmaxf((top - m) * c, kLog2Zero), f = exp2_fast(d);
-        s = f * fmaf(d, z, s);
-        z *= f;
-        top = m;
-    };
     rebase(max_wave(top));
     z = sum_wave(z);
     s = sum_wave(s);
@@ -286,7 +284,7 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
         z1 += z;
         s1 += s;
     }
-    const Scale sc = scale_of(m, c);
+    const Above sc = above(m, c);
     const PolicyRow r = policy_row<LOSS>(p, z1, s1, sc.log2_weight(taken), old, adv, w);
     if (tid == 0) policy_outputs<LOSS>(p, row, r);
     if (!g) return;

@@ -46,9 +46,10 @@ struct SampleRow {
     int64_t top_k;  // >= V: all
 };
 
-// log2(e) / temperature, or infinity for a temperature of 0 (or none, or too small to divide by).
+// log2(e) / temperature, or infinity for a temperature of 0 (or none, or too small to divide by). Not 0 for
+// one of infinity: -inf times that has to stay -inf.
 __device__ __forceinline__ float sample_scale(const SampleRow& s) {
-    return s.temperature > 0.f ? kLog2e / s.temperature : __builtin_inff();
+    return s.temperature > 0.f ? fmaxf(kLog2e / s.temperature, 1.1754944e-38f) : kInf;
 }
 
 __device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, int64_t row) {
@@ -152,16 +153,20 @@ struct Threshold {
     bool cut;
 };
 
-// A row in memory, its weights' scale.
-template <typename DT>
+// Scales of up to this much have scores x c - log E that are rounded to 2^-12 at most, and weights at most
+// 2^(2^-13) of the largest; rows beyond it (a temperature small against their logits, or finite masks
+// everywhere) go the general way.
+constexpr float kNear = 4096.f;
+__device__ __forceinline__ bool near_scale(float top, float c) { return fabsf(top * c) < kNear; }
+
+// A row in memory, its weights' scale (Scale or Above). NaN counts as -inf and +inf as the largest
+// float, so that all weights are numbers of at most a little over 1.
+template <typename DT, class S>
 struct RowView {
     const DT* x;
     int64_t V;
-    Scale scale;
-    __device__ __forceinline__ float logit(int64_t j) const {
-        const float v = widen(x[j]);
-        return v == v ? v : kNegInf;
-    }
+    S scale;
+    __device__ __forceinline__ float logit(int64_t j) const { return fminf(fmaxf(widen(x[j]), kNegInf), kLargest); }
     __device__ __forceinline__ float log2_weight(float v) const { return scale.log2_weight(v); }
     // A weight (at most a little over 1) as an integer: its 2^-6 and 2^-38 parts, exact in float32.
     static __device__ __forceinline__ uint64_t mass_of(float w) {
@@ -172,14 +177,14 @@ struct RowView {
 };
 
 // The weight that min-p asks for (the largest logit always has it).
-template <typename DT>
-__device__ __forceinline__ float least_weight(const SampleRow& s, const RowView<DT>& r, float top) {
+template <class R>
+__device__ __forceinline__ float least_weight(const SampleRow& s, const R& r, float top) {
     return s.min_p > 0.f ? fminf(s.min_p, 1.f) * exp2_fast(r.log2_weight(top)) : 0.f;
 }
 
 // The k-th largest logit (k < V).
-template <typename DT, int W>
-__device__ Threshold descend_count(const RowView<DT>& r, uint64_t k, uint64_t* bins) {
+template <class R, int W>
+__device__ Threshold descend_count(const R& r, uint64_t k, uint64_t* bins) {
     const int tid = threadIdx.x;
     uint32_t prefix = 0;
     uint64_t want = k, equal = 0;
@@ -204,8 +209,8 @@ __device__ Threshold descend_count(const RowView<DT>& r, uint64_t k, uint64_t* b
 }
 
 // The element of what `t` keeps before which the mass first is p of the whole.
-template <typename DT, int W>
-__device__ Threshold descend_mass(const RowView<DT>& r, Threshold t, float p, uint64_t* bins) {
+template <class R, int W>
+__device__ Threshold descend_mass(const R& r, Threshold t, float p, uint64_t* bins) {
     const int tid = threadIdx.x;
     uint32_t prefix = 0;
     uint64_t target = 0, equal = 0;
@@ -244,15 +249,19 @@ __device__ Threshold descend_mass(const RowView<DT>& r, Threshold t, float p, ui
     return Threshold{prefix, quota, quota < count || (prefix == t.key && t.cut)};
 }
 
-// The general way: one row, any settings, by a workgroup of W waves.
+// The general way: one row, any settings but a temperature of 0, by a workgroup of W waves. `top`: its largest
+// logit, not -inf.
 template <typename DT, int W>
-__device__ __forceinline__ void sample_general(const SampleArgs& a, const SampleRow& s, RowView<DT> r, const float* noise, float top, int64_t row,
-                               uint64_t* bins, uint64_t* slots) {
+__device__ __forceinline__ void sample_general(const SampleArgs& a, const SampleRow& s, const DT* x, const float* noise, float top, int64_t row,
+                                               uint64_t* bins, uint64_t* slots) {
+    typedef RowView<DT, Above> Row;
+    top = fminf(top, kLargest);
+    const Row r{x, a.V, above(top, sample_scale(s))};
     constexpr int kLanes = W * kWave;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     Threshold t{0u, ~0ull, false};
-    if (s.top_k < a.V) t = descend_count<DT, W>(r, uint64_t(s.top_k), bins);
-    if (s.top_p < 1.f) t = descend_mass<DT, W>(r, t, s.top_p, bins);
+    if (s.top_k < a.V) t = descend_count<Row, W>(r, uint64_t(s.top_k), bins);
+    if (s.top_p < 1.f) t = descend_mass<Row, W>(r, t, s.top_p, bins);
     const float least = least_weight(s, r, top);
     float z = 0.f;
     uint64_t winner = 0, ties = 0;
@@ -335,10 +344,11 @@ struct RowWalk {
                 for (int k = 0; k < K; ++k) f(fmaxf(v[u].at(k), kNegInf), uint32_t((i0 + u * kLanes) * K + k));
         });
     }
-    // The lane's largest element, and the sum of its weights relative to that. NaN as -inf.
-    __device__ __forceinline__ void statistics(float c, float& top, float& z) const {
+    // The lane's largest element, its scale, and the sum of its weights by that. NaN as -inf.
+    __device__ __forceinline__ void statistics(float c, float& top, Scale& sc, float& z) const {
         top = kNegInf;
         z = 0.f;
+        sc = scale_of(top, c);
         chunks([&](const RowVec<DT>(&v)[U], int64_t) {
             float t = top;
 #pragma unroll
@@ -346,10 +356,11 @@ struct RowWalk {
 #pragma unroll
                 for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
             if (t > top) {
-                z *= exp2_fast((top - t) * c);
+                const Scale to = scale_of(t, c);
+                z *= exp2_fast(scale_step(sc, to));
+                sc = to;
                 top = t;
             }
-            const Scale sc = scale_of(top, c);
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -408,8 +419,8 @@ struct Drawn {
     uint64_t winner;
     float z;
 };
-template <typename DT>
-__device__ __forceinline__ Drawn draw_sorted(const uint64_t* sorted, int most, const RowView<DT>& r, const float* noise, float above,
+template <class R>
+__device__ __forceinline__ Drawn draw_sorted(const uint64_t* sorted, int most, const R& r, const float* noise, float above,
                                              float target, float least, bool first_kept) {
     const int lane = threadIdx.x & 63;
     Drawn d{0, 0.f};
@@ -455,9 +466,10 @@ template <typename DT, int W, int U, bool ONE>
 __device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk, const float* noise, float c, uint32_t first,
                                               uint64_t* slots, float* slots_f) {
     constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
-    const bool greedy = !(c < __builtin_inff());  // (temperature 0)
+    const bool greedy = !(c < kInf);  // (temperature 0)
     const bool race = noise && !greedy;
     float top = kNegInf, z = 0.f, best = kNegInf;
+    Scale sc = scale_of(top, c);
     uint32_t at = 0;
     walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
         RowVec<float> e[U][K / 4];
@@ -473,10 +485,11 @@ __device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk
 #pragma unroll
             for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
         if (t > top) {
-            z *= exp2_fast((top - t) * c);
+            const Scale to = scale_of(t, c);
+            z *= exp2_fast(scale_step(sc, to));
+            sc = to;
             top = t;
         }
-        const Scale sc = scale_of(top, c);
         int where = -1;  // in this chunk
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -495,24 +508,23 @@ __device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk
     OpenPart p;
     p.top = max_group_f<W>(top, slots_f);
     p.winner = max_group<W>(best == kNegInf ? 0 : race_entry(order_key(best), first + at), slots);
-    p.z = sum_group<W>(top == kNegInf || greedy ? 0.f : z * exp2_fast((top - p.top) * c), slots);
+    p.z = sum_group<W>(top == kNegInf || greedy ? 0.f : z * exp2_fast(scale_step(sc, scale_of(p.top, c))), slots);
     return p;
 }
 
-// The row's outputs from its whole part. False: the scores overflow (logits beyond 10^38 / c), or none is
-// above -inf (noise out of its range), and the general way has to take the row.
+// The row's outputs from its whole part. False: the general way has to take it, as its logits are not near
+// (infinity among them), or none is above -inf (noise out of its range).
 template <typename DT>
-__device__ __forceinline__ bool open_finish(const SampleArgs& a, const OpenPart& p, RowView<DT>& r, float c, int64_t row) {
+__device__ __forceinline__ bool open_finish(const SampleArgs& a, const OpenPart& p, const DT* x, float c, int64_t row) {
     if (p.top == kNegInf) {
         if (threadIdx.x == 0) sample_none(a, row);
         return true;
     }
-    const bool greedy = !(c < __builtin_inff());
-    r.scale = scale_of(p.top, c);
-    if (!greedy && (r.scale.c != c || p.winner == 0)) return false;
+    const bool greedy = !(c < kInf);
+    if (!greedy && (!near_scale(p.top, c) || p.winner == 0)) return false;
     if (threadIdx.x == 0) {
         const uint32_t j = race_index(p.winner);
-        sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(p.z));
+        sample_outputs(a, row, j, greedy ? 0.f : scale_of(p.top, c).log2_weight(widen(x[j])) - log2_fast(p.z));
     }
     return true;
 }
@@ -522,12 +534,12 @@ __global__ __launch_bounds__(W * kWave) void sample_open_kernel(SampleArgs a) {
     __shared__ uint64_t s_bins[kDigits], s_slots[W];
     __shared__ float s_slots_f[W];
     const int64_t row = blockIdx.x;
-    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
     const float c = sample_scale(s);
-    const OpenPart p = open_part<DT, W, U, ONE>(RowWalk<DT, W, U, ONE>(r.x, a.V), noise, c, 0u, s_slots, s_slots_f);
-    if (!open_finish<DT>(a, p, r, c, row)) sample_general<DT, W>(a, s, r, noise, p.top, row, s_bins, s_slots);
+    const OpenPart p = open_part<DT, W, U, ONE>(RowWalk<DT, W, U, ONE>(x, a.V), noise, c, 0u, s_slots, s_slots_f);
+    if (!open_finish<DT>(a, p, x, c, row)) sample_general<DT, W>(a, s, x, noise, p.top, row, s_bins, s_slots);
 }
 
 // Few long rows: parts of `length` elements (a multiple of a vector) on workgroups of their own,
@@ -549,16 +561,16 @@ __global__ __launch_bounds__(4 * kWave) void sample_join_kernel(SampleArgs a, co
     __shared__ uint64_t s_bins[kDigits], s_slots[4];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63;
-    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     const SampleRow s = sample_row(a, row);
     const float c = sample_scale(s);
     const OpenPart mine = lane < count ? parts[row * count + lane] : OpenPart{0, kNegInf, 0.f};
     OpenPart p;
     p.top = max_wave(mine.top);
     p.winner = max_wave(mine.winner);
-    p.z = sum_wave(mine.top == kNegInf ? 0.f : mine.z * exp2_fast(mine.top == p.top ? 0.f : (mine.top - p.top) * c));
-    if (!open_finish<DT>(a, p, r, c, row))
-        sample_general<DT, 4>(a, s, r, a.noise ? a.noise + row * a.ld_noise : nullptr, p.top, row, s_bins, s_slots);
+    p.z = sum_wave(mine.top == kNegInf ? 0.f : mine.z * exp2_fast(scale_step(scale_of(mine.top, c), scale_of(p.top, c))));
+    if (!open_finish<DT>(a, p, x, c, row))
+        sample_general<DT, 4>(a, s, x, a.noise ? a.noise + row * a.ld_noise : nullptr, p.top, row, s_bins, s_slots);
 }
 
 // One row per workgroup of W waves, with its filters. The cases that the quicker ways leave end in
@@ -569,20 +581,20 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
     constexpr int kLanes = W * kWave, K = RowVec<DT>::K;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63;
-    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
-    const RowWalk<DT, W, U, ONE> walk(r.x, a.V);
+    const RowWalk<DT, W, U, ONE> walk(x, a.V);
     const float c = sample_scale(s);
     const bool by_k = s.top_k < a.V, by_p = s.top_p < 1.f, by_min = s.min_p > 0.f;
     float top = kNegInf;
 
     auto quick = [&]() -> bool {
-        if (!(c < __builtin_inff()) || (!by_k && !by_p && !by_min))
+        if (!(c < kInf) || (!by_k && !by_p && !by_min))
         {
             const OpenPart p = open_part<DT, W, U, ONE>(walk, noise, c, 0u, sh.slots, sh.slots_f);
             top = p.top;
-            return open_finish<DT>(a, p, r, c, row);
+            return open_finish<DT>(a, p, x, c, row);
         }
 
         if (by_k && s.top_k <= kFewest) {
@@ -640,7 +652,8 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
                 if (tid == 0) sample_none(a, row);
                 return true;
             }
-            r.scale = scale_of(top, c);
+            const RowView<DT, Above> r{x, a.V, above(top, c)};
+            if (top == kInf) return false;
             const float from = sh.pivot > order_key(kNegInf) ? key_value(sh.pivot) : kNegInf;
             walk.each([&](float v, uint32_t j) {
                 if (v >= from && v > kNegInf) {
@@ -654,7 +667,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
             rank_list<W>(sh.list, sh.sorted, n);
             if (tid >= kWave) return true;
             const int most = n < s.top_k ? n : int(s.top_k);
-            float target = __builtin_inff();
+            float target = kInf;
             if (by_p) {
                 float sum = 0.f;
                 for (int i = lane; i < most; i += kWave) sum += exp2_fast(r.log2_weight(key_value(uint32_t(sh.sorted[i] >> 32))));
@@ -667,22 +680,23 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
 
         // the largest logit and the sum of weights
         float own_top, z;
-        walk.statistics(c, own_top, z);
+        Scale own;
+        walk.statistics(c, own_top, own, z);
         top = max_group_f<W>(own_top, sh.slots_f);
         if (top == kNegInf) {
             if (tid == 0) sample_none(a, row);
             return true;
         }
-        r.scale = scale_of(top, c);
-        if (by_k || r.scale.c != c) return false;
+        if (by_k || !near_scale(top, c)) return false;
+        const RowView<DT, Scale> r{x, a.V, scale_of(top, c)};
         const float least = least_weight(s, r, top);
-        z = own_top == kNegInf ? 0.f : z * exp2_fast((own_top - top) * c);
+        z = own_top == kNegInf ? 0.f : z * exp2_fast(scale_step(own, r.scale));
         z = sum_group<W>(z, sh.slots);
 
         // without top-p everything is above the crossing bin
         int cross = kMassBins;
         float above = 0.f;
-        const float target = by_p ? s.top_p * z : __builtin_inff();
+        const float target = by_p ? s.top_p * z : kInf;
         if (by_p) {
             // the smallest elements, of less than 1 - p in all, cannot be in: at most V of them below this
             const float low = log2_fast(0.99f * (1.f - s.top_p) * z / float(a.V));
@@ -745,7 +759,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
         // through a buffer of the wave's own, so that the few kept ones of many are weighed, and their
         // noise fetched, by full waves.
         // (the first bin takes logarithms that rounding leaves above 0, too)
-        const float sure = !by_p ? kNegInf : cross > 0 ? -float(cross) / kBinsPerOctave : __builtin_inff();
+        const float sure = !by_p ? kNegInf : cross > 0 ? -float(cross) / kBinsPerOctave : kInf;
         const float edge = by_p ? -float(cross + 1) / kBinsPerOctave : kNegInf;
         __syncthreads();  // (the bins' memory)
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -830,7 +844,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
         if (tid == 0) sample_outputs(a, row, race_index(winner), r.log2_weight(r.logit(race_index(winner))) - log2_fast(zk));
         return true;
     };
-    if (!quick()) sample_general<DT, W>(a, s, r, noise, top, row, sh.bins, sh.slots);
+    if (!quick()) sample_general<DT, W>(a, s, x, noise, top, row, sh.bins, sh.slots);
 }
 
 // Rows of up to 64 * E logits with filters, one per wave, logits and keys in registers (lane i has
@@ -842,11 +856,11 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t row = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= a.M) return;
-    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    RowView<DT, Above> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
     const float c = sample_scale(s);
-    const bool greedy = !(c < __builtin_inff());
+    const bool greedy = !(c < kInf);
     constexpr uint32_t kOut = 0u, kLowest = 0x00800000u;  // keys: of a dropped element; of the lowest finite number
     float v[E], n[E], top = kNegInf;
     uint32_t key[E];
@@ -863,7 +877,7 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
         if (lane == 0) sample_none(a, row);
         return;
     }
-    r.scale = scale_of(top, c);
+    r.scale = above(top, c);
     auto count = [&](uint32_t from) {
         int x = 0;
 #pragma unroll
@@ -963,11 +977,11 @@ __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63, i = lane % L;
     const int64_t row = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
     if (row >= a.M) return;  // (a whole group of L lanes leaves together)
-    RowView<DT> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
+    RowView<DT, Above> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
-    const float c = kLog2e / s.temperature;
-    const bool greedy = !(s.temperature > 0.f) || !(c < __builtin_inff());
+    const float c = sample_scale(s);
+    const bool greedy = !(c < kInf);
     float v[E], n[E], top = kNegInf;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -981,7 +995,7 @@ __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
         if (i == 0) sample_none(a, row);
         return;
     }
-    r.scale = scale_of(top, c);
+    r.scale = above(top, c);
     float z = 0.f;
     uint64_t winner = 0;
 #pragma unroll

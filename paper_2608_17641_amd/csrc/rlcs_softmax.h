@@ -8,7 +8,8 @@ namespace rlcs {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kNegInf = -__builtin_inff();
+constexpr float kInf = __builtin_inff(), kNegInf = -kInf;
+constexpr float kLargest = 3.4028234663852886e38f;  // the largest float
 
 // v_exp_f32 and v_log_f32: base 2, 1 ulp.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -22,20 +23,39 @@ __device__ __forceinline__ bf16_t narrow(float x, bf16_t) {  // to nearest, ties
 }
 __device__ __forceinline__ float narrow(float x, float) { return x; }
 
-// Weights of a row whose largest element is `top`: 2^(x c - m), with c = log2(e) / temperature and
-// m = top c. The fused multiply-add of x c - m rounds once, and the rounding of m is common to
-// every element, so it cancels in a softmax. Where top c overflows, whatever differs from top at all
-// is at least 2^100 below it in base 2: a power of two in c's place, with which top c is
-// exact, tells the elements equal to top (2^0) from the others (0).
+// Logarithms of weights are kept from -inf, whose product with a weight of 0 is NaN: 2^-150 is 0.
+constexpr float kLog2Zero = -150.f;
+
+// Weights of a row whose largest element is `top`: 2^((x - top) c), with c = log2(e) / temperature. The
+// difference is exact where it counts. Of -inf alone (above() gives them a top of 0) all weights are 0;
+// next to +inf or NaN they are NaN.
+struct Above {
+    float top, c;
+    __device__ __forceinline__ float log2_weight(float x) const { return (x - top) * c; }
+};
+__device__ __forceinline__ Above above(float top, float c) { return Above{top == kNegInf ? 0.f : top, c}; }
+
+// The same with one operation: 2^(x c - m), m = top c. The fused multiply-add rounds once, and the
+// rounding of m, up to 64 below 2^31, is a factor common to every element, which cancels in a softmax.
+// From 2^31 on whatever differs from top at all is at least 128 below it in base 2: a power of two
+// in c's place, with which m is exact, tells the elements equal to top (2^0) from the others (less
+// than 2^-64).
 struct Scale {
     float c, m;
     __device__ __forceinline__ float log2_weight(float x) const { return fmaf(x, c, -m); }
 };
 __device__ __forceinline__ Scale scale_of(float top, float c) {
     const float m = top * c;
-    if (fabsf(m) < __builtin_inff() || top == kNegInf) return Scale{c, m};
-    const float p = ldexpf(1.f, 126 - ilogbf(top));
+    if (fabsf(m) < 2147483648.f) return Scale{c, m};
+    if (top == kNegInf) return Scale{kInf, 0.f};
+    const int e = 126 - ilogbf(top), of_c = ilogbf(c);
+    const float p = ldexpf(1.f, of_c < e ? of_c : e);
     return Scale{p, top * p};
+}
+// Logarithm of the factor from weights of one top to those of a larger one: by the rounded m, as those
+// are what the weights are relative to. Tops of different c are far apart.
+__device__ __forceinline__ float scale_step(const Scale& from, const Scale& to) {
+    return from.c == to.c ? fmaxf(from.m - to.m, kLog2Zero) : kLog2Zero;
 }
 
 // Over each group of L lanes, every lane with the result; the tree is fixed, so the sums are too.
@@ -89,9 +109,6 @@ __device__ __forceinline__ float max_wave(float v) {
 __device__ __forceinline__ uint64_t max_wave(uint64_t v) {
     return fold_wave(v, uint64_t(0), [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
-
-// Logarithms of weights are kept from -inf, whose product with a weight of 0 is NaN: 2^-150 is 0.
-constexpr float kLog2Zero = -150.f;
 
 // 16 bytes of a row at any element address (elements before `from` read nothing: `fill`).
 template <typename DT>

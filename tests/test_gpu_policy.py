@@ -176,3 +176,55 @@ def test_other_stream():
         got = rl.rlcs_policy_loss(x, tokens, old, adv, weight, **CLIP)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [18, 100, 700, 3001, 20001, 70000])
+def test_finite_masks(V, dtype):
+    """Large negative numbers as masks: next to other logits they count as -inf, alone they weigh alike."""
+    x, tokens, old, adv, weight = (t.cuda() for t in inputs(4, V, dtype, V))
+    weight = weight + 0.5
+    tokens = (V - 1 - tokens % (V // 3)).to(torch.int32)
+    old = old * 0 - 3.0
+    hidden = x.clone()
+    hidden[:, :V - V // 3] = -math.inf
+    for low in (-1e4, -1e6, -1e9, -1e10, -1e30, torch.finfo(dtype).min):
+        masked = torch.where(torch.isinf(hidden), torch.full_like(x, low), hidden)
+        for T in (0.7, 1.0, 2.0):
+            got = rl.rlcs_policy_loss(masked, tokens, old, adv, weight, ent_coef=0.02, temperature=T, **CLIP)
+            check(hidden, tokens, old, adv, weight, got, 0.02, T)
+            got = rl.rlcs_policy_loss(torch.full_like(x, low), tokens, old, adv, weight, ent_coef=0.02, temperature=T, **CLIP)
+            check(torch.zeros_like(x), tokens, old, adv, weight, got, 0.02, T)
+
+
+@pytest.mark.parametrize("V", [18, 100, 700, 3001, 20001, 70000])
+def test_far_tokens(V):
+    """The log-probability of a token far below the largest: its distance, to a few roundings."""
+    x = torch.zeros(4, V, device="cuda")
+    x[:, V // 2] = torch.tensor([1e3, 1e7, 1e10, 1e30], device="cuda")
+    tokens = torch.full((4,), V - 1, dtype=torch.int32, device="cuda")
+    for T in (0.7, 1.0, 3.0):
+        logp, ent = rl.rlcs_token_logp(x, tokens, temperature=T)
+        want = -x[:, V // 2].double() / T
+        assert float((logp.double() / want - 1).abs().max()) <= 8 * EPS
+        assert float(ent.abs().max()) <= 1e-12
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [18, 100, 700, 3001, 20001, 70000])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_bad_logits_show(V, dtype, bad):
+    """A NaN or +inf logit makes its row's outputs NaN, as the formulas do, and no other row's."""
+    x, tokens, old, adv, weight = (t.cuda() for t in inputs(5, V, dtype, V, masked=0.2))
+    weight = weight + 0.5
+    p = dict(ent_coef=0.02, **CLIP)
+    want = rl.rlcs_policy_loss(x, tokens, old, adv, weight, **p)
+    y = x.clone()
+    y[1, V // 2] = bad
+    y[3] = -math.inf
+    y[3, V - 1] = bad
+    got = rl.rlcs_policy_loss(y, tokens, old, adv, weight, **p)
+    lp = rl.rlcs_token_logp(y, tokens)
+    for a, b in list(zip(got, want)) + list(zip(lp, rl.rlcs_token_logp(x, tokens))):
+        assert bool(torch.isnan(a[[1, 3]]).all())
+        assert torch.equal(a[[0, 2, 4]], b[[0, 2, 4]])

@@ -173,3 +173,48 @@ def test_distribution():
     got = torch.bincount(tokens.long(), minlength=V)[kept].double() / M
     assert bool(((got - p).abs() <= 6 * torch.sqrt(p * (1 - p) / M)).all())
     assert torch.allclose(torch.exp(logp.double()), p[torch.searchsorted(kept, tokens.long())], rtol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [18, 700, 3001, 20001, 70000])
+def test_finite_masks(V, dtype):
+    """Large negative numbers as masks: next to other logits they weigh nothing, alone they weigh alike,
+    however large, where their products with log2(e) / T round by more than all the weights differ."""
+    x, noise = (t.cuda() for t in inputs(5, V, dtype, V))
+    hidden = x.clone()
+    hidden[:, :V - V // 3] = -math.inf
+    flat = torch.zeros_like(x)
+    for low in (-1e4, -1e6, -1e9, -1e10, -1e30, torch.finfo(dtype).min):
+        masked = torch.where(torch.isinf(hidden), torch.full_like(x, low), hidden)
+        for T in (0.7, 1.0, 2.0):
+            for kw in (dict(), dict(top_k=V // 5 + 1), dict(top_p=0.6 + 0.3 / V), dict(min_p=0.1)):
+                got, want = (rl.rlcs_sample(t, noise, temperature=T, **kw) for t in (masked, hidden))
+                assert torch.equal(got[0], want[0]), (low, T, kw)
+                assert float((got[1] - want[1]).abs().max()) <= EPS * (V / 64 + 400), (low, T, kw)
+                got, want = (rl.rlcs_sample(t, noise, temperature=T, **kw) for t in (flat + low, flat))
+                assert torch.equal(got[0], want[0]), (low, T, kw)
+                assert float((got[1] - want[1]).abs().max()) <= EPS * (V / 64 + 40), (low, T, kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [18, 700, 3001, 20001, 70000])
+def test_infinite_logits(V, dtype):
+    """+inf takes the whole mass, several share it."""
+    x, noise = (t.cuda() for t in inputs(3, V, dtype, V, masked=0.2))
+    x[1, V // 2] = math.inf
+    x[2, V // 3], x[2, V - 1] = math.inf, math.inf
+    faster = V // 3 if float(noise[2, V // 3]) < float(noise[2, V - 1]) else V - 1
+    for kw in (dict(), dict(top_k=5), dict(top_k=V // 2), dict(top_p=0.9), dict(top_k=V // 2, top_p=0.9), dict(min_p=0.3)):
+        tokens, logp = rl.rlcs_sample(x, noise, **kw)
+        assert tokens[1:].tolist() == [V // 2, faster], kw
+        assert float(logp[1]) == 0.0 and abs(float(logp[2]) + math.log(2)) <= 4 * EPS
+        check(x[:1], noise[:1], (tokens[:1], logp[:1]), k=kw.get("top_k", 0), p=kw.get("top_p", 1.0), mp=kw.get("min_p", 0.0))
+    for kw in (dict(top_k=1), dict(temperature=0.0)):
+        assert rl.rlcs_sample(x, noise, **kw)[0][1:].tolist() == [V // 2, V // 3]
+
+
+@pytest.mark.parametrize("V", [18, 700, 3001, 20001, 70000])
+def test_infinite_temperature(V):
+    x, noise = (t.cuda() for t in inputs(5, V, torch.float32, V, masked=0.3))
+    for k, p, mp in ((0, 1.0, 0.0), (9, 1.0, 0.0), (0, 0.55 + 0.3 / V, 0.0), (0, 1.0, 0.5)):
+        check(x, noise, rl.rlcs_sample(x, noise, temperature=math.inf, top_k=k, top_p=p, min_p=mp), T=math.inf, k=k, p=p, mp=mp)
