@@ -419,7 +419,8 @@ size_t rlcs_workspace_size_sample(int64_t M, int64_t V);
  *            of 16 bytes, as are q, kp, vp, ks, vs and o; those of tokens are below 2^24
  *   ws       rlcs_workspace_size_attn(...) bytes, 16-byte aligned, need not be cleared
  * D a multiple of 8 up to 256; P and S up to 2^30. Scores, sums and the output's accumulator are
- * float32; bfloat16 weights e^{s - m} are rounded to bfloat16 for the product with V.         */
+ * float32, for |s_j| up to 10^9; bfloat16 weights e^{s - m} are rounded to bfloat16 for the product
+ * with V.                                                                                    */
 typedef struct {
     int64_t q[3];  /* group, sequence, head */
     int64_t kp[3]; /* group, token, head */

@@ -702,7 +702,7 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void attn_kernel(AttnArgs a, At
     __shared__ __attribute__((aligned(16))) char s_mem[attn_mem<DT, ND, PR, EXACT>()];
     const int wave = SOLO ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : -1;
     AttnItem it;
-    if (!it.of(a, plan, int(blockIdx.x), PR == kPrefixOne ? wave : -1, wave)) return;
+    if (!it.of(a, plan, int(grid_row()), PR == kPrefixOne ? wave : -1, wave)) return;
     if constexpr (PR == kPrefixShared64) {
         if (it.prefix) {
             attn_share_keys<DT, ND, 1, kAttnWaves, EXACT>(a, plan, it, s_mem);
@@ -723,7 +723,7 @@ template <typename DT, int ND, int QT, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) void attn_prefix_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ __attribute__((aligned(16))) char s_mem[SharedKeys<DT, ND, QT, W, EXACT>::kLds];
     AttnItem it;
-    if (!it.of(a, plan, int(blockIdx.x), -1, -1)) return;
+    if (!it.of(a, plan, int(grid_row()), -1, -1)) return;
     attn_share_keys<DT, ND, QT, W, EXACT>(a, plan, it, s_mem);
 }
 
@@ -734,7 +734,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
     __shared__ f32x4 s_o[256];
     __shared__ float s_z[256];
     const int lanes = a.D / 4, groups = 256 / lanes;
-    const int64_t rows = a.N * a.G * a.Hq, out = blockIdx.x;
+    const int64_t rows = a.N * a.G * a.Hq, out = grid_row();
+    if (out >= rows) return;
     const int group = int(threadIdx.x) / lanes, d = 4 * (int(threadIdx.x) % lanes);
     const int seq = int(out) / a.Hq;
     const int plen = plan.whole ? 0 : clamp_len(a.prefix_len, seq / a.G, a.P), slen = clamp_len(a.suffix_len, seq, a.S);

@@ -84,7 +84,7 @@ bool make_plan(AttnPlan& p, int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64
     }
     const int64_t prefix_groups = ceil_div(prefix_items, kGroup * (prefix_solo ? kAttnWaves : 1));
     const int64_t groups = prefix_groups + ceil_div(suffix_items, kGroup * (p.solo ? kAttnWaves : 1));
-    if (prefix_items + suffix_items > INT32_MAX - 4 * kGroup * kAttnWaves || groups > INT32_MAX / kGroup) return false;
+    if (prefix_items + suffix_items > INT32_MAX - 4 * kGroup * kAttnWaves || groups > (INT32_MAX >> kGridBits << kGridBits) / kGroup) return false;
     p.prefix_items = int32_t(prefix_items);
     p.suffix_items = int32_t(suffix_items);
     p.prefix_groups = int32_t(prefix_groups);
@@ -110,7 +110,7 @@ AttnPlan only(AttnPlan p, bool prefix) {
 
 template <typename DT, int ND, PrefixRows PR, bool SOLO>
 void launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(kAttnWaves * kWave);
+    const dim3 grid = row_grid(int64_t(p.groups) * kGroup), block(kAttnWaves * kWave);
     if (a.D == 16 * ND) hipLaunchKernelGGL((attn_kernel<DT, ND, PR, SOLO, true>), grid, block, 0, s, a, p);
     else hipLaunchKernelGGL((attn_kernel<DT, ND, PR, SOLO, false>), grid, block, 0, s, a, p);
 }
@@ -123,7 +123,7 @@ void launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
 
 template <typename DT, int ND, int QT, int W>
 void launch_prefix(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(p.groups * kGroup)), block(W * kWave);
+    const dim3 grid = row_grid(int64_t(p.groups) * kGroup), block(W * kWave);
     if (a.D == 16 * ND) hipLaunchKernelGGL((attn_prefix_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a, p);
     else hipLaunchKernelGGL((attn_prefix_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a, p);
 }
@@ -145,7 +145,7 @@ rlcs_status run_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
         }
     }
     if (p.part_acc)
-        hipLaunchKernelGGL((attn_join_kernel<DT>), dim3(unsigned(a.N * a.G * a.Hq)), dim3(256), 0, s, a, p);
+        hipLaunchKernelGGL((attn_join_kernel<DT>), row_grid(int64_t(a.N) * a.G * a.Hq), dim3(256), 0, s, a, p);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
 

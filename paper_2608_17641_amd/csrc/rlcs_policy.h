@@ -84,7 +84,7 @@ __device__ __forceinline__ float policy_gradient(const PolicyRow& r, const Above
 template <typename DT, bool LOSS, int L, int E>
 __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     const int lane = threadIdx.x & 63, i = lane % L;
-    const int64_t row = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
+    const int64_t row = (grid_row() * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
     if (row >= p.M) return;  // (a whole group of L lanes leaves together)
     const DT* x = reinterpret_cast<const DT*>(p.logits) + row * p.ld;
     int64_t a;
@@ -136,7 +136,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void policy_vec_kernel(Po
     __shared__ float s_m[W], s_z[W], s_s[W];
     constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
     const int tid = W == 1 ? int(threadIdx.x) & 63 : int(threadIdx.x), wave = tid >> 6;
-    const int64_t row = W == 1 ? int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : int64_t(blockIdx.x);
+    const int64_t row = W == 1 ? grid_row() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : grid_row();
     if (row >= p.M) return;
     const DT* x = reinterpret_cast<const DT*>(p.logits) + row * p.ld;
     DT* g = LOSS && p.grad ? reinterpret_cast<DT*>(p.grad) + row * p.ld_grad : nullptr;
@@ -217,7 +217,8 @@ template <typename DT, bool LOSS, int W>
 __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
     __shared__ float s_m[W], s_z[W], s_s[W];
     constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
-    const int64_t row = blockIdx.x;
+    const int64_t row = grid_row();
+    if (row >= p.M) return;
     const int tid = threadIdx.x;
     const DT* x = reinterpret_cast<const DT*>(p.logits) + row * p.ld;
     DT* g = LOSS && p.grad ? reinterpret_cast<DT*>(p.grad) + row * p.ld_grad : nullptr;

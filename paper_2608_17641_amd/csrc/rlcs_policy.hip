@@ -12,13 +12,13 @@ namespace {
 template <typename DT, bool LOSS, int L, int E>
 void launch_small(const PolicyArgs& p, hipStream_t s) {
     const int64_t rows = 4 * (kWave / L);
-    hipLaunchKernelGGL((policy_small_kernel<DT, LOSS, L, E>), dim3(unsigned((p.M + rows - 1) / rows)), dim3(4 * kWave), 0, s, p);
+    hipLaunchKernelGGL((policy_small_kernel<DT, LOSS, L, E>), row_grid((p.M + rows - 1) / rows), dim3(4 * kWave), 0, s, p);
 }
 
 template <typename DT, bool LOSS, int W, int U>
 void launch_vec(const PolicyArgs& p, hipStream_t s) {
     const int64_t rows = W == 1 ? 4 : 1;
-    hipLaunchKernelGGL((policy_vec_kernel<DT, LOSS, W, U>), dim3(unsigned((p.M + rows - 1) / rows)), dim3((W == 1 ? 4 : W) * kWave), 0, s, p);
+    hipLaunchKernelGGL((policy_vec_kernel<DT, LOSS, W, U>), row_grid((p.M + rows - 1) / rows), dim3((W == 1 ? 4 : W) * kWave), 0, s, p);
 }
 
 // Rows that do not fit the registers of eight waves (with sixteen, one workgroup would have the CU to
@@ -31,7 +31,7 @@ constexpr int64_t kFewRows = 256, kLongRow = 200 << 10;
 
 template <typename DT, bool LOSS, int W>
 void launch_rows(const PolicyArgs& p, hipStream_t s) {
-    hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, W>), dim3(unsigned(p.M)), dim3(W * kWave), 0, s, p);
+    hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, W>), row_grid(p.M), dim3(W * kWave), 0, s, p);
 }
 
 template <typename DT, bool LOSS>

@@ -533,7 +533,8 @@ template <typename DT, int W, int U, bool ONE>
 __global__ __launch_bounds__(W * kWave) void sample_open_kernel(SampleArgs a) {
     __shared__ uint64_t s_bins[kDigits], s_slots[W];
     __shared__ float s_slots_f[W];
-    const int64_t row = blockIdx.x;
+    const int64_t row = grid_row();
+    if (row >= a.M) return;
     const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
     const SampleRow s = sample_row(a, row);
@@ -579,7 +580,8 @@ template <typename DT, int W, int U, bool ONE>
 __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
     __shared__ SampleShared<W> sh;
     constexpr int kLanes = W * kWave, K = RowVec<DT>::K;
-    const int64_t row = blockIdx.x;
+    const int64_t row = grid_row();
+    if (row >= a.M) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
@@ -854,7 +856,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
 template <typename DT, int E>
 __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63;
-    const int64_t row = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = grid_row() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= a.M) return;
     RowView<DT, Above> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;
@@ -975,7 +977,7 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
 template <typename DT, int L, int E>
 __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63, i = lane % L;
-    const int64_t row = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
+    const int64_t row = (grid_row() * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
     if (row >= a.M) return;  // (a whole group of L lanes leaves together)
     RowView<DT, Above> r{reinterpret_cast<const DT*>(a.logits) + row * a.ld, a.V, {}};
     const float* noise = a.noise ? a.noise + row * a.ld_noise : nullptr;

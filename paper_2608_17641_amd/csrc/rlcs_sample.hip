@@ -10,19 +10,19 @@ namespace {
 template <typename DT, int L, int E>
 void launch_small(const SampleArgs& a, hipStream_t s) {
     const int64_t rows = 4 * (kWave / L);
-    hipLaunchKernelGGL((sample_small_kernel<DT, L, E>), dim3(unsigned((a.M + rows - 1) / rows)), dim3(4 * kWave), 0, s, a);
+    hipLaunchKernelGGL((sample_small_kernel<DT, L, E>), row_grid((a.M + rows - 1) / rows), dim3(4 * kWave), 0, s, a);
 }
 
 template <typename DT, int W, int U, bool ONE>
 void launch_rows(const SampleArgs& a, bool open, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(a.M)), block(W * kWave);
+    const dim3 grid = row_grid(a.M), block(W * kWave);
     if (open) hipLaunchKernelGGL((sample_open_kernel<DT, W, U, ONE>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((sample_rows_kernel<DT, W, U, ONE>), grid, block, 0, s, a);
 }
 
 template <typename DT, int E>
 void launch_wave(const SampleArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((sample_wave_kernel<DT, E>), dim3(unsigned((a.M + 3) / 4)), dim3(4 * kWave), 0, s, a);
+    hipLaunchKernelGGL((sample_wave_kernel<DT, E>), row_grid((a.M + 3) / 4), dim3(4 * kWave), 0, s, a);
 }
 
 // Unfiltered rows of at least kSplitFrom logits are split over workgroups where there are few of them:

@@ -6,6 +6,15 @@
 
 namespace rlcs {
 
+// One workgroup a row, as a grid of two axes: a launch counts the lanes of each in 32 bits, which 2^23 rows
+// of 512 lanes would pass.
+constexpr int kGridBits = 20;
+inline dim3 row_grid(int64_t rows) {
+    const int64_t x = int64_t(1) << kGridBits;
+    return rows <= x ? dim3(unsigned(rows)) : dim3(unsigned(x), unsigned((rows + x - 1) >> kGridBits));
+}
+__device__ __forceinline__ int64_t grid_row() { return (int64_t(blockIdx.y) << kGridBits) + blockIdx.x; }
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff(), kNegInf = -kInf;
