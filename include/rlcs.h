@@ -382,7 +382,7 @@ rlcs_status rlcs_policy_loss(const void* logits, const int32_t* tokens, const fl
  * y_j - log(noise_j), the lowest index among equal ones, which has the distribution above if the
  * noise is exponential (rate 1) and independent.
  *   logits   [M, V] dtype, row m at m * ld; -inf masks an entry; NaN counts as -inf, +inf as the
- *            largest float
+ *            type's largest number
  *   noise    [M, V] float32, row m at m * ld_noise, positive and finite, used at kept tokens only;
  *            NULL = the largest logit
  *   temperature, top_k, top_p, min_p  [M] of each row's own, or NULL: `all_...` for every row.

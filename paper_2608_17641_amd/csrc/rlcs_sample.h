@@ -159,14 +159,19 @@ struct Threshold {
 constexpr float kNear = 4096.f;
 __device__ __forceinline__ bool near_scale(float top, float c) { return fabsf(top * c) < kNear; }
 
-// A row in memory, its weights' scale (Scale or Above). NaN counts as -inf and +inf as the largest
-// float, so that all weights are numbers of at most a little over 1.
+// A row in memory, its weights' scale (Scale or Above). NaN counts as -inf and +inf as the type's largest
+// number, so that all weights are numbers of at most a little over 1.
 template <typename DT, class S>
 struct RowView {
     const DT* x;
     int64_t V;
     S scale;
-    __device__ __forceinline__ float logit(int64_t j) const { return fminf(fmaxf(widen(x[j]), kNegInf), kLargest); }
+    static __device__ __forceinline__ float finite(float v) { return fminf(v, sizeof(DT) == 4 ? 0x1.fffffep127f : 0x1.fep127f); }
+    static __device__ __forceinline__ float number(DT v) { return finite(fmaxf(widen(v), kNegInf)); }
+    __device__ __forceinline__ float logit(int64_t j) const { return number(x[j]); }
+    // Element j of a short row, or what stands for the ones past its end; all of a lane's are asked for
+    // before any is looked at.
+    __device__ __forceinline__ DT ask(int j) const { return x[j < V ? j : int(V) - 1]; }
     __device__ __forceinline__ float log2_weight(float v) const { return scale.log2_weight(v); }
     // A weight (at most a little over 1) as an integer: its 2^-6 and 2^-38 parts, exact in float32.
     static __device__ __forceinline__ uint64_t mass_of(float w) {
@@ -255,7 +260,7 @@ template <typename DT, int W>
 __device__ __forceinline__ void sample_general(const SampleArgs& a, const SampleRow& s, const DT* x, const float* noise, float top, int64_t row,
                                                uint64_t* bins, uint64_t* slots) {
     typedef RowView<DT, Above> Row;
-    top = fminf(top, kLargest);
+    top = Row::finite(top);
     const Row r{x, a.V, above(top, sample_scale(s))};
     constexpr int kLanes = W * kWave;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -850,9 +855,13 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
 }
 
 // Rows of up to 64 * E logits with filters, one per wave, logits and keys in registers (lane i has
-// elements i, 64 + i, ...). A threshold is searched for by halving the range of keys: each step counts,
+// elements i, 64 + i, ...). A threshold is searched for by halving the range of logits: each step counts,
 // or weighs, what lies above the middle, and the search ends when the cut falls between two elements
-// (12 to 14 steps on random logits) or at equal ones, of which the first by index stay.
+// (about ten steps on random logits) or at equal ones, of which the first by index stay. Bound by the
+// latency of these steps, some 50 instructions each for a count of 1000 logits, 100 for a mass: 8 x 1000
+// bfloat16 8 us with top-k, 10 with top-p, 14 with both and min-p; halving the range of keys alone, most of
+// which lie near 0, took twice the steps (31 among equal bfloat16 logits), and loads of a lane one
+// after another 3 us more: 14, 18 and 20.
 template <typename DT, int E>
 __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63;
@@ -863,16 +872,27 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
     const SampleRow s = sample_row(a, row);
     const float c = sample_scale(s);
     const bool greedy = !(c < kInf);
-    constexpr uint32_t kOut = 0u, kLowest = 0x00800000u;  // keys: of a dropped element; of the lowest finite number
-    float v[E], n[E], top = kNegInf;
+    // Keys in as many bits as the type has; 0 is a dropped element's.
+    constexpr uint32_t kOut = 0u;
+    constexpr int kShift = 32 - 8 * int(sizeof(DT));
+    auto key_of = [](float x) { return order_key(x) >> kShift; };
+    auto value_of = [](uint32_t k) {
+        const uint32_t u = k << kShift;
+        return key_value(u & 0x80000000u ? u : u | ((1u << kShift) - 1));
+    };
+    DT asked[E];
+    float v[E], n[E], top = kNegInf, low = kInf;
     uint32_t key[E];
 #pragma unroll
+    for (int e = 0; e < E; ++e) asked[e] = r.ask(lane + kWave * e);
+#pragma unroll
+    for (int e = 0; e < E; ++e) n[e] = noise && !greedy ? noise[lane + kWave * e < a.V ? lane + kWave * e : int(a.V) - 1] : 1.f;
+#pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int j = lane + kWave * e;
-        v[e] = j < a.V ? r.logit(j) : kNegInf;
-        n[e] = j < a.V && noise && !greedy ? noise[j] : 1.f;
-        key[e] = v[e] > kNegInf ? order_key(v[e]) : kOut;
+        v[e] = lane + kWave * e < a.V ? r.number(asked[e]) : kNegInf;
+        key[e] = v[e] > kNegInf ? key_of(v[e]) : kOut;
         top = fmaxf(top, v[e]);
+        low = v[e] > kNegInf ? fminf(low, v[e]) : low;
     }
     top = max_wave(top);
     if (top == kNegInf) {
@@ -898,13 +918,21 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
         }
     };
     if (!greedy) {
+        // The middle is that of the values first, then of the keys, which ends where values are far from even.
+        constexpr int kByValue = 14;
+        auto middle = [&](uint32_t lo, uint32_t hi, int step) {
+            if (step >= kByValue) return lo + (hi - lo) / 2;
+            const uint32_t m = key_of(0.5f * value_of(lo) + 0.5f * value_of(hi));
+            return m <= lo ? lo + 1 : m >= hi ? hi - 1 : m;
+        };
+        const uint32_t first = key_of(-max_wave(-low)), last = key_of(top) + 1;  // (of all; above all)
         if (s.top_k < a.V) {
             const int k = int(s.top_k);
-            uint32_t lo = kLowest, hi = order_key(top) + 1;
+            uint32_t lo = first, hi = last;
             int above_lo = count(lo), above_hi = 0;
             if (above_lo > k) {
-                while (hi - lo > 1 && above_lo > k) {
-                    const uint32_t mid = lo + (hi - lo) / 2;
+                for (int step = 0; hi - lo > 1 && above_lo > k; ++step) {
+                    const uint32_t mid = middle(lo, hi, step);
                     const int x = count(mid);
                     if (x >= k) {
                         lo = mid;
@@ -925,27 +953,32 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
                 z += w[e];
             }
             const float target = fmaxf(s.top_p * sum_wave(z), 1e-30f);
-            uint32_t lo = kLowest, hi = order_key(top) + 1;
+            uint32_t lo = first, hi = last;
             int above_lo = count(lo), above_hi = 0;
             float mass_hi = 0.f;
-            while (hi - lo > 1 && above_lo - above_hi > 1) {
-                const uint32_t mid = lo + (hi - lo) / 2;
+            for (int step = 0; hi - lo > 1 && above_lo - above_hi > 1; ++step) {
+                const uint32_t mid = middle(lo, hi, step);
                 float m = 0.f;
+                int x = 0;
 #pragma unroll
-                for (int e = 0; e < E; ++e) m += key[e] >= mid ? w[e] : 0.f;
+                for (int e = 0; e < E; ++e) {
+                    const bool in = key[e] >= mid;
+                    m += in ? w[e] : 0.f;
+                    x += __popcll(__ballot(in));
+                }
                 m = sum_wave(m);
                 if (m >= target) {
                     lo = mid;
-                    above_lo = count(mid);
+                    above_lo = x;
                 } else {
                     hi = mid;
-                    above_hi = count(mid);
+                    above_hi = x;
                     mass_hi = m;
                 }
             }
             int quota = kWave * E;
             if (above_lo - above_hi > 1) {  // equal ones: as many as begin below the target
-                const float one = exp2_fast(r.log2_weight(key_value(lo)));
+                const float one = exp2_fast(r.log2_weight(value_of(lo)));
                 quota = one > 0.f ? int(fminf(fmaxf(ceilf((target - mass_hi) / one), 1.f), float(kWave * E))) : 1;
             }
             drop(lo, quota);
@@ -984,12 +1017,15 @@ __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
     const SampleRow s = sample_row(a, row);
     const float c = sample_scale(s);
     const bool greedy = !(c < kInf);
+    DT asked[E];
     float v[E], n[E], top = kNegInf;
 #pragma unroll
+    for (int e = 0; e < E; ++e) asked[e] = r.ask(i + L * e);
+#pragma unroll
+    for (int e = 0; e < E; ++e) n[e] = noise && !greedy ? noise[i + L * e < a.V ? i + L * e : int(a.V) - 1] : 1.f;
+#pragma unroll
     for (int e = 0; e < E; ++e) {
-        const bool in = i + L * e < a.V;
-        v[e] = in ? r.logit(i + L * e) : kNegInf;
-        n[e] = in && noise && !greedy ? noise[i + L * e] : 1.f;
+        v[e] = i + L * e < a.V ? r.number(asked[e]) : kNegInf;
         top = fmaxf(top, v[e]);
     }
     top = max_lanes<L>(top);

@@ -18,7 +18,6 @@ __device__ __forceinline__ int64_t grid_row() { return (int64_t(blockIdx.y) << k
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff(), kNegInf = -kInf;
-constexpr float kLargest = 3.4028234663852886e38f;  // the largest float
 
 // v_exp_f32 and v_log_f32: base 2, 1 ulp.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
