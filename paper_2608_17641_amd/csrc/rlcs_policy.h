@@ -94,13 +94,17 @@ __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     Above sc{};
     float l2z = 0.f;
     if (part) {
+        // (all of a lane's logits are asked for before any is looked at)
+        DT asked[E];
         float top = kNegInf;
 #pragma unroll
+        for (int e = 0; e < E; ++e) asked[e] = x[i + L * e < p.V ? i + L * e : int(p.V) - 1];
+        const float taken = widen(x[a]);
+#pragma unroll
         for (int e = 0; e < E; ++e) {
-            v[e] = i + L * e < p.V ? widen(x[i + L * e]) : kNegInf;
+            v[e] = i + L * e < p.V ? widen(asked[e]) : kNegInf;
             top = fmaxf(top, v[e]);
         }
-        const float taken = widen(x[a]);
         top = max_lanes<L>(top);
         sc = above(top, kLog2e * p.inv_temp);
         float z = 0.f, s = 0.f;
