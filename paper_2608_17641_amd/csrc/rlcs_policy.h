@@ -80,9 +80,11 @@ __device__ __forceinline__ float policy_gradient(const PolicyRow& r, const Above
     return exp2_fast(l) * fmaf(r.a, l, r.b);
 }
 
-// Rows of up to L * E logits, L lanes a row, E logits a lane in registers.
+// Rows of up to L * E logits, L lanes a row, E logits a lane in registers: neighbours, where they make a
+// vector, else L apart.
 template <typename DT, bool LOSS, int L, int E>
 __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
+    constexpr bool VEC = E == RowVec<DT>::K;
     const int lane = threadIdx.x & 63, i = lane % L;
     const int64_t row = (grid_row() * 4 + (threadIdx.x >> 6)) * (kWave / L) + lane / L;
     if (row >= p.M) return;  // (a whole group of L lanes leaves together)
@@ -95,16 +97,23 @@ __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     float l2z = 0.f;
     if (part) {
         // (all of a lane's logits are asked for before any is looked at)
-        DT asked[E];
-        float top = kNegInf;
+        float top = kNegInf, taken;
+        if constexpr (VEC) {
+            RowVec<DT> asked;
+            asked.load(x, i, p.V);
+            taken = widen(x[a]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) asked[e] = x[i + L * e < p.V ? i + L * e : int(p.V) - 1];
-        const float taken = widen(x[a]);
+            for (int e = 0; e < E; ++e) v[e] = asked.at(e);
+        } else {
+            DT asked[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[e] = i + L * e < p.V ? widen(asked[e]) : kNegInf;
-            top = fmaxf(top, v[e]);
+            for (int e = 0; e < E; ++e) asked[e] = x[i + L * e < p.V ? i + L * e : int(p.V) - 1];
+            taken = widen(x[a]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = i + L * e < p.V ? widen(asked[e]) : kNegInf;
         }
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = fmaxf(top, v[e]);
         top = max_lanes<L>(top);
         sc = above(top, kLog2e * p.inv_temp);
         float z = 0.f, s = 0.f;
@@ -121,13 +130,18 @@ __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     }
     if (LOSS && p.grad) {
         DT* g = reinterpret_cast<DT*>(p.grad) + row * p.ld_grad;
+        float d[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int64_t j = i + L * e;
-            if (j >= p.V) continue;
-            float d = part && r.some ? policy_gradient(r, sc, l2z, v[e]) : 0.f;
-            if (part && j == a) d += r.d;
-            g[j] = narrow(d, DT{});
+            d[e] = part && r.some ? policy_gradient(r, sc, l2z, v[e]) : 0.f;
+            if (part && (VEC ? i * E + e : i + L * e) == a) d[e] += r.d;
+        }
+        if constexpr (VEC) {
+            if (i * E < p.V) store_row_vec<DT>(g, i, p.V, d);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (i + L * e < p.V) g[i + L * e] = narrow(d[e], DT{});
         }
     }
     if (i == 0) policy_outputs<LOSS>(p, row, r);

@@ -34,12 +34,17 @@ void launch_rows(const PolicyArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((policy_rows_kernel<DT, LOSS, W>), row_grid(p.M), dim3(W * kWave), 0, s, p);
 }
 
+// Short rows: as few lanes a row as hold it, four at least (131072 x 18 float32 8.5 us with four lanes of six
+// logits, 9.8 with eight of four; 65536 x 120 14.5 with sixteen of eight, 15.4 with 32 of four; 65536 x 250
+// 23 with 32 of eight, 31 with 64 of four), neighbours in a vector where that has as many (131072 x 31
+// float32 11 us with eight lanes' vectors, 13 with four lanes of eight logits apart; 65536 x 200 bfloat16 17.5 and 23).
 template <typename DT, bool LOSS>
 rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
     constexpr int64_t kVec = 16 / sizeof(DT);
     if (p.V <= 8) launch_small<DT, LOSS, 4, 2>(p, s);
     else if (p.V <= 16) launch_small<DT, LOSS, 4, 4>(p, s);
     else if (p.V <= 24) launch_small<DT, LOSS, 4, 6>(p, s);
+    else if (sizeof(DT) == 4 && p.V <= 32) launch_small<DT, LOSS, 8, 4>(p, s);
     else if (p.V <= 32) launch_small<DT, LOSS, 4, 8>(p, s);
     else if (p.V <= 64) launch_small<DT, LOSS, 8, 8>(p, s);
     else if (p.V <= 128) launch_small<DT, LOSS, 16, 8>(p, s);
