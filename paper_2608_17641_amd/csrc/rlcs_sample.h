@@ -767,7 +767,8 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
         // noise fetched, by full waves.
         // (the first bin takes logarithms that rounding leaves above 0, too)
         const float sure = !by_p ? kNegInf : cross > 0 ? -float(cross) / kBinsPerOctave : kInf;
-        const float edge = by_p ? -float(cross + 1) / kBinsPerOctave : kNegInf;
+        // (min-p's bound, less the rounding of a logarithm and an exponential, spares what lies below it the trip)
+        const float edge = fmaxf(by_p ? -float(cross + 1) / kBinsPerOctave : kNegInf, by_min ? log2_fast(least) - 0.01f : kNegInf);
         __syncthreads();  // (the bins' memory)
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         float* kept_v = sh.kept.v[wave];
