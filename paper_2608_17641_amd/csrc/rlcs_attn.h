@@ -697,6 +697,13 @@ constexpr size_t attn_mem() {
     return PR == kPrefixShared64 && k > n ? k : n;
 }
 
+// Every item but a prefix of more than 64 rows. Bound by memory: a key and its value
+// (512 bytes in bfloat16, D = 128) meet 256 multiply-adds of each query row, of which a suffix has as many as a
+// key head serves heads.
+// Solo waves on full suffixes, 64 sequences x 4096 tokens x 8 heads x 128 bfloat16 (1.07 GB): 190 us,
+// 5.7 TB/s, 512 sequences 1393 us, 6.2 TB/s; with lengths at random 126 us for half the bytes, 4.3 TB/s: what
+// is left when the short ones have ended does not fill the CUs. A launch bound of four waves a SIMD
+// spills and is slower; keys loaded straight into the operand's layout spare LDS one of its two passes.
 template <typename DT, int ND, PrefixRows PR, bool SOLO, bool EXACT>
 __global__ __launch_bounds__(kAttnWaves * kWave) void attn_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ __attribute__((aligned(16))) char s_mem[attn_mem<DT, ND, PR, EXACT>()];
@@ -718,7 +725,13 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void attn_kernel(AttnArgs a, At
     }
 }
 
-// The prefix alone: its registers (two tiles a wave) would halve the suffix's waves on a CU.
+// The prefix alone: its registers (two tiles a wave) would halve the suffix's waves on a CU. Bound by the
+// vector unit: a step's weights take some 6 of its operations for each matrix instruction, and a SIMD's two
+// waves, which meet at a barrier every 64 keys, want both units at the same time. 256 rows of 32768
+// keys, 8 heads, D = 128, bfloat16 (34 GFLOP): 54 us, 640 TFLOP/s, where a product of 8192^3 reaches 1227.
+// Measured and left: four waves of two tiles, two workgroups a CU, 86 us (every key is staged twice); one
+// tile a wave in the launch of the suffixes 137; the next step's scores issued before this step's
+// weights, with a third block in LDS, 58; the products' accumulators held in vector registers, the same.
 template <typename DT, int ND, int QT, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) void attn_prefix_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ __attribute__((aligned(16))) char s_mem[SharedKeys<DT, ND, QT, W, EXACT>::kLds];
@@ -727,8 +740,9 @@ __global__ __launch_bounds__(W * kWave) void attn_prefix_kernel(AttnArgs a, Attn
     attn_share_keys<DT, ND, QT, W, EXACT>(a, plan, it, s_mem);
 }
 
-// Joins the parts of a row: one row a workgroup, `groups` of D / 4 lanes (four dimensions each) on
-// every groups-th part.
+// Joins the parts of a row, o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i: one row a workgroup,
+// `groups` of D / 4 lanes (four dimensions each) on every groups-th part. Bound by latency and by reading
+// again what the parts wrote, 4 D + 8 bytes a part and row: 512 rows 4 us, 4096 rows 10, 16384 rows 22.
 template <typename DT>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan) {
     __shared__ f32x4 s_o[256];

@@ -534,6 +534,9 @@ __device__ __forceinline__ bool open_finish(const SampleArgs& a, const OpenPart&
     return true;
 }
 
+// A row without filters, one per workgroup: a pass over logits and noise, 6 bytes a bfloat16 logit,
+// with the running maximum and sum of a softmax beside the race, so bound by memory: 512 x 128000 bfloat16
+// (393 MB) 70 us, 5.6 TB/s.
 template <typename DT, int W, int U, bool ONE>
 __global__ __launch_bounds__(W * kWave) void sample_open_kernel(SampleArgs a) {
     __shared__ uint64_t s_bins[kDigits], s_slots[W];
@@ -548,7 +551,8 @@ __global__ __launch_bounds__(W * kWave) void sample_open_kernel(SampleArgs a) {
     if (!open_finish<DT>(a, p, x, c, row)) sample_general<DT, W>(a, s, x, noise, p.top, row, s_bins, s_slots);
 }
 
-// Few long rows: parts of `length` elements (a multiple of a vector) on workgroups of their own,
+// Few long rows, on which one CU's loads are what bounds: parts of `length` elements (a multiple of a
+// vector) on workgroups of their own (4 x 128000 bfloat16 5.5 us),
 template <typename DT, int W, int U>
 __global__ __launch_bounds__(W * kWave) void sample_parts_kernel(SampleArgs a, OpenPart* parts, int64_t length) {
     __shared__ uint64_t s_slots[W];
@@ -561,7 +565,7 @@ __global__ __launch_bounds__(W * kWave) void sample_parts_kernel(SampleArgs a, O
     if (threadIdx.x == 0) parts[row * gridDim.x + blockIdx.x] = p;
 }
 
-// and their join, four waves a row (one does, unless the general way has to take it).
+// and their join, four waves a row (one does, unless the general way has to take it; 2 us).
 template <typename DT>
 __global__ __launch_bounds__(4 * kWave) void sample_join_kernel(SampleArgs a, const OpenPart* parts, int count) {
     __shared__ uint64_t s_bins[kDigits], s_slots[4];
@@ -579,7 +583,14 @@ __global__ __launch_bounds__(4 * kWave) void sample_join_kernel(SampleArgs a, co
         sample_general<DT, 4>(a, s, x, a.noise ? a.noise + row * a.ld_noise : nullptr, p.top, row, s_bins, s_slots);
 }
 
-// One row per workgroup of W waves, with its filters. The cases that the quicker ways leave end in
+// One row per workgroup of W waves, with its filters. Bound by the vector unit and by barriers, a row having
+// a CU or a part of one: 64 x 32000 bfloat16 with top-k of 50 11 us, top-p of 0.9 19, min-p 12; 256 x 128000
+// float32 with top-k 45 us (2.9 TB/s), with top-p of 0.95 83: the first pass, at the memory's rate, 27, the
+// histogram 22 (16 vector operations a logit above its bound), what picks out the kept ones, to weigh
+// them with full waves, 15, and their noise 18, as some 9000 of a row touch nine tenths of its lines.
+// Measured and left: the next vectors read ahead (85 us), the kept ones in a column of LDS for each lane
+// with no count over lanes (85). top-k beyond 256 takes the general way (64 x 32000 of 2000 78 us).
+// The cases that the quicker ways leave end in
 // the general one, at the end (one place, so that it is compiled into the kernel, not called).
 template <typename DT, int W, int U, bool ONE>
 __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
@@ -1007,7 +1018,9 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
     if (lane == 0) sample_outputs(a, row, j, greedy ? 0.f : r.log2_weight(r.logit(j)) - log2_fast(z));
 }
 
-// Rows of up to L * E logits, L lanes a row, no filters.
+// Rows of up to L * E logits, L lanes a row, no filters: all of a lane's loads at once, then one fold for
+// the maximum and one each for the sum and the race. Bound by a launch's latency up to some thousand rows
+// (8192 x 18 float32 3.2 us), then by memory (8192 x 1000 bfloat16 13 us, 3.8 TB/s).
 template <typename DT, int L, int E>
 __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63, i = lane % L;
