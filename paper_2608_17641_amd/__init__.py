@@ -726,7 +726,8 @@ def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlog
                      want_grad: bool = True):
     """(loss, dlogits, logp, ent): the clipped policy loss of each token with its weight, and the
     gradient of their sum by the logits. logp_old, adv, weight are float32 of the leading shape; a
-    token of weight 0, or outside [0, V), is left out (all its outputs 0). `dlogits` may be `logits`."""
+    token of weight 0, or outside [0, V), is left out (all its outputs 0). A logit of -inf is masked; a NaN or +inf makes its
+    row's outputs NaN. `dlogits` may be `logits`."""
     done = (_fast or _load_fast()).policy_loss(logits, tokens, logp_old, adv, weight, loss, dlogits, logp, ent,
                                                clip_low, clip_high, ent_coef, temperature, want_grad)
     if done is not NotImplemented:
@@ -770,7 +771,8 @@ def rlcs_sample(logits, noise=None, tokens=None, logp=None, *, temperature=1.0, 
     """(tokens, logp): one token per row from softmax(logits / temperature) after top-k, top-p and
     min-p, and its log-probability there. `noise`: float32 of the logits' shape, exponential numbers
     (``torch.empty_like(...).exponential_()``); without it the most likely token. Each setting is a
-    number, or a tensor of the leading shape (float32; top_k int32)."""
+    number, or a tensor of the leading shape (float32; top_k int32). A logit of -inf or NaN is masked,
+    +inf takes all; a row of masked logits gives token -1."""
     done = (_fast or _load_fast()).sample(logits, noise, tokens, logp, temperature, top_k, top_p, min_p, want_logp, ws)
     if done is not NotImplemented:
         return done
