@@ -363,6 +363,7 @@ rlcs_status rlcs_token_logp(const void* logits, const int32_t* tokens, float* lo
  *   weight   [M] float32, optional (NULL = 1): mask and normalisation of the mean. A row of weight 0
  *            (or a token outside [0, V)) is left out: none of its inputs is read, loss, logp,
  *            ent and its gradient are 0
+ *            A NaN in logp_old, adv or weight makes its token's loss and gradient NaN
  *   loss     [M] float32 out;  logp, ent  [M] float32 out, optional
  *   dlogits  [M, V] dtype out, optional, row m at m * ld_grad; may be `logits` itself (then
  *            ld_grad = ld)

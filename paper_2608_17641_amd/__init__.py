@@ -726,8 +726,9 @@ def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlog
                      want_grad: bool = True):
     """(loss, dlogits, logp, ent): the clipped policy loss of each token with its weight, and the
     gradient of their sum by the logits. logp_old, adv, weight are float32 of the leading shape; a
-    token of weight 0, or outside [0, V), is left out (all its outputs 0). A logit of -inf is masked; a NaN or +inf makes its
-    row's outputs NaN. `dlogits` may be `logits`."""
+    token of weight 0, or outside [0, V), is left out (all its outputs 0). A logit of -inf is masked; a
+    NaN or +inf makes its row's outputs NaN, a NaN in logp_old, adv or weight the token's loss and
+    gradient. `dlogits` may be `logits`."""
     done = (_fast or _load_fast()).policy_loss(logits, tokens, logp_old, adv, weight, loss, dlogits, logp, ent,
                                                clip_low, clip_high, ent_coef, temperature, want_grad)
     if done is not NotImplemented:

@@ -43,8 +43,12 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, float z, fl
     if (LOSS) {
         const float rho = exp2_fast(kLog2e * (r.logp - logp_old));
         const float free = rho * adv, held = fminf(fmaxf(rho, p.low), p.high) * adv;
-        r.loss = w * (-fminf(free, held) - p.ent_coef * r.ent);
-        const float g = free <= held ? -w * free : 0.f;
+        // (fminf and fmaxf pass over NaN, and so does a comparison: one in logp_old or adv has to show. An infinite
+        // ratio with an advantage of 0, whose product is NaN too, is held at the bound, and adds 0.)
+        const bool bad = __builtin_isunordered(rho, adv);
+        const float gain = bad ? __builtin_nanf("") : fminf(free, held);
+        r.loss = w * (-gain - p.ent_coef * r.ent);
+        const float g = bad ? gain : free <= held ? -w * free : 0.f;
         const float c = w * p.ent_coef;
         r.a = c * kLn2 * p.inv_temp;
         r.b = (c * r.ent - g) * p.inv_temp;
