@@ -414,7 +414,8 @@ size_t rlcs_workspace_size_sample(int64_t M, int64_t V);
  *   q        [N, G, Hq, D] dtype;  o  [N, G, Hq, D] dtype out, contiguous
  *   kp, vp   [N, P, Hkv, D] dtype;  ks, vs  [N, G, S, Hkv, D] dtype (NULL only if P, S is 0)
  *   prefix_len [N], suffix_len [N, G] int32, optional (NULL = P, S): clamped to [0, P], [0, S].
- *            Keys and values past the lengths may hold anything, NaN included
+ *            Keys and values past the lengths may hold anything, NaN included; a NaN within them, or in
+ *            a query, makes what it takes part in NaN
  *   lse      [N, G, Hq] float32 out, optional
  *   layout   strides in elements, NULL = contiguous. D is contiguous; strides are >= 0 and multiples
  *            of 16 bytes, as are q, kp, vp, ks, vs and o; those of tokens are below 2^24

@@ -532,8 +532,10 @@ struct AttnItem {
         }
     }
     template <typename DT>
+    // (a sum of 0 has no keys; one of NaN, of a NaN among them or the query, makes the row NaN)
     static __device__ __forceinline__ void finish(const AttnArgs& a, int64_t out, int d, f32x4 o, float m, float z) {
-        o = z > 0.f ? o / z : f32x4{0.f, 0.f, 0.f, 0.f};
+        const bool none = z == 0.f;
+        o = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o / z;
         DT* p = reinterpret_cast<DT*>(a.o) + out * a.D + d;
         if constexpr (sizeof(DT) == 4) {
             *reinterpret_cast<f32x4*>(p) = o;
@@ -543,7 +545,7 @@ struct AttnItem {
             for (int e = 0; e < 4; ++e) b[e] = static_cast<__bf16>(o[e]);
             *reinterpret_cast<bf16x4*>(p) = b;
         }
-        if (d == 0 && a.lse) a.lse[out] = z > 0.f ? kLn2 * (m + log2_fast(z)) : kNegInf;
+        if (d == 0 && a.lse) a.lse[out] = none ? kNegInf : kLn2 * (m + log2_fast(z));
     }
 };
 
