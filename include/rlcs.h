@@ -341,7 +341,7 @@ size_t rlcs_workspace_size_columns(int64_t columns, int64_t T);
  * Around a group rollout: attention over a shared prompt, the sampling of the next token, and the
  * policy loss of the tokens with its gradient. The conventions above hold (device pointers, dtype,
  * checks on the host, streams, errors); rows of logits may lie a stride apart, and a size of 0 is a
- * no-op.                                                                                   */
+ * no-op: with V = 0 or D = 0 outputs of other sizes are not written.                       */
 
 /* Log-probability of the taken token and entropy of the policy, for M rows of V logits:
  *   y = x / temperature,  logp = y_a - log sum_j e^{y_j},  ent = -sum_j p_j log p_j.

@@ -698,6 +698,14 @@ def _out_lead(name, t, lead, dtype, device, want=True):
     return _check_lead(name, t, lead, dtype, device)
 
 
+def _fill(value, *outputs):
+    # rows without logits: every token is outside and there is none to draw (the library's calls
+    # do nothing at a size of 0)
+    for t in outputs:
+        if t is not None:
+            t.fill_(value)
+
+
 def _required(**tensors):
     for name, t in tensors.items():
         if t is None:
@@ -718,6 +726,8 @@ def rlcs_token_logp(logits, tokens, logp=None, ent=None, *, temperature: float =
     with _on(dev):
         _call("rlcs_token_logp", _ptr(logits), _ptr(tokens), _ptr(logp), _ptr(ent), M, V, ld, temperature,
               _DTYPES[dt], _stream(dev))
+    if V == 0:
+        _fill(0, logp, ent)
     return logp, ent
 
 
@@ -753,6 +763,8 @@ def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlog
         _call("rlcs_policy_loss", _ptr(logits), _ptr(tokens), _ptr(logp_old), _ptr(adv), _ptr(weight), _ptr(loss),
               _ptr(dlogits), _ptr(logp), _ptr(ent), M, V, ld, ldg, clip_low, clip_high, ent_coef, temperature,
               _DTYPES[dt], _stream(dev))
+    if V == 0:
+        _fill(0, loss, logp, ent)
     return loss, dlogits, logp, ent
 
 
@@ -797,6 +809,9 @@ def rlcs_sample(logits, noise=None, tokens=None, logp=None, *, temperature=1.0, 
     with _on(dev):
         _call("rlcs_sample", _ptr(logits), _ptr(noise), tp, kp, pp, mp, _ptr(tokens), _ptr(logp), M, V, ld, ldn, t, k,
               p, m, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+    if V == 0:
+        _fill(-1, tokens)
+        _fill(float("-inf"), logp)
     return tokens, logp
 
 
@@ -841,6 +856,8 @@ def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix
     if q.device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
     N, G, Hq, D = (int(x) for x in q.shape)
+    if D == 0 and N * G * Hq > 0:
+        raise ValueError("q must have heads of D >= 8 dimensions")
     dt, dev = q.dtype, q.device
     _attn_operand("q", q, 4, dt, dev)
     _attn_operand("kp", kp, 4, dt, dev); _attn_operand("vp", vp, 4, dt, dev)
@@ -869,5 +886,5 @@ def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix
     with _on(dev):
         _call("rlcs_shared_prefix_attn", _ptr(q), _ptr(kp), _ptr(vp), _ptr(ks), _ptr(vs), _ptr(prefix_len),
               _ptr(suffix_len), _ptr(o), _ptr(lse), N, G, Hq, Hkv, D, P, S, _native.ctypes.addressof(at),
-              1.0 / D ** 0.5 if scale is None and D else scale or 0.0, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+              1.0 / max(D, 1) ** 0.5 if scale is None else scale, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
     return o, lse

@@ -514,6 +514,7 @@ struct Rows {
     }
 };
 
+// (Rows without logits are left to the Python function.)
 void* rows_input(Call& c, PyObject* o, Rows& r) {
     const at::Tensor* t = c.plain(o);
     if (!t) {
@@ -523,7 +524,7 @@ void* rows_input(Call& c, PyObject* o, Rows& r) {
     c.dtype = t->scalar_type();
     c.device = t->device();
     c.ok = c.ok && (c.dtype == at::kFloat || c.dtype == at::kBFloat16) && c.device.is_cuda() &&
-           c.device.index() == c10::hip::current_device() && r.of(*t);
+           c.device.index() == c10::hip::current_device() && r.of(*t) && r.V > 0;
     return c.ok ? t->data_ptr() : nullptr;
 }
 
@@ -701,6 +702,7 @@ PyObject* shared_prefix_attn(Argv x, Py_ssize_t nargs) {
     c.ok = (c.dtype == at::kFloat || c.dtype == at::kBFloat16) && c.device.is_cuda() && c.device.index() == c10::hip::current_device();
     const int64_t N = q->size(0), G = q->size(1), Hq = q->size(2), D = q->size(3), P = kp->size(1), Hkv = kp->size(2);
     const int64_t S = ks && ks->dim() == 5 ? ks->size(2) : 0;
+    if (D == 0) Py_RETURN_NOTIMPLEMENTED;
     rlcs_attn_layout at{};
     auto operand = [&](const at::Tensor* t, at::IntArrayRef sizes, int64_t* strides) -> const void* {
         if (!t) return nullptr;
@@ -714,7 +716,7 @@ PyObject* shared_prefix_attn(Argv x, Py_ssize_t nargs) {
     const int32_t* pl = static_cast<int32_t*>(c.checked(x[5], at::kInt, {N}, false));
     const int32_t* sl = static_cast<int32_t*>(c.checked(x[6], at::kInt, {N, G}, false));
     Result o(c, x[7], true, c.dtype, {N, G, Hq, D}), lse(c, x[8], c.truth(x[10]), at::kFloat, {N, G, Hq});
-    const float scale = x[9] == Py_None ? (D > 0 ? float(1.0 / std::sqrt(double(D))) : 0.f) : c.number(x[9]);
+    const float scale = x[9] == Py_None ? float(1.0 / std::sqrt(double(D))) : c.number(x[9]);
     size_t wb = 0;
     void* ws = c.workspace(x[11], wb);
     const size_t make = c.ok && !ws ? g_lib.workspace_size_attn(N, G, Hq, Hkv, D, P, S) : 0;

@@ -1,0 +1,60 @@
+"""The operators around a group rollout on rows without logits, and on tensors that autograd has saved."""
+import math
+
+import pytest
+import torch
+
+import paper_2608_17641_amd as rl
+
+pytestmark = pytest.mark.gpu
+
+CLIP = dict(clip_low=0.2, clip_high=0.28)
+
+
+class _Python:
+    def __getattr__(self, name):
+        return lambda *a: NotImplemented
+
+
+@pytest.fixture(params=["native", "python"])
+def side(request, monkeypatch):
+    """Both sides of the binding."""
+    monkeypatch.setattr(rl, "_fast", rl._load_fast() if request.param == "native" else _Python())
+    return request.param
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("given", [False, True])
+def test_rows_without_logits(side, dtype, given):
+    """V = 0: no token to choose, every token outside. The outputs say so instead of holding what the
+    memory held."""
+    M = 5
+    x = torch.empty((M, 0), dtype=dtype, device="cuda")
+    noise = torch.empty((M, 0), device="cuda")
+    t = torch.zeros(M, dtype=torch.int32, device="cuda")
+    f = torch.ones(M, device="cuda")
+    full = lambda dt=torch.float32: torch.full((M,), 77, dtype=dt, device="cuda")  # noqa: E731
+    if not given:  # (memory that the calls' own outputs are likely to get)
+        junk = [full() for _ in range(16)]
+        del junk
+    tokens, logp = rl.rlcs_sample(x, noise, *((full(torch.int32), full()) if given else ()), top_p=0.9)
+    assert tokens.tolist() == [-1] * M and logp.tolist() == [-math.inf] * M
+    assert rl.rlcs_sample(x, want_logp=False)[1] is None
+    logp, ent = rl.rlcs_token_logp(x, t, *((full(), full()) if given else ()))
+    assert not bool(logp.any()) and not bool(ent.any())
+    assert rl.rlcs_token_logp(x, t, want_ent=False)[1] is None
+    kw = dict(loss=full(), logp=full(), ent=full()) if given else {}
+    loss, grad, logp, ent = rl.rlcs_policy_loss(x, t, f, f, **kw, **CLIP)
+    assert not bool(loss.any()) and not bool(logp.any()) and not bool(ent.any()) and grad.shape == (M, 0)
+    if given:
+        assert loss is kw["loss"] and logp is kw["logp"] and ent is kw["ent"]
+    with pytest.raises(rl.RlcsError, match="INVALID_ARG"):
+        rl.rlcs_token_logp(x, t, temperature=-1.0)
+
+
+def test_heads_without_dimensions(side):
+    q, kv = torch.empty((1, 2, 4, 0), device="cuda"), torch.empty((1, 9, 2, 0), device="cuda")
+    with pytest.raises(ValueError, match="D"):
+        rl.rlcs_shared_prefix_attn(q, kv, kv)
+    o, lse = rl.rlcs_shared_prefix_attn(q[:0], kv[:0], kv[:0])  # (nothing to say)
+    assert o.shape == (0, 2, 4, 0) and lse.shape == (0, 2, 4)
