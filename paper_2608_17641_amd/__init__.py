@@ -698,6 +698,18 @@ def _out_lead(name, t, lead, dtype, device, want=True):
     return _check_lead(name, t, lead, dtype, device)
 
 
+def _given(*outputs):
+    return [t for t in outputs if t is not None]
+
+
+def _written(given):
+    # tells autograd that the caller's tensors have new contents: a backward that saved the old ones
+    # raises an error
+    for t in given:
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _fill(value, *outputs):
     # rows without logits: every token is outside and there is none to draw (the library's calls
     # do nothing at a size of 0)
@@ -714,18 +726,21 @@ def _required(**tensors):
 
 def rlcs_token_logp(logits, tokens, logp=None, ent=None, *, temperature: float = 1.0, want_ent: bool = True):
     """(logp, ent): log-probability of each taken token and entropy of its policy,
-    softmax(logits / temperature). tokens int32; one outside [0, V) leaves its row out (0, 0)."""
+    softmax(logits / temperature). tokens int32; one outside [0, V) leaves its row out (0, 0). Values
+    only: the outputs are detached, also where the logits require a gradient."""
     done = (_fast or _load_fast()).token_logp(logits, tokens, logp, ent, temperature, want_ent)
     if done is not NotImplemented:
         return done
     M, V, ld, lead, dt, dev = _prep_logits(logits)
     _required(tokens=tokens)
     _check_lead("tokens", tokens, lead, torch.int32, dev)
+    given = _given(logp, ent)
     logp = _out_lead("logp", logp, lead, torch.float32, dev)
     ent = _out_lead("ent", ent, lead, torch.float32, dev, want_ent)
     with _on(dev):
         _call("rlcs_token_logp", _ptr(logits), _ptr(tokens), _ptr(logp), _ptr(ent), M, V, ld, temperature,
               _DTYPES[dt], _stream(dev))
+    _written(given)
     if V == 0:
         _fill(0, logp, ent)
     return logp, ent
@@ -738,7 +753,11 @@ def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlog
     gradient of their sum by the logits. logp_old, adv, weight are float32 of the leading shape; a
     token of weight 0, or outside [0, V), is left out (all its outputs 0). A logit of -inf is masked; a
     NaN or +inf makes its row's outputs NaN, a NaN in logp_old, adv or weight the token's loss and
-    gradient. `dlogits` may be `logits`."""
+    gradient. `dlogits` may be `logits`.
+
+    Nothing here is recorded by autograd: the outputs are detached, also where the logits require a
+    gradient. ``logits.backward(dlogits)`` carries it on; other terms of a loss need a graph of their own. `logits`
+    overwritten by their gradient count as modified in place."""
     done = (_fast or _load_fast()).policy_loss(logits, tokens, logp_old, adv, weight, loss, dlogits, logp, ent,
                                                clip_low, clip_high, ent_coef, temperature, want_grad)
     if done is not NotImplemented:
@@ -748,6 +767,7 @@ def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlog
     _check_lead("tokens", tokens, lead, torch.int32, dev)
     for name, t in (("logp_old", logp_old), ("adv", adv), ("weight", weight)):
         _check_lead(name, t, lead, torch.float32, dev)
+    given = _given(loss, dlogits, logp, ent)
     loss = _out_lead("loss", loss, lead, torch.float32, dev)
     logp = _out_lead("logp", logp, lead, torch.float32, dev)
     ent = _out_lead("ent", ent, lead, torch.float32, dev)
@@ -763,6 +783,7 @@ def rlcs_policy_loss(logits, tokens, logp_old, adv, weight=None, loss=None, dlog
         _call("rlcs_policy_loss", _ptr(logits), _ptr(tokens), _ptr(logp_old), _ptr(adv), _ptr(weight), _ptr(loss),
               _ptr(dlogits), _ptr(logp), _ptr(ent), M, V, ld, ldg, clip_low, clip_high, ent_coef, temperature,
               _DTYPES[dt], _stream(dev))
+    _written(given)
     if V == 0:
         _fill(0, loss, logp, ent)
     return loss, dlogits, logp, ent
@@ -801,6 +822,7 @@ def rlcs_sample(logits, noise=None, tokens=None, logp=None, *, temperature=1.0, 
     pp, p = _setting("top_p", top_p, lead, torch.float32, dev)
     mp, m = _setting("min_p", min_p, lead, torch.float32, dev)
     k = max(-1, min(int(k), 2 ** 31 - 1))
+    given = _given(tokens, logp)
     tokens = _out_lead("tokens", tokens, lead, torch.int32, dev)
     logp = _out_lead("logp", logp, lead, torch.float32, dev, want_logp)
     if ws is None:
@@ -809,6 +831,7 @@ def rlcs_sample(logits, noise=None, tokens=None, logp=None, *, temperature=1.0, 
     with _on(dev):
         _call("rlcs_sample", _ptr(logits), _ptr(noise), tp, kp, pp, mp, _ptr(tokens), _ptr(logp), M, V, ld, ldn, t, k,
               p, m, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+    _written(given)
     if V == 0:
         _fill(-1, tokens)
         _fill(float("-inf"), logp)
@@ -874,6 +897,7 @@ def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix
             raise ValueError(f"ks and vs have shapes {tuple(ks.shape)} and {tuple(vs.shape)}, expected [N, G, S, Hkv, D]")
     _check_lead("prefix_len", prefix_len, (N,), torch.int32, dev)
     _check_lead("suffix_len", suffix_len, (N, G), torch.int32, dev)
+    given = _given(o, lse)
     o = _out_lead("o", o, (N, G, Hq, D), dt, dev)
     lse = _out_lead("lse", lse, (N, G, Hq), torch.float32, dev, want_lse)
     if ws is None:
@@ -887,4 +911,5 @@ def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix
         _call("rlcs_shared_prefix_attn", _ptr(q), _ptr(kp), _ptr(vp), _ptr(ks), _ptr(vs), _ptr(prefix_len),
               _ptr(suffix_len), _ptr(o), _ptr(lse), N, G, Hq, Hkv, D, P, S, _native.ctypes.addressof(at),
               1.0 / max(D, 1) ** 0.5 if scale is None else scale, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+    _written(given)
     return o, lse

@@ -567,6 +567,12 @@ struct Result {
         Py_INCREF(o);
         return o;
     }
+    // Tells autograd that the caller's tensor has new contents: a backward that saved the old ones raises an error.
+    void written() const {
+        if (!given) return;
+        const at::Tensor& t = THPVariable_Unpack(given);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
     float* f32() const { return static_cast<float*>(ptr); }
 };
 
@@ -594,6 +600,7 @@ PyObject* run_results(Call& c, const char* name, std::initializer_list<Result*> 
         }
         return nullptr;
     }
+    for (const Result* r : results) r->written();
     PyObject* tuple = PyTuple_New(Py_ssize_t(results.size()));
     Py_ssize_t i = 0;
     for (Result* r : results) {

@@ -58,3 +58,43 @@ def test_heads_without_dimensions(side):
         rl.rlcs_shared_prefix_attn(q, kv, kv)
     o, lse = rl.rlcs_shared_prefix_attn(q[:0], kv[:0], kv[:0])  # (nothing to say)
     assert o.shape == (0, 2, 4, 0) and lse.shape == (0, 2, 4)
+
+
+def test_outputs_over_saved_tensors(side):
+    """Outputs written over a tensor that a backward needs: it raises instead of using them. Without,
+    the gradient goes on through the logits."""
+    M, V = 6, 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.randn(V, V, device="cuda", generator=g, requires_grad=True)
+    h = torch.randn(M, V, device="cuda", generator=g)
+    t = torch.zeros(M, dtype=torch.int32, device="cuda")
+    adv, old = torch.randn(M, device="cuda", generator=g), torch.full((M,), -5.0, device="cuda")
+    logits = h @ w
+    loss, grad, logp, ent = rl.rlcs_policy_loss(logits, t, old, adv, ent_coef=0.01, **CLIP)
+    assert not any(x.requires_grad for x in (loss, grad, logp, ent))
+    logits.backward(grad)
+    assert torch.allclose(w.grad, h.t() @ grad, rtol=1e-4, atol=1e-5)
+    for name in ("dlogits", "loss", "logp", "ent"):
+        logits = h @ w
+        saved = logits if name == "dlogits" else torch.ones(M, device="cuda")
+        later = (logits * logits).sum() if name == "dlogits" else (logits[:, 0] * saved).sum()
+        before = saved._version
+        rl.rlcs_policy_loss(logits, t, old, adv, **{name: saved.detach()}, **CLIP)
+        assert saved._version == before + 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            later.backward()
+    x = torch.randn(M, V, device="cuda", generator=g)
+    own = lambda dt=torch.float32: torch.zeros(M, dtype=dt, device="cuda")  # noqa: E731
+    a, b, c, d = own(), own(), own(torch.int32), own()
+    q, kv = torch.randn(1, M, 4, 64, device="cuda"), torch.randn(1, 9, 2, 64, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty(1, M, 4, device="cuda")
+    before = [u._version for u in (a, b, c, d, o, lse)]
+    rl.rlcs_token_logp(x, t, a, b)
+    rl.rlcs_sample(x, None, c, d)
+    rl.rlcs_shared_prefix_attn(q, kv, kv, o=o, lse=lse)
+    assert [u._version - v for u, v in zip((a, b, c, d, o, lse), before)] == [1] * 6
+    with torch.inference_mode():
+        frozen = own()
+        rl.rlcs_token_logp(x, t, frozen)
+    rl.rlcs_token_logp(x, t, frozen)  # (has no version)
+    assert bool(frozen.any())
