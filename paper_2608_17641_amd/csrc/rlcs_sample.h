@@ -68,6 +68,12 @@ __device__ __forceinline__ uint64_t race_entry(uint32_t key, uint32_t index) {
 }
 __device__ __forceinline__ uint32_t race_index(uint64_t e) { return ~uint32_t(e); }
 
+// Logarithm of a random number. v_log_f32 takes what lies below 2^-126 for 0: those are scaled first.
+__device__ __forceinline__ float noise_log2(float e) {
+    const bool small = e < 0x1p-126f;
+    return log2_fast(small ? e * 0x1p32f : e) - (small ? 32.f : 0.f);
+}
+
 template <int L>
 __device__ __forceinline__ uint64_t max_lanes(uint64_t v) {
 #pragma unroll
@@ -293,7 +299,7 @@ __device__ __forceinline__ void sample_general(const SampleArgs& a, const Sample
         const float u = r.log2_weight(v), w = exp2_fast(u);
         if (!(w >= least)) continue;
         z += w;
-        const float score = noise ? u - log2_fast(noise[j]) : v;
+        const float score = noise ? u - noise_log2(noise[j]) : v;
         const uint64_t e = race_entry(order_key(score), uint32_t(j));
         winner = e > winner ? e : winner;
     }
@@ -446,7 +452,7 @@ __device__ __forceinline__ Drawn draw_sorted(const uint64_t* sorted, int most, c
         const bool keep = in && (before < target || (first_kept && i == 0)) && w >= least;
         if (keep) {
             d.z += w;
-            const float score = noise ? u - log2_fast(noise[j]) : v;
+            const float score = noise ? u - noise_log2(noise[j]) : v;
             const uint64_t x = race_entry(order_key(score), j);
             d.winner = x > d.winner ? x : d.winner;
         }
@@ -518,7 +524,8 @@ __device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk
 }
 
 // The row's outputs from its whole part. False: the general way has to take it, as its logits are not near
-// (infinity among them), or none is above -inf (noise out of its range).
+// (infinity among them), no score is above -inf (noise out of its range), or the best is infinite (noise
+// below 2^-126, whose logarithm one operation does not give: a check here costs nothing a logit).
 template <typename DT>
 __device__ __forceinline__ bool open_finish(const SampleArgs& a, const OpenPart& p, const DT* x, float c, int64_t row) {
     if (p.top == kNegInf) {
@@ -526,7 +533,7 @@ __device__ __forceinline__ bool open_finish(const SampleArgs& a, const OpenPart&
         return true;
     }
     const bool greedy = !(c < kInf);
-    if (!greedy && (!near_scale(p.top, c) || p.winner == 0)) return false;
+    if (!greedy && (!near_scale(p.top, c) || p.winner == 0 || uint32_t(p.winner >> 32) == order_key(kInf))) return false;
     if (threadIdx.x == 0) {
         const uint32_t j = race_index(p.winner);
         sample_outputs(a, row, j, greedy ? 0.f : scale_of(p.top, c).log2_weight(widen(x[j])) - log2_fast(p.z));
@@ -808,7 +815,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
                     continue;
                 }
                 zk += w;
-                const uint64_t y = race_entry(order_key(noise ? l - log2_fast(e[q]) : x[q]), j[q]);
+                const uint64_t y = race_entry(order_key(noise ? l - noise_log2(e[q]) : x[q]), j[q]);
                 winner = y > winner ? y : winner;
             }
         };
@@ -1009,7 +1016,7 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
         if (key[e] == kOut) continue;
         const float u = r.log2_weight(v[e]);
         z += exp2_fast(u);
-        const uint64_t x = race_entry(noise && !greedy ? order_key(u - log2_fast(n[e])) : key[e], uint32_t(lane + kWave * e));
+        const uint64_t x = race_entry(noise && !greedy ? order_key(u - noise_log2(n[e])) : key[e], uint32_t(lane + kWave * e));
         winner = x > winner ? x : winner;
     }
     z = sum_wave(z);
@@ -1054,7 +1061,7 @@ __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
     for (int e = 0; e < E; ++e) {
         const float u = r.log2_weight(v[e]);
         z += exp2_fast(u);
-        const float score = noise && !greedy ? u - log2_fast(n[e]) : v[e];
+        const float score = noise && !greedy ? u - noise_log2(n[e]) : v[e];
         const uint64_t x = v[e] > kNegInf ? race_entry(order_key(score), uint32_t(i + L * e)) : 0;
         winner = x > winner ? x : winner;
     }
