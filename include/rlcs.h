@@ -349,7 +349,7 @@ size_t rlcs_workspace_size_columns(int64_t columns, int64_t T);
  *            logits are all -inf has logp = -inf and ent = 0, one with a NaN or +inf has NaN
  *   tokens   [M] int32. A token outside [0, V) leaves its row out: logp = ent = 0, no logit read
  *   logp     [M] float32 out;  ent  [M] float32 out, optional
- * temperature > 0, finite. Sums are float32, over at most 2^30 logits a row.               */
+ * temperature > 0, finite. Sums are float32, from chunk to chunk of a long row float64; V <= 2^30. */
 rlcs_status rlcs_token_logp(const void* logits, const int32_t* tokens, float* logp, float* ent,
                             int64_t M, int64_t V, int64_t ld, float temperature, rlcs_dtype dtype,
                             rlcs_stream_t stream);

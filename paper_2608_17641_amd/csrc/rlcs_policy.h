@@ -266,10 +266,14 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
     }
     const float c = kLog2e * p.inv_temp;
     const float taken = widen(x[a]);
-    float top = kNegInf, z = 0.f, s = 0.f;
-    auto rebase = [&](float t) {  // the sums so far, relative to a new maximum
+    // A lane's sums go chunk by chunk into 64 bits: one addition after another in 32 bits, 2^20 of them in the
+    // longest rows, drifts by as much as a hundredth where weights are alike.
+    float top = kNegInf;
+    double zl = 0., sl = 0.;
+    // sums relative to `top`, brought to a new maximum
+    auto rebase = [&](auto& z, auto& s, float& top, float t) {
         const float d = top == t ? 0.f : fmaxf((top - t) * c, kLog2Zero), f = exp2_fast(d);
-        s = f * fmaf(d, z, s);
+        s = f * (d * z + s);
         z *= f;
         top = t;
     };
@@ -282,8 +286,9 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
-        if (t > top) rebase(t);
+        if (t > top) rebase(zl, sl, top, t);
         const Above sc = above(top, c);
+        float z = 0.f, s = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -292,11 +297,12 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
                 z += e;
                 s = fmaf(e, l, s);
             }
+        zl += z;
+        sl += s;
     }
     // over the wave, then the workgroup: every lane's sums relative to one maximum
-    rebase(max_wave(top));
-    z = sum_wave(z);
-    s = sum_wave(s);
+    rebase(zl, sl, top, max_wave(top));
+    const float z = sum_wave(float(zl)), s = sum_wave(float(sl));
     if ((tid & 63) == 0) {
         s_m[tid >> 6] = top;
         s_z[tid >> 6] = z;
@@ -309,12 +315,10 @@ __global__ __launch_bounds__(W * kWave) void policy_rows_kernel(PolicyArgs p) {
     float z1 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        top = s_m[i];
-        z = s_z[i];
-        s = s_s[i];
-        rebase(m);
-        z1 += z;
-        s1 += s;
+        float zw = s_z[i], sw = s_s[i], mw = s_m[i];
+        rebase(zw, sw, mw, m);
+        z1 += zw;
+        s1 += sw;
     }
     const Above sc = above(m, c);
     const PolicyRow r = policy_row<LOSS>(p, z1, s1, sc.log2_weight(taken), old, adv, w);

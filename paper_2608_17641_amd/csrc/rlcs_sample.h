@@ -276,7 +276,7 @@ __device__ __forceinline__ void sample_general(const SampleArgs& a, const Sample
     if (s.top_k < a.V) t = descend_count<Row, W>(r, uint64_t(s.top_k), bins);
     if (s.top_p < 1.f) t = descend_mass<Row, W>(r, t, s.top_p, bins);
     const float least = least_weight(s, r, top);
-    float z = 0.f;
+    double zl = 0.;
     uint64_t winner = 0, ties = 0;
     for (int64_t j0 = 0; j0 < a.V; j0 += kLanes) {
         const int64_t j = j0 + tid;
@@ -300,13 +300,13 @@ __device__ __forceinline__ void sample_general(const SampleArgs& a, const Sample
         if (!keep) continue;
         const float u = r.log2_weight(v), w = exp2_fast(u);
         if (!(w >= least)) continue;
-        z += w;
+        zl += w;
         const float score = noise ? u - noise_log2(noise[j]) : v;
         const uint64_t e = race_entry(order_key(score), uint32_t(j));
         winner = e > winner ? e : winner;
     }
     winner = max_group<W>(winner, slots);
-    z = sum_group<W>(z, slots);
+    const float z = sum_group<W>(float(zl), slots);
     if (tid == 0) sample_outputs(a, row, race_index(winner), r.log2_weight(r.logit(race_index(winner))) - log2_fast(z));
 }
 
@@ -357,10 +357,11 @@ struct RowWalk {
                 for (int k = 0; k < K; ++k) f(fmaxf(v[u].at(k), kNegInf), uint32_t((i0 + u * kLanes) * K + k));
         });
     }
-    // The lane's largest element, its scale, and the sum of its weights by that. NaN as -inf.
+    // The lane's largest element, its scale, and the sum of its weights by that (its
+    // chunks' in 64 bits: a lane of the longest rows adds 2^16 weights). NaN as -inf.
     __device__ __forceinline__ void statistics(float c, float& top, Scale& sc, float& z) const {
         top = kNegInf;
-        z = 0.f;
+        double zl = 0.;
         sc = scale_of(top, c);
         chunks([&](const RowVec<DT>(&v)[U], int64_t) {
             float t = top;
@@ -370,15 +371,18 @@ struct RowWalk {
                 for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
             if (t > top) {
                 const Scale to = scale_of(t, c);
-                z *= exp2_fast(scale_step(sc, to));
+                zl *= exp2_fast(scale_step(sc, to));
                 sc = to;
                 top = t;
             }
+            float zc = 0.f;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int k = 0; k < K; ++k) z += fmaxf(exp2_fast(sc.log2_weight(v[u].at(k))), 0.f);
+                for (int k = 0; k < K; ++k) zc += fmaxf(exp2_fast(sc.log2_weight(v[u].at(k))), 0.f);
+            zl += zc;
         });
+        z = float(zl);
     }
 };
 
@@ -481,7 +485,8 @@ __device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk
     constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
     const bool greedy = !(c < kInf);  // (temperature 0)
     const bool race = noise && !greedy;
-    float top = kNegInf, z = 0.f, best = kNegInf;
+    float top = kNegInf, best = kNegInf;
+    double z = 0.;  // (chunk by chunk, as in statistics())
     Scale sc = scale_of(top, c);
     uint32_t at = 0;
     walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
@@ -504,24 +509,26 @@ __device__ __forceinline__ OpenPart open_part(const RowWalk<DT, W, U, ONE>& walk
             top = t;
         }
         int where = -1;  // in this chunk
+        float zc = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const float x = v[u].at(k);
-                z += fmaxf(exp2_fast(sc.log2_weight(x)), 0.f);  // (NaN, of a NaN or while all is -inf: 0)
+                zc += fmaxf(exp2_fast(sc.log2_weight(x)), 0.f);  // (NaN, of a NaN or while all is -inf: 0)
                 const float score = race ? fmaf(x, c, -log2_fast(e[u][k / 4].at(k % 4))) : x;
                 if (score > best) {  // (never of NaN or of a masked logit)
                     best = score;
                     where = u * K + k;
                 }
             }
+        z += zc;
         if (where >= 0) at = uint32_t((i0 + where / K * kLanes) * K + where % K);
     });
     OpenPart p;
     p.top = max_group_f<W>(top, slots_f);
     p.winner = max_group<W>(best == kNegInf ? 0 : race_entry(order_key(best), first + at), slots);
-    p.z = sum_group<W>(top == kNegInf || greedy ? 0.f : z * exp2_fast(scale_step(sc, scale_of(p.top, c))), slots);
+    p.z = sum_group<W>(top == kNegInf || greedy ? 0.f : float(z) * exp2_fast(scale_step(sc, scale_of(p.top, c))), slots);
     return p;
 }
 
@@ -793,11 +800,12 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         float* kept_v = sh.kept.v[wave];
         uint32_t* kept_j = sh.kept.j[wave];
-        float zk = 0.f;
+        double zl = 0.;
         uint64_t winner = 0;
         auto draw = [&](int n) {  // the buffer's first n (at most kBatch)
             float x[kBatch / kWave], e[kBatch / kWave];
             uint32_t j[kBatch / kWave];
+            float zb = 0.f;
             wave_lds_sync();
 #pragma unroll
             for (int q = 0; q < kBatch / kWave; ++q) {
@@ -816,10 +824,11 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
                     if (i < kList) sh.list[i] = race_entry(order_key(x[q]), j[q]);
                     continue;
                 }
-                zk += w;
+                zb += w;
                 const uint64_t y = race_entry(order_key(noise ? l - noise_log2(e[q]) : x[q]), j[q]);
                 winner = y > winner ? y : winner;
             }
+            zl += zb;
         };
         int held = 0;
         walk.chunks([&](const RowVec<DT>(&v)[U], int64_t i0) {
@@ -857,7 +866,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
                 }
         });
         if (held) draw(held);
-        zk = sum_group<W>(zk, sh.slots);
+        float zk = sum_group<W>(float(zl), sh.slots);
         winner = max_group<W>(winner, sh.slots);
         if (by_p) {
             __syncthreads();
