@@ -21,6 +21,13 @@ void launch_vec(const PolicyArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((policy_vec_kernel<DT, LOSS, W, U>), row_grid((p.M + rows - 1) / rows), dim3((W == 1 ? 4 : W) * kWave), 0, s, p);
 }
 
+// Rows of up to 64 * E logits, a wave a row: float32 logits apart, bfloat16 ones in vectors.
+template <typename DT, bool LOSS, int E>
+void launch_wave(const PolicyArgs& p, hipStream_t s) {
+    if constexpr (sizeof(DT) == 4) launch_small<DT, LOSS, 64, E>(p, s);
+    else launch_vec<DT, LOSS, 1, E / 8>(p, s);
+}
+
 // Rows that do not fit the registers of eight waves (with sixteen, one workgroup would have the CU to
 // itself and nothing to do while it waits: 4096 x 40000 bfloat16 196 us against 148) take sixteen
 // waves where few rows leave CUs to them (64 x 128000 bfloat16 27 -> 24 us), and from this length
@@ -40,24 +47,21 @@ void launch_rows(const PolicyArgs& p, hipStream_t s) {
 // float32 11 us with eight lanes' vectors, 13 with four lanes of eight logits apart; 65536 x 200 bfloat16 17.5 and 23).
 template <typename DT, bool LOSS>
 rlcs_status run_policy(const PolicyArgs& p, hipStream_t s) {
-    constexpr int64_t kVec = 16 / sizeof(DT);
+    constexpr bool kWide = sizeof(DT) == 4;
     if (p.V <= 8) launch_small<DT, LOSS, 4, 2>(p, s);
     else if (p.V <= 16) launch_small<DT, LOSS, 4, 4>(p, s);
     else if (p.V <= 24) launch_small<DT, LOSS, 4, 6>(p, s);
-    else if (sizeof(DT) == 4 && p.V <= 32) launch_small<DT, LOSS, 8, 4>(p, s);
-    else if (p.V <= 32) launch_small<DT, LOSS, 4, 8>(p, s);
+    else if (p.V <= 32) launch_small<DT, LOSS, kWide ? 8 : 4, kWide ? 4 : 8>(p, s);
     else if (p.V <= 64) launch_small<DT, LOSS, 8, 8>(p, s);
     else if (p.V <= 128) launch_small<DT, LOSS, 16, 8>(p, s);
     else if (p.V <= 256) launch_small<DT, LOSS, 32, 8>(p, s);
-    else if (sizeof(DT) == 4 && p.V <= 512) launch_small<DT, LOSS, 64, 8>(p, s);
-    else if (sizeof(DT) == 4 && p.V <= 1024) launch_small<DT, LOSS, 64, 16>(p, s);
-    else if (p.V <= 64 * kVec) launch_vec<DT, LOSS, 1, 1>(p, s);
-    else if (p.V <= 64 * 2 * kVec) launch_vec<DT, LOSS, 1, 2>(p, s);
-    else if (p.V <= 64 * 4 * kVec) launch_vec<DT, LOSS, 1, 4>(p, s);
-    else if (p.V <= 64 * 8 * kVec) launch_vec<DT, LOSS, 1, 8>(p, s);
-    else if (p.V <= 256 * 4 * kVec) launch_vec<DT, LOSS, 4, 4>(p, s);
-    else if (p.V <= 256 * 8 * kVec) launch_vec<DT, LOSS, 4, 8>(p, s);
-    else if (p.V <= 512 * 8 * kVec) launch_vec<DT, LOSS, 8, 8>(p, s);
+    else if (p.V <= 512) launch_wave<DT, LOSS, 8>(p, s);
+    else if (p.V <= 1024) launch_wave<DT, LOSS, 16>(p, s);
+    else if (p.V <= 2048) launch_vec<DT, LOSS, 1, kWide ? 8 : 4>(p, s);
+    else if (p.V <= 4096) launch_vec<DT, LOSS, kWide ? 4 : 1, kWide ? 4 : 8>(p, s);
+    else if (p.V <= 8192) launch_vec<DT, LOSS, 4, kWide ? 8 : 4>(p, s);
+    else if (p.V <= 16384) launch_vec<DT, LOSS, kWide ? 8 : 4, 8>(p, s);
+    else if (!kWide && p.V <= 32768) launch_vec<DT, LOSS, 8, 8>(p, s);
     else if (p.M <= kFewRows || p.V * int64_t(sizeof(DT)) >= kLongRow) launch_rows<DT, LOSS, 16>(p, s);
     else launch_rows<DT, LOSS, 8>(p, s);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
