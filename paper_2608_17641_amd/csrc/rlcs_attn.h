@@ -146,9 +146,8 @@ __device__ __forceinline__ float max_of_four(float x) {
     return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
-// One softmax step of a query tile: scores of 16 * KT keys to weights (rounded to bfloat16 in `p`: to
-// nearest, for the product; the sums keep all bits), the running maximum, sum and outputs brought
-// to the new maximum.
+// One softmax step of a query tile: scores of 16 * KT keys become their weights, in place, and the
+// running maximum, sum and outputs are brought to the new maximum.
 template <int KT, int ND>
 __device__ __forceinline__ void softmax_step(f32x4 (&s)[KT], float scale, float& m, float& l, f32x4 (&acc)[ND]) {
     float top = kNegInf;
@@ -173,7 +172,8 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[KT], float scale, float&
         }
 }
 
-// Weights of 32 keys (two tiles of scores) as an operand.
+// Weights of 32 keys (two tiles of scores) as an operand, rounded to bfloat16, to nearest, for the product alone:
+// their sum keeps all bits.
 __device__ __forceinline__ bf16x8 weights_operand(f32x4 a, f32x4 b) {
     bf16x8 p;
 #pragma unroll

@@ -315,6 +315,9 @@ constexpr int kFewest = 256;     // top-k that goes by lanes' maxima
 constexpr int kMassBins = 2048;  // 64 an octave of weight: down to 2^-32 of the largest
 constexpr float kBinsPerOctave = 64.f;
 constexpr int kBatch = 256;  // kept elements a wave draws from at a time
+// What holds them: less than a batch is left over when a wave adds up to four from each lane.
+constexpr int kRoom = 2 * kBatch;
+static_assert(kBatch - 1 + 4 * kWave <= kRoom, "a wave's kept elements fit their buffer");
 
 // A row as its workgroup walks it, U vectors a lane at a time: f(vectors, index of the first; the
 // others follow kLanes vectors apart). Past the row's end vectors are -inf. With ONE the row is no longer
@@ -392,8 +395,8 @@ struct SampleShared {
         uint64_t bins[kMassBins];
         float maxima[W * kWave];
         struct {
-            float v[W][kBatch * 2];
-            uint32_t j[W][kBatch * 2];
+            float v[W][kRoom];
+            uint32_t j[W][kRoom];
         } kept;
     };
     uint64_t list[kList], sorted[kList];
@@ -845,7 +848,7 @@ __global__ __launch_bounds__(W * kWave) void sample_rows_kernel(SampleArgs a) {
                         kept_j[i] = uint32_t((i0 + u * kLanes) * K + k);
                     }
                     held += __popcll(passed);
-                    if (k % 4 == 3 && held >= kBatch) {  // (at most kBatch + 4 * 63 by then)
+                    if (k % 4 == 3 && held >= kBatch) {  // (every four elements of a lane: up to kRoom by then)
                         draw(kBatch);
                         held -= kBatch;
                         wave_lds_sync();

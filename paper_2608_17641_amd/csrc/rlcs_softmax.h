@@ -118,7 +118,7 @@ __device__ __forceinline__ uint64_t max_wave(uint64_t v) {
     return fold_wave(v, uint64_t(0), [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
 
-// 16 bytes of a row at any element address (elements before `from` read nothing: `fill`).
+// 16 bytes of a row, at any element address.
 template <typename DT>
 struct RowVec {
     static constexpr int K = 16 / sizeof(DT);
