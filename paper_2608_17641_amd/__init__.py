@@ -804,7 +804,7 @@ def rlcs_sample(logits, noise=None, tokens=None, logp=None, *, temperature=1.0, 
                 want_logp: bool = True, ws=None):
     """(tokens, logp): one token per row from softmax(logits / temperature) after top-k, top-p and
     min-p, and its log-probability there. `noise`: float32 of the logits' shape, exponential numbers
-    (``torch.empty_like(...).exponential_()``); without it the most likely token. Each setting is a
+    (``torch.empty_like(logits, dtype=torch.float32).exponential_()``); without it the most likely token. Each setting is a
     number, or a tensor of the leading shape (float32; top_k int32). A logit of -inf or NaN is masked,
     +inf takes all; a row of masked logits gives token -1."""
     done = (_fast or _load_fast()).sample(logits, noise, tokens, logp, temperature, top_k, top_p, min_p, want_logp, ws)
@@ -865,9 +865,11 @@ def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix
     """(o, lse): attention of one query token per sequence over its group's prefix and its own suffix.
 
     q [N, G, Hq, D]; kp, vp [N, P, Hkv, D], shared by the G sequences of a group; ks, vs
-    [N, G, S, Hkv, D]. Any strides with D contiguous. prefix_len [N], suffix_len [N, G] int32: how many
-    keys of each count (default all). scale defaults to 1 / sqrt(D). o [N, G, Hq, D] of q's type,
-    lse float32 [N, G, Hq]."""
+    [N, G, S, Hkv, D]. D is contiguous, a multiple of 8 up to 256; other strides are any multiples of 16
+    bytes. prefix_len [N], suffix_len [N, G] int32: how many keys of each count (default all); a NaN among
+    these, or in a query, shows in what it takes part in. scale defaults to 1 / sqrt(D). o [N, G, Hq, D]
+    of q's type, lse float32 [N, G, Hq]. With bfloat16 the softmax weights, too, are rounded to it for
+    the product with the values."""
     done = (_fast or _load_fast()).shared_prefix_attn(q, kp, vp, ks, vs, prefix_len, suffix_len, o, lse, scale,
                                                       want_lse, ws)
     if done is not NotImplemented:

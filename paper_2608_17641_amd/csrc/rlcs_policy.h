@@ -86,8 +86,8 @@ __device__ __forceinline__ float policy_gradient(const PolicyRow& r, const Above
 
 // Rows of up to L * E logits, L lanes a row, E logits a lane in registers: neighbours, where they make a
 // vector, else L apart. Four lanes for the shortest, so that what is done once a row (a logarithm, two
-// exponentials, the clip: some 150 operations) is done four times, not 64. Bound by vector operations:
-// 131072 x 18 float32, loss and gradient, 8.5 us (2.6 TB/s), 65536 x 200 bfloat16 17.5 (3 TB/s).
+// exponentials, the clip: some 150 operations) is done four times, not 64. 131072 x 18 float32, loss and gradient, 8.2 us (2.7 TB/s): one round of waves, which loads,
+// computes (278 vector operations a wave, 3.7 us of a SIMD's eight) and stores. 65536 x 200 bfloat16 17.5 (3 TB/s).
 template <typename DT, bool LOSS, int L, int E>
 __global__ __launch_bounds__(4 * kWave) void policy_small_kernel(PolicyArgs p) {
     constexpr bool VEC = E == RowVec<DT>::K;

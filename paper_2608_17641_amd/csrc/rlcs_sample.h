@@ -1045,7 +1045,7 @@ __global__ __launch_bounds__(4 * kWave) void sample_wave_kernel(SampleArgs a) {
 
 // Rows of up to L * E logits, L lanes a row, no filters: all of a lane's loads at once, then one fold for
 // the maximum and one each for the sum and the race. Bound by a launch's latency up to some thousand rows
-// (8192 x 18 float32 3.2 us), then by memory (8192 x 1000 bfloat16 13 us, 3.8 TB/s).
+// (8192 x 18 float32 3.2 us), then by memory (8192 x 1000 bfloat16 12.3 us, 4 TB/s).
 template <typename DT, int L, int E>
 __global__ __launch_bounds__(4 * kWave) void sample_small_kernel(SampleArgs a) {
     const int lane = threadIdx.x & 63, i = lane % L;
