@@ -440,6 +440,156 @@ rlcs_status rlcs_shared_prefix_attn(const void* q, const void* kp, const void* v
 size_t rlcs_workspace_size_attn(int64_t N, int64_t G, int64_t Hq, int64_t Hkv, int64_t D, int64_t P,
                                 int64_t S);
 
+/* ---------------------------------------------------------------------------------------
+ * Speculative rollouts over a paged cache: attention of a chunk of new tokens, the cache's pages, the check of
+ * drafted tokens and the loss that trains who drafts them. The conventions above hold; a size of 0 is a no-op.
+ *
+ * A cache is `pages` pages of `page` tokens each (a power of two from 16 to 65536), Hkv heads of D dimensions a
+ * token. table [B, W] int32, row b at b * ld_table: the numbers of the pages that hold sequence b, in the order
+ * of its tokens; W * page <= 2^30. An entry outside [0, pages) is no page: its tokens are left out. length [B]
+ * int32: tokens of each sequence, clamped to [0, W * page].
+ * The T_b new tokens of sequence b are its last ones, positions length[b] - T_b to length[b] - 1. Those of all
+ * sequences lie one after the other: rows q_start[b] to q_start[b + 1] - 1 of `tokens` rows, q_start [B + 1]
+ * int32 and not falling; rows in front of q_start[0] and from q_start[B] on are left alone. q_start NULL: all sequences have
+ * tokens / B. max_chunk: no sequence has more new tokens (0: no more than `tokens`); those past it are left out. */
+typedef struct {
+    int64_t q[2];       /* strides in elements: token, head. Of q, */
+    int64_t k_new[2];   /* of new keys and */
+    int64_t v_new[2];   /* values: token, head */
+    int64_t k_cache[3]; /* page, token, head */
+    int64_t v_cache[3];
+} rlcs_paged_layout;
+
+/* Attention of every new token over its sequence up to itself, Hq query heads on Hkv key heads: the token at
+ * position i sees the keys j <= i,
+ *   s_j = scale * q . k_j,  o = sum_j e^{s_j - m} v_j / sum_j e^{s_j - m},  lse = log sum_j e^{s_j}.
+ * The new tokens' own keys and values are in the cache already (rlcs_paged_write). Without any key (a position
+ * below 0, or only entries that are no page) o = 0 and lse = -inf.
+ *   q        [tokens, Hq, D] dtype;  o  [tokens, Hq, D] dtype out, contiguous
+ *   k_cache, v_cache  [pages, page, Hkv, D] dtype. What lies past a length may be anything, NaN included; a NaN
+ *            among the keys and values that count, or in a query, shows in what it takes part in
+ *   lse      [tokens, Hq] float32 out, optional
+ *   layout   NULL = contiguous. D is contiguous; strides are >= 0 and multiples of 16 bytes, as are q, the caches
+ *            and o; those of tokens in a page are below 2^24
+ *   ws       rlcs_workspace_size_paged(...) bytes, 16-byte aligned, need not be cleared; of one call at a time
+ * D a multiple of 8 up to 256. Scores, sums and the output's accumulator are float32, for |s_j| up to 10^9; bfloat16
+ * weights e^{s - m} are rounded to bfloat16 for the product with V.                           */
+rlcs_status rlcs_paged_attn(const void* q, const void* k_cache, const void* v_cache,
+                            const int32_t* table, const int32_t* length, const int32_t* q_start,
+                            void* o, float* lse, int64_t tokens, int64_t B, int64_t W,
+                            int64_t ld_table, int64_t pages, int64_t page, int64_t Hq, int64_t Hkv,
+                            int64_t D, int64_t max_chunk, const rlcs_paged_layout* layout,
+                            float scale, rlcs_dtype dtype, void* ws, size_t ws_bytes,
+                            rlcs_stream_t stream);
+size_t rlcs_workspace_size_paged(int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv, int64_t D,
+                                 int64_t max_chunk);
+
+/* The new tokens' keys and values to their places in the cache.
+ *   k, v     [tokens, Hkv, D] dtype;  k_cache, v_cache  [pages, page, Hkv, D] dtype, written at the new tokens'
+ *            positions only. Positions below 0 and entries that are no page are passed over
+ * Two sequences whose new tokens lie in the same page write over each other: rlcs_pages_resize gives each its
+ * own. Strides, alignment and D as above.                                                    */
+rlcs_status rlcs_paged_write(const void* k, const void* v, void* k_cache, void* v_cache,
+                             const int32_t* table, const int32_t* length, const int32_t* q_start,
+                             int64_t tokens, int64_t B, int64_t W, int64_t ld_table, int64_t pages,
+                             int64_t page, int64_t Hkv, int64_t D,
+                             const rlcs_paged_layout* layout, rlcs_dtype dtype,
+                             rlcs_stream_t stream);
+
+/* The cache's pages. table is [B, W], contiguous; refs [pages] int32: how many of its entries hold each page; a
+ * page with 0 (or less) is free. A sequence holds the pages of its length; entries past them are not looked at and come
+ * out as -1. `..._out` may be the input itself where not said otherwise, and else overlaps none.
+ * ws: rlcs_workspace_size_pages(B, pages) bytes, 16-byte aligned, need not be cleared.
+ *
+ * Fork: sequence b becomes what sequence parent[b] is, sharing its pages (parent[b] outside [0, B), or b: it
+ * stays). All of a call at once: parents are read as they are before it. table_out and length_out are not the inputs.  */
+rlcs_status rlcs_pages_fork(const int32_t* table, const int32_t* length, const int32_t* refs,
+                            const int32_t* parent, int32_t* table_out, int32_t* length_out,
+                            int32_t* refs_out, int64_t B, int64_t W, int64_t pages, int64_t page,
+                            void* ws, size_t ws_bytes, rlcs_stream_t stream);
+
+/* Resize: sequence b gets new_length[b] tokens (below 0, or above W * page: it stays as it is). First the
+ * sequences that shrink give back the pages they no longer need (all, with length 0). Then those that grow get
+ * the free pages with the lowest numbers, in the order of sequences and of places in them. A sequence that grows
+ * from within a page which it shares leaves that page to the others and goes on in a copy:
+ *   moves    [B, 2] int32 out: (that page, its copy), or (-1, -1); rlcs_pages_copy moves what they hold
+ * A sequence that would need more free pages than there are, counted with the needs of all sequences before it,
+ * stays as it was: length_out tells.                                                          */
+rlcs_status rlcs_pages_resize(const int32_t* table, const int32_t* length, const int32_t* refs,
+                              const int32_t* new_length, int32_t* table_out, int32_t* length_out,
+                              int32_t* refs_out, int32_t* moves, int64_t B, int64_t W,
+                              int64_t pages, int64_t page, void* ws, size_t ws_bytes,
+                              rlcs_stream_t stream);
+
+/* Compaction: of U pages in use, those from number U on move, in order, to the free pages in front of it.
+ *   moves    [pages / 2, 2] int32 out: (from, to), then (-1, -1);  count  [1] int32 out: U
+ * table_out: entries with their pages' new numbers, those of free pages and of no page -1.     */
+rlcs_status rlcs_pages_compact(const int32_t* table, const int32_t* refs, int32_t* table_out,
+                               int32_t* refs_out, int32_t* moves, int32_t* count, int64_t B,
+                               int64_t W, int64_t pages, void* ws, size_t ws_bytes,
+                               rlcs_stream_t stream);
+size_t rlcs_workspace_size_pages(int64_t B, int64_t pages);
+
+/* Copies pages: for each (from, to) of moves [n, 2] int32, in every layer, page `from` onto page `to`. Moves with a
+ * number outside [0, pages) are passed over. No page is the `to` of one move and in another.
+ * Page p of layer l is the page_bytes bytes at l * layer_stride + p * page_stride (bytes; distinct pages and
+ * layers do not overlap).                                                                    */
+rlcs_status rlcs_pages_copy(void* cache, const int32_t* moves, int64_t n, int64_t layers,
+                            int64_t pages, int64_t layer_stride, int64_t page_stride,
+                            int64_t page_bytes, rlcs_stream_t stream);
+
+/* Which of a sequence's drafted tokens stand under the target policy p, given the draft's policy q, and the
+ * token that follows them: with p_i = softmax(target row i / temperature) and q_i = softmax(draft row i /
+ * draft_temperature), drafted token x_i stands if u_i q_i(x_i) < p_i(x_i). After the first that falls, at i, one
+ * token is drawn from max(p_i - q_i, 0), after the last drafted one from p_i (as also where p_i exceeds q_i nowhere): the
+ * largest log of that - log(noise), the lowest index among equal ones. The tokens are then
+ * distributed as p is, whatever q, if u is uniform on [0, 1) and noise exponential (rate 1), all independent.
+ *   target   [B, K + 1, V] dtype, row (b, i) at b * target_seq + i * target_ld
+ *   draft    [B, K, V] dtype, strides draft_seq, draft_ld; NULL: q_i is 1 at x_i and 0 elsewhere
+ *   draft_tokens  [B, K] int32; one outside [0, V) falls.  u  [B, K] float32.  noise  [B, V] float32, row b at b * noise_ld,
+ *            positive and finite
+ *   n_draft  [B] int32, optional (NULL = K), clamped to [0, K]: drafted tokens of each sequence; u, draft_tokens and rows
+ *            past them are not read
+ *   temperature, draft_temperature  [B] of each sequence's own, or NULL: `all_...`. A target temperature of 0
+ *            (or less) is all mass on the largest logit, the lowest index among equal ones; a draft's
+ *            on its largest logits alike. +inf weighs all alike
+ *   tokens   [B, K + 1] int32 out: those that stand, the drawn one, then -1;  count  [B] int32 out: how many
+ *   logp     [B, K + 1] float32 out, optional: their log-probabilities under p, then 0
+ *   ws       rlcs_workspace_size_verify(B, K, V) bytes, 16-byte aligned, need not be cleared
+ * A logit of -inf masks its entry, NaN counts as -inf, +inf as the type's largest number. Of a target row of masked logits no
+ * token stands, the one drawn is -1, and logp is -inf. V <= 2^24, K <= 1024. Probabilities are float32: a token whose
+ * u q is within their rounding of p may fall on either side.                                  */
+rlcs_status rlcs_verify_draft(const void* target, const void* draft, const int32_t* draft_tokens,
+                              const float* u, const float* noise, const int32_t* n_draft,
+                              const float* temperature, const float* draft_temperature,
+                              int32_t* tokens, int32_t* count, float* logp, int64_t B, int64_t K,
+                              int64_t V, int64_t target_seq, int64_t target_ld, int64_t draft_seq,
+                              int64_t draft_ld, int64_t noise_ld, float all_temperature,
+                              float all_draft_temperature, rlcs_dtype dtype, void* ws,
+                              size_t ws_bytes, rlcs_stream_t stream);
+size_t rlcs_workspace_size_verify(int64_t B, int64_t K, int64_t V);
+
+/* Distillation from a teacher's K largest logits, and its gradient by the student's logits: with p the
+ * student's softmax(logits / temperature) and t the teacher's probabilities of the listed tokens,
+ *   loss = weight * sum_k t_k (log t_k - log p_k),   dlogits_j = weight / temperature * (p_j - t_j),
+ *   tail = 0:  t_k = e^{top_logp_k} / sum_k e^{top_logp_k}  (any logits will do);
+ *   tail = 1:  t_k = e^{top_logp_k}, and what they leave, t' = max(0, 1 - sum_k t_k), is the mass of one more
+ *            class, of all tokens that are not listed, p' in the student's: loss += weight * t' (log t' - log p'), and there
+ *            dlogits_j = weight / temperature * p_j (1 - t' / p'). Left out where p' or t' is 0.
+ *   logits   [M, V] dtype, row m at m * ld; -inf masks an entry (p = 0)
+ *   top_ids  [M, K] int32; one outside [0, V) is not listed (t = 0). One listed twice has both shares
+ *   top_logp [M, K] float32, at the temperature of the loss; -inf: t = 0
+ *   weight   [M] float32, optional (NULL = 1). A row of weight 0 is left out: none of its inputs is read, loss and gradient are 0;
+ *            and so is one with nothing listed and tail = 0, with loss and gradient 0
+ *   loss     [M] float32 out;  dlogits  [M, V] dtype out, optional, row m at m * ld_grad; may be `logits` itself
+ *            (then ld_grad = ld)
+ * A NaN or +inf logit makes its row's outputs NaN, as a NaN in top_logp or weight makes what it takes part in. V <= 2^30,
+ * K <= 1024; temperature > 0, finite.                                                        */
+rlcs_status rlcs_distill_loss(const void* logits, const int32_t* top_ids, const float* top_logp,
+                              const float* weight, float* loss, void* dlogits, int64_t M,
+                              int64_t V, int64_t K, int64_t ld, int64_t ld_grad, float temperature,
+                              int tail, rlcs_dtype dtype, rlcs_stream_t stream);
+
 /* Static description of a status code. Never NULL. */
 const char* rlcs_status_string(rlcs_status status);
 

@@ -13,7 +13,9 @@ outputs are float32 ``[N, T]`` (allocated when not given). All tensors must live
 GPU. ``ws`` is an optional zero-initialised uint8 workspace (see ``make_workspace``).
 
 The operators around a group rollout (``rlcs_shared_prefix_attn``, ``rlcs_sample``,
-``rlcs_token_logp``, ``rlcs_policy_loss``) document their own shapes.
+``rlcs_token_logp``, ``rlcs_policy_loss``) and those of speculative rollouts over a paged cache
+(``rlcs_paged_attn``, ``rlcs_paged_write``, ``rlcs_pages_...``, ``rlcs_verify_draft``,
+``rlcs_distill_loss``) document their own shapes.
 """
 from __future__ import annotations
 
@@ -37,6 +39,9 @@ __all__ = [
     "rlcs_workspace_size_masked", "rlcs_gae_masked_noalloc",
     "rlcs_token_logp", "rlcs_policy_loss", "rlcs_sample", "rlcs_workspace_size_sample",
     "rlcs_shared_prefix_attn", "rlcs_workspace_size_attn",
+    "rlcs_paged_attn", "rlcs_workspace_size_paged", "rlcs_paged_write",
+    "rlcs_pages_fork", "rlcs_pages_resize", "rlcs_pages_compact", "rlcs_pages_copy", "rlcs_workspace_size_pages",
+    "rlcs_verify_draft", "rlcs_workspace_size_verify", "rlcs_distill_loss",
 ]
 
 _fast = None  # the native functions, once loaded
@@ -915,3 +920,350 @@ def rlcs_shared_prefix_attn(q, kp, vp, ks=None, vs=None, prefix_len=None, suffix
               1.0 / max(D, 1) ** 0.5 if scale is None else scale, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
     _written(given)
     return o, lse
+
+
+# ---------------------------------------------------------------- a paged cache
+# A cache is [pages, page, Hkv, D]: pages of `page` tokens (a power of two from 16 to 65536). table int32
+# [B, W] holds the numbers of each sequence's pages in the order of its tokens (any number outside [0, pages) is no
+# page), length int32 [B] its tokens.
+
+def rlcs_workspace_size_paged(tokens: int, B: int, Hq: int, Hkv: int, D: int, max_chunk: int = 0) -> int:
+    return int(_native.load().rlcs_workspace_size_paged(*(int(x) for x in (tokens, B, Hq, Hkv, D, max_chunk))))
+
+
+def _vectors(name, t, dims, dtype, device):
+    if not isinstance(t, torch.Tensor) or t.dim() != dims:
+        raise ValueError(f"{name} must be a {dims}-D tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _paged(first, name, k_cache, v_cache, table, length, q_start, Hkv=None):
+    """What attention and writing check alike: (tokens, D, B, W, ld, pages, page, Hkv, dtype, device)."""
+    if not isinstance(first, torch.Tensor) or first.dim() != 3:
+        raise ValueError(f"{name} must be a [tokens, heads, D] tensor")
+    if first.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {first.dtype}")
+    if first.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    n, D, dt, dev = int(first.shape[0]), int(first.shape[2]), first.dtype, first.device
+    _vectors(name, first, 3, dt, dev)
+    _vectors("k_cache", k_cache, 4, dt, dev)
+    pages, page, heads = (int(x) for x in k_cache.shape[:3])
+    _vectors("v_cache", v_cache, 4, dt, dev)
+    if tuple(k_cache.shape) != (pages, page, heads, D) or tuple(v_cache.shape) != tuple(k_cache.shape):
+        raise ValueError(f"k_cache and v_cache have shapes {tuple(k_cache.shape)} and {tuple(v_cache.shape)}, expected [pages, page, Hkv, {D}]")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.dtype != torch.int32 or table.device != dev:
+        raise ValueError(f"table must be an int32 [B, W] tensor on {dev}")
+    B, W = int(table.shape[0]), int(table.shape[1])
+    ld = int(table.stride(0)) if B > 1 else W
+    if (W > 1 and table.stride(1) != 1) or ld < W:
+        raise ValueError("table must have contiguous rows that do not overlap")
+    _required(length=length)
+    _check_lead("length", length, (B,), torch.int32, dev)
+    _check_lead("q_start", q_start, (B + 1,), torch.int32, dev)
+    if q_start is None and (n % B if B else n):
+        raise ValueError(f"{name} has {n} tokens for {B} sequences: q_start says whose they are")
+    return n, D, B, W, ld, pages, page, heads, dt, dev
+
+
+def _paged_layout(**tensors):
+    at = _native.PagedLayout()
+    for name, t in tensors.items():
+        for i, x in enumerate(_attn_strides(t)):
+            getattr(at, name)[i] = x
+    return at
+
+
+def rlcs_paged_attn(q, k_cache, v_cache, table, length, q_start=None, o=None, lse=None, *, scale: Optional[float] = None,
+                    max_chunk: Optional[int] = None, ws=None, want_lse: bool = True):
+    """(o, lse): attention of every sequence's new tokens over its pages, each up to itself.
+
+    q [tokens, Hq, D]: the new tokens of all sequences, sequence b's rows q_start[b] to q_start[b + 1] - 1 (int32
+    [B + 1], not falling; None: as many for each sequence). They are the last of its length[b] tokens, and their keys and values
+    are in the cache already (rlcs_paged_write). k_cache, v_cache [pages, page, Hkv, D] of q's type: D contiguous, a
+    multiple of 8 up to 256, other strides any multiples of 16 bytes. table int32 [B, W], its rows any stride apart.
+    Hq is a multiple of Hkv. max_chunk: no sequence has more new tokens (fewer kernels and less workspace where that is little).
+    scale defaults to 1 / sqrt(D). o [tokens, Hq, D] of q's type, lse float32 [tokens, Hq]; rows of no sequence are left as
+    they are, a token that sees no key has 0 and -inf."""
+    done = (_fast or _load_fast()).paged_attn(q, k_cache, v_cache, table, length, q_start, o, lse, scale, max_chunk, want_lse, ws)
+    if done is not NotImplemented:
+        return done
+    n, D, B, W, ld, pages, page, Hkv, dt, dev = _paged(q, "q", k_cache, v_cache, table, length, q_start)
+    Hq = int(q.shape[1])
+    if D == 0 and n * Hq > 0:
+        raise ValueError("q must have heads of D >= 8 dimensions")
+    given = _given(o, lse)
+    o = _out_lead("o", o, (n, Hq, D), dt, dev)
+    lse = _out_lead("lse", lse, (n, Hq), torch.float32, dev, want_lse)
+    most = 0 if max_chunk is None else int(max_chunk)
+    if ws is None:
+        size = rlcs_workspace_size_paged(n, B, Hq, Hkv, D, most if q_start is not None or not B else n // B)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+    at = _paged_layout(q=q, k_cache=k_cache, v_cache=v_cache)
+    with _on(dev):
+        _call("rlcs_paged_attn", _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(table), _ptr(length), _ptr(q_start), _ptr(o), _ptr(lse), n, B, W, ld,
+              pages, page, Hq, Hkv, D, most, _native.ctypes.addressof(at), 1.0 / max(D, 1) ** 0.5 if scale is None else scale, _DTYPES[dt],
+              *_ws(ws, dev), _stream(dev))
+    _written(given)
+    return o, lse
+
+
+def rlcs_paged_write(k, v, k_cache, v_cache, table, length, q_start=None):
+    """The keys and values [tokens, Hkv, D] of every sequence's new tokens to their places in the cache, the last of its
+    length[b] tokens; q_start and the other arguments as in rlcs_paged_attn. Returns (k_cache, v_cache), which count as
+    modified in place."""
+    done = (_fast or _load_fast()).paged_write(k, v, k_cache, v_cache, table, length, q_start)
+    if done is not NotImplemented:
+        return done
+    n, D, B, W, ld, pages, page, Hkv, dt, dev = _paged(k, "k", k_cache, v_cache, table, length, q_start)
+    _vectors("v", v, 3, dt, dev)
+    if tuple(k.shape) != (n, Hkv, D) or tuple(v.shape) != (n, Hkv, D):
+        raise ValueError(f"k and v have shapes {tuple(k.shape)} and {tuple(v.shape)}, expected [tokens, {Hkv}, {D}]")
+    at = _paged_layout(k_new=k, v_new=v, k_cache=k_cache, v_cache=v_cache)
+    with _on(dev):
+        _call("rlcs_paged_write", _ptr(k), _ptr(v), _ptr(k_cache), _ptr(v_cache), _ptr(table), _ptr(length), _ptr(q_start), n, B, W, ld, pages, page,
+              Hkv, D, _native.ctypes.addressof(at), _DTYPES[dt], _stream(dev))
+    _written([k_cache, v_cache])
+    return k_cache, v_cache
+
+
+def rlcs_workspace_size_pages(B: int, pages: int) -> int:
+    return int(_native.load().rlcs_workspace_size_pages(int(B), int(pages)))
+
+
+def _pages(table, refs):
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be a [B, W] tensor")
+    if table.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    dev = table.device
+    _check_lead("table", table, tuple(table.shape), torch.int32, dev)
+    if not isinstance(refs, torch.Tensor) or refs.dim() != 1 or refs.numel() == 0:
+        raise ValueError("refs must be a [pages] tensor of at least one page")
+    _check_lead("refs", refs, tuple(refs.shape), torch.int32, dev)
+    return int(table.shape[0]), int(table.shape[1]), int(refs.shape[0]), dev
+
+
+def _pages_ws(ws, B, pages, device):
+    if ws is None:
+        ws = torch.empty(rlcs_workspace_size_pages(B, pages), dtype=torch.uint8, device=device)
+    return _ws(ws, device)
+
+
+def _some_sequences(table):
+    if table.numel() == 0:
+        raise ValueError(f"table has shape {tuple(table.shape)}: it must have a sequence and a column at least")
+
+
+def rlcs_pages_fork(table, length, refs, parent, table_out=None, length_out=None, refs_out=None, *, page: int, ws=None):
+    """(table, length, refs) after every sequence b became what sequence parent[b] was, sharing its pages; parent[b]
+    outside [0, B), or b: as it was. table int32 [B, W], length and parent int32 [B], refs int32 [pages]: how many entries
+    of the table hold each page (0: free). All contiguous. refs_out may be refs."""
+    done = (_fast or _load_fast()).pages_fork(table, length, refs, parent, table_out, length_out, refs_out, page, ws)
+    if done is not NotImplemented:
+        return done
+    B, W, pages, dev = _pages(table, refs)
+    _some_sequences(table)
+    _required(length=length, parent=parent)
+    _check_lead("length", length, (B,), torch.int32, dev); _check_lead("parent", parent, (B,), torch.int32, dev)
+    given = _given(table_out, length_out, refs_out)
+    table_out = _out_lead("table_out", table_out, (B, W), torch.int32, dev)
+    length_out = _out_lead("length_out", length_out, (B,), torch.int32, dev)
+    refs_out = _out_lead("refs_out", refs_out, (pages,), torch.int32, dev)
+    with _on(dev):
+        _call("rlcs_pages_fork", _ptr(table), _ptr(length), _ptr(refs), _ptr(parent), _ptr(table_out), _ptr(length_out), _ptr(refs_out), B, W, pages,
+              int(page), *_pages_ws(ws, B, pages, dev), _stream(dev))
+    _written(given)
+    return table_out, length_out, refs_out
+
+
+def rlcs_pages_resize(table, length, refs, new_length, table_out=None, length_out=None, refs_out=None, moves=None, *, page: int, ws=None):
+    """(table, length, refs, moves) after every sequence got new_length[b] tokens (below 0, or more than its row of
+    the table holds: as it was). Sequences that shrink give back pages; those that grow get the free pages with the
+    lowest numbers, in order. One that grows from within a shared page goes on in a copy of it: moves int32 [B, 2] is (that page, its copy) or
+    (-1, -1), for rlcs_pages_copy. One that there are not pages enough for stays as it was. Other arguments
+    as in rlcs_pages_fork; each of the first three outputs may be its input."""
+    done = (_fast or _load_fast()).pages_resize(table, length, refs, new_length, table_out, length_out, refs_out, moves, page, ws)
+    if done is not NotImplemented:
+        return done
+    B, W, pages, dev = _pages(table, refs)
+    _some_sequences(table)
+    _required(length=length, new_length=new_length)
+    _check_lead("length", length, (B,), torch.int32, dev); _check_lead("new_length", new_length, (B,), torch.int32, dev)
+    given = _given(table_out, length_out, refs_out, moves)
+    table_out = _out_lead("table_out", table_out, (B, W), torch.int32, dev)
+    length_out = _out_lead("length_out", length_out, (B,), torch.int32, dev)
+    refs_out = _out_lead("refs_out", refs_out, (pages,), torch.int32, dev)
+    moves = _out_lead("moves", moves, (B, 2), torch.int32, dev)
+    with _on(dev):
+        _call("rlcs_pages_resize", _ptr(table), _ptr(length), _ptr(refs), _ptr(new_length), _ptr(table_out), _ptr(length_out), _ptr(refs_out),
+              _ptr(moves), B, W, pages, int(page), *_pages_ws(ws, B, pages, dev), _stream(dev))
+    _written(given)
+    return table_out, length_out, refs_out, moves
+
+
+def rlcs_pages_compact(table, refs, table_out=None, refs_out=None, moves=None, count=None, *, ws=None):
+    """(table, refs, moves, count) after the pages in use moved to the front: count int32 [1] is how many there are, moves
+    int32 [pages // 2, 2] the (from, to) of those that move, in order, then (-1, -1), for rlcs_pages_copy. Entries of free pages become
+    -1. Outputs may be their inputs."""
+    done = (_fast or _load_fast()).pages_compact(table, refs, table_out, refs_out, moves, count, ws)
+    if done is not NotImplemented:
+        return done
+    B, W, pages, dev = _pages(table, refs)
+    given = _given(table_out, refs_out, moves, count)
+    table_out = _out_lead("table_out", table_out, (B, W), torch.int32, dev)
+    refs_out = _out_lead("refs_out", refs_out, (pages,), torch.int32, dev)
+    moves = _out_lead("moves", moves, (pages // 2, 2), torch.int32, dev)
+    count = _out_lead("count", count, (1,), torch.int32, dev)
+    with _on(dev):
+        _call("rlcs_pages_compact", _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(moves), _ptr(count), B, W, pages,
+              *_pages_ws(ws, B, pages, dev), _stream(dev))
+    _written(given)
+    return table_out, refs_out, moves, count
+
+
+def rlcs_pages_copy(cache, moves):
+    """Copies page moves[i, 0] onto page moves[i, 1] in every layer of cache [layers, pages, ...] (any type; a page's
+    contents contiguous, layers and pages any stride apart that keeps them apart). moves int32 [n, 2]; those with a number outside
+    [0, pages) are passed over. No page is the target of one move and in another. Returns the cache, which counts as modified in place."""
+    done = (_fast or _load_fast()).pages_copy(cache, moves)
+    if done is not NotImplemented:
+        return done
+    if not isinstance(cache, torch.Tensor) or cache.dim() < 3:
+        raise ValueError("cache must be a [layers, pages, ...] tensor of at least three dimensions")
+    if cache.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    dev, es = cache.device, cache.element_size()
+    if not isinstance(moves, torch.Tensor) or moves.dim() != 2 or int(moves.shape[1]) != 2:
+        raise ValueError("moves must be an [n, 2] tensor")
+    _check_lead("moves", moves, tuple(moves.shape), torch.int32, dev)
+    layers, pages = int(cache.shape[0]), int(cache.shape[1])
+    size = es
+    for n in cache.shape[2:]:
+        size *= int(n)
+    if cache.numel() and not cache[0, 0].is_contiguous():
+        raise ValueError("a page of cache must be contiguous")
+    with _on(dev):
+        _call("rlcs_pages_copy", _ptr(cache), _ptr(moves), int(moves.shape[0]), layers, pages, int(cache.stride(0)) * es if layers > 1 else 0,
+              int(cache.stride(1)) * es if pages > 1 else 0, size, _stream(dev))
+    _written([cache])
+    return cache
+
+
+# ---------------------------------------------------------------- drafted tokens
+
+def rlcs_workspace_size_verify(B: int, K: int, V: int) -> int:
+    return int(_native.load().rlcs_workspace_size_verify(int(B), int(K), int(V)))
+
+
+def _batch_rows(name, t, B, n, V, dtype, device):
+    """(sequence stride, row stride) of [B, n, V] logits with contiguous rows."""
+    if not isinstance(t, torch.Tensor) or tuple(t.shape) != (B, n, V):
+        raise ValueError(f"{name} must be a {[B, n, V]} tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if V > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return int(t.stride(0)), int(t.stride(1))
+
+
+def rlcs_verify_draft(target, draft, draft_tokens, u, noise, n_draft=None, tokens=None, count=None, logp=None, *, temperature=1.0,
+                      draft_temperature=None, want_logp: bool = True, ws=None):
+    """(tokens, count, logp): the drafted tokens that stand under the target policy, and one more token drawn from it.
+
+    target [B, K + 1, V] and draft [B, K, V] float32 / bfloat16 logits (rows contiguous, any strides between them; draft None:
+    each drafted token had all of the draft's mass); draft_tokens int32, u float32 [B, K] (uniform on [0, 1)); noise float32
+    [B, V] (exponential, rows any stride apart); n_draft int32 [B]: how many tokens each sequence drafted (default K).
+    Token x stands if u q(x) < p(x); where the first falls, one is drawn from max(p - q, 0), after the last from p. temperature and
+    draft_temperature (default: temperature) are numbers or float32 [B]; 0 takes the target's largest logit.
+    tokens int32 [B, K + 1] (then -1), count int32 [B], logp float32 [B, K + 1] (under the target, then 0)."""
+    if draft_temperature is None:
+        draft_temperature = temperature
+    done = (_fast or _load_fast()).verify_draft(target, draft, draft_tokens, u, noise, n_draft, tokens, count, logp, temperature, draft_temperature,
+                                                want_logp, ws)
+    if done is not NotImplemented:
+        return done
+    if not isinstance(target, torch.Tensor) or target.dim() != 3 or int(target.shape[1]) < 1:
+        raise ValueError("target must be a [B, K + 1, V] tensor")
+    if target.dtype not in _DTYPES:
+        raise TypeError(f"target must be float32 or bfloat16, got {target.dtype}")
+    if target.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    B, K, V, dt, dev = int(target.shape[0]), int(target.shape[1]) - 1, int(target.shape[2]), target.dtype, target.device
+    t_seq, t_ld = _batch_rows("target", target, B, K + 1, V, dt, dev)
+    d_seq, d_ld = _batch_rows("draft", draft, B, K, V, dt, dev) if draft is not None else (0, 0)
+    _required(draft_tokens=draft_tokens, u=u, noise=noise)
+    _check_lead("draft_tokens", draft_tokens, (B, K), torch.int32, dev)
+    _check_lead("u", u, (B, K), torch.float32, dev)
+    if not isinstance(noise, torch.Tensor) or noise.dtype != torch.float32 or noise.device != dev or tuple(noise.shape) != (B, V):
+        raise ValueError(f"noise must be a float32 {[B, V]} tensor on {dev}")
+    n_ld = _rows("noise", noise)[2]
+    _check_lead("n_draft", n_draft, (B,), torch.int32, dev)
+    tp, t = _setting("temperature", temperature, (B,), torch.float32, dev)
+    dp, d = _setting("draft_temperature", draft_temperature, (B,), torch.float32, dev)
+    given = _given(tokens, count, logp)
+    tokens = _out_lead("tokens", tokens, (B, K + 1), torch.int32, dev)
+    count = _out_lead("count", count, (B,), torch.int32, dev)
+    logp = _out_lead("logp", logp, (B, K + 1), torch.float32, dev, want_logp)
+    if ws is None:
+        n = rlcs_workspace_size_verify(B, K, V)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    with _on(dev):
+        _call("rlcs_verify_draft", _ptr(target), _ptr(draft), _ptr(draft_tokens), _ptr(u), _ptr(noise), _ptr(n_draft), tp, dp, _ptr(tokens),
+              _ptr(count), _ptr(logp), B, K, V, t_seq, t_ld, d_seq, d_ld, n_ld, t, d, _DTYPES[dt], *_ws(ws, dev), _stream(dev))
+    _written(given)
+    if V == 0:  # (no token stands and there is none to draw)
+        _fill(-1, tokens)
+        _fill(1, count)
+        _fill(0, logp)
+        if logp is not None:
+            logp[:, 0] = float("-inf")
+    return tokens, count, logp
+
+
+# ---------------------------------------------------------------- distillation
+
+def rlcs_distill_loss(logits, top_ids, top_logp, weight=None, loss=None, dlogits=None, *, temperature: float = 1.0, tail: bool = False,
+                      want_grad: bool = True):
+    """(loss, dlogits): the loss of each row of logits [..., V] against a teacher's K largest logits, sum t (log t - log p) with its weight,
+    and its gradient by the logits. top_ids int32 and top_logp float32 [..., K] (an id outside [0, V) is none), weight
+    float32 of the leading shape; a row of weight 0 is left out. With tail false the listed shares are made to add up to 1 (any
+    logits will do for top_logp); with tail true top_logp are log-probabilities, and what they leave of 1 is the mass of one
+    more class, everything that is not listed. `dlogits` may be `logits`.
+
+    Nothing here is recorded by autograd, as in rlcs_policy_loss: ``logits.backward(dlogits)`` carries the gradient on."""
+    done = (_fast or _load_fast()).distill_loss(logits, top_ids, top_logp, weight, loss, dlogits, temperature, tail, want_grad)
+    if done is not NotImplemented:
+        return done
+    M, V, ld, lead, dt, dev = _prep_logits(logits)
+    _required(top_ids=top_ids, top_logp=top_logp)
+    if not isinstance(top_ids, torch.Tensor) or top_ids.dim() != len(lead) + 1:
+        raise ValueError("top_ids must be a tensor of the logits' leading shape and K")
+    K = int(top_ids.shape[-1])
+    _check_lead("top_ids", top_ids, lead + (K,), torch.int32, dev)
+    _check_lead("top_logp", top_logp, lead + (K,), torch.float32, dev)
+    _check_lead("weight", weight, lead, torch.float32, dev)
+    given = _given(loss, dlogits)
+    loss = _out_lead("loss", loss, lead, torch.float32, dev)
+    ldg = V
+    if dlogits is not None:
+        if not isinstance(dlogits, torch.Tensor) or dlogits.dtype != dt or dlogits.device != dev \
+                or tuple(dlogits.shape) != tuple(logits.shape):
+            raise ValueError(f"dlogits must be a {dt} tensor of the logits' shape on {dev}")
+        ldg = _rows("dlogits", dlogits)[2]
+    elif want_grad:
+        dlogits = torch.empty(lead + (V,), dtype=dt, device=dev)
+    with _on(dev):
+        _call("rlcs_distill_loss", _ptr(logits), _ptr(top_ids), _ptr(top_logp), _ptr(weight), _ptr(loss), _ptr(dlogits), M, V, K, ld, ldg,
+              temperature, 1 if tail else 0, _DTYPES[dt], _stream(dev))
+    _written(given)
+    if V == 0:
+        _fill(0, loss)
+    return loss, dlogits

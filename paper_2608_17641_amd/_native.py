@@ -38,6 +38,11 @@ class AttnLayout(ctypes.Structure):
     _fields_ = [("q", _I64 * 3), ("kp", _I64 * 3), ("vp", _I64 * 3), ("ks", _I64 * 4), ("vs", _I64 * 4)]
 
 
+class PagedLayout(ctypes.Structure):
+    """rlcs_paged_layout: strides in elements."""
+    _fields_ = [("q", _I64 * 2), ("k_new", _I64 * 2), ("v_new", _I64 * 2), ("k_cache", _I64 * 3), ("v_cache", _I64 * 3)]
+
+
 # name -> argtypes, in the order of include/rlcs.h
 PROTOTYPES = {
     "rlcs_gae": [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _F, _F, _INT, _P, _SZ, _P],
@@ -81,6 +86,20 @@ PROTOTYPES = {
     "rlcs_shared_prefix_attn": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64,
                                 _I64, _P, _F, _INT, _P, _SZ, _P],
     "rlcs_workspace_size_attn": [_I64, _I64, _I64, _I64, _I64, _I64, _I64],
+    "rlcs_paged_attn": [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64,
+                        _I64, _P, _F, _INT, _P, _SZ, _P],
+    "rlcs_workspace_size_paged": [_I64, _I64, _I64, _I64, _I64, _I64],
+    "rlcs_paged_write": [_P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _P, _INT,
+                         _P],
+    "rlcs_pages_fork": [_P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _P, _SZ, _P],
+    "rlcs_pages_resize": [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _P, _SZ, _P],
+    "rlcs_pages_compact": [_P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _P, _SZ, _P],
+    "rlcs_workspace_size_pages": [_I64, _I64],
+    "rlcs_pages_copy": [_P, _P, _I64, _I64, _I64, _I64, _I64, _I64, _P],
+    "rlcs_verify_draft": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64, _I64,
+                          _I64, _F, _F, _INT, _P, _SZ, _P],
+    "rlcs_workspace_size_verify": [_I64, _I64, _I64],
+    "rlcs_distill_loss": [_P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _F, _INT, _INT, _P],
     "rlcs_status_string": [_INT],
     "rlcs_version": [],
     "rlcs_testing_set_variant": [_INT],
@@ -88,7 +107,8 @@ PROTOTYPES = {
 }
 RESTYPES = {"rlcs_workspace_size": _SZ, "rlcs_workspace_size_columns": _SZ,
             "rlcs_workspace_size_masked": _SZ, "rlcs_workspace_size_sample": _SZ,
-            "rlcs_workspace_size_attn": _SZ,
+            "rlcs_workspace_size_attn": _SZ, "rlcs_workspace_size_paged": _SZ,
+            "rlcs_workspace_size_pages": _SZ, "rlcs_workspace_size_verify": _SZ,
             "rlcs_status_string": ctypes.c_char_p}
 
 _lib = None

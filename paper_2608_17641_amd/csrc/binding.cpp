@@ -59,6 +59,17 @@ struct Library {
     decltype(&rlcs_workspace_size_sample) workspace_size_sample;
     decltype(&rlcs_shared_prefix_attn) shared_prefix_attn;
     decltype(&rlcs_workspace_size_attn) workspace_size_attn;
+    decltype(&rlcs_paged_attn) paged_attn;
+    decltype(&rlcs_workspace_size_paged) workspace_size_paged;
+    decltype(&rlcs_paged_write) paged_write;
+    decltype(&rlcs_pages_fork) pages_fork;
+    decltype(&rlcs_pages_resize) pages_resize;
+    decltype(&rlcs_pages_compact) pages_compact;
+    decltype(&rlcs_workspace_size_pages) workspace_size_pages;
+    decltype(&rlcs_pages_copy) pages_copy;
+    decltype(&rlcs_verify_draft) verify_draft;
+    decltype(&rlcs_workspace_size_verify) workspace_size_verify;
+    decltype(&rlcs_distill_loss) distill_loss;
 } g_lib;
 bool g_bound = false;
 
@@ -196,6 +207,15 @@ struct Call {
         }
         ok = false;
         return 0.f;
+    }
+    int64_t integer(PyObject* o) {
+        if (PyLong_CheckExact(o)) {
+            int over = 0;
+            const long long v = PyLong_AsLongLongAndOverflow(o, &over);
+            if (!over) return v;
+        }
+        ok = false;
+        return 0;
     }
     bool truth(PyObject* o) {
         if (o != Py_True && o != Py_False) ok = false;
@@ -733,6 +753,264 @@ PyObject* shared_prefix_attn(Argv x, Py_ssize_t nargs) {
     });
 }
 
+// ------------------------------------------------------------- a paged cache, drafted tokens, distillation
+
+// A tensor that is not the call's first input, contiguous in its last dimension; its other strides go to `strides`.
+void* rows_of(Call& c, PyObject* o, at::IntArrayRef sizes, int64_t* strides) {
+    const at::Tensor* t = c.plain(o);
+    c.ok = c.ok && t && t->scalar_type() == c.dtype && t->device() == c.device && t->sizes() == sizes &&
+           (sizes.back() <= 1 || t->stride(-1) == 1);
+    if (!c.ok) return nullptr;
+    for (size_t i = 0; i + 1 < sizes.size(); ++i) strides[i] = sizes[i] <= 1 ? 0 : t->stride(int64_t(i));
+    return t->data_ptr();
+}
+int32_t* ints(Call& c, PyObject* o, at::IntArrayRef sizes) { return static_cast<int32_t*>(c.checked(o, at::kInt, sizes, false)); }
+
+// What a call changes in place.
+struct InPlace : Result {
+    InPlace(Call& c, PyObject* o, void* p) : Result(c, Py_None, false, c.dtype, {}) {
+        given = o;
+        ptr = p;
+    }
+};
+
+// Cache, table and sequences of the calls on a paged cache; `first` is [tokens, heads, D].
+struct Paged {
+    int64_t n = 0, heads = 0, D = 0, B = 0, W = 0, ld = 0, pages = 0, page = 0, Hkv = 0;
+    void *k = nullptr, *v = nullptr;
+    const int32_t *table = nullptr, *length = nullptr, *start = nullptr;
+    rlcs_paged_layout at{};
+
+    void of(Call& c, PyObject* first, PyObject* k_cache, PyObject* v_cache, PyObject* t, PyObject* len, PyObject* q_start) {
+        const at::Tensor *f = c.plain(first), *kc = c.plain(k_cache), *tb = c.plain(t);
+        c.ok = c.ok && f && kc && tb && len != Py_None && f->dim() == 3 && kc->dim() == 4 && tb->dim() == 2;
+        if (!c.ok) return;
+        c.dtype = f->scalar_type();
+        c.device = f->device();
+        n = f->size(0); heads = f->size(1); D = f->size(2);
+        pages = kc->size(0); page = kc->size(1); Hkv = kc->size(2);
+        B = tb->size(0); W = tb->size(1);
+        ld = B > 1 ? tb->stride(0) : W;
+        c.ok = (c.dtype == at::kFloat || c.dtype == at::kBFloat16) && c.device.is_cuda() && c.device.index() == c10::hip::current_device() && D > 0 &&
+               B > 0 && tb->scalar_type() == at::kInt && tb->device() == c.device && (W <= 1 || tb->stride(1) == 1) && ld >= W;
+        if (!c.ok) return;
+        k = rows_of(c, k_cache, {pages, page, Hkv, D}, at.k_cache);
+        v = rows_of(c, v_cache, {pages, page, Hkv, D}, at.v_cache);
+        table = static_cast<const int32_t*>(tb->data_ptr());
+        length = ints(c, len, {B});
+        start = ints(c, q_start, {B + 1});
+        c.ok = c.ok && (start || n % B == 0);
+    }
+};
+
+// paged_attn(q, k_cache, v_cache, table, length, q_start, o, lse, scale, max_chunk, want_lse, ws)
+PyObject* paged_attn(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(12);
+    Call c(false);
+    Paged p;
+    p.of(c, x[0], x[1], x[2], x[3], x[4], x[5]);
+    if (!c.ok) Py_RETURN_NOTIMPLEMENTED;
+    const void* q = rows_of(c, x[0], {p.n, p.heads, p.D}, p.at.q);
+    Result o(c, x[6], true, c.dtype, {p.n, p.heads, p.D}), lse(c, x[7], c.truth(x[10]), at::kFloat, {p.n, p.heads});
+    const float scale = x[8] == Py_None ? float(1.0 / std::sqrt(double(p.D))) : c.number(x[8]);
+    const int64_t most = x[9] == Py_None ? 0 : c.integer(x[9]);
+    size_t wb = 0;
+    void* ws = c.workspace(x[11], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_paged(p.n, p.B, p.heads, p.Hkv, p.D, p.start ? most : p.n / p.B) : 0;
+    return run_results(c, "rlcs_paged_attn", {&o, &lse}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.paged_attn(q, p.k, p.v, p.table, p.length, p.start, o.ptr, lse.f32(), p.n, p.B, p.W, p.ld, p.pages, p.page, p.heads, p.Hkv, p.D, most,
+                                &p.at, scale, c.type(), made ? made : ws, made ? make : wb, s);
+    });
+}
+
+// paged_write(k, v, k_cache, v_cache, table, length, q_start)
+PyObject* paged_write(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(7);
+    Call c(false);
+    Paged p;
+    p.of(c, x[0], x[2], x[3], x[4], x[5], x[6]);
+    if (!c.ok || p.heads != p.Hkv) Py_RETURN_NOTIMPLEMENTED;
+    const void *k = rows_of(c, x[0], {p.n, p.Hkv, p.D}, p.at.k_new), *v = rows_of(c, x[1], {p.n, p.Hkv, p.D}, p.at.v_new);
+    InPlace to_k(c, x[2], p.k), to_v(c, x[3], p.v);
+    return run_results(c, "rlcs_paged_write", {&to_k, &to_v}, 0, [&](rlcs_stream_t s, void*) {
+        return g_lib.paged_write(k, v, p.k, p.v, p.table, p.length, p.start, p.n, p.B, p.W, p.ld, p.pages, p.page, p.Hkv, p.D, &p.at, c.type(), s);
+    });
+}
+
+// Table and references of the calls on pages.
+struct Pages {
+    int64_t B = 0, W = 0, pages = 0;
+    const int32_t *table = nullptr, *refs = nullptr;
+
+    Pages(Call& c, PyObject* t, PyObject* r) {
+        const at::Tensor *tb = c.plain(t), *rf = c.plain(r);
+        c.ok = c.ok && tb && rf && tb->dim() == 2 && rf->dim() == 1 && tb->device().is_cuda() && tb->device().index() == c10::hip::current_device();
+        if (!c.ok) return;
+        c.device = tb->device();
+        B = tb->size(0); W = tb->size(1); pages = rf->size(0);
+        c.ok = B > 0 && W > 0 && pages > 0;
+        table = ints(c, t, {B, W});
+        refs = ints(c, r, {pages});
+    }
+};
+
+// pages_fork(table, length, refs, parent, table_out, length_out, refs_out, page, ws)
+PyObject* pages_fork(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(9);
+    if (x[1] == Py_None || x[3] == Py_None) Py_RETURN_NOTIMPLEMENTED;
+    Call c(false);
+    const Pages p(c, x[0], x[2]);
+    const int32_t *length = ints(c, x[1], {p.B}), *parent = ints(c, x[3], {p.B});
+    Result table(c, x[4], true, at::kInt, {p.B, p.W}), out(c, x[5], true, at::kInt, {p.B}), refs(c, x[6], true, at::kInt, {p.pages});
+    const int64_t page = c.integer(x[7]);
+    size_t wb = 0;
+    void* ws = c.workspace(x[8], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_pages(p.B, p.pages) : 0;
+    return run_results(c, "rlcs_pages_fork", {&table, &out, &refs}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.pages_fork(p.table, length, p.refs, parent, static_cast<int32_t*>(table.ptr), static_cast<int32_t*>(out.ptr),
+                                static_cast<int32_t*>(refs.ptr), p.B, p.W, p.pages, page, made ? made : ws, made ? make : wb, s);
+    });
+}
+
+// pages_resize(table, length, refs, new_length, table_out, length_out, refs_out, moves, page, ws)
+PyObject* pages_resize(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(10);
+    if (x[1] == Py_None || x[3] == Py_None) Py_RETURN_NOTIMPLEMENTED;
+    Call c(false);
+    const Pages p(c, x[0], x[2]);
+    const int32_t *length = ints(c, x[1], {p.B}), *wanted = ints(c, x[3], {p.B});
+    Result table(c, x[4], true, at::kInt, {p.B, p.W}), out(c, x[5], true, at::kInt, {p.B}), refs(c, x[6], true, at::kInt, {p.pages});
+    Result moves(c, x[7], true, at::kInt, {p.B, 2});
+    const int64_t page = c.integer(x[8]);
+    size_t wb = 0;
+    void* ws = c.workspace(x[9], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_pages(p.B, p.pages) : 0;
+    return run_results(c, "rlcs_pages_resize", {&table, &out, &refs, &moves}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.pages_resize(p.table, length, p.refs, wanted, static_cast<int32_t*>(table.ptr), static_cast<int32_t*>(out.ptr),
+                                  static_cast<int32_t*>(refs.ptr), static_cast<int32_t*>(moves.ptr), p.B, p.W, p.pages, page, made ? made : ws,
+                                  made ? make : wb, s);
+    });
+}
+
+// pages_compact(table, refs, table_out, refs_out, moves, count, ws)
+PyObject* pages_compact(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(7);
+    Call c(false);
+    const Pages p(c, x[0], x[1]);
+    Result table(c, x[2], true, at::kInt, {p.B, p.W}), refs(c, x[3], true, at::kInt, {p.pages}), moves(c, x[4], true, at::kInt, {p.pages / 2, 2});
+    Result count(c, x[5], true, at::kInt, {1});
+    size_t wb = 0;
+    void* ws = c.workspace(x[6], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_pages(p.B, p.pages) : 0;
+    return run_results(c, "rlcs_pages_compact", {&table, &refs, &moves, &count}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.pages_compact(p.table, p.refs, static_cast<int32_t*>(table.ptr), static_cast<int32_t*>(refs.ptr), static_cast<int32_t*>(moves.ptr),
+                                   static_cast<int32_t*>(count.ptr), p.B, p.W, p.pages, made ? made : ws, made ? make : wb, s);
+    });
+}
+
+// pages_copy(cache, moves)
+PyObject* pages_copy(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(2);
+    Call c(false);
+    const at::Tensor *t = c.plain(x[0]), *m = c.plain(x[1]);
+    if (!c.ok || !t || !m || t->dim() < 3 || m->dim() != 2 || !t->device().is_cuda() || t->device().index() != c10::hip::current_device())
+        Py_RETURN_NOTIMPLEMENTED;
+    c.device = t->device();
+    const int64_t es = t->element_size(), layers = t->size(0), pages = t->size(1), n = m->size(0);
+    int64_t size = es;
+    for (int64_t i = t->dim() - 1; i >= 2; --i) {  // a page's contents are contiguous
+        c.ok = c.ok && (t->size(i) <= 1 || t->stride(i) * es == size);
+        size *= t->size(i);
+    }
+    if (t->numel() == 0) Py_RETURN_NOTIMPLEMENTED;
+    const int32_t* moves = ints(c, x[1], {n, 2});
+    if (!c.ok) Py_RETURN_NOTIMPLEMENTED;
+    InPlace cache(c, x[0], t->data_ptr());
+    PyObject* one = run_results(c, "rlcs_pages_copy", {&cache}, 0, [&](rlcs_stream_t s, void*) {
+        return g_lib.pages_copy(cache.ptr, moves, n, layers, pages, layers > 1 ? t->stride(0) * es : 0, pages > 1 ? t->stride(1) * es : 0, size, s);
+    });
+    if (!one || one == Py_NotImplemented) return one;
+    PyObject* o = PyTuple_GET_ITEM(one, 0);
+    Py_INCREF(o);
+    Py_DECREF(one);
+    return o;
+}
+
+// verify_draft(target, draft, draft_tokens, u, noise, n_draft, tokens, count, logp, temperature, draft_temperature, want_logp, ws)
+PyObject* verify_draft(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(13);
+    if (x[2] == Py_None || x[3] == Py_None || x[4] == Py_None) Py_RETURN_NOTIMPLEMENTED;
+    Call c(false);
+    const at::Tensor* t = c.plain(x[0]);
+    if (!c.ok || !t || t->dim() != 3 || t->size(1) < 1 || t->size(2) < 1) Py_RETURN_NOTIMPLEMENTED;
+    c.dtype = t->scalar_type();
+    c.device = t->device();
+    c.ok = (c.dtype == at::kFloat || c.dtype == at::kBFloat16) && c.device.is_cuda() && c.device.index() == c10::hip::current_device();
+    const int64_t B = t->size(0), K = t->size(1) - 1, V = t->size(2);
+    int64_t ts[2] = {}, ds[2] = {}, ns = 0;
+    auto operand = [&](PyObject* o, int64_t rows, int64_t* s) -> const void* {
+        const at::Tensor* r = c.plain(o);
+        if (!r) return nullptr;
+        c.ok = c.ok && r->scalar_type() == c.dtype && r->device() == c.device && r->sizes() == at::IntArrayRef({B, rows, V}) && (V <= 1 || r->stride(2) == 1);
+        if (!c.ok) return nullptr;
+        s[0] = r->stride(0);
+        s[1] = r->stride(1);
+        return r->data_ptr();
+    };
+    const void *target = operand(x[0], K + 1, ts), *draft = operand(x[1], K, ds);
+    const int32_t* drawn = ints(c, x[2], {B, K});
+    const float* u = static_cast<float*>(c.checked(x[3], at::kFloat, {B, K}, false));
+    Rows like;
+    like.V = V;
+    like.lead = {B};
+    const float* noise = static_cast<float*>(rows_beside(c, x[4], at::kFloat, like, ns));
+    const int32_t* n_draft = ints(c, x[5], {B});
+    Result tokens(c, x[6], true, at::kInt, {B, K + 1}), count(c, x[7], true, at::kInt, {B}), logp(c, x[8], c.truth(x[11]), at::kFloat, {B, K + 1});
+    float all[2] = {0.f, 0.f};
+    const float* own[2] = {nullptr, nullptr};
+    for (int i = 0; i < 2; ++i) {
+        if (THPVariable_CheckExact(x[9 + i])) own[i] = static_cast<float*>(c.checked(x[9 + i], at::kFloat, {B}, false));
+        else all[i] = c.number(x[9 + i]);
+    }
+    size_t wb = 0;
+    void* ws = c.workspace(x[12], wb);
+    const size_t make = c.ok && !ws ? g_lib.workspace_size_verify(B, K, V) : 0;
+    return run_results(c, "rlcs_verify_draft", {&tokens, &count, &logp}, make, [&](rlcs_stream_t s, void* made) {
+        return g_lib.verify_draft(target, draft, drawn, u, noise, n_draft, own[0], own[1], static_cast<int32_t*>(tokens.ptr),
+                                  static_cast<int32_t*>(count.ptr), logp.f32(), B, K, V, ts[0], ts[1], ds[0], ds[1], ns, all[0], all[1], c.type(),
+                                  made ? made : ws, made ? make : wb, s);
+    });
+}
+
+// distill_loss(logits, top_ids, top_logp, weight, loss, dlogits, temperature, tail, want_grad)
+PyObject* distill_loss(Argv x, Py_ssize_t nargs) {
+    RLCS_ARGS(9);
+    if (x[1] == Py_None || x[2] == Py_None) Py_RETURN_NOTIMPLEMENTED;
+    Call c(false);
+    Rows r;
+    void* logits = rows_input(c, x[0], r);
+    const at::Tensor* t = c.plain(x[1]);
+    if (!c.ok || !t || t->dim() != int64_t(r.lead.size()) + 1) Py_RETURN_NOTIMPLEMENTED;
+    std::vector<int64_t> listed = r.lead, full = r.lead;
+    listed.push_back(t->size(-1));
+    full.push_back(r.V);
+    const int32_t* ids = ints(c, x[1], listed);
+    const float* top = static_cast<float*>(c.checked(x[2], at::kFloat, listed, false));
+    const float* weight = static_cast<float*>(c.checked(x[3], at::kFloat, r.lead, false));
+    Result loss(c, x[4], true, at::kFloat, r.lead), grad(c, Py_None, c.truth(x[8]), c.dtype, full);
+    int64_t ld_grad = r.V;
+    if (x[5] != Py_None) {  // rows of its own stride
+        grad.make = false;
+        grad.given = x[5];
+        grad.ptr = rows_beside(c, x[5], c.dtype, r, ld_grad);
+    }
+    const float temperature = c.number(x[6]);
+    const int tail = c.truth(x[7]) ? 1 : 0;
+    return run_results(c, "rlcs_distill_loss", {&loss, &grad}, 0, [&](rlcs_stream_t s, void*) {
+        return g_lib.distill_loss(logits, ids, top, weight, loss.f32(), grad.ptr, r.M, r.V, listed.back(), r.ld, ld_grad, temperature, tail, c.type(), s);
+    });
+}
+
 // bind(handle, error, device): the dlopen handle of librlcs.so, the exception class of its status
 // codes and the class of torch's default-device mode
 PyObject* bind(PyObject*, PyObject* args) {
@@ -770,6 +1048,17 @@ PyObject* bind(PyObject*, PyObject* args) {
     get(g_lib.workspace_size_sample, "rlcs_workspace_size_sample");
     get(g_lib.shared_prefix_attn, "rlcs_shared_prefix_attn");
     get(g_lib.workspace_size_attn, "rlcs_workspace_size_attn");
+    get(g_lib.paged_attn, "rlcs_paged_attn");
+    get(g_lib.workspace_size_paged, "rlcs_workspace_size_paged");
+    get(g_lib.paged_write, "rlcs_paged_write");
+    get(g_lib.pages_fork, "rlcs_pages_fork");
+    get(g_lib.pages_resize, "rlcs_pages_resize");
+    get(g_lib.pages_compact, "rlcs_pages_compact");
+    get(g_lib.workspace_size_pages, "rlcs_workspace_size_pages");
+    get(g_lib.pages_copy, "rlcs_pages_copy");
+    get(g_lib.verify_draft, "rlcs_verify_draft");
+    get(g_lib.workspace_size_verify, "rlcs_workspace_size_verify");
+    get(g_lib.distill_loss, "rlcs_distill_loss");
     if (!all) {
         PyErr_SetString(PyExc_RuntimeError, "librlcs.so lacks a function of the binding");
         return nullptr;
@@ -799,7 +1088,9 @@ PyMethodDef g_methods[] = {
     fast<episodic_prefix<false>>("episodic_prefix"), fast<episodic_prefix<true>>("episodic_prefix_strided"),
     fast<affine_scan>("affine_scan"), fast<elig_trace_vec>("elig_trace_vec"), fast<gae_masked>("gae_masked"),
     fast<token_logp>("token_logp"), fast<policy_loss>("policy_loss"), fast<sample>("sample"),
-    fast<shared_prefix_attn>("shared_prefix_attn"),
+    fast<shared_prefix_attn>("shared_prefix_attn"), fast<paged_attn>("paged_attn"), fast<paged_write>("paged_write"),
+    fast<pages_fork>("pages_fork"), fast<pages_resize>("pages_resize"), fast<pages_compact>("pages_compact"),
+    fast<pages_copy>("pages_copy"), fast<verify_draft>("verify_draft"), fast<distill_loss>("distill_loss"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,402 @@
+// Distillation from a teacher's largest logits: the loss of each row and its gradient by the logits.
+//
+// With u = (x - max x) * log2(e) / temperature and z = sum 2^u, log p_j = ln 2 (u_j - log2 z). The gradient is
+// p_j - t_j at the K listed tokens and p_j times one factor a row everywhere else: a row is written as if nothing
+// were listed, then the listed places again. What lies outside the list is summed apart, by a bit for each logit in LDS
+// (as the difference of two sums it would be lost where the list has almost all of the mass).
+#pragma once
+
+#include "rlcs_softmax.h"
+
+namespace rlcs {
+
+constexpr int kMaxListed = 1024;
+constexpr int64_t kBits = 1 << 18;  // logits whose bits are in LDS at a time
+
+struct DistillArgs {
+    const void* logits;
+    const int32_t* ids;
+    const float *top, *weight;
+    float* loss;
+    void* grad;
+    int64_t M, V, ld, ld_grad;
+    int32_t K, words;  // words: of a row's bits, a multiple of 4
+    float inv_temp;
+};
+
+// LDS of a row: its bits, and the listed tokens: id (-1: none), logit, share t, and log t.
+struct DistillLds {
+    uint32_t* bits;
+    int32_t* id;
+    float *x, *t, *lt;
+    __device__ __forceinline__ DistillLds(char* mem, const DistillArgs& a) {
+        bits = reinterpret_cast<uint32_t*>(mem);
+        id = reinterpret_cast<int32_t*>(bits + a.words);
+        x = reinterpret_cast<float*>(id + a.K);
+        t = x + a.K;
+        lt = t + a.K;
+    }
+};
+inline size_t distill_lds(const DistillArgs& a) { return (size_t(a.words) * 4 + size_t(a.K) * 16 + 15) / 16 * 16; }
+
+// The lanes of a row: W waves of a workgroup, or with W = 1 a wave of a workgroup of four.
+template <int W>
+struct Team {
+    static constexpr int kLanes = W * kWave;
+    float* slots;  // W words, unused with W = 1
+    int lane;
+    __device__ __forceinline__ void sync() const {
+        if constexpr (W == 1) wave_lds_sync();
+        else __syncthreads();
+    }
+    // Stores of any lane before it come before stores of any lane after it.
+    __device__ __forceinline__ void order_stores() const {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        if constexpr (W > 1) __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    }
+    template <class F>
+    __device__ __forceinline__ float fold(float v, F&& f) const {
+        if constexpr (W > 1) {
+            __syncthreads();
+            if ((lane & 63) == 0) slots[lane >> 6] = v;
+            __syncthreads();
+            v = slots[0];
+#pragma unroll
+            for (int i = 1; i < W; ++i) v = f(v, slots[i]);
+        }
+        return v;
+    }
+    __device__ __forceinline__ float sum(float v) const {
+        return fold(sum_wave(v), [](float x, float y) { return x + y; });
+    }
+    __device__ __forceinline__ float max(float v) const {
+        return fold(max_wave(v), [](float x, float y) { return fmaxf(x, y); });
+    }
+    __device__ __forceinline__ bool any(bool b) const { return max(__any(b) ? 1.f : 0.f) > 0.f; }
+};
+
+// What a row's list says.
+struct Listed {
+    bool some;   // a share is not 0
+    bool twice;  // a token may be listed twice
+    float rest;  // the mass that the list leaves (TAIL)
+};
+
+__device__ __forceinline__ void mark(uint32_t* bits, int64_t id, bool& twice) {
+    const uint32_t at = uint32_t(id) & uint32_t(kBits - 1), bit = 1u << (at & 31);
+    twice |= (atomicOr(&bits[at >> 5], bit) & bit) != 0;
+}
+
+template <typename DT, bool TAIL, int W>
+__device__ __forceinline__ Listed read_list(const DistillArgs& a, const DistillLds& l, const Team<W>& team, int64_t row) {
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
+    for (int i = team.lane; i < a.words; i += Team<W>::kLanes) l.bits[i] = 0;
+    team.sync();
+    bool some = false, twice = false;
+    float top = kNegInf;
+    for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+        const int32_t id = a.ids[row * a.K + k];
+        const bool is = id >= 0 && id < a.V;
+        const float lt = is ? a.top[row * a.K + k] : kNegInf;
+        l.id[k] = is ? id : -1;
+        l.x[k] = is ? widen(x[id]) : 0.f;
+        l.lt[k] = lt;
+        if (is) mark(l.bits, id, twice);
+        some |= !(lt == kNegInf);  // (NaN is some)
+        top = fmaxf(top, lt);
+    }
+    Listed r{team.any(some), team.any(twice), 0.f};
+    if constexpr (TAIL) {
+        // (in 64 bits: what is left of 1 may be small)
+        double sum = 0.;
+        for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+            const double t = exp(double(l.lt[k]));
+            l.t[k] = float(t);
+            sum += t;
+        }
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
+        // as two floats over the waves: the sum's high part, and what it leaves out
+        const float high = float(sum), low = float(sum - double(high));
+        double left = 1.;
+        if constexpr (W > 1) {
+            __syncthreads();
+            if ((team.lane & 63) == 0) {
+                team.slots[team.lane >> 6] = high;
+                team.slots[W + (team.lane >> 6)] = low;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < W; ++i) left -= double(team.slots[i]) + double(team.slots[W + i]);
+        } else {
+            left -= sum;
+        }
+        r.rest = left < 0. ? 0.f : float(left);
+    } else {
+        top = team.max(top);
+        float sum = 0.f;
+        for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+            const float t = l.lt[k] == kNegInf ? 0.f : exp2_fast((l.lt[k] - top) * kLog2e);
+            l.t[k] = t;
+            sum += t;
+        }
+        sum = team.sum(sum);
+        const float log_sum = kLn2 * log2_fast(sum), inv = 1.f / sum;
+        for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+            l.t[k] *= inv;
+            l.lt[k] = l.lt[k] - top - log_sum;
+        }
+    }
+    team.sync();
+    return r;
+}
+
+// A row once its sums are known: weights' scale, log2 of their sum, what a logit that is not listed has as its gradient's factor.
+struct DistillRow {
+    Above sc;
+    float l2z, factor, amount;
+    bool some;  // a logit is not masked
+    __device__ __forceinline__ float probability(float x) const {
+        return some ? exp2_fast(__builtin_elementwise_maximum(fmaf(x - sc.top, sc.c, -l2z), kLog2Zero)) : 0.f;
+    }
+};
+
+// The row's loss, by all lanes; z: sums of the weights outside the list and in it.
+template <bool TAIL, int W>
+__device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const DistillLds& l, const Team<W>& team, const Listed& list, Above sc,
+                                               float z_out, float z_in, float w, int64_t row) {
+    DistillRow r;
+    const float z = TAIL ? z_out + z_in : z_out;
+    r.sc = sc;
+    r.some = !(z == 0.f);  // (NaN is some)
+    r.l2z = r.some ? log2_fast(z) : 0.f;
+    r.amount = w * a.inv_temp;
+    r.factor = r.amount;
+    float loss = 0.f;
+    for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+        // (not by way of the base 2: 1.44 times a finite mask of the type's lowest value overflows)
+        const float t = l.t[k], lp = r.some ? fmaf(l.x[k] - sc.top, a.inv_temp, -kLn2 * r.l2z) : kNegInf;
+        if (!(t == 0.f)) loss = fmaf(t, l.lt[k] - lp, loss);
+    }
+    loss = team.sum(loss);
+    if constexpr (TAIL) {
+        const float p = z_out / z;
+        if (!(list.rest == 0.f) && !(z_out == 0.f)) {
+            loss = fmaf(list.rest, kLn2 * (log2_fast(list.rest) - log2_fast(p)), loss);
+            r.factor = r.amount * (1.f - list.rest / p);
+        }
+    }
+    if (team.lane == 0) a.loss[row] = w * loss;
+    return r;
+}
+
+// The listed places of the gradient, once everything else of the row is written.
+template <typename DT, int W>
+__device__ __forceinline__ void listed_gradient(const DistillArgs& a, const DistillLds& l, const Team<W>& team, const Listed& list, const DistillRow& r,
+                                                DT* g) {
+    team.order_stores();
+    for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+        const int32_t id = l.id[k];
+        if (id < 0) continue;
+        float t = l.t[k];
+        if (list.twice) {  // the first of a token's places writes the sum of its shares
+            bool first = true;
+            t = 0.f;
+            for (int j = 0; j < a.K; ++j) {
+                if (l.id[j] != id) continue;
+                first = first && j >= k;
+                t += l.t[j];
+            }
+            if (!first) continue;
+        }
+        g[id] = narrow(r.amount * (r.probability(l.x[k]) - t), DT{});
+    }
+}
+
+template <typename DT, int L>
+__device__ __forceinline__ void zero_row(DT* g, int64_t V, int lane) {
+    constexpr int K = RowVec<DT>::K;
+    const float zero[K] = {};
+    const int64_t vecs = (V + K - 1) / K;
+    for (int64_t i = lane; i < vecs; i += L) store_row_vec<DT>(g, i, V, zero);
+}
+
+// Bits of the logits of vector i.
+template <int K>
+__device__ __forceinline__ uint32_t vector_bits(const uint32_t* bits, int64_t i) {
+    if constexpr (K == 8) return reinterpret_cast<const uint8_t*>(bits)[i];
+    else return reinterpret_cast<const uint8_t*>(bits)[i >> 1] >> (4 * (i & 1)) & 15u;
+}
+
+// A vector's weights, added to what they belong to.
+template <bool TAIL, class V>
+__device__ __forceinline__ void add_weights(const V& v, const Above& sc, uint32_t bits, float& z_out, float& z_in) {
+    float e[V::K];
+#pragma unroll
+    for (int k = 0; k < V::K; ++k) e[k] = exp2_fast(__builtin_elementwise_maximum(sc.log2_weight(v.at(k)), kLog2Zero));
+    if (TAIL && bits) {
+#pragma unroll
+        for (int k = 0; k < V::K; ++k) {
+            const bool in = bits >> k & 1;
+            z_out += in ? 0.f : e[k];
+            z_in += in ? e[k] : 0.f;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V::K; ++k) z_out += e[k];
+    }
+}
+
+// Rows of up to U vectors a lane of W waves, which stay in registers. Every logit is read and every gradient
+// written once. Bound by memory.
+template <typename DT, bool TAIL, int W, int U>
+__global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(DistillArgs a, int row_lds) {
+    extern __shared__ __attribute__((aligned(16))) char s_mem[];
+    __shared__ float s_slots[2 * W];
+    constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = W == 1 ? grid_row() * 4 + wave : grid_row();
+    if (row >= a.M) return;
+    const Team<W> team{s_slots, W == 1 ? int(threadIdx.x) & 63 : int(threadIdx.x)};
+    const DistillLds l(s_mem + (W == 1 ? wave * row_lds : 0), a);
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
+    DT* g = a.grad ? reinterpret_cast<DT*>(a.grad) + row * a.ld_grad : nullptr;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    bool part = w != 0.f;
+    RowVec<DT> v[U];
+    Listed list{};
+    if (part) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(x, team.lane + u * kLanes, a.V);  // (past the end: -inf)
+        list = read_list<DT, TAIL, W>(a, l, team, row);
+        part = TAIL || list.some;
+    }
+    if (!part) {
+        if (team.lane == 0) a.loss[row] = 0.f;
+        if (g) zero_row<DT, kLanes>(g, a.V, team.lane);
+        return;
+    }
+    float top = kNegInf;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < K; ++k) top = fmaxf(top, v[u].at(k));
+    const Above sc = above(team.max(top), kLog2e * a.inv_temp);
+    float z_out = 0.f, z_in = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = team.lane + u * kLanes;
+        const uint32_t bits = TAIL && i * K < a.V ? vector_bits<K>(l.bits, i) : 0u;
+        add_weights<TAIL>(v[u], sc, bits, z_out, z_in);
+    }
+    z_out = team.sum(z_out);
+    if (TAIL) z_in = team.sum(z_in);
+    const DistillRow r = row_loss<TAIL, W>(a, l, team, list, sc, z_out, z_in, w, row);
+    if (!g) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = team.lane + u * kLanes;
+        float d[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) d[k] = r.factor * r.probability(v[u].at(k));
+        if (i * K < a.V) store_row_vec<DT>(g, i, a.V, d);
+    }
+    listed_gradient<DT, W>(a, l, team, list, r, g);
+}
+
+// Longer rows, one per workgroup of W waves: one pass for the sums, each lane relative to its own running
+// maximum, and one that writes the gradient.
+template <typename DT, bool TAIL, int W>
+__global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char s_mem[];
+    __shared__ float s_slots[2 * W];
+    constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
+    const int64_t row = grid_row();
+    if (row >= a.M) return;
+    const int tid = threadIdx.x;
+    const Team<W> team{s_slots, tid};
+    const DistillLds l(s_mem, a);
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
+    DT* g = a.grad ? reinterpret_cast<DT*>(a.grad) + row * a.ld_grad : nullptr;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    bool part = w != 0.f;
+    Listed list{};
+    if (part) {
+        list = read_list<DT, TAIL, W>(a, l, team, row);
+        part = TAIL || list.some;
+    }
+    if (!part) {
+        if (tid == 0) a.loss[row] = 0.f;
+        if (g) zero_row<DT, kLanes>(g, a.V, tid);
+        return;
+    }
+    const float c = kLog2e * a.inv_temp;
+    const int64_t vecs = (a.V + K - 1) / K;
+    // (sums from chunk to chunk in 64 bits: one addition after another in 32 drifts in the longest rows)
+    float top = kNegInf;
+    double out = 0., in = 0.;
+    auto rebase = [&](float t) {
+        const double f = top == t ? 1. : double(exp2_fast(fmaxf((top - t) * c, kLog2Zero)));
+        out *= f;
+        in *= f;
+        top = t;
+    };
+    const int64_t span = TAIL ? kBits / K : vecs;  // vectors whose bits are there
+    for (int64_t from = 0; from < vecs; from += span) {
+        const int64_t end = from + span < vecs ? from + span : vecs;
+        if (TAIL && a.V > kBits) {  // the bits of this part of the row
+            __syncthreads();
+            for (int i = tid; i < a.words; i += kLanes) l.bits[i] = 0;
+            __syncthreads();
+            bool unused = false;
+            for (int k = tid; k < a.K; k += kLanes) {
+                const int64_t id = l.id[k];
+                if (id >= from * K && id < end * K) mark(l.bits, id, unused);
+            }
+            __syncthreads();
+        }
+        for (int64_t i0 = from + tid; i0 < end; i0 += U * kLanes) {
+            RowVec<DT> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, i0 + u * kLanes < end ? a.V : 0);  // (past the end: -inf)
+            float t = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
+            if (t > top) rebase(t);
+            const Above sc = above(top, c);
+            float z_out = 0.f, z_in = 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t i = i0 + u * kLanes;
+                const uint32_t bits = TAIL && i < end ? vector_bits<K>(l.bits, i - from) : 0u;
+                add_weights<TAIL>(v[u], sc, bits, z_out, z_in);
+            }
+            out += z_out;
+            in += z_in;
+        }
+    }
+    rebase(team.max(top));
+    const float z_out = team.sum(float(out)), z_in = TAIL ? team.sum(float(in)) : 0.f;
+    const DistillRow r = row_loss<TAIL, W>(a, l, team, list, above(top, c), z_out, z_in, w, row);
+    if (!g) return;
+    // backwards: what the first pass read last is nearest in the caches
+    for (int64_t i0 = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid; i0 >= 0; i0 -= U * kLanes) {
+        RowVec<DT> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, a.V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * kLanes;
+            float d[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) d[k] = r.factor * r.probability(v[u].at(k));
+            if (i < vecs) store_row_vec<DT>(g, i, a.V, d);
+        }
+    }
+    listed_gradient<DT, W>(a, l, team, list, r, g);
+}
+
+}  // namespace rlcs

@@ -1,0 +1,248 @@
+// Entry points of attention over a paged cache and of writing into it.
+#include "rlcs_paged.h"
+#include "rlcs_dispatch.h"
+
+#include <cmath>
+
+using namespace rlcs;
+using namespace rlcs::host;
+
+namespace {
+
+constexpr int64_t kMaxHeadDim = 256;
+constexpr int64_t kMaxTokenStride = int64_t(1) << 24;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool reachable(std::initializer_list<int64_t> sizes, const int64_t* strides) {
+    int64_t last = kMaxHeadDim;
+    int i = 0;
+    for (const int64_t n : sizes) {
+        const int64_t s = strides[i++];
+        if (s < 0) return false;
+        if (n <= 1 || s == 0) continue;
+        if (s > (INT64_MAX / 8 - last) / (n - 1)) return false;
+        last += (n - 1) * s;
+    }
+    return true;
+}
+bool whole_vectors(const int64_t* s, int n, int64_t vec) {
+    for (int i = 0; i < n; ++i)
+        if (s[i] % vec) return false;
+    return true;
+}
+
+// Sequences of up to this many rows a key head are the first kernel's.
+constexpr int64_t kFewRows = 2 * kTileRows;
+// Items that parts should come to, and the keys of the shortest part.
+constexpr int64_t kWantFew = 1536, kWantMany = 512, kLeastFew = 256, kLeastMany = 512;
+
+// Which kernels a call takes, and their parts.
+struct PagedPlan {
+    bool few, many;
+    int few_tiles;       // of sixteen rows, of the first kernel
+    int64_t many_rows;   // of a tile of the second: 64, 128 or 256
+    int64_t few_want, few_slots, many_want, many_slots;
+};
+
+bool make_plan(PagedPlan& p, int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_chunk, bool ragged, bool bf16) {
+    const int64_t r = Hq / Hkv, most = max_chunk * r;
+    p = PagedPlan{};
+    p.few = ragged || most <= kFewRows;
+    p.many = most > kFewRows;
+    p.few_tiles = most <= kTileRows ? 1 : 2;
+    p.many_rows = D > 128 || tokens * r <= 64 * B ? 64 : bf16 ? 256 : 128;
+    p.few_want = ceil_div(kWantFew, Hkv);
+    p.few_slots = p.few_want + B;
+    const int64_t tiles = tokens * r / p.many_rows;
+    p.many_want = tiles * Hkv >= kWantMany ? 0 : ceil_div(kWantMany, Hkv);
+    p.many_slots = p.many_want + tiles + B;
+    return p.few_slots <= INT32_MAX / Hkv && p.many_slots <= INT32_MAX / Hkv;
+}
+size_t part_bytes(int64_t want, int64_t slots, int64_t rows, int64_t Hkv, int64_t D) {
+    return want ? size_t(Hkv * slots * rows) * size_t(4 * D + 8) : 0;
+}
+size_t plan_bytes(const PagedPlan& p, int64_t Hkv, int64_t D) {
+    const size_t x = p.few ? part_bytes(p.few_want, p.few_slots, p.few_tiles * kTileRows, Hkv, D) : 0;
+    const size_t y = p.many ? part_bytes(p.many_want, p.many_slots, p.many_rows, Hkv, D) : 0;
+    return x > y ? x : y;
+}
+
+// Gives a kernel its parts.
+void cut(PagedArgs& a, int64_t want, int64_t slots, int64_t least, int64_t rows, void* ws) {
+    a.want = int32_t(want);
+    a.slots = int32_t(slots);
+    a.least = int32_t(least);
+    a.part_acc = static_cast<float*>(ws);
+    a.part_ml = want ? reinterpret_cast<float2*>(a.part_acc + int64_t(a.Hkv) * slots * rows * a.D) : nullptr;
+}
+
+template <typename DT, int ND, int QT>
+void launch_few(const PagedArgs& a, hipStream_t s) {
+    const dim3 grid = row_grid(int64_t(a.slots) * a.Hkv), block(kAttnWaves * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((paged_few_kernel<DT, ND, QT, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_few_kernel<DT, ND, QT, false>), grid, block, 0, s, a);
+    if (a.want) hipLaunchKernelGGL((paged_join_kernel<DT, true, QT * kTileRows>), row_grid(a.tokens * a.Hq), dim3(256), 0, s, a);
+}
+template <typename DT, int ND, int QT, int W>
+void launch_many(const PagedArgs& a, hipStream_t s) {
+    const dim3 grid = row_grid(int64_t(a.slots) * a.Hkv), block(W * kWave);
+    if (a.D == 16 * ND) hipLaunchKernelGGL((paged_many_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_many_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a);
+    if (a.want) hipLaunchKernelGGL((paged_join_kernel<DT, false, W * QT * kTileRows>), row_grid(a.tokens * a.Hq), dim3(256), 0, s, a);
+}
+
+template <typename DT, int ND>
+rlcs_status run_paged(PagedArgs a, const PagedPlan& p, void* ws, hipStream_t s) {
+    if (p.few) {
+        cut(a, p.few_want, p.few_slots, kLeastFew, p.few_tiles * kTileRows, ws);
+        if (p.few_tiles == 1) launch_few<DT, ND, 1>(a, s);
+        else launch_few<DT, ND, 2>(a, s);
+    }
+    if (p.many) {
+        cut(a, p.many_want, p.many_slots, kLeastMany, p.many_rows, ws);
+        if constexpr (ND > 8) {
+            launch_many<DT, ND, 1, 4>(a, s);
+        } else {
+            if (p.many_rows == 64) launch_many<DT, ND, 1, 4>(a, s);
+            else if constexpr (sizeof(DT) == 2) launch_many<DT, ND, 2, 8>(a, s);
+            else launch_many<DT, ND, 1, 8>(a, s);
+        }
+    }
+    return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
+}
+template <typename DT>
+rlcs_status run_paged(const PagedArgs& a, const PagedPlan& p, void* ws, hipStream_t s) {
+    return a.D <= 64 ? run_paged<DT, 4>(a, p, ws, s) : a.D <= 128 ? run_paged<DT, 8>(a, p, ws, s) : run_paged<DT, 16>(a, p, ws, s);
+}
+
+bool good_page(int64_t page) { return page >= 16 && page <= 65536 && (page & (page - 1)) == 0; }
+bool good_dim(int64_t D) { return D >= 8 && D <= kMaxHeadDim && D % 8 == 0; }
+
+// What both calls share: the cache, the table and the sequences.
+rlcs_status prepare(PagedArgs& a, const int32_t* table, const int32_t* length, const int32_t* q_start, int64_t tokens, int64_t B, int64_t W,
+                    int64_t ld_table, int64_t pages, int64_t page, int64_t Hkv, int64_t D, const int64_t* ks, const int64_t* vs, rlcs_dtype dtype) {
+    if (!good_page(page) || !good_dim(D) || Hkv < 1) return RLCS_ERR_INVALID_ARG;
+    if (tokens > INT32_MAX - (1 << 20) || B > INT32_MAX / 2 || pages > kMaxT || W > kMaxT / page || Hkv > INT32_MAX / D) return RLCS_ERR_INVALID_ARG;
+    if (ld_table < W || (B > 1 && ld_table > INT64_MAX / 8 / B)) return RLCS_ERR_INVALID_ARG;
+    if (!length || (W && !table)) return RLCS_ERR_INVALID_ARG;
+    for (const void* p : {table, length, q_start})
+        if (!aligned(p, 4)) return RLCS_ERR_INVALID_ARG;
+    if (!q_start && tokens % B) return RLCS_ERR_INVALID_ARG;
+    const int64_t vec = 16 / int64_t(dtype_size(dtype));
+    if (!whole_vectors(ks, 3, vec) || !whole_vectors(vs, 3, vec)) return RLCS_ERR_INVALID_ARG;
+    // (a group's rows lie within 31 bits of bytes of each other)
+    if (ks[1] >= kMaxTokenStride || vs[1] >= kMaxTokenStride) return RLCS_ERR_INVALID_ARG;
+    if (!reachable({pages, page, Hkv}, ks) || !reachable({pages, page, Hkv}, vs)) return RLCS_ERR_INVALID_ARG;
+    a.table = table; a.length = length; a.q_start = q_start;
+    a.ld_table = ld_table; a.tokens = tokens;
+    a.B = int32_t(B); a.W = int32_t(W); a.pages = int32_t(pages);
+    while ((int64_t(1) << a.shift) < page) ++a.shift;
+    a.Hkv = int32_t(Hkv); a.D = int32_t(D);
+    for (int i = 0; i < 3; ++i) {
+        a.ks[i] = ks[i];
+        a.vs[i] = vs[i];
+    }
+    return RLCS_OK;
+}
+
+rlcs_paged_layout contiguous(int64_t page, int64_t Hq, int64_t Hkv, int64_t D) {
+    const int64_t t = Hkv * D;
+    return rlcs_paged_layout{{Hq * D, D}, {t, D}, {t, D}, {page * t, t, D}, {page * t, t, D}};
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rlcs_workspace_size_paged(int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv, int64_t D,
+                                 int64_t max_chunk) {
+    if (tokens < 1 || B < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || !good_dim(D) || max_chunk < 0) return 0;
+    if (B > INT32_MAX / 2 || Hq > INT32_MAX || tokens > (INT32_MAX - (1 << 20)) / Hq) return 0;
+    if (max_chunk == 0 || max_chunk > tokens) max_chunk = tokens;
+    size_t most = 0;
+    for (const bool bf16 : {false, true}) {
+        PagedPlan p;
+        if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, true, bf16)) return 0;
+        const size_t n = plan_bytes(p, Hkv, D);
+        most = n > most ? n : most;
+    }
+    return most;
+}
+
+rlcs_status rlcs_paged_attn(const void* q, const void* k_cache, const void* v_cache,
+                            const int32_t* table, const int32_t* length, const int32_t* q_start,
+                            void* o, float* lse, int64_t tokens, int64_t B, int64_t W,
+                            int64_t ld_table, int64_t pages, int64_t page, int64_t Hq, int64_t Hkv,
+                            int64_t D, int64_t max_chunk, const rlcs_paged_layout* layout,
+                            float scale, rlcs_dtype dtype, void* ws, size_t ws_bytes,
+                            rlcs_stream_t stream) {
+    if (tokens < 0 || B < 0 || W < 0 || pages < 0 || page < 0 || Hq < 0 || Hkv < 0 || D < 0 || max_chunk < 0) return RLCS_ERR_INVALID_ARG;
+    if (dtype != RLCS_F32 && dtype != RLCS_BF16) return RLCS_ERR_DTYPE;
+    if (!std::isfinite(scale)) return RLCS_ERR_INVALID_ARG;
+    if (tokens == 0 || B == 0 || Hq == 0 || D == 0) return RLCS_OK;
+    if (Hkv < 1 || Hq % Hkv || Hq > INT32_MAX / kMaxHeadDim || tokens > (INT32_MAX - (1 << 20)) / Hq) return RLCS_ERR_INVALID_ARG;
+    PagedArgs a{};
+    const rlcs_paged_layout at = layout ? *layout : contiguous(page, Hq, Hkv, D);
+    const rlcs_status st = prepare(a, table, length, q_start, tokens, B, W, ld_table, pages, page, Hkv, D, at.k_cache, at.v_cache, dtype);
+    if (st != RLCS_OK) return st;
+    if (!q || !o || (pages && W && (!k_cache || !v_cache))) return RLCS_ERR_INVALID_ARG;
+    for (const void* p : {q, k_cache, v_cache, static_cast<const void*>(o)})
+        if (!aligned(p, 16)) return RLCS_ERR_INVALID_ARG;
+    if (!aligned(lse, 4)) return RLCS_ERR_INVALID_ARG;
+    if (!whole_vectors(at.q, 2, 16 / int64_t(dtype_size(dtype))) || !reachable({tokens, Hq}, at.q)) return RLCS_ERR_INVALID_ARG;
+    const bool bf16 = dtype == RLCS_BF16;
+    if (max_chunk == 0 || max_chunk > tokens) max_chunk = tokens;
+    if (!q_start) max_chunk = tokens / B;
+    PagedPlan p;
+    if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, q_start != nullptr, bf16)) return RLCS_ERR_INVALID_ARG;
+    if (const size_t need = plan_bytes(p, Hkv, D)) {
+        if (!ws || ws_bytes < need) return RLCS_ERR_WORKSPACE;
+        if (!aligned(ws, 16)) return RLCS_ERR_INVALID_ARG;
+    }
+    a.q = q; a.k = k_cache; a.v = v_cache; a.o = o; a.lse = lse;
+    a.qs[0] = at.q[0]; a.qs[1] = at.q[1];
+    a.Hq = int32_t(Hq); a.r = int32_t(Hq / Hkv);
+    a.max_chunk = int32_t(max_chunk);
+    a.few_rows = int32_t(p.few_tiles * kTileRows);
+    a.scale2 = scale * kLog2e;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return bf16 ? run_paged<bf16_t>(a, p, ws, s) : run_paged<float>(a, p, ws, s);
+}
+
+rlcs_status rlcs_paged_write(const void* k, const void* v, void* k_cache, void* v_cache,
+                             const int32_t* table, const int32_t* length, const int32_t* q_start,
+                             int64_t tokens, int64_t B, int64_t W, int64_t ld_table, int64_t pages,
+                             int64_t page, int64_t Hkv, int64_t D,
+                             const rlcs_paged_layout* layout, rlcs_dtype dtype,
+                             rlcs_stream_t stream) {
+    if (tokens < 0 || B < 0 || W < 0 || pages < 0 || page < 0 || Hkv < 0 || D < 0) return RLCS_ERR_INVALID_ARG;
+    if (dtype != RLCS_F32 && dtype != RLCS_BF16) return RLCS_ERR_DTYPE;
+    if (tokens == 0 || B == 0 || W == 0 || pages == 0 || Hkv == 0 || D == 0) return RLCS_OK;
+    PagedWriteArgs a{};
+    const rlcs_paged_layout at = layout ? *layout : contiguous(page, 1, Hkv, D);
+    const rlcs_status st = prepare(a.at, table, length, q_start, tokens, B, W, ld_table, pages, page, Hkv, D, at.k_cache, at.v_cache, dtype);
+    if (st != RLCS_OK) return st;
+    if (!k || !v || !k_cache || !v_cache) return RLCS_ERR_INVALID_ARG;
+    for (const void* p : {k, v, static_cast<const void*>(k_cache), static_cast<const void*>(v_cache)})
+        if (!aligned(p, 16)) return RLCS_ERR_INVALID_ARG;
+    const int64_t vec = 16 / int64_t(dtype_size(dtype));
+    if (!whole_vectors(at.k_new, 2, vec) || !whole_vectors(at.v_new, 2, vec) || !reachable({tokens, Hkv}, at.k_new) ||
+        !reachable({tokens, Hkv}, at.v_new))
+        return RLCS_ERR_INVALID_ARG;
+    a.at.max_chunk = INT32_MAX;
+    a.k_new = k; a.v_new = v;
+    a.k = static_cast<char*>(k_cache); a.v = static_cast<char*>(v_cache);
+    for (int i = 0; i < 2; ++i) {
+        a.kn[i] = at.k_new[i];
+        a.vn[i] = at.v_new[i];
+    }
+    a.pieces = int32_t(D / vec);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const dim3 grid = row_grid((tokens + 3) / 4);
+    if (dtype == RLCS_BF16) hipLaunchKernelGGL((paged_write_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_write_kernel<float>), grid, dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
+}
+
+}  // extern "C"

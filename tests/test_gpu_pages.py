@@ -1,0 +1,148 @@
+"""rlcs_pages_fork, _resize, _compact and _copy against one entry after the other."""
+import random
+
+import pytest
+import torch
+
+import paged_plain as plain
+import paper_2608_17641_amd as rl
+
+pytestmark = pytest.mark.gpu
+
+I32 = torch.int32
+SIZES = [(1, 1, 1), (3, 4, 9), (17, 5, 64), (40, 30, 700), (70, 9, 65), (9, 1100, 1500), (200, 400, 70000), (5000, 20, 3000)]
+
+
+def ints(x):
+    return torch.tensor(x, dtype=I32, device="cuda")
+
+
+def start(B, W, pages, page, rng, share=0.3):
+    """Sequences that hold some of the pages, some of them the same, some entries no page."""
+    free = list(range(pages))
+    rng.shuffle(free)
+    table, length, refs = [], [], [0] * pages
+    for b in range(B):
+        n = rng.choice([0, rng.randint(0, W * page), W * page, rng.randint(0, W) * page])
+        held = (n + page - 1) // page
+        row = []
+        for i in range(held):
+            if table and rng.random() < share:
+                p = rng.choice(rng.choice(table) or [-1])
+            else:
+                p = free.pop() if len(free) > pages // 4 else -1
+            row.append(p)
+            if 0 <= p < pages:
+                refs[p] += 1
+        if rng.random() < 0.05 and row:  # (what no call makes, but a caller might)
+            if 0 <= row[0] < pages:
+                refs[row[0]] -= 1
+            row[0] = rng.choice([-5, pages, 2 ** 31 - 1])
+        table.append(row + [rng.choice([-1, rng.randint(0, pages - 1)])] * (W - held))
+        length.append(n)
+    return table, length, refs
+
+
+def lists(*tensors):
+    return [t.tolist() for t in tensors]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("size", range(len(SIZES)))
+def test_life(size, in_place):
+    """Forks and resizes, one after the other, each from the last one's outputs."""
+    B, W, pages = SIZES[size]
+    rng = random.Random(size)
+    page = rng.choice([16, 64])
+    table, length, refs = start(B, W, pages, page, rng)
+    cache = plain.Cache(table, length, refs, page)
+    t, n, r = ints(table), ints(length), ints(refs)
+    for step in range(4):
+        parent = [rng.choice([b, rng.randint(0, B - 1), rng.randint(0, B - 1), -1, B]) for b in range(B)]
+        cache.fork(parent)
+        was = [x.clone() for x in (t, n, r)]
+        got = rl.rlcs_pages_fork(t, n, r, ints(parent), refs_out=r if in_place else None, page=page)
+        if not in_place:
+            assert all(torch.equal(x, y) for x, y in zip(was, (t, n, r)))
+        t, n, r = got
+        assert lists(t, n, r) == [cache.table(), cache.length, cache.refs]
+        new = [rng.choice([-1, cache.length[b], rng.randint(0, W * page), min(W * page, cache.length[b] + rng.randint(0, 40)), 0, W * page + 1])
+               if rng.random() < 0.9 else cache.length[b] for b in range(B)]
+        moves = cache.resize(new)
+        outs = dict(table_out=t, length_out=n, refs_out=r) if in_place else {}
+        t, n, r, m = rl.rlcs_pages_resize(t, n, r, ints(new), page=page, **outs)
+        assert lists(t, n, r, m) == [cache.table(), cache.length, cache.refs, moves]
+        table, moves, count = cache.compact(cache.table())
+        outs = dict(table_out=t, refs_out=r) if in_place else {}
+        t, r, m, c = rl.rlcs_pages_compact(t, r, **outs)
+        assert lists(t, r, m, c) == [table, cache.refs, moves, [count]]
+        cache = plain.Cache(table, cache.length, cache.refs, page)
+
+
+def test_all_free_all_used_and_none_left():
+    for pages in (1, 2, 64, 1025):
+        table, refs = ints([[-1] * 4]), ints([0] * pages)
+        t, r, m, c = rl.rlcs_pages_compact(table, refs)
+        assert c.item() == 0 and not bool(r.any()) and bool((m == -1).all()) and m.shape == (pages // 2, 2)
+        t, r, m, c = rl.rlcs_pages_compact(table, refs + 2)
+        assert c.item() == pages and bool((r == 2).all()) and bool((m == -1).all())
+        # one page too few, then just enough; the first in line gets what there is
+        W = pages + 1
+        table, length = ints([[-1] * W] * 3), ints([0, 0, 0])
+        t, n, r, m = rl.rlcs_pages_resize(table, length, refs, ints([16 * (pages + 1), 0, 0]), page=16)
+        assert n.tolist() == [0, 0, 0] and not bool(r.any()) and bool((t == -1).all())
+        t, n, r, m = rl.rlcs_pages_resize(table, length, refs, ints([0, 16 * pages, 16]), page=16)
+        assert n.tolist() == [0, 16 * pages, 0] and t[1, :pages].tolist() == list(range(pages)) and bool((r == 1).all())
+        t, n, r, m = rl.rlcs_pages_resize(t, n, r, ints([1, 0, -1]), page=16)  # what is given back can be had at once
+        assert n.tolist() == [1, 0, 0] and t[0, 0].item() == 0 and int(r.sum()) == 1
+
+
+def test_copy_on_growth():
+    """Three sequences share a page that they end in: those that grow leave it, a whole page is shared on."""
+    table, refs = ints([[4, 2, -1], [-1] * 3, [-1] * 3, [-1] * 3]), ints([0, 0, 1, 0, 1, 0, 0, 0])
+    t, n, r = rl.rlcs_pages_fork(table, ints([20, 0, 0, 0]), refs, ints([0, 0, 0, 7]), page=16)
+    assert t.tolist() == [[4, 2, -1]] * 3 + [[-1] * 3] and n.tolist() == [20, 20, 20, 0] and r.tolist() == [0, 0, 3, 0, 3, 0, 0, 0]
+    t, n, r, m = rl.rlcs_pages_resize(t, n, r, ints([20, 21, 40, 0]), page=16)
+    assert m.tolist() == [[-1, -1], [2, 0], [2, 1], [-1, -1]]
+    assert t.tolist() == [[4, 2, -1], [4, 0, -1], [4, 1, 3], [-1] * 3] and r.tolist() == [1, 1, 1, 1, 3, 0, 0, 0]
+    cache = torch.randn((2, 8, 16, 3), device="cuda")
+    want = cache.clone()
+    want[:, [0, 1]] = want[:, [2, 2]]
+    before = cache._version
+    assert rl.rlcs_pages_copy(cache, m) is cache and cache._version == before + 1
+    assert torch.equal(cache, want)
+    # cut back to within a page that others hold: growing again copies
+    t, n, r, m = rl.rlcs_pages_resize(t, n, r, ints([5, -1, -1, 0]), page=16)
+    t, n, r, m = rl.rlcs_pages_resize(t, n, r, ints([6, -1, -1, 0]), page=16)
+    assert m[0].tolist() == [4, 2] and t[0].tolist() == [2, -1, -1] and n[0].item() == 6
+
+
+@pytest.mark.parametrize("dtype,shape", [(torch.bfloat16, (2, 40, 16, 2, 64)), (torch.float32, (1, 9, 5, 7)), (torch.uint8, (3, 33, 21)), (torch.int16, (2, 6, 20000)),
+                                         (torch.float32, (1, 4, 1 << 18))])
+def test_copy(dtype, shape):
+    g = torch.Generator().manual_seed(3)
+    cache = torch.randint(0, 100, shape, generator=g).to(dtype)
+    pages = shape[1]
+    half = torch.randperm(pages, generator=g)[:pages // 2 * 2].reshape(-1, 2)
+    moves = torch.cat([half, torch.tensor([[-1, -1], [0, pages], [-1, 0], [pages - 1, pages - 1], [2 ** 31 - 1, 1]])]).to(I32)
+    want = cache.clone()
+    want[:, half[:, 1]] = want[:, half[:, 0]]
+    assert torch.equal(rl.rlcs_pages_copy(cache.cuda(), moves.cuda()).cpu(), want)
+    # pages outside layers, and gaps between them
+    room = torch.zeros((pages, shape[0] + 1) + shape[2:], dtype=dtype, device="cuda")
+    view = room[:, :shape[0]].transpose(0, 1)
+    view.copy_(cache)
+    rl.rlcs_pages_copy(view, moves.cuda())
+    assert torch.equal(view.cpu(), want) and not bool(room[:, shape[0]].any())
+    odd = torch.zeros((shape[0], pages) + shape[2:-1] + (shape[-1] + 1,), dtype=dtype, device="cuda")
+    if len(shape) == 3:
+        odd[..., 1:].copy_(cache)
+        rl.rlcs_pages_copy(odd[..., 1:], moves.cuda())
+        assert torch.equal(odd[..., 1:].cpu(), want) and not bool(odd[..., 0].any())
+
+
+def test_nothing():
+    cache = torch.ones((1, 4, 16), device="cuda")
+    assert rl.rlcs_pages_copy(cache, torch.empty((0, 2), dtype=I32, device="cuda")) is cache
+    t, r, m, c = rl.rlcs_pages_compact(torch.empty((0, 5), dtype=I32, device="cuda"), ints([0, 3]))
+    assert t.shape == (0, 5) and r.tolist() == [3, 0] and m.tolist() == [[1, 0]] and c.item() == 1
