@@ -1,0 +1,231 @@
+"""The operators of speculative rollouts together: the example's completions against a dense forward pass, both
+sides of the Python binding, other streams, captured graphs."""
+import os
+import sys
+
+import pytest
+import torch
+
+import paper_2608_17641_amd as rl
+
+pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "examples"))
+
+I32 = torch.int32
+EPS = 2.0 ** -24
+
+
+def dense_logits(model, tokens):
+    """The model's logits at every token of one sequence, in 64 bits, without cache or pages."""
+    x = model.embed[tokens.long()].double()
+    n, r = x.shape[0], model.heads // model.key_heads
+    q = (x @ model.wq.double()).view(n, model.heads, model.head_dim)
+    kv = (x @ model.wkv.double()).view(n, 2, model.key_heads, model.head_dim).repeat_interleave(r, 2)
+    s = torch.stack([q[:, h] @ kv[:, 0, h].t().contiguous() for h in range(model.heads)]) / model.head_dim ** 0.5
+    s = s.masked_fill(torch.ones((n, n), dtype=torch.bool, device="cuda").triu(1), -torch.inf)
+    p = torch.softmax(s, -1)
+    o = torch.stack([p[h] @ kv[:, 1, h] for h in range(model.heads)], 1)
+    h = x + o.reshape(n, -1) @ model.wo.double()
+    return (h * torch.rsqrt((h * h).mean(-1, keepdim=True) + 1e-6)) @ model.head.double()
+
+
+def test_example():
+    """Every token's log-probability, as the rounds reported it, is the dense target's: pages, forks, copies, cut-backs and
+    chunks put every key where it belongs. float32; logits of about 60 at most are sums of 128 products whose inputs have
+    passed three more such sums: 2^-24 * 4 * 128 * 60 bounds what they are off."""
+    import speculative_rollout as sr
+    r = sr.Rollout(groups=3, completions=5, prompt=50, tokens=30, drafted=3, dtype=torch.float32, seed=1)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for step in range(2):  # (the second on pages that the first gave back)
+        prompts = torch.randint(0, r.vocab, (3, 50), device="cuda", generator=g, dtype=I32)
+        lens = torch.tensor([50, 17, 33], dtype=I32, device="cuda")
+        out, logps, have, a_round, rows = r.draw(prompts, lens)
+        assert 1.0 <= a_round <= 4.0 and int(have.min()) >= 30
+        table, length, refs = r.table.cpu(), r.length.cpu(), r.refs.cpu()
+        held = [table[b, :(int(length[b]) + 15) // 16] for b in range(15)]
+        assert torch.equal(torch.bincount(torch.cat(held).long(), minlength=refs.numel()).int(), refs) and int(refs.max()) == 5
+        for b in range(15):
+            n, start = int(have[b]), int(lens[b // 5])
+            seq = torch.cat([prompts[b // 5, :start], out[b, :n]])
+            want = torch.log_softmax(dense_logits(r.target, seq), -1)[start - 1:start - 1 + n].gather(1, out[b, :n].long()[:, None])[:, 0]
+            assert float((want - logps[b, :n].double()).abs().max()) <= EPS * 4 * 128 * 60
+            assert int(length[b]) == start - 1 + n
+        r.free()
+        assert not bool(r.refs.any()) and bool((r.table == -1).all())
+
+
+def test_example_gradient():
+    """The step on the draft's head is the formula's: autograd's of the same loss in 64 bits."""
+    import speculative_rollout as sr
+    r = sr.Rollout(groups=2, completions=2, prompt=20, tokens=6, dtype=torch.float32, seed=2)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rows = r.draw(torch.randint(0, r.vocab, (2, 20), device="cuda", generator=g, dtype=I32), torch.tensor([20, 11], dtype=I32, device="cuda"))[-1]
+    was = r.draft.head.clone()
+    loss = r.distill(rows, listed=16, rate=1.0)
+    h, logits = (torch.cat([x[i] for x in rows]).flatten(0, 1) for i in range(2))
+    head = was.double().requires_grad_()
+    lp = torch.log_softmax(h.double() @ head, -1)
+    top = torch.topk(torch.log_softmax(logits, -1), 16)
+    t, at = torch.exp(top.values.double()), top.indices
+    rest = 1.0 - t.sum(-1)
+    outside = torch.ones_like(lp, dtype=torch.bool).scatter(1, at, False)
+    p_rest = torch.where(outside, lp.exp(), 0.0).sum(-1)
+    want = ((t * (top.values.double() - lp.gather(1, at))).sum(-1) + rest * (torch.log(rest) - torch.log(p_rest))).mean()
+    want.backward()
+    # (logits off by 2^-24 * 128 * 60 move a share by as much of itself; the step is a mean of products of these with h)
+    off = EPS * 128 * 60
+    assert abs(float(loss) - float(want.detach())) <= 16 * off
+    moved = was.double() - r.draft.head.double()
+    scale = float((h.abs().double().t() @ (lp.exp() + torch.zeros_like(lp).scatter(1, at, t))).max()) / h.shape[0]
+    assert float((moved - head.grad).abs().max()) <= 16 * off * scale + 2 * EPS * float(was.abs().max())
+    assert len(sr.train(steps=1, groups=2, completions=2, tokens=5, prompt=9)) == 1
+
+
+class _Python:
+    def __getattr__(self, name):
+        return lambda *a: NotImplemented
+
+
+def _calls(dtype):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(*s, device="cuda", generator=g).to(dtype)  # noqa: E731
+    ints = lambda x: torch.tensor(x, dtype=I32, device="cuda")  # noqa: E731
+    k, v = rand(12, 16, 2, 64), rand(12, 16, 2, 64)
+    table, length = ints([[3, 1, -1], [0, 5, 7]]), ints([20, 48])
+    q, start = rand(41, 8, 64), ints([0, 1, 41])
+    kn, vn = rand(41, 2, 64), rand(41, 2, 64)
+    refs, parent = ints([1, 1, 0, 1, 0, 1, 0, 1, 0, 0, 0, 0]), ints([1, 1])
+    target, draft = rand(3, 4, 700), rand(3, 3, 700)
+    drawn = torch.randint(0, 700, (3, 3), device="cuda", generator=g, dtype=I32)
+    u, noise = torch.rand((3, 3), device="cuda", generator=g), torch.empty((3, 700), device="cuda").exponential_(generator=g)
+    T = torch.rand(3, device="cuda", generator=g) + 0.2
+    ids = torch.randint(0, 700, (3, 4, 5), device="cuda", generator=g, dtype=I32)
+    lp = torch.log_softmax(torch.randn((3, 4, 5), device="cuda", generator=g), -1)
+    w = torch.rand((3, 4), device="cuda", generator=g)
+    grad = torch.empty_like(target)
+    return [lambda: rl.rlcs_paged_attn(q, k, v, table, length, start),
+            lambda: rl.rlcs_paged_attn(q[:6], k, v, table, length, scale=0.3, max_chunk=3, want_lse=False),
+            lambda: rl.rlcs_paged_attn(q[:2], k, v, table, length),
+            lambda: rl.rlcs_paged_write(kn, vn, k.clone(), v.clone(), table, length, start),
+            lambda: rl.rlcs_pages_fork(table, length, refs, parent, page=16),
+            lambda: rl.rlcs_pages_resize(table, length, refs, ints([33, 5]), page=16),
+            lambda: rl.rlcs_pages_compact(table, refs),
+            lambda: (rl.rlcs_pages_copy(k.clone()[None], ints([[1, 2], [-1, -1]])),),
+            lambda: rl.rlcs_verify_draft(target, draft, drawn, u, noise),
+            lambda: rl.rlcs_verify_draft(target, None, drawn, u, noise, ints([3, 0, 1]), temperature=T, draft_temperature=1.5, want_logp=False),
+            lambda: rl.rlcs_distill_loss(target, ids, lp),
+            lambda: rl.rlcs_distill_loss(target, ids, lp, w, None, grad, temperature=0.5, tail=True),
+            lambda: rl.rlcs_distill_loss(target, ids, lp, w, want_grad=False)]
+
+
+def _same(a, b):
+    assert len(a) == len(b)
+    for x, y in zip(a, b):
+        assert (x is None) == (y is None)
+        if x is not None:
+            assert x.shape == y.shape and x.dtype == y.dtype and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_both_sides_of_the_binding(monkeypatch, dtype):
+    native = rl._load_fast()
+    for i, call in enumerate(_calls(dtype)):
+        taken = []
+
+        class Counting:
+            def __getattr__(self, name):
+                def f(*a):
+                    r = getattr(native, name)(*a)
+                    taken.append(r is not NotImplemented)
+                    return r
+                return f
+
+        monkeypatch.setattr(rl, "_fast", Counting())
+        a = [t.clone() if t is not None else None for t in call()]
+        assert taken == [True], i
+        monkeypatch.setattr(rl, "_fast", _Python())
+        _same(a, call())
+
+
+def test_on_another_stream():
+    """Calls on a stream of their own wait for nothing but it, and allocate there."""
+    calls = _calls(torch.float32)
+    want = [[t.clone() if t is not None else None for t in c()] for c in calls]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = [c() for c in calls]
+    side.synchronize()
+    for a, b in zip(want, got):
+        _same(a, b)
+
+
+def test_captured_graphs():
+    """Two graphs, each with a round's calls and workspaces of its own, replayed in turn with new inputs in the same tensors and
+    eager work between them."""
+    B, K, V = 6, 2, 3000
+    dev = "cuda"
+
+    class Side:
+        def __init__(self):
+            self.k, self.v = torch.zeros(40, 16, 2, 64, device=dev), torch.zeros(40, 16, 2, 64, device=dev)
+            self.q = torch.zeros(B * (K + 1), 8, 64, device=dev)
+            self.kn, self.vn = torch.zeros(B * (K + 1), 2, 64, device=dev), torch.zeros(B * (K + 1), 2, 64, device=dev)
+            self.table, self.length, self.refs = torch.zeros(B, 6, dtype=I32, device=dev), torch.zeros(B, dtype=I32, device=dev), torch.zeros(40, dtype=I32, device=dev)
+            self.new = torch.zeros(B, dtype=I32, device=dev)
+            self.t, self.d = torch.zeros(B, K + 1, V, device=dev), torch.zeros(B, K, V, device=dev)
+            self.drawn, self.u, self.noise = torch.zeros(B, K, dtype=I32, device=dev), torch.zeros(B, K, device=dev), torch.ones(B, V, device=dev)
+            self.ids, self.lp = torch.zeros(B, K + 1, 4, dtype=I32, device=dev), torch.zeros(B, K + 1, 4, device=dev)
+
+        def fill(self, seed):
+            g = torch.Generator(device=dev).manual_seed(seed)
+            for x in (self.k, self.v, self.q, self.kn, self.vn, self.t, self.d):
+                x.normal_(generator=g)
+            self.noise.exponential_(generator=g)
+            self.u.uniform_(generator=g)
+            self.drawn.random_(0, V, generator=g)
+            self.ids.random_(0, V, generator=g)
+            self.lp.normal_(generator=g).sub_(4.0)
+            self.table.copy_(torch.randperm(40, device=dev, generator=g)[:B * 6].view(B, 6))
+            self.length.random_(0, 60, generator=g)
+            self.new.copy_(self.length + K + 1)
+            held = (self.length + 15) // 16
+            self.refs.zero_()
+            at = self.table[torch.arange(6, device=dev)[None] < held[:, None]].long()
+            self.refs[at] = 1
+            self.refs[at[::3]] = 2  # (as if shared)
+
+        def calls(self):
+            table, length, refs, moves = rl.rlcs_pages_resize(self.table, self.length, self.refs, self.new, page=16)
+            rl.rlcs_pages_copy(self.k[None], moves)
+            rl.rlcs_pages_copy(self.v[None], moves)
+            rl.rlcs_paged_write(self.kn, self.vn, self.k, self.v, table, length)
+            o, lse = rl.rlcs_paged_attn(self.q, self.k, self.v, table, length)
+            more = rl.rlcs_verify_draft(self.t, self.d, self.drawn, self.u, self.noise)
+            return (table, length, refs, moves, o, lse, self.k, self.v) + more + rl.rlcs_distill_loss(self.t, self.ids, self.lp, tail=True)
+
+    sides = [Side(), Side()]
+    graphs = []
+    for i, s in enumerate(sides):
+        s.fill(i)
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            s.calls()
+        torch.cuda.current_stream().wait_stream(stream)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = s.calls()
+        graphs.append((graph, out))
+    for seed in range(10, 14):
+        for i, s in enumerate(sides):
+            s.fill(seed + 100 * i)
+        for graph, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        got = [[t.clone() for t in out] for _, out in graphs]
+        for i, s in enumerate(sides):
+            s.fill(seed + 100 * i)
+            _same(got[i], s.calls())
+        torch.cuda.synchronize()
