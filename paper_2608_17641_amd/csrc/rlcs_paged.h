@@ -23,14 +23,16 @@ struct PagedArgs {
     void* o;
     float* lse;
     int64_t ld_table, tokens;
-    int64_t qs[2], ks[3], vs[3];
+    int64_t qs[2];         // strides of q in elements
+    int64_t ks[3], vs[3];  // of the caches in bytes: page, token (below 2^26), head
     int32_t B, W, pages, shift, Hq, Hkv, D, r, max_chunk;
+    double rise;   // units by which a tile has more keys than the one before
+    int32_t unit;  // work is counted in 2^unit keys, 64 at least, so that all of it counts in 31 bits
     float scale2;  // scale * log2(e)
     // Tiles of at most few_rows rows are the first kernel's, the others the second's.
     int32_t few_rows;
-    // How many items a key head the parts of this kernel should come to (0: no parts), at least how many keys a part
-    // has, and places for parts in the workspace.
-    int32_t want, least, slots;
+    // Pieces a key head that its keys are dealt out in; 0: whole tiles only.
+    int32_t pieces;
     float* part_acc;   // [key head][slot][row][D]: outputs relative to the part's own maximum
     float2* part_ml;   // [key head][slot][row]: maximum (base 2) and sum
 };
@@ -39,8 +41,7 @@ constexpr int kKeyGroup = 16;  // keys that are addressed together
 
 // A sequence: its first row of q, its new tokens, how many of these count, and all of its tokens.
 struct PagedSeq {
-    int64_t first;
-    int n, taken, length;
+    int first, n, taken, length;
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int b) {
     PagedSeq s;
@@ -48,11 +49,11 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int b) {
         int64_t x = a.q_start[b], y = a.q_start[b + 1];
         x = x < 0 ? 0 : x > a.tokens ? a.tokens : x;
         y = y < x ? x : y > a.tokens ? a.tokens : y;
-        s.first = x;
+        s.first = int(x);
         s.n = int(y - x);
     } else {
         const int64_t n = a.tokens / a.B;
-        s.first = b * n;
+        s.first = int(b * n);
         s.n = int(n);
     }
     s.taken = s.n < a.max_chunk ? s.n : a.max_chunk;
@@ -61,112 +62,221 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int b) {
     return s;
 }
 
-// How a kernel's tiles of R rows are cut: tiles of a sequence (none, if it is the other kernel's), and parts of each.
-struct PagedCut {
-    int chunk;  // keys of a part (a multiple of 64), or 0: one part
-    template <bool FEW, int R>
-    static __device__ __forceinline__ int tiles(const PagedArgs& a, const PagedSeq& s) {
-        const int64_t rows = int64_t(s.taken) * a.r;
-        if (FEW) return rows > 0 && rows <= a.few_rows ? 1 : 0;
-        return rows > a.few_rows ? int((rows + R - 1) / R) : 0;
+// What all lanes agree on, in scalar registers.
+__device__ __forceinline__ int agreed(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Inclusive sums over the lanes.
+__device__ __forceinline__ int scan_wave(int v) {
+    auto step = [&](auto ctrl, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});  // row_shr:1
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // row_bcast:15
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // row_bcast:31
+    return v;
+}
+
+// The sequences, the first 64 of them in the lanes.
+struct PagedSeqs {
+    const PagedArgs& a;
+    PagedSeq mine;
+    __device__ __forceinline__ PagedSeqs(const PagedArgs& args) : a(args) {
+        const int lane = threadIdx.x & 63;
+        mine = lane < a.B ? paged_seq(a, lane) : PagedSeq{0, 0, 0, 0};
     }
-    __device__ __forceinline__ int parts(const PagedSeq& s) const {
-        if (chunk == 0 || s.length <= chunk) return 1;
-        return (s.length + chunk - 1) / chunk;
+    __device__ __forceinline__ PagedSeq of_lane(int b0) const {  // b0 + lane
+        if (b0 == 0) return mine;
+        const int b = b0 + (int(threadIdx.x) & 63);
+        return b < a.B ? paged_seq(a, b) : PagedSeq{0, 0, 0, 0};
     }
-    // From the sum over all sequences of keys that tiles read: every wave for itself.
-    template <bool FEW, int R>
-    __device__ __forceinline__ void plan(const PagedArgs& a) {
-        chunk = 0;
-        if (a.want == 0) return;
-        int64_t blocks = 0;
-        for (int b = int(threadIdx.x) & 63; b < a.B; b += kWave) {
-            const PagedSeq s = paged_seq(a, b);
-            blocks += int64_t(tiles<FEW, R>(a, s)) * ((s.length + 63) / 64);
+    __device__ __forceinline__ PagedSeq get(int b) const {
+        if (b >= kWave) return paged_seq(a, b);
+        return PagedSeq{__builtin_amdgcn_readlane(mine.first, b), __builtin_amdgcn_readlane(mine.n, b), __builtin_amdgcn_readlane(mine.taken, b),
+                        __builtin_amdgcn_readlane(mine.length, b)};
+    }
+    // The sequence within which x lies, where each is as long as f says: what is left of x there, or -1 past the last.
+    template <class F>
+    __device__ __forceinline__ int locate(int x, int& b, F&& f) const {
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            const int own = f(of_lane(b0)), upto = scan_wave(own);
+            const uint64_t past = __ballot(upto > x);
+            if (past) {
+                const int i = __ffsll((unsigned long long)past) - 1;
+                b = b0 + i;
+                return x - __builtin_amdgcn_readlane(upto - own, i);
+            }
+            x -= __builtin_amdgcn_readlane(upto, 63);
         }
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) blocks += __shfl_xor(blocks, d);
-        int64_t each = (blocks + a.want - 1) / a.want * 64;
-        if (each < a.least) each = a.least;
-        chunk = int(each < (int64_t(1) << 30) ? each : int64_t(1) << 30);
-        chunk = __builtin_amdgcn_readfirstlane(chunk);
+        return -1;
+    }
+    template <class F>
+    __device__ __forceinline__ int sum(int before, F&& f) const {  // of the sequences before that one
+        int all = 0;
+        for (int b0 = 0; b0 < before; b0 += kWave) all += b0 + (int(threadIdx.x) & 63) < before ? f(of_lane(b0)) : 0;
+        return __builtin_amdgcn_readlane(scan_wave(all), 63);
     }
 };
 
-// What a workgroup takes.
+// How the tiles of a kernel, R rows each, are dealt out within a key head. Tiles lie one after the other on a line, each as long
+// as its work: its keys, and kTileWork units for what a tile costs beside them. The line is cut into pieces of equal length, whole tiles and parts
+// of tiles, so that all end together however lengths differ. Where they lie follows from the lengths on the device, which
+// every wave adds up for itself. Where there are more tiles than pieces, all but the last few tiles are not cut (many rows).
+constexpr int kTileWork = 2;
+constexpr int kLeastWork = 4;  // units of a piece, at least
+template <bool FEW, int R>
+struct PagedLine {
+    int origin, each;  // where the pieces begin, their length;
+    int more, pieces;  // the first `more` are longer by one
+    int uncut;         // tiles before them
+
+    // Tiles of a sequence: none, if it is the other kernel's.
+    static __device__ __forceinline__ int tiles(const PagedArgs& a, const PagedSeq& s) {
+        const int rows = s.taken * a.r;
+        if (FEW) return rows > 0 && rows <= a.few_rows ? 1 : 0;
+        return rows > a.few_rows ? (rows + R - 1) / R : 0;
+    }
+    // Where tile t of a sequence begins. (A tile's keys are those before the chunk and as many tokens as its rows and the
+    // ones before are.)
+    static __device__ __forceinline__ int begin(const PagedArgs& a, const PagedSeq& s, int t) {
+        if (FEW) return t * (kTileWork + (s.length >> a.unit));
+        const int before = s.length > s.n ? s.length - s.n : 0;
+        return t * (kTileWork + (before >> a.unit)) + int(double(int64_t(t) * (t + 1) / 2) * a.rise);
+    }
+    static __device__ __forceinline__ int work(const PagedArgs& a, const PagedSeq& s) { return begin(a, s, tiles(a, s)); }
+    __device__ __forceinline__ void plan(const PagedArgs& a, const PagedSeqs& seqs) {
+        uncut = origin = pieces = each = more = 0;
+        auto count = [&](const PagedSeq& s) { return tiles(a, s); };
+        auto length = [&](const PagedSeq& s) { return work(a, s); };
+        if (!FEW) {
+            const int n = seqs.sum(a.B, count);
+            uncut = n / a.pieces * a.pieces;
+            if (uncut == n) return;
+            if (uncut > 0) {
+                int b = 0;
+                const int t = seqs.locate(uncut, b, count);
+                origin = seqs.sum(b, length) + begin(a, seqs.get(b), t);
+            }
+        }
+        const int total = seqs.sum(a.B, length) - origin, most = (total + kLeastWork - 1) / kLeastWork;
+        pieces = most < a.pieces ? most : a.pieces;
+        if (pieces <= 0) {
+            pieces = 0;
+            return;
+        }
+        each = int(unsigned(total) / unsigned(pieces));
+        more = total - each * pieces;
+    }
+    __device__ __forceinline__ int piece(int w) const { return origin + w * each + (w < more ? w : more); }
+    // The key, a multiple of 64 or past the last, at which a tile is cut that many units after its begin; `sees`: its keys.
+    static __device__ __forceinline__ int cut(const PagedArgs& a, int at, int length, int sees) {
+        if (at >= length) return sees;
+        const int64_t key = at <= kTileWork ? 0 : int64_t(at - kTileWork) << a.unit;
+        return key < sees ? int(key) : sees;
+    }
+};
+
+// A tile, and what is done of it.
 struct PagedItem {
     PagedSeq s;
-    int b, hk, tile, parts, part, from, end;  // end: past the last key that any of the tile's rows sees
-    int slot;
-    int64_t rows;  // of the sequence
+    int b, hk, tile, tiles;
+    int rows;             // of the sequence
+    int at, length;       // of the tile: the place in it, and its length on the line
+    int all;              // keys that the last of its rows sees
+    int from, end, slot;  // keys of this part; slot: of the workspace, or -1: these are all
 
-    // Item `item` of a key head; false: there are fewer.
+    template <class Line>
+    __device__ __forceinline__ void enter(const PagedArgs& a, const PagedSeqs& seqs) {
+        s = seqs.get(b);
+        tiles = Line::tiles(a, s);
+        rows = s.taken * a.r;
+    }
+    template <class Line, int R>
+    __device__ __forceinline__ void aim(const PagedArgs& a) {
+        length = Line::begin(a, s, tile + 1) - Line::begin(a, s, tile);
+        all = sees((tile + 1) * R - 1, a);
+    }
+    // Tile number k of all, to be taken whole.
     template <bool FEW, int R>
-    __device__ __forceinline__ bool of(const PagedArgs& a, const PagedCut& cut, int item, int head) {
-        const int lane = threadIdx.x & 63;
-        int64_t base = 0;
-        int found = -1, local = 0;
-        for (int b0 = 0; b0 < a.B; b0 += kWave) {
-            int items = 0;
-            if (b0 + lane < a.B) {
-                const PagedSeq s = paged_seq(a, b0 + lane);
-                items = tiles_of<FEW, R>(a, s) * cut.parts(s);
-            }
-            int upto = items;
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const int o = __shfl_up(upto, d);
-                if (lane >= d) upto += o;
-            }
-            const uint64_t past = __ballot(base + upto > item);
-            if (past) {
-                const int at = __ffsll((unsigned long long)past) - 1;
-                found = b0 + at;
-                local = int(item - base) - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(items, at));
-                break;
-            }
-            base += __builtin_amdgcn_readlane(upto, 63);
-        }
-        if (found < 0) return false;
-        b = __builtin_amdgcn_readfirstlane(found);
-        hk = head;
-        s = paged_seq(a, b);
-        rows = int64_t(s.taken) * a.r;
-        parts = cut.parts(s);
-        const int tiles = tiles_of<FEW, R>(a, s);
-        part = local % parts;
-        tile = tiles - 1 - local / parts;  // (those that see the most keys first)
-        slot = item;
-        end = sees(int64_t(tile + 1) * R - 1, a);
-        from = part * cut.chunk;
-        if (parts > 1 && end - from > cut.chunk) end = from + cut.chunk;
+    __device__ __forceinline__ bool number(const PagedArgs& a, const PagedSeqs& seqs, int k) {
+        typedef PagedLine<FEW, R> Line;
+        tile = seqs.locate(k, b, [&](const PagedSeq& o) { return Line::tiles(a, o); });
+        if (tile < 0) return false;
+        enter<Line>(a, seqs);
+        aim<Line, R>(a);
+        at = 0;
         return true;
     }
+    // The tile at place x of the line.
     template <bool FEW, int R>
-    static __device__ __forceinline__ int tiles_of(const PagedArgs& a, const PagedSeq& s) {
-        return PagedCut::tiles<FEW, R>(a, s);
+    __device__ __forceinline__ bool find(const PagedArgs& a, const PagedSeqs& seqs, int x) {
+        typedef PagedLine<FEW, R> Line;
+        at = seqs.locate(x, b, [&](const PagedSeq& o) { return Line::work(a, o); });
+        if (at < 0) return false;
+        enter<Line>(a, seqs);
+        int lo = 0, hi = tiles;  // the last tile that begins at `at` or before
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (Line::begin(a, s, mid) <= at) lo = mid;
+            else hi = mid;
+        }
+        tile = lo;
+        at -= Line::begin(a, s, tile);
+        aim<Line, R>(a);
+        return true;
+    }
+    // The tile after it, if there is one.
+    template <bool FEW, int R>
+    __device__ __forceinline__ bool next(const PagedArgs& a, const PagedSeqs& seqs) {
+        typedef PagedLine<FEW, R> Line;
+        at = 0;
+        if (++tile >= tiles) {
+            tile = 0;
+            do {
+                if (++b >= a.B) return false;
+                enter<Line>(a, seqs);
+            } while (tiles == 0);
+        }
+        aim<Line, R>(a);
+        return true;
+    }
+    // What piece w does of the tile with `units` of the line from its place on. False: nothing.
+    template <class Line>
+    __device__ __forceinline__ bool take(const PagedArgs& a, int w, int units) {
+        from = Line::cut(a, at, length, all);
+        end = Line::cut(a, at + units, length, all);
+        if (all == 0) {
+            slot = -1;
+            return at == 0;
+        }
+        slot = from == 0 && end == all ? -1 : from > 0 ? 2 * w : 2 * w + 1;
+        return true;
     }
     // How many keys row i of the sequence sees (a row past its last: as many as that).
-    __device__ __forceinline__ int sees(int64_t i, const PagedArgs& a) const {
+    __device__ __forceinline__ int sees(int i, const PagedArgs& a) const {
         if (i >= rows) i = rows - 1;
-        const int n = s.length - s.n + int(i / a.r) + 1;
+        const int n = s.length - s.n + int(unsigned(i) / unsigned(a.r)) + 1;
         return n < 0 ? 0 : n > s.length ? s.length : n;
     }
-    __device__ __forceinline__ int64_t out_row(int64_t i, const PagedArgs& a) const { return (s.first + i / a.r) * a.Hq + hk * a.r + i % a.r; }
-    template <typename DT>
-    __device__ __forceinline__ const DT* query(int64_t i, const PagedArgs& a) const {
-        if (i >= rows) return nullptr;
-        return reinterpret_cast<const DT*>(a.q) + (s.first + i / a.r) * a.qs[0] + (hk * a.r + i % a.r) * a.qs[1];
+    __device__ __forceinline__ int64_t out_row(int i, const PagedArgs& a) const {
+        const unsigned t = unsigned(i) / unsigned(a.r);
+        return int64_t(s.first + t) * a.Hq + hk * a.r + (i - int(t) * a.r);
     }
-    // Four dimensions of row i: to the part, or finished. R: rows of a tile.
+    template <typename DT>
+    __device__ __forceinline__ const DT* query(int i, const PagedArgs& a) const {
+        if (i >= rows) return nullptr;
+        const unsigned t = unsigned(i) / unsigned(a.r);
+        return reinterpret_cast<const DT*>(a.q) + int64_t(s.first + t) * a.qs[0] + (hk * a.r + (i - int(t) * a.r)) * a.qs[1];
+    }
+    // A row's outputs, four dimensions of them at `d`: to the part, or finished. R: rows of a tile.
     template <typename DT, int R>
-    __device__ __forceinline__ void store(int64_t i, int d, f32x4 o, float m, float z, const PagedArgs& a) const {
-        if (parts > 1) {
-            const int64_t at = (int64_t(hk) * a.slots + slot) * R + i % R;
-            *reinterpret_cast<f32x4*>(a.part_acc + at * a.D + d) = o;
-            if (d == 0) a.part_ml[at] = float2{m, z};
+    __device__ __forceinline__ void store(int i, int64_t out, int d, f32x4 o, float m, float z, const PagedArgs& a) const {
+        if (slot >= 0) {
+            const int64_t place = (int64_t(hk) * a.pieces * 2 + slot) * R + i % R;
+            *reinterpret_cast<f32x4*>(a.part_acc + place * a.D + d) = o;
+            if (d == 0) a.part_ml[place] = float2{m, z};
         } else {
-            finish<DT>(out_row(i, a), d, o, m, z, a);
+            finish<DT>(out, d, o, m, z, a);
         }
     }
     // (a sum of 0 has no keys; one of NaN, of a NaN among them or the query, makes the row NaN)
@@ -224,18 +334,17 @@ struct PageNumbers {
 
 // Sixteen keys: where the first is, how far the last that exists is from it, and whether there is a page.
 struct KeyGroup {
-    int64_t at_k, at_v;  // bytes from the caches' begin
+    uint64_t at_k, at_v;  // bytes from the key head's begin
     int last;
     bool there;
-    template <typename DT>
-    __device__ __forceinline__ void of(const PagedArgs& a, int page, int key, int end, int hk) {
+    __device__ __forceinline__ void of(const PagedArgs& a, int page, int key, int end) {
         const int in_end = (end - 1) & ~(kKeyGroup - 1);
         key = key < in_end ? key : in_end;
         last = end - 1 - key < kKeyGroup - 1 ? end - 1 - key : kKeyGroup - 1;
         there = unsigned(page) < unsigned(a.pages);
-        const int64_t p = there ? page : 0, t = key & ((1 << a.shift) - 1);
-        at_k = (p * a.ks[0] + t * a.ks[1] + hk * a.ks[2]) * int64_t(sizeof(DT));
-        at_v = (p * a.vs[0] + t * a.vs[1] + hk * a.vs[2]) * int64_t(sizeof(DT));
+        const uint64_t p = there ? page : 0, t = unsigned(key) & ((1u << a.shift) - 1);
+        at_k = p * uint64_t(a.ks[0]) + t * uint32_t(a.ks[1]);
+        at_v = p * uint64_t(a.vs[0]) + t * uint32_t(a.vs[1]);
     }
 };
 
@@ -276,6 +385,30 @@ __device__ __forceinline__ void hide_scores(f32x4 (&s)[KT], int first, int sees,
             if (first + 16 * kt + i >= sees || (out >> kt & 1)) s[kt][i] = kNegInf;
 }
 
+// Share k of a key head: a tile that is not cut, or a piece of the line, tile by tile.
+template <bool FEW, int R, class F>
+__device__ __forceinline__ void paged_share(const PagedArgs& a, const PagedSeqs& seqs, int k, int hk, F&& tile) {
+    PagedLine<FEW, R> line;
+    line.plan(a, seqs);
+    PagedItem it;
+    it.hk = hk;
+    int x = 0, end = 0, w = k - line.uncut;
+    if (w < 0) {
+        if (!it.number<FEW, R>(a, seqs, k)) return;
+    } else {
+        if (w >= line.pieces) return;
+        x = line.piece(w);
+        end = line.piece(w + 1);
+        if (!it.find<FEW, R>(a, seqs, x)) return;
+    }
+    for (;;) {
+        const int rest = it.length - it.at, units = w < 0 || rest < end - x ? rest : end - x;
+        if (it.take<PagedLine<FEW, R>>(a, w, units)) tile(it);
+        x += units;
+        if (x >= end || !it.next<FEW, R>(a, seqs)) return;
+    }
+}
+
 // ------------------------------------------------------------- few rows: keys dealt to waves
 
 // Keys [from, end) of one item, blocks wave, wave + W, ..., by a wave with QT tiles of sixteen rows.
@@ -293,17 +426,18 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
     Block b;
     KeyGroup at[G];
     const uint32_t sk = uint32_t(a.ks[1]), sv = uint32_t(a.vs[1]);
+    const char *keys = reinterpret_cast<const char*>(a.k) + it.hk * a.ks[2], *values = reinterpret_cast<const char*>(a.v) + it.hk * a.vs[2];
     auto aim = [&](int n, int key) {  // block n of the wave, at `key`
 #pragma unroll
-        for (int x = 0; x < G; ++x) at[x].template of<DT>(a, numbers.get(n, x), key + kKeyGroup * x, end, it.hk);
+        for (int x = 0; x < G; ++x) at[x].of(a, numbers.get(n, x), key + kKeyGroup * x, end);
     };
     auto row = [&](int r, const KeyGroup& k) { return uint32_t(r < k.last ? r : k.last); };
     auto load_k = [&]() {
         constexpr int kSteps = ND / Block::kKRows;
 #pragma unroll
         for (int kt = 0; kt < Block::kKRows; ++kt) {
-            const char* base = reinterpret_cast<const char*>(a.k) + at[kt].at_k;
-            const uint32_t first = row(c, at[kt]) * sk * uint32_t(sizeof(DT)) + 16u * g;
+            const char* base = keys + at[kt].at_k;
+            const uint32_t first = row(c, at[kt]) * sk + 16u * g;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 uint32_t o = first + 64u * s;
@@ -317,10 +451,10 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
     };
     auto load_v = [&]() {
         if constexpr (kWide) {
-            const char* base = reinterpret_cast<const char*>(a.v) + at[0].at_v;
+            const char* base = values + at[0].at_v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t first = (row(4 * g + i, at[0]) * sv + c) * 4u;
+                const uint32_t first = row(4 * g + i, at[0]) * sv + 4u * c;
 #pragma unroll
                 for (int t = 0; t < ND; ++t) {
                     uint32_t o = first + 64u * t;
@@ -337,8 +471,8 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
                 constexpr int kRows = 64 / kVecs;  // of a load
                 const KeyGroup& k = at[i * kRows / kKeyGroup];
                 const int r = (lane / kVecs + i * kRows) % kKeyGroup, piece = lane % kVecs;
-                const uint32_t o = (row(r, k) * sv + 8u * (EXACT || 8 * piece < D ? piece : D / 8 - 1)) * 2u;
-                b.v[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v) + k.at_v + o);
+                const uint32_t o = row(r, k) * sv + 16u * (EXACT || 8 * piece < D ? piece : D / 8 - 1);
+                b.v[i] = *reinterpret_cast<const u32x4*>(values + k.at_v + o);
             }
         }
     };
@@ -434,15 +568,8 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
 
 // Sequences of few rows: four waves on the same rows, each with keys of its own.
 template <typename DT, int ND, int QT, bool EXACT>
-__global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs a) {
+__device__ __forceinline__ void paged_few_tile(const PagedArgs& a, const PagedItem& it, char* mem, float (*s_m)[kTileRows], float (*s_l)[kTileRows]) {
     constexpr int W = kAttnWaves, R = QT * kTileRows;
-    __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, W>()];
-    __shared__ float s_m[W][kTileRows], s_l[W][kTileRows];
-    const int block = int(grid_row());
-    PagedCut cut;
-    cut.plan<true, R>(a);
-    PagedItem it;
-    if (!it.template of<true, R>(a, cut, block / a.Hkv, block % a.Hkv)) return;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = EXACT ? 16 * ND : int(a.D);
@@ -451,17 +578,16 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs
     int sees[QT];
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
-        w.load_query(x, it.template query<DT>(kTileRows * x + c, a), D, query_sign<DT>(a.scale2), lane);
+        w.load_query(x, it.query<DT>(kTileRows * x + c, a), D, query_sign<DT>(a.scale2), lane);
         sees[x] = it.sees(kTileRows * x + c, a);
         if (sees[x] > it.end) sees[x] = it.end;
     }
     int least = it.sees(0, a);
     if (least > it.end) least = it.end;
-    paged_run<DT, ND, QT, W, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(s_mem) + wave * 32 * (16 * ND + 16), wave,
-                                    lane);
+    paged_run<DT, ND, QT, W, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(mem) + wave * 32 * (16 * ND + 16), wave, lane);
 
     // the waves join, sixteen rows at a time
-    float* join = reinterpret_cast<float*>(s_mem);
+    float* join = reinterpret_cast<float*>(mem);
     constexpr int kJoinRow = 16 * ND + 4;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
@@ -492,9 +618,57 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs
                 z = fmaf(keep, s_l[v][i], z);
                 o += keep * *reinterpret_cast<const f32x4*>(join + (v * kTileRows + i) * kJoinRow + d);
             }
-            it.template store<DT, R>(row0 + i, d, o, m, z, a);
+            it.template store<DT, R>(row0 + i, it.out_row(row0 + i, a), d, o, m, z, a);
         }
     }
+}
+
+template <typename DT, int ND, int QT, bool EXACT>
+__global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs a) {
+    __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, kAttnWaves>()];
+    __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
+    const int block = int(grid_row());
+    const PagedSeqs seqs(a);
+    PagedItem it;
+    it.hk = block % a.Hkv;
+    if (it.number<true, QT * kTileRows>(a, seqs, block / a.Hkv) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length)) paged_few_tile<DT, ND, QT, EXACT>(a, it, s_mem, s_m, s_l);
+}
+
+// The same with a wave on each piece of the line: no barrier, and nothing to join within the workgroup.
+template <typename DT, int ND, int QT, bool EXACT>
+__global__ __launch_bounds__(kAttnWaves * kWave) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_solo_kernel(PagedArgs a) {
+    constexpr int R = QT * kTileRows;
+    __shared__ __attribute__((aligned(16))) char s_mem[sizeof(DT) == 2 ? kAttnWaves * 32 * (16 * ND + 16) * 2 : 16];
+    const int block = int(grid_row()), lane = threadIdx.x & 63, c = lane & 15, g4 = lane >> 4;
+    const int wave = agreed(int(threadIdx.x >> 6));
+    const int D = EXACT ? 16 * ND : int(a.D);
+    const PagedSeqs seqs(a);
+    paged_share<true, R>(a, seqs, block / a.Hkv * kAttnWaves + wave, block % a.Hkv, [&](const PagedItem& it) {
+        AttnWave<DT, ND, QT, EXACT> w;
+        w.clear();
+        int sees[QT];
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+            w.load_query(x, it.query<DT>(kTileRows * x + c, a), D, query_sign<DT>(a.scale2), lane);
+            sees[x] = it.sees(kTileRows * x + c, a);
+            if (sees[x] > it.end) sees[x] = it.end;
+        }
+        int least = it.sees(0, a);
+        if (least > it.end) least = it.end;
+        paged_run<DT, ND, QT, 1, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(s_mem) + wave * 32 * (16 * ND + 16), 0, lane);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+            float l = w.l[x];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            const int row = kTileRows * x + c;
+            if (row >= it.rows) continue;
+            const int64_t out = it.out_row(row, a);
+#pragma unroll
+            for (int t = 0; t < ND; ++t)
+                if (EXACT || 16 * t + 4 * g4 < D) it.store<DT, R>(row, out, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
+        }
+    });
 }
 
 // ------------------------------------------------------------- many rows: waves share keys
@@ -527,6 +701,7 @@ struct PagedShared {
         numbers.begin(a.table + int64_t(it.b) * a.ld_table, from, kKeys, end, a.shift,
                       [&](int i) { return first_row(i) / kKeyGroup * kKeyGroup; });
         const uint32_t sk = uint32_t(a.ks[1]), sv = uint32_t(a.vs[1]);
+        const char *keys = reinterpret_cast<const char*>(a.k) + it.hk * a.ks[2], *values = reinterpret_cast<const char*>(a.v) + it.hk * a.vs[2];
         u32x4 k[kPieces], v[kPieces];
         uint32_t out = 0;  // pieces without a page
         auto load = [&](int n) {
@@ -535,12 +710,12 @@ struct PagedShared {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 KeyGroup at;
-                at.template of<DT>(a, numbers.get(n, i), j + first_row(i) / kKeyGroup * kKeyGroup, end, it.hk);
+                at.of(a, numbers.get(n, i), j + first_row(i) / kKeyGroup * kKeyGroup, end);
                 out |= at.there ? 0u : 1u << i;
                 const int piece = lane % kVecs, r = (first_row(i) + lane / kVecs) % kKeyGroup;
-                const uint32_t row = r < at.last ? r : at.last, d = uint32_t(kVec) * (EXACT || kVec * piece < D ? piece : D / kVec - 1);
-                k[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.k) + at.at_k + (row * sk + d) * uint32_t(sizeof(DT)));
-                v[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v) + at.at_v + (row * sv + d) * uint32_t(sizeof(DT)));
+                const uint32_t row = r < at.last ? r : at.last, d = 16u * (EXACT || kVec * piece < D ? piece : D / kVec - 1);
+                k[i] = *reinterpret_cast<const u32x4*>(keys + at.at_k + row * sk + d);
+                v[i] = *reinterpret_cast<const u32x4*>(values + at.at_v + row * sv + d);
             }
         };
         auto put = [&](int turn) {
@@ -585,15 +760,24 @@ struct PagedShared {
                                 s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[i], __uint_as_float(w.q[x][t][i]), s[x][kt], 0, 0, 0);
                     }
             } else {
+                // (the next keys' operand is on its way while this one's products run)
+                bf16x8 k8[2][ND / 2];
+                auto ask = [&](int kt) {
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
+                    for (int d = 0; d < ND / 2; ++d) k8[kt & 1][d] = *reinterpret_cast<const bf16x8*>(lk + (16 * kt + c) * kKRow + 32 * d + 8 * g);
+                };
+                ask(0);
 #pragma unroll
-                    for (int d = 0; d < ND / 2; ++d) {
-                        const bf16x8 k8 = *reinterpret_cast<const bf16x8*>(lk + (16 * kt + c) * kKRow + 32 * d + 8 * g);
+                for (int kt = 0; kt < KT; ++kt) {
+                    if (kt + 1 < KT) ask(kt + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int d = 0; d < ND / 2; ++d)
 #pragma unroll
                         for (int x = 0; x < QT; ++x)
-                            s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(bf16x8, w.q[x][d]), s[x][kt], 0, 0, 0);
-                    }
+                            s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[kt & 1][d], __builtin_bit_cast(bf16x8, w.q[x][d]), s[x][kt], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             uint32_t hidden = 0;
 #pragma unroll
@@ -618,18 +802,34 @@ struct PagedShared {
                                 w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v1, s[x][kt][i], w.acc[x][t], 0, 0, 0);
                         }
             } else {
+                constexpr int kStep = 4;  // dimensions' tiles asked for at a time
+                bf16x8 p[QT][KT / 2], v8[2][kStep];
 #pragma unroll
-                for (int h = 0; h < KT / 2; ++h) {
-                    bf16x8 p[QT];
+                for (int h = 0; h < KT / 2; ++h)
 #pragma unroll
-                    for (int x = 0; x < QT; ++x) p[x] = weights_operand(s[x][2 * h], s[x][2 * h + 1]);
-                    const DT* at = lv + (32 * h + 4 * g + (c >> 2)) * kVRow + 4 * (c & 3);
+                    for (int x = 0; x < QT; ++x) p[x][h] = weights_operand(s[x][2 * h], s[x][2 * h + 1]);
+                const DT* base = lv + (4 * g + (c >> 2)) * kVRow + 4 * (c & 3);
+                auto ask = [&](int n) {
 #pragma unroll
-                    for (int t = 0; t < ND; ++t) {
-                        const bf16x8 b = values_operand(reinterpret_cast<const bf16_t*>(at + 16 * t), kVRow);
-#pragma unroll
-                        for (int x = 0; x < QT; ++x) w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, p[x], w.acc[x][t], 0, 0, 0);
+                    for (int i = 0; i < kStep; ++i) {
+                        const int t = n % (ND / kStep) * kStep + i, h = n / (ND / kStep);
+                        v8[n & 1][i] = values_operand(reinterpret_cast<const bf16_t*>(base + 32 * h * kVRow + 16 * t), kVRow);
                     }
+                };
+                ask(0);
+                constexpr int kSteps = ND / kStep * (KT / 2);
+#pragma unroll
+                for (int n = 0; n < kSteps; ++n) {
+                    if (n + 1 < kSteps) ask(n + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < kStep; ++i)
+#pragma unroll
+                        for (int x = 0; x < QT; ++x) {
+                            const int t = n % (ND / kStep) * kStep + i;
+                            w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8[n & 1][i], p[x][n / (ND / kStep)], w.acc[x][t], 0, 0, 0);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
@@ -637,20 +837,13 @@ struct PagedShared {
 };
 
 template <typename DT, int ND, int QT, int W, bool EXACT>
-__global__ __launch_bounds__(W * kWave) void paged_many_kernel(PagedArgs a) {
+__device__ __forceinline__ void paged_many_tile(const PagedArgs& a, const PagedItem& it, char* mem, uint32_t (*s_out)[4]) {
     constexpr int R = W * QT * kTileRows;
     typedef PagedShared<DT, ND, QT, W, EXACT> Shared;
-    __shared__ __attribute__((aligned(16))) char s_mem[Shared::kLds];
-    __shared__ uint32_t s_out[2][4];
-    const int block = int(grid_row());
-    PagedCut cut;
-    cut.plan<false, R>(a);
-    PagedItem it;
-    if (!it.template of<false, R>(a, cut, block / a.Hkv, block % a.Hkv)) return;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = EXACT ? 16 * ND : int(a.D);
-    const int64_t row0 = int64_t(it.tile) * R + wave * QT * kTileRows;
+    const int row0 = it.tile * R + wave * QT * kTileRows;
     AttnWave<DT, ND, QT, EXACT> w;
     w.clear();
     int sees[QT];
@@ -662,19 +855,33 @@ __global__ __launch_bounds__(W * kWave) void paged_many_kernel(PagedArgs a) {
     }
     int least = it.sees(row0, a), most = row0 < it.rows ? it.sees(row0 + QT * kTileRows - 1, a) : 0;
     if (least > it.end) least = it.end;
-    Shared::run(w, a, it, sees, least, most, D, score_scale(a.scale2), reinterpret_cast<DT*>(s_mem), s_out, tid);
+    Shared::run(w, a, it, sees, least, most, D, score_scale(a.scale2), reinterpret_cast<DT*>(mem), s_out, tid);
     const int g4 = lane >> 4;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
         float l = w.l[x];
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-        const int64_t row = row0 + x * kTileRows + c;
+        const int row = row0 + x * kTileRows + c;
         if (row >= it.rows) continue;
+        const int64_t out = it.out_row(row, a);
 #pragma unroll
         for (int t = 0; t < ND; ++t)
-            if (EXACT || 16 * t + 4 * g4 < D) it.template store<DT, R>(row, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
+            if (EXACT || 16 * t + 4 * g4 < D) it.template store<DT, R>(row, out, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
     }
+}
+
+template <typename DT, int ND, int QT, int W, bool EXACT>
+__global__ __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(ND > 8 ? 1 : 2, ND > 8 ? 1 : 2))) void paged_many_kernel(PagedArgs a) {
+    constexpr int R = W * QT * kTileRows;
+    __shared__ __attribute__((aligned(16))) char s_mem[PagedShared<DT, ND, QT, W, EXACT>::kLds];
+    __shared__ uint32_t s_out[2][4];
+    const int block = int(grid_row());
+    const PagedSeqs seqs(a);
+    paged_share<false, R>(a, seqs, block / a.Hkv, block % a.Hkv, [&](const PagedItem& it) {
+        paged_many_tile<DT, ND, QT, W, EXACT>(a, it, s_mem, s_out);
+        __syncthreads();  // (what is in LDS has been read)
+    });
 }
 
 // The sequence that row t of q belongs to, or -1: every lane with the answer. Each round looks at 64 of the
@@ -700,61 +907,78 @@ __device__ __forceinline__ int sequence_of(const PagedArgs& a, int64_t t) {
     return lo < a.B && a.q_start[lo] <= t && t < a.q_start[lo + 1] ? lo : -1;
 }
 
-// Joins the parts of a row, o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i: one row a workgroup,
-// `groups` of D / 4 lanes (four dimensions each) on every groups-th part.
+// Joins the parts of the tiles that are cut, o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i: a tile by the workgroups of the
+// first cut in it, each with kJoinRows of its rows, D / 4 lanes (four dimensions each) a row; where that leaves lanes, several
+// groups of them on parts in turn.
+constexpr int kJoinRows = 16;
 template <typename DT, bool FEW, int R>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     __shared__ f32x4 s_o[256];
     __shared__ float s_z[256];
-    const int64_t out = grid_row(), t = out / a.Hq;
-    if (t >= a.tokens) return;
-    const int b = __builtin_amdgcn_readfirstlane(sequence_of(a, t));
-    if (b < 0) return;
-    const int h = int(out % a.Hq), hk = h / a.r;
-    const PagedSeq s = paged_seq(a, b);
-    const int tiles = PagedCut::tiles<FEW, R>(a, s);
-    if (tiles == 0 || t < s.first || t - s.first >= s.taken) return;
-    PagedCut cut;
-    cut.plan<FEW, R>(a);
-    const int parts = cut.parts(s);
-    if (parts == 1) return;
-    // the sequence's first slot: the items of those before it
-    int64_t before = 0;
-    for (int i = int(threadIdx.x) & 63; i < b; i += kWave) {
-        const PagedSeq o = paged_seq(a, i);
-        before += int64_t(PagedCut::tiles<FEW, R>(a, o)) * cut.parts(o);
+    int64_t item = grid_row();
+    const int block = int(item % (R / kJoinRows));
+    item /= R / kJoinRows;
+    const int hk = int(item % a.Hkv), w0 = int(item / a.Hkv);  // the cut after piece w0
+    const PagedSeqs seqs(a);
+    PagedLine<FEW, R> line;
+    line.plan(a, seqs);
+    if (w0 + 1 >= line.pieces) return;
+    PagedItem it;
+    it.hk = hk;
+    const int x = line.piece(w0 + 1);
+    if (!it.find<FEW, R>(a, seqs, x) || it.at == 0 || it.all == 0) return;
+    const int tile = x - it.at;  // its begin on the line
+    if (line.piece(w0) > tile) return;  // (a piece before ends in it, too)
+    const int first_row = it.tile * R + block * kJoinRows;
+    if (first_row >= it.rows) return;
+    int parts = 2;
+    while (w0 + parts < line.pieces && line.piece(w0 + parts) < tile + it.length) ++parts;
+    // nothing to join where one of them has all of the keys
+    bool alone = false;
+    for (int i = int(threadIdx.x) & 63; i < parts; i += kWave) {
+        const int y = line.piece(w0 + i), z = line.piece(w0 + i + 1);
+        alone |= line.cut(a, y > tile ? y - tile : 0, it.length, it.all) == 0 && line.cut(a, z - tile, it.length, it.all) == it.all;
     }
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) before += __shfl_xor(before, d);
-    if (before + int64_t(tiles) * parts > a.slots) return;  // (starts that fall: more rows than there are)
-    const int64_t row = (t - s.first) * a.r + h % a.r;
-    const int tile = int(row / R);
-    const int64_t first = int64_t(hk) * a.slots + before + int64_t(tiles - 1 - tile) * parts;
-    auto place = [&](int i) { return (first + i) * R + row % R; };
-    const int lanes = a.D / 4, groups = 256 / lanes;
-    const int group = int(threadIdx.x) / lanes, d = 4 * (int(threadIdx.x) % lanes);
-    float m = kNegInf;
-    for (int i = int(threadIdx.x) & 63; i < parts; i += kWave) m = fmaxf(m, a.part_ml[place(i)].x);
-    m = max_wave(m);
-    float z = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (group < groups) {
-        for (int i = group; i < parts; i += groups) {
-            const float2 ml = a.part_ml[place(i)];
-            const float keep = ml.x == kNegInf ? 0.f : exp2_fast(ml.x - m);
-            z = fmaf(keep, ml.y, z);
-            o += keep * *reinterpret_cast<const f32x4*>(a.part_acc + place(i) * a.D + d);
+    if (__any(alone)) return;
+    const int lanes = a.D / 4, fit = 256 / lanes;
+    const int count = it.rows - first_row < kJoinRows ? it.rows - first_row : kJoinRows;
+    const int at_once = count < fit ? count : fit, groups = fit / at_once;
+    const int which = int(threadIdx.x) / lanes, d = 4 * (int(threadIdx.x) % lanes);
+    for (int r0 = 0; r0 < count; r0 += at_once) {
+        const int row = r0 + which % at_once, group = which / at_once;
+        const bool on = group < groups && row < count;
+        auto place = [&](int i) {
+            const int w = w0 + i;
+            const int y = line.piece(w);
+            const bool later = y > tile && line.cut(a, y - tile, it.length, it.all) > 0;
+            return (int64_t(hk) * a.pieces * 2 + 2 * w + (later ? 0 : 1)) * R + block * kJoinRows + row;
+        };
+        float m = kNegInf, z = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        if (on) {
+            for (int i = 0; i < parts; ++i) m = fmaxf(m, a.part_ml[place(i)].x);
+            for (int i = group; i < parts; i += groups) {
+                const float2 ml = a.part_ml[place(i)];
+                const float keep = ml.x == kNegInf ? 0.f : exp2_fast(ml.x - m);
+                z = fmaf(keep, ml.y, z);
+                o += keep * *reinterpret_cast<const f32x4*>(a.part_acc + place(i) * a.D + d);
+            }
+        }
+        if (groups > 1) {
+            __syncthreads();
+            s_o[threadIdx.x] = o;
+            s_z[threadIdx.x] = z;
+            __syncthreads();
+            if (on && group == 0)
+                for (int i = 1; i < groups; ++i) {
+                    o += s_o[threadIdx.x + i * at_once * lanes];
+                    z += s_z[threadIdx.x + i * at_once * lanes];
+                }
+        }
+        if (on && group == 0) {
+            PagedItem::finish<DT>(it.out_row(first_row + row, a), d, o, m, z, a);
         }
     }
-    s_o[threadIdx.x] = o;
-    s_z[threadIdx.x] = z;
-    __syncthreads();
-    if (group != 0) return;
-    for (int i = 1; i < groups; ++i) {
-        o += s_o[threadIdx.x + i * lanes];
-        z += s_z[threadIdx.x + i * lanes];
-    }
-    PagedItem::finish<DT>(out, d, o, m, z, a);
 }
 
 // ------------------------------------------------------------- writing
@@ -796,16 +1020,16 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
     const int page = a.at.table[b * a.at.ld_table + (place >> a.at.shift)];
     if (unsigned(page) >= unsigned(a.at.pages)) return;
     const int64_t in = place & ((1 << a.at.shift) - 1);
-    DT* to_k = reinterpret_cast<DT*>(a.k) + page * a.at.ks[0] + in * a.at.ks[1];
-    DT* to_v = reinterpret_cast<DT*>(a.v) + page * a.at.vs[0] + in * a.at.vs[1];
+    char* to_k = a.k + page * a.at.ks[0] + in * a.at.ks[1];
+    char* to_v = a.v + page * a.at.vs[0] + in * a.at.vs[1];
     for (int at = lane; at < all; at += U * kWave) {
         if (at != lane) load(at);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = at + u * kWave, h = i / a.pieces, d = i % a.pieces * kVec;
             if (i < all) {
-                *reinterpret_cast<u32x4*>(to_k + h * a.at.ks[2] + d) = x[u];
-                *reinterpret_cast<u32x4*>(to_v + h * a.at.vs[2] + d) = y[u];
+                *reinterpret_cast<u32x4*>(to_k + h * a.at.ks[2] + d * int(sizeof(DT))) = x[u];
+                *reinterpret_cast<u32x4*>(to_v + h * a.at.vs[2] + d * int(sizeof(DT))) = y[u];
             }
         }
     }

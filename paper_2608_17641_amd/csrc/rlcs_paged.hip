@@ -34,73 +34,87 @@ bool whole_vectors(const int64_t* s, int n, int64_t vec) {
 
 // Sequences of up to this many rows a key head are the first kernel's.
 constexpr int64_t kFewRows = 2 * kTileRows;
-// Items that parts should come to, and the keys of the shortest part.
-constexpr int64_t kWantFew = 1536, kWantMany = 512, kLeastFew = 256, kLeastMany = 512;
+// Pieces that all keys are dealt out in: as many as the GPU holds at once. Waves of the first kernel, two a SIMD with one tile of
+// rows and one with two; workgroups of the second, one a CU.
+constexpr int64_t kPiecesFew = 1024, kPiecesFew2 = 1024, kPiecesMany = 256;
+// Where no sequence can have more keys than this, all are taken whole: no second kernel.
+constexpr int64_t kWholeKeys = 512;
 
 // Which kernels a call takes, and their parts.
 struct PagedPlan {
     bool few, many;
     int few_tiles;       // of sixteen rows, of the first kernel
     int64_t many_rows;   // of a tile of the second: 64, 128 or 256
-    int64_t few_want, few_slots, many_want, many_slots;
+    int64_t few_pieces, many_pieces;  // a key head
 };
 
-bool make_plan(PagedPlan& p, int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_chunk, bool ragged, bool bf16) {
+// `most_keys`: no sequence has more (0: not known).
+bool make_plan(PagedPlan& p, int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_chunk, bool ragged, bool bf16,
+               int64_t most_keys = 0) {
     const int64_t r = Hq / Hkv, most = max_chunk * r;
     p = PagedPlan{};
     p.few = ragged || most <= kFewRows;
     p.many = most > kFewRows;
     p.few_tiles = most <= kTileRows ? 1 : 2;
     p.many_rows = D > 128 || tokens * r <= 64 * B ? 64 : bf16 ? 256 : 128;
-    p.few_want = ceil_div(kWantFew, Hkv);
-    p.few_slots = p.few_want + B;
-    const int64_t tiles = tokens * r / p.many_rows;
-    p.many_want = tiles * Hkv >= kWantMany ? 0 : ceil_div(kWantMany, Hkv);
-    p.many_slots = p.many_want + tiles + B;
-    return p.few_slots <= INT32_MAX / Hkv && p.many_slots <= INT32_MAX / Hkv;
+    p.few_pieces = most_keys && most_keys <= kWholeKeys ? 0 : ceil_div(ceil_div(p.few_tiles == 1 ? kPiecesFew : kPiecesFew2, Hkv), kAttnWaves) * kAttnWaves;
+    p.many_pieces = ceil_div(kPiecesMany, Hkv);
+    return B <= INT32_MAX / Hkv && tokens * r / 64 + B <= INT32_MAX / Hkv;
 }
-size_t part_bytes(int64_t want, int64_t slots, int64_t rows, int64_t Hkv, int64_t D) {
-    return want ? size_t(Hkv * slots * rows) * size_t(4 * D + 8) : 0;
-}
+size_t part_bytes(int64_t pieces, int64_t rows, int64_t Hkv, int64_t D) { return size_t(Hkv * 2 * pieces * rows) * size_t(4 * D + 8); }
 size_t plan_bytes(const PagedPlan& p, int64_t Hkv, int64_t D) {
-    const size_t x = p.few ? part_bytes(p.few_want, p.few_slots, p.few_tiles * kTileRows, Hkv, D) : 0;
-    const size_t y = p.many ? part_bytes(p.many_want, p.many_slots, p.many_rows, Hkv, D) : 0;
+    const size_t x = p.few ? part_bytes(p.few_pieces, p.few_tiles * kTileRows, Hkv, D) : 0;
+    const size_t y = p.many ? part_bytes(p.many_pieces, p.many_rows, Hkv, D) : 0;
     return x > y ? x : y;
 }
 
-// Gives a kernel its parts.
-void cut(PagedArgs& a, int64_t want, int64_t slots, int64_t least, int64_t rows, void* ws) {
-    a.want = int32_t(want);
-    a.slots = int32_t(slots);
-    a.least = int32_t(least);
+// Gives a kernel its pieces and their places in the workspace.
+void deal(PagedArgs& a, int64_t pieces, int64_t rows, void* ws) {
+    a.pieces = int32_t(pieces);
+    a.rise = double(rows) / (double(a.r) * double(1 << a.unit));
     a.part_acc = static_cast<float*>(ws);
-    a.part_ml = want ? reinterpret_cast<float2*>(a.part_acc + int64_t(a.Hkv) * slots * rows * a.D) : nullptr;
+    a.part_ml = pieces ? reinterpret_cast<float2*>(a.part_acc + int64_t(a.Hkv) * 2 * pieces * rows * a.D) : nullptr;
 }
 
+template <typename DT, bool FEW, int R>
+void launch_join(const PagedArgs& a, hipStream_t s) {
+    if (a.pieces > 1)
+        hipLaunchKernelGGL((paged_join_kernel<DT, FEW, R>), row_grid(int64_t(a.pieces - 1) * a.Hkv * (R / kJoinRows)), dim3(256), 0, s, a);
+}
+
+template <typename DT, int ND, int QT, bool EXACT>
+void launch_few(const PagedArgs& a, hipStream_t s) {
+    const dim3 block(kAttnWaves * kWave);
+    if (a.pieces == 0) {
+        hipLaunchKernelGGL((paged_few_kernel<DT, ND, QT, EXACT>), row_grid(int64_t(a.B) * a.Hkv), block, 0, s, a);
+    } else {
+        hipLaunchKernelGGL((paged_solo_kernel<DT, ND, QT, EXACT>), row_grid(int64_t(a.pieces / kAttnWaves) * a.Hkv), block, 0, s, a);
+        launch_join<DT, true, QT * kTileRows>(a, s);
+    }
+}
 template <typename DT, int ND, int QT>
 void launch_few(const PagedArgs& a, hipStream_t s) {
-    const dim3 grid = row_grid(int64_t(a.slots) * a.Hkv), block(kAttnWaves * kWave);
-    if (a.D == 16 * ND) hipLaunchKernelGGL((paged_few_kernel<DT, ND, QT, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((paged_few_kernel<DT, ND, QT, false>), grid, block, 0, s, a);
-    if (a.want) hipLaunchKernelGGL((paged_join_kernel<DT, true, QT * kTileRows>), row_grid(a.tokens * a.Hq), dim3(256), 0, s, a);
+    if (a.D == 16 * ND) launch_few<DT, ND, QT, true>(a, s);
+    else launch_few<DT, ND, QT, false>(a, s);
 }
 template <typename DT, int ND, int QT, int W>
 void launch_many(const PagedArgs& a, hipStream_t s) {
-    const dim3 grid = row_grid(int64_t(a.slots) * a.Hkv), block(W * kWave);
+    constexpr int64_t R = W * QT * kTileRows;
+    const dim3 grid = row_grid((a.tokens * a.r / R + a.B + a.pieces) * a.Hkv), block(W * kWave);
     if (a.D == 16 * ND) hipLaunchKernelGGL((paged_many_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((paged_many_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a);
-    if (a.want) hipLaunchKernelGGL((paged_join_kernel<DT, false, W * QT * kTileRows>), row_grid(a.tokens * a.Hq), dim3(256), 0, s, a);
+    launch_join<DT, false, R>(a, s);
 }
 
 template <typename DT, int ND>
 rlcs_status run_paged(PagedArgs a, const PagedPlan& p, void* ws, hipStream_t s) {
     if (p.few) {
-        cut(a, p.few_want, p.few_slots, kLeastFew, p.few_tiles * kTileRows, ws);
+        deal(a, p.few_pieces, p.few_tiles * kTileRows, ws);
         if (p.few_tiles == 1) launch_few<DT, ND, 1>(a, s);
         else launch_few<DT, ND, 2>(a, s);
     }
     if (p.many) {
-        cut(a, p.many_want, p.many_slots, kLeastMany, p.many_rows, ws);
+        deal(a, p.many_pieces, p.many_rows, ws);
         if constexpr (ND > 8) {
             launch_many<DT, ND, 1, 4>(a, s);
         } else {
@@ -114,6 +128,15 @@ rlcs_status run_paged(PagedArgs a, const PagedPlan& p, void* ws, hipStream_t s) 
 template <typename DT>
 rlcs_status run_paged(const PagedArgs& a, const PagedPlan& p, void* ws, hipStream_t s) {
     return a.D <= 64 ? run_paged<DT, 4>(a, p, ws, s) : a.D <= 128 ? run_paged<DT, 8>(a, p, ws, s) : run_paged<DT, 16>(a, p, ws, s);
+}
+
+// The unit of work, in which all of a key head's counts in 31 bits: tiles of 64 rows, of all keys that a table row may hold.
+int work_unit(const PagedArgs& a) {
+    const double tiles = double(a.tokens) * a.r / 64 + a.B, held = double(a.W) * double(1 << a.shift);
+    const double keys = held > double(a.tokens) ? held : double(a.tokens);
+    int unit = 6;
+    while (unit < 30 && tiles * (kTileWork + 3 + keys / double(1 << unit)) > double(1 << 30)) ++unit;
+    return unit;
 }
 
 bool good_page(int64_t page) { return page >= 16 && page <= 65536 && (page & (page - 1)) == 0; }
@@ -139,9 +162,10 @@ rlcs_status prepare(PagedArgs& a, const int32_t* table, const int32_t* length, c
     a.B = int32_t(B); a.W = int32_t(W); a.pages = int32_t(pages);
     while ((int64_t(1) << a.shift) < page) ++a.shift;
     a.Hkv = int32_t(Hkv); a.D = int32_t(D);
+    const int64_t es = int64_t(dtype_size(dtype));
     for (int i = 0; i < 3; ++i) {
-        a.ks[i] = ks[i];
-        a.vs[i] = vs[i];
+        a.ks[i] = ks[i] * es;
+        a.vs[i] = vs[i] * es;
     }
     return RLCS_OK;
 }
@@ -195,7 +219,7 @@ rlcs_status rlcs_paged_attn(const void* q, const void* k_cache, const void* v_ca
     if (max_chunk == 0 || max_chunk > tokens) max_chunk = tokens;
     if (!q_start) max_chunk = tokens / B;
     PagedPlan p;
-    if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, q_start != nullptr, bf16)) return RLCS_ERR_INVALID_ARG;
+    if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, q_start != nullptr, bf16, W * page)) return RLCS_ERR_INVALID_ARG;
     if (const size_t need = plan_bytes(p, Hkv, D)) {
         if (!ws || ws_bytes < need) return RLCS_ERR_WORKSPACE;
         if (!aligned(ws, 16)) return RLCS_ERR_INVALID_ARG;
@@ -205,6 +229,7 @@ rlcs_status rlcs_paged_attn(const void* q, const void* k_cache, const void* v_ca
     a.Hq = int32_t(Hq); a.r = int32_t(Hq / Hkv);
     a.max_chunk = int32_t(max_chunk);
     a.few_rows = int32_t(p.few_tiles * kTileRows);
+    a.unit = work_unit(a);
     a.scale2 = scale * kLog2e;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return bf16 ? run_paged<bf16_t>(a, p, ws, s) : run_paged<float>(a, p, ws, s);

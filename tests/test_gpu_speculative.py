@@ -77,7 +77,7 @@ def test_example_gradient():
     off = EPS * 128 * 60
     assert abs(float(loss) - float(want.detach())) <= 16 * off
     moved = was.double() - r.draft.head.double()
-    scale = float((h.abs().double().t() @ (lp.exp() + torch.zeros_like(lp).scatter(1, at, t))).max()) / h.shape[0]
+    scale = float((h.abs().double().t() @ (lp.exp() + torch.zeros_like(lp).scatter(1, at, t))).detach().max()) / h.shape[0]
     assert float((moved - head.grad).abs().max()) <= 16 * off * scale + 2 * EPS * float(was.abs().max())
     assert len(sr.train(steps=1, groups=2, completions=2, tokens=5, prompt=9)) == 1
 
