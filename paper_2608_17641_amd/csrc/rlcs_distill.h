@@ -39,11 +39,12 @@ struct DistillLds {
 };
 inline size_t distill_lds(const DistillArgs& a) { return (size_t(a.words) * 4 + size_t(a.K) * 16 + 15) / 16 * 16; }
 
-// The lanes of a row: W waves of a workgroup, or with W = 1 a wave of a workgroup of four.
+// The lanes of a row: W waves of a workgroup, or with W = 1 a wave of a workgroup of four. Folds take several values with one
+// wait; `slots`: kFolds floats a wave, every fold of a row with its own (from `at` on), so that none waits for the one before.
 template <int W>
 struct Team {
-    static constexpr int kLanes = W * kWave;
-    float* slots;  // W words, unused with W = 1
+    static constexpr int kLanes = W * kWave, kFolds = 9;
+    float* slots;
     int lane;
     __device__ __forceinline__ void sync() const {
         if constexpr (W == 1) wave_lds_sync();
@@ -55,32 +56,35 @@ struct Team {
         if constexpr (W > 1) __syncthreads();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
     }
-    template <class F>
-    __device__ __forceinline__ float fold(float v, F&& f) const {
+    // v[i] folded over the waves by f.
+    template <int N, class F>
+    __device__ __forceinline__ void fold(float (&v)[N], int at, F&& f) const {
         if constexpr (W > 1) {
-            __syncthreads();
-            if ((lane & 63) == 0) slots[lane >> 6] = v;
-            __syncthreads();
-            v = slots[0];
+            if ((lane & 63) == 0) {
 #pragma unroll
-            for (int i = 1; i < W; ++i) v = f(v, slots[i]);
+                for (int i = 0; i < N; ++i) slots[(at + i) * W + (lane >> 6)] = v[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                v[i] = slots[(at + i) * W];
+#pragma unroll
+                for (int w = 1; w < W; ++w) v[i] = f(v[i], slots[(at + i) * W + w]);
+            }
         }
-        return v;
     }
-    __device__ __forceinline__ float sum(float v) const {
-        return fold(sum_wave(v), [](float x, float y) { return x + y; });
+    template <int N>
+    __device__ __forceinline__ void largest(float (&v)[N], int at) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = max_wave(v[i]);
+        fold(v, at, [](float x, float y) { return fmaxf(x, y); });
     }
-    __device__ __forceinline__ float max(float v) const {
-        return fold(max_wave(v), [](float x, float y) { return fmaxf(x, y); });
+    template <int N>
+    __device__ __forceinline__ void sums(float (&v)[N], int at) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = sum_wave(v[i]);
+        fold(v, at, [](float x, float y) { return x + y; });
     }
-    __device__ __forceinline__ bool any(bool b) const { return max(__any(b) ? 1.f : 0.f) > 0.f; }
-};
-
-// What a row's list says.
-struct Listed {
-    bool some;   // a share is not 0
-    bool twice;  // a token may be listed twice
-    float rest;  // the mass that the list leaves (TAIL)
 };
 
 __device__ __forceinline__ void mark(uint32_t* bits, int64_t id, bool& twice) {
@@ -88,27 +92,68 @@ __device__ __forceinline__ void mark(uint32_t* bits, int64_t id, bool& twice) {
     twice |= (atomicOr(&bits[at >> 5], bit) & bit) != 0;
 }
 
-template <typename DT, bool TAIL, int W>
-__device__ __forceinline__ Listed read_list(const DistillArgs& a, const DistillLds& l, const Team<W>& team, int64_t row) {
-    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
+// The listed ids and their bits, first of all; true: one may be there twice (ids that are kBits apart share a bit).
+template <int W>
+__device__ __forceinline__ bool read_ids(const DistillArgs& a, const DistillLds& l, const Team<W>& team, int64_t row) {
     for (int i = team.lane; i < a.words; i += Team<W>::kLanes) l.bits[i] = 0;
     team.sync();
-    bool some = false, twice = false;
-    float top = kNegInf;
+    bool twice = false;
     for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
         const int32_t id = a.ids[row * a.K + k];
         const bool is = id >= 0 && id < a.V;
-        const float lt = is ? a.top[row * a.K + k] : kNegInf;
         l.id[k] = is ? id : -1;
-        l.x[k] = is ? widen(x[id]) : 0.f;
-        l.lt[k] = lt;
         if (is) mark(l.bits, id, twice);
-        some |= !(lt == kNegInf);  // (NaN is some)
-        top = fmaxf(top, lt);
     }
-    Listed r{team.any(some), team.any(twice), 0.f};
+    return twice;
+}
+
+// The largest logit of the row, and of its list.
+struct RowStats {
+    Above sc;
+    float top_listed;
+    bool some, twice;  // a share is not 0; a token may be listed twice
+};
+// From each lane's largest logit; the logits of the listed tokens and the logarithms of their shares are read here, by the
+// lanes that keep them.
+template <typename DT, int W>
+__device__ __forceinline__ RowStats row_tops(const DistillArgs& a, const DistillLds& l, const Team<W>& team, int64_t row, float top, bool twice) {
+    const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
+    float listed = kNegInf;
+    bool some = false;
+    for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
+        const int32_t id = l.id[k];
+        const float lt = id >= 0 ? a.top[row * a.K + k] : kNegInf;
+        l.x[k] = id >= 0 ? widen(x[id]) : 0.f;
+        l.lt[k] = lt;
+        some |= !(lt == kNegInf);  // (NaN is some)
+        listed = fmaxf(listed, lt);
+    }
+    float v[4] = {top, listed, some ? 1.f : 0.f, twice ? 1.f : 0.f};
+    team.largest(v, 0);
+    return RowStats{above(v[0], kLog2e * a.inv_temp), v[1], v[2] > 0.f, v[3] > 0.f};
+}
+
+// A row once its sums are known: weights' scale, log2 of their sum, what a logit that is not listed has as its gradient's factor.
+struct DistillRow {
+    Above sc;
+    float l2z, factor, amount, share;  // share: what the weights of the list are multiplied by
+    bool some;                         // a logit is not masked
+    __device__ __forceinline__ float probability(float x) const {
+        return some ? exp2_fast(__builtin_elementwise_maximum(fmaf(x - sc.top, sc.c, -l2z), kLog2Zero)) : 0.f;
+    }
+};
+
+// From each lane's sums of the weights outside the list and in it: the row's, and its loss.
+template <bool TAIL, int W>
+__device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const DistillLds& l, const Team<W>& team, const RowStats& st, float z_out,
+                                               float z_in, float w, int64_t row) {
+    DistillRow r;
+    r.sc = st.sc;
+    r.amount = w * a.inv_temp;
+    r.factor = r.amount;
+    float rest = 0.f, log_sum = 0.f, loss = 0.f, z;
     if constexpr (TAIL) {
-        // (in 64 bits: what is left of 1 may be small)
+        // (in 64 bits: what is left of 1 may be small. Over the waves as two floats, the sum's high part and what it leaves out)
         double sum = 0.;
         for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
             const double t = exp(double(l.lt[k]));
@@ -117,90 +162,67 @@ __device__ __forceinline__ Listed read_list(const DistillArgs& a, const DistillL
         }
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
-        // as two floats over the waves: the sum's high part, and what it leaves out
-        const float high = float(sum), low = float(sum - double(high));
+        const float high = float(sum);
+        if (W > 1 && (team.lane & 63) == 0) {
+            team.slots[6 * W + (team.lane >> 6)] = high;
+            team.slots[7 * W + (team.lane >> 6)] = float(sum - double(high));
+        }
+        float v[2] = {z_out, z_in};
+        team.sums(v, 4);
         double left = 1.;
         if constexpr (W > 1) {
-            __syncthreads();
-            if ((team.lane & 63) == 0) {
-                team.slots[team.lane >> 6] = high;
-                team.slots[W + (team.lane >> 6)] = low;
-            }
-            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < W; ++i) left -= double(team.slots[i]) + double(team.slots[W + i]);
+            for (int i = 0; i < W; ++i) left -= double(team.slots[6 * W + i]) + double(team.slots[7 * W + i]);
         } else {
             left -= sum;
         }
-        r.rest = left < 0. ? 0.f : float(left);
+        z_out = v[0];
+        z = v[0] + v[1];
+        rest = left < 0. ? 0.f : float(left);
+        r.share = 1.f;
     } else {
-        top = team.max(top);
         float sum = 0.f;
         for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
-            const float t = l.lt[k] == kNegInf ? 0.f : exp2_fast((l.lt[k] - top) * kLog2e);
+            const float t = l.lt[k] == kNegInf ? 0.f : exp2_fast((l.lt[k] - st.top_listed) * kLog2e);
             l.t[k] = t;
             sum += t;
         }
-        sum = team.sum(sum);
-        const float log_sum = kLn2 * log2_fast(sum), inv = 1.f / sum;
-        for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
-            l.t[k] *= inv;
-            l.lt[k] = l.lt[k] - top - log_sum;
-        }
+        float v[2] = {z_out, sum};
+        team.sums(v, 4);
+        z = v[0];
+        r.share = 1.f / v[1];
+        log_sum = kLn2 * log2_fast(v[1]);
     }
-    team.sync();
-    return r;
-}
-
-// A row once its sums are known: weights' scale, log2 of their sum, what a logit that is not listed has as its gradient's factor.
-struct DistillRow {
-    Above sc;
-    float l2z, factor, amount;
-    bool some;  // a logit is not masked
-    __device__ __forceinline__ float probability(float x) const {
-        return some ? exp2_fast(__builtin_elementwise_maximum(fmaf(x - sc.top, sc.c, -l2z), kLog2Zero)) : 0.f;
-    }
-};
-
-// The row's loss, by all lanes; z: sums of the weights outside the list and in it.
-template <bool TAIL, int W>
-__device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const DistillLds& l, const Team<W>& team, const Listed& list, Above sc,
-                                               float z_out, float z_in, float w, int64_t row) {
-    DistillRow r;
-    const float z = TAIL ? z_out + z_in : z_out;
-    r.sc = sc;
     r.some = !(z == 0.f);  // (NaN is some)
     r.l2z = r.some ? log2_fast(z) : 0.f;
-    r.amount = w * a.inv_temp;
-    r.factor = r.amount;
-    float loss = 0.f;
+    const float top_listed = TAIL ? 0.f : st.top_listed;
     for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
         // (not by way of the base 2: 1.44 times a finite mask of the type's lowest value overflows)
-        const float t = l.t[k], lp = r.some ? fmaf(l.x[k] - sc.top, a.inv_temp, -kLn2 * r.l2z) : kNegInf;
-        if (!(t == 0.f)) loss = fmaf(t, l.lt[k] - lp, loss);
+        const float t = l.t[k] * r.share, lp = r.some ? fmaf(l.x[k] - st.sc.top, a.inv_temp, -kLn2 * r.l2z) : kNegInf;
+        if (!(t == 0.f)) loss = fmaf(t, (l.lt[k] - top_listed) - log_sum - lp, loss);
     }
-    loss = team.sum(loss);
     if constexpr (TAIL) {
-        const float p = z_out / z;
-        if (!(list.rest == 0.f) && !(z_out == 0.f)) {
-            loss = fmaf(list.rest, kLn2 * (log2_fast(list.rest) - log2_fast(p)), loss);
-            r.factor = r.amount * (1.f - list.rest / p);
+        const float p_out = z_out / z;
+        if (!(rest == 0.f) && !(z_out == 0.f)) {
+            if (team.lane == 0) loss = fmaf(rest, kLn2 * (log2_fast(rest) - log2_fast(p_out)), loss);
+            r.factor = r.amount * (1.f - rest / p_out);
         }
     }
-    if (team.lane == 0) a.loss[row] = w * loss;
+    float v[1] = {loss};
+    team.sums(v, 8);
+    if (team.lane == 0) a.loss[row] = w * v[0];
     return r;
 }
 
 // The listed places of the gradient, once everything else of the row is written.
 template <typename DT, int W>
-__device__ __forceinline__ void listed_gradient(const DistillArgs& a, const DistillLds& l, const Team<W>& team, const Listed& list, const DistillRow& r,
-                                                DT* g) {
+__device__ __forceinline__ void listed_gradient(const DistillArgs& a, const DistillLds& l, const Team<W>& team, bool twice, const DistillRow& r, DT* g) {
     team.order_stores();
     for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
         const int32_t id = l.id[k];
         if (id < 0) continue;
         float t = l.t[k];
-        if (list.twice) {  // the first of a token's places writes the sum of its shares
+        if (twice) {  // the first of a token's places writes the sum of its shares
             bool first = true;
             t = 0.f;
             for (int j = 0; j < a.K; ++j) {
@@ -210,7 +232,7 @@ __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Dist
             }
             if (!first) continue;
         }
-        g[id] = narrow(r.amount * (r.probability(l.x[k]) - t), DT{});
+        g[id] = narrow(r.amount * (r.probability(l.x[k]) - t * r.share), DT{});
     }
 }
 
@@ -253,7 +275,7 @@ __device__ __forceinline__ void add_weights(const V& v, const Above& sc, uint32_
 template <typename DT, bool TAIL, int W, int U>
 __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(DistillArgs a, int row_lds) {
     extern __shared__ __attribute__((aligned(16))) char s_mem[];
-    __shared__ float s_slots[2 * W];
+    __shared__ float s_slots[Team<W>::kFolds * W];
     constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = W == 1 ? grid_row() * 4 + wave : grid_row();
@@ -263,36 +285,33 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
     const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     DT* g = a.grad ? reinterpret_cast<DT*>(a.grad) + row * a.ld_grad : nullptr;
     const float w = a.weight ? a.weight[row] : 1.f;
-    bool part = w != 0.f;
     RowVec<DT> v[U];
-    Listed list{};
-    if (part) {
+    RowStats st{};
+    float top = kNegInf;
+    if (w != 0.f) {
 #pragma unroll
         for (int u = 0; u < U; ++u) v[u].load(x, team.lane + u * kLanes, a.V);  // (past the end: -inf)
-        list = read_list<DT, TAIL, W>(a, l, team, row);
-        part = TAIL || list.some;
+        const bool twice = read_ids<W>(a, l, team, row);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) top = fmaxf(top, v[u].at(k));
+        st = row_tops<DT, W>(a, l, team, row, top, twice);
+        if (TAIL && W == 1) team.sync();  // (all bits are there)
     }
-    if (!part) {
+    if (w == 0.f || !(TAIL || st.some)) {
         if (team.lane == 0) a.loss[row] = 0.f;
         if (g) zero_row<DT, kLanes>(g, a.V, team.lane);
         return;
     }
-    float top = kNegInf;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < K; ++k) top = fmaxf(top, v[u].at(k));
-    const Above sc = above(team.max(top), kLog2e * a.inv_temp);
     float z_out = 0.f, z_in = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t i = team.lane + u * kLanes;
         const uint32_t bits = TAIL && i * K < a.V ? vector_bits<K>(l.bits, i) : 0u;
-        add_weights<TAIL>(v[u], sc, bits, z_out, z_in);
+        add_weights<TAIL>(v[u], st.sc, bits, z_out, z_in);
     }
-    z_out = team.sum(z_out);
-    if (TAIL) z_in = team.sum(z_in);
-    const DistillRow r = row_loss<TAIL, W>(a, l, team, list, sc, z_out, z_in, w, row);
+    const DistillRow r = row_loss<TAIL, W>(a, l, team, st, z_out, z_in, w, row);
     if (!g) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -302,7 +321,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
         for (int k = 0; k < K; ++k) d[k] = r.factor * r.probability(v[u].at(k));
         if (i * K < a.V) store_row_vec<DT>(g, i, a.V, d);
     }
-    listed_gradient<DT, W>(a, l, team, list, r, g);
+    listed_gradient<DT, W>(a, l, team, st.twice, r, g);
 }
 
 // Longer rows, one per workgroup of W waves: one pass for the sums, each lane relative to its own running
@@ -310,7 +329,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
 template <typename DT, bool TAIL, int W>
 __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) {
     extern __shared__ __attribute__((aligned(16))) char s_mem[];
-    __shared__ float s_slots[2 * W];
+    __shared__ float s_slots[Team<W>::kFolds * W];
     constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
     const int64_t row = grid_row();
     if (row >= a.M) return;
@@ -320,17 +339,13 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
     const DT* x = reinterpret_cast<const DT*>(a.logits) + row * a.ld;
     DT* g = a.grad ? reinterpret_cast<DT*>(a.grad) + row * a.ld_grad : nullptr;
     const float w = a.weight ? a.weight[row] : 1.f;
-    bool part = w != 0.f;
-    Listed list{};
-    if (part) {
-        list = read_list<DT, TAIL, W>(a, l, team, row);
-        part = TAIL || list.some;
-    }
-    if (!part) {
+    if (w == 0.f) {
         if (tid == 0) a.loss[row] = 0.f;
         if (g) zero_row<DT, kLanes>(g, a.V, tid);
         return;
     }
+    const bool twice = read_ids<W>(a, l, team, row);
+    __syncthreads();
     const float c = kLog2e * a.inv_temp;
     const int64_t vecs = (a.V + K - 1) / K;
     // (sums from chunk to chunk in 64 bits: one addition after another in 32 drifts in the longest rows)
@@ -378,9 +393,14 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
             in += z_in;
         }
     }
-    rebase(team.max(top));
-    const float z_out = team.sum(float(out)), z_in = TAIL ? team.sum(float(in)) : 0.f;
-    const DistillRow r = row_loss<TAIL, W>(a, l, team, list, above(top, c), z_out, z_in, w, row);
+    const RowStats st = row_tops<DT, W>(a, l, team, row, top, twice);
+    if (!TAIL && !st.some) {
+        if (tid == 0) a.loss[row] = 0.f;
+        if (g) zero_row<DT, kLanes>(g, a.V, tid);
+        return;
+    }
+    if (top > kNegInf) rebase(st.sc.top);
+    const DistillRow r = row_loss<TAIL, W>(a, l, team, st, float(out), float(in), w, row);
     if (!g) return;
     // backwards: what the first pass read last is nearest in the caches
     for (int64_t i0 = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid; i0 >= 0; i0 -= U * kLanes) {
@@ -396,7 +416,7 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
             if (i < vecs) store_row_vec<DT>(g, i, a.V, d);
         }
     }
-    listed_gradient<DT, W>(a, l, team, list, r, g);
+    listed_gradient<DT, W>(a, l, team, st.twice, r, g);
 }
 
 }  // namespace rlcs

@@ -8,7 +8,7 @@ using namespace rlcs::host;
 namespace {
 
 // Calls of at most this many pages and table entries run as one workgroup.
-constexpr int64_t kSmallPages = 65536;
+constexpr int64_t kSmallPages = 4096;
 constexpr int64_t kMaxGroups = 2048;
 
 bool good_page(int64_t page) { return page >= 16 && page <= 65536 && (page & (page - 1)) == 0; }

@@ -172,22 +172,20 @@ struct RowSoftmax {
     __device__ __forceinline__ float weight(float x) const { return exp2_fast(sc.log2_weight(x)); }
     __device__ __forceinline__ float probability(float x) const { return sum > 0.f ? weight(x) / sum : 0.f; }
 };
+// By a wave, from the row's parts, one a lane.
 __device__ __forceinline__ RowSoftmax row_softmax(const VerifyArgs& a, int64_t row, float c) {
-    const RowSum* s = a.sums + row * a.sum_parts;
-    float top = kNegInf;
-    for (int i = 0; i < a.sum_parts; ++i) top = fmaxf(top, s[i].top);
-    float sum = 0.f;
-    for (int i = 0; i < a.sum_parts; ++i) {
-        const float f = s[i].top == top ? 1.f : exp2_fast(fmaxf((s[i].top - top) * c, kLog2Zero));
-        sum = fmaf(f, s[i].sum, sum);
-    }
-    return RowSoftmax{above(top, c), sum};
+    const int lane = threadIdx.x & 63;
+    RowSum s;
+    s.top = kNegInf;
+    s.sum = 0.f;
+    if (lane < a.sum_parts) s = a.sums[row * a.sum_parts + lane];
+    const float top = max_wave(s.top);
+    const float f = s.top == top ? 1.f : exp2_fast(fmaxf((s.top - top) * c, kLog2Zero));
+    return RowSoftmax{above(top, c), sum_wave(f * s.sum)};
 }
 __device__ __forceinline__ uint64_t row_largest(const VerifyArgs& a, int64_t row) {
-    const RowSum* s = a.sums + row * a.sum_parts;
-    uint64_t best = 0;
-    for (int i = 0; i < a.sum_parts; ++i) best = s[i].entry > best ? s[i].entry : best;
-    return best;
+    const int lane = threadIdx.x & 63;
+    return max_wave(lane < a.sum_parts ? a.sums[row * a.sum_parts + lane].entry : uint64_t(0));
 }
 
 // The drawn token of sequence b: place n, and what is -1 and 0 after it.
@@ -225,28 +223,34 @@ __global__ __launch_bounds__(kVerifyWaves * kWave) void verify_race_kernel(Verif
     const int64_t targets = b * (a.K + 1), drafts = a.B * (a.K + 1) + b * a.K;
     if (tid == 0) s_first = n_draft;
     __syncthreads();
-    for (int i = tid; i < n_draft; i += kLanes) {
+    // a wave a drafted token; the ones after a token that fell do not matter
+    for (int i = tid >> 6; i < n_draft && i < *static_cast<volatile int*>(&s_first); i += W) {
         const int64_t token = a.draft_tokens[b * a.K + i];
         bool stands = false;
         float logp = 0.f;
         if (token >= 0 && token < a.V) {
-            const float q = a.draft ? row_softmax(a, drafts + i, draft_scale(a, b)).probability(counted<DT>(widen(draft_row<DT>(a, b, i)[token]))) : 1.f;
-            float p;
+            const float u = a.u[b * a.K + i], x = counted<DT>(widen(target_row<DT>(a, b, i)[token]));
+            float q = 1.f, p;
+            if (a.draft) {
+                const float y = counted<DT>(widen(draft_row<DT>(a, b, i)[token]));
+                q = row_softmax(a, drafts + i, draft_scale(a, b)).probability(y);
+            }
             if (greedy) {
                 const uint64_t e = row_largest(a, targets + i);
                 p = e && race_index(e) == uint32_t(token) ? 1.f : 0.f;
             } else {
                 const RowSoftmax s = row_softmax(a, targets + i, c);
-                const float x = counted<DT>(widen(target_row<DT>(a, b, i)[token]));
                 p = s.probability(x);
                 logp = kLn2 * (s.sc.log2_weight(x) - log2_fast(s.sum));
             }
-            stands = a.u[b * a.K + i] * q < p;
+            stands = u * q < p;
         }
-        if (!stands) atomicMin(&s_first, i);
-        if (part == 0) {  // (places from the first that falls on are written again)
-            a.tokens[targets + i] = int32_t(token);
-            if (a.logp) a.logp[targets + i] = logp;
+        if ((tid & 63) == 0) {
+            if (!stands) atomicMin(&s_first, i);
+            if (part == 0) {  // (places from the first that falls on are written again)
+                a.tokens[targets + i] = int32_t(token);
+                if (a.logp) a.logp[targets + i] = logp;
+            }
         }
     }
     __syncthreads();
