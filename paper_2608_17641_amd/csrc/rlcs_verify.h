@@ -29,7 +29,7 @@ struct VerifyArgs {
     int64_t sum_length, race_length;
     struct RowSum* sums;    // [row][sum_parts]: target rows, then draft rows
     struct Verdict* verdict;  // [B]
-    uint64_t* best;         // [B][race_parts][2]: of what is left, and of all
+    uint64_t* best;         // [B][race_parts]
 };
 
 // A part of a row: its largest logit and the sum of the weights relative to it; of a temperature of 0 the place of the
@@ -195,17 +195,73 @@ __device__ __forceinline__ void verify_finish(const VerifyArgs& a, int64_t b, in
     a.count[b] = n + 1;
     if (a.logp) a.logp[row + n] = logp;
 }
-// From the races' winners: of what q leaves, or, where that is nothing, of all of p.
 template <typename DT>
-__device__ __forceinline__ void verify_drawn(const VerifyArgs& a, int64_t b, const Verdict& v, uint64_t left, uint64_t all) {
-    const uint64_t e = left ? left : all;
-    if (!e) {
+__device__ __forceinline__ void verify_drawn(const VerifyArgs& a, int64_t b, const Verdict& v, uint64_t winner) {
+    if (!winner) {
         verify_finish(a, b, v.n, -1, kNegInf);
         return;
     }
-    const int32_t token = int32_t(race_index(e));
+    const int32_t token = int32_t(race_index(winner));
     const float u = Above{v.top, v.c}.log2_weight(counted<DT>(widen(target_row<DT>(a, b, v.n)[token])));
     verify_finish(a, b, v.n, token, kLn2 * (u - v.l2z));
+}
+
+// A lane's share of a race over vectors [from, end) of a row, as an entry (0: it has none). w(logits, i, k) is the weight of
+// element k of vector i, a number from 0 to 1; none has a weight of 0. Scores are w / E, which order as log w - log E does; where the best is
+// near an end of float32's range (numbers E that no exponential draw gives) the lane takes logarithms.
+template <typename DT, class F>
+__device__ __forceinline__ uint64_t race_lane(const DT* x, const float* noise, int64_t V, int64_t from, int64_t end, int step, F&& weight) {
+    constexpr int K = RowVec<DT>::K;
+    auto run = [&](auto logs) {
+        float best = kNegInf;
+        uint32_t at = 0;
+        bool some = false;
+        for (int64_t i = from; i < end; i += step) {
+            RowVec<DT> r;
+            r.load(x, i, V);
+            float e[K], w[K];
+            if ((i + 1) * K <= V) {
+#pragma unroll
+                for (int k = 0; k < K; k += 4) {
+                    const u32x4 word = *reinterpret_cast<const u32x4_any*>(noise + i * K + k);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) e[k + m] = __uint_as_float(word[m]);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < K; ++k) e[k] = i * K + k < V ? noise[i * K + k] : 1.f;
+            }
+            weight(r, i, w);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const float score = decltype(logs)::value ? noise_log2(w[k]) - noise_log2(e[k]) : w[k] * __builtin_amdgcn_rcpf(e[k]);
+                const bool ahead = w[k] > 0.f && (score > best || !some);
+                best = ahead ? score : best;
+                at = ahead ? uint32_t(i * K + k) : at;
+                some |= ahead;
+            }
+        }
+        if (!some) return uint64_t(0);
+        if (!decltype(logs)::value) {
+            if (!(best > 0x1p-100f && best < 0x1p100f)) return ~uint64_t(0);
+            best = log2_fast(best);
+        }
+        return race_entry(order_key(best), at);
+    };
+    const uint64_t fast = run(std::false_type{});
+    return fast == ~uint64_t(0) ? run(std::true_type{}) : fast;
+}
+// The race over all of p: where no token fell, and where q leaves nothing.
+template <typename DT>
+__device__ __forceinline__ uint64_t race_all(const DT* x, const float* noise, int64_t V, int64_t from, int64_t end, int step, Above sc) {
+    return race_lane<DT>(x, noise, V, from, end, step, [&](const RowVec<DT>& r, int64_t, float (&w)[RowVec<DT>::K]) {
+#pragma unroll
+        for (int k = 0; k < RowVec<DT>::K; ++k) {
+            const float y = counted<DT>(r.at(k));
+            // (a token that is not masked takes part, however little it weighs)
+            w[k] = y > kNegInf ? fmaxf(exp2_fast(sc.log2_weight(y)), 0x1p-126f) : 0.f;
+        }
+    });
 }
 
 // Part blockIdx of a sequence's race, after the comparison of its drafted tokens, which every part makes for itself.
@@ -282,74 +338,56 @@ __global__ __launch_bounds__(kVerifyWaves * kWave) void verify_race_kernel(Verif
     const DT *xp = target_row<DT>(a, b, n), *xq = minus ? draft_row<DT>(a, b, n) : xp;
     const float* noise = a.noise + b * a.noise_ld;
     const float inv_p = 1.f / p.sum, inv_q = q.sum > 0.f ? 1.f / q.sum : 0.f;
-    const int64_t from = part * a.race_length / K, most = (a.V + K - 1) / K;
-    const int64_t end = from + a.race_length / K < most ? from + a.race_length / K : most;
-    uint64_t left = 0, all = 0;
-    for (int64_t i = from + tid; i < end; i += kLanes) {
-        RowVec<DT> rp, rq;
-        rp.load(xp, i, a.V);
-        if (minus) rq.load(xq, i, a.V);
-        float e[K];
-        if ((i + 1) * K <= a.V) {
+    const int64_t from = part * a.race_length / K + tid, most = (a.V + K - 1) / K;
+    const int64_t past = (part + 1) * a.race_length / K, end = past < most ? past : most;
+    uint64_t winner;
+    if (minus) {
+        winner = race_lane<DT>(xp, noise, a.V, from, end, kLanes, [&](const RowVec<DT>& r, int64_t i, float (&w)[K]) {
+            RowVec<DT> rq;
+            rq.load(xq, i, a.V);
 #pragma unroll
-            for (int k = 0; k < K; k += 4) {
-                const u32x4 w = *reinterpret_cast<const u32x4_any*>(noise + i * K + k);
-#pragma unroll
-                for (int m = 0; m < 4; ++m) e[k + m] = __uint_as_float(w[m]);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = i * K + k < a.V ? noise[i * K + k] : 1.f;
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t j = i * K + k;
-            const float x = counted<DT>(rp.at(k));
-            if (!(x > kNegInf)) continue;
-            const float u = p.sc.log2_weight(x), l = noise_log2(e[k]);
-            const uint64_t whole = race_entry(order_key(u - l), uint32_t(j));
-            all = whole > all ? whole : all;
-            if (!fell || j == fallen) continue;
-            float rest = exp2_fast(u);
-            if (minus) {
+            for (int k = 0; k < K; ++k) {
                 // (each product rounded by itself, so that of equal rows nothing is left)
 #pragma clang fp contract(off)
-                const float of_p = rest * inv_p, of_q = q.weight(counted<DT>(rq.at(k))) * inv_q;
-                rest = of_p - of_q;
+                const float of_p = p.weight(counted<DT>(r.at(k))) * inv_p, of_q = q.weight(counted<DT>(rq.at(k))) * inv_q;
+                w[k] = of_p - of_q;
             }
-            if (!(rest > 0.f)) continue;
-            const uint64_t some = race_entry(order_key(noise_log2(rest) - l), uint32_t(j));
-            left = some > left ? some : left;
-        }
+        });
+    } else if (fell) {
+        winner = race_lane<DT>(xp, noise, a.V, from, end, kLanes, [&](const RowVec<DT>& r, int64_t i, float (&w)[K]) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) w[k] = i * K + k == fallen ? 0.f : p.weight(counted<DT>(r.at(k)));
+        });
+    } else {
+        winner = race_all<DT>(xp, noise, a.V, from, end, kLanes, p.sc);
     }
-    left = max_group<W>(left, s_slots);
-    all = max_group<W>(all, s_slots);
-    if (tid != 0) return;
-    if (a.race_parts == 1) {
-        verify_drawn<DT>(a, b, v, left, all);
+    winner = max_group<W>(winner, s_slots);
+    if (a.race_parts > 1) {
+        if (tid == 0) {
+            if (part == 0) a.verdict[b] = v;
+            a.best[item] = winner;
+        }
         return;
     }
-    if (part == 0) a.verdict[b] = v;
-    a.best[2 * item] = left;
-    a.best[2 * item + 1] = all;
+    if (!winner) winner = max_group<W>(race_all<DT>(xp, noise, a.V, tid, most, kLanes, p.sc), s_slots);
+    if (tid == 0) verify_drawn<DT>(a, b, v, winner);
 }
 
-// The best of a race's parts: a wave a sequence.
+// The best of a race's parts, a workgroup a sequence; where q has left nothing, the race over all of p.
 template <typename DT>
-__global__ __launch_bounds__(kWave) void verify_join_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(kVerifyWaves * kWave) void verify_join_kernel(VerifyArgs a) {
+    constexpr int W = kVerifyWaves, K = RowVec<DT>::K;
+    __shared__ uint64_t s_slots[W];
     const int64_t b = grid_row();
     if (b >= a.B) return;
     const Verdict v = a.verdict[b];
     if (v.greedy != -2) return;  // (written already)
-    uint64_t left = 0, all = 0;
-    for (int i = threadIdx.x; i < a.race_parts; i += kWave) {
-        const uint64_t x = a.best[2 * (b * a.race_parts + i)], y = a.best[2 * (b * a.race_parts + i) + 1];
-        left = x > left ? x : left;
-        all = y > all ? y : all;
-    }
-    left = max_wave(left);
-    all = max_wave(all);
-    if (threadIdx.x == 0) verify_drawn<DT>(a, b, v, left, all);
+    const int tid = threadIdx.x, lane = tid & 63;
+    uint64_t winner = max_wave(lane < a.race_parts ? a.best[b * a.race_parts + lane] : uint64_t(0));
+    if (!winner)
+        winner = max_group<W>(race_all<DT>(target_row<DT>(a, b, v.n), a.noise + b * a.noise_ld, a.V, tid, (a.V + K - 1) / K, W * kWave, Above{v.top, v.c}),
+                              s_slots);
+    if (tid == 0) verify_drawn<DT>(a, b, v, winner);
 }
 
 }  // namespace rlcs

@@ -34,7 +34,7 @@ VerifySpace space_of(int64_t B, int64_t K, int64_t V) {
     };
     s.sums = take(size_t(rows * s.sum_parts) * sizeof(RowSum));
     s.verdict = take(size_t(B) * sizeof(Verdict));
-    s.best = take(size_t(B * s.race_parts) * 16);
+    s.best = take(size_t(B * s.race_parts) * 8);
     return s;
 }
 // Length of a part, a multiple of eight logits, with which there are no more than `parts`.
@@ -53,7 +53,7 @@ rlcs_status run_verify(const VerifyArgs& a, hipStream_t s) {
     if (a.sum_length <= kWaveRow) hipLaunchKernelGGL((verify_sums_kernel<DT, 1>), row_grid(rows * a.sum_parts), dim3(kWave), 0, s, a);
     else hipLaunchKernelGGL((verify_sums_kernel<DT, kVerifyWaves>), row_grid(rows * a.sum_parts), dim3(kVerifyWaves * kWave), 0, s, a);
     hipLaunchKernelGGL((verify_race_kernel<DT>), row_grid(a.B * a.race_parts), dim3(kVerifyWaves * kWave), 0, s, a);
-    if (a.race_parts > 1) hipLaunchKernelGGL((verify_join_kernel<DT>), row_grid(a.B), dim3(kWave), 0, s, a);
+    if (a.race_parts > 1) hipLaunchKernelGGL((verify_join_kernel<DT>), row_grid(a.B), dim3(kVerifyWaves * kWave), 0, s, a);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
 
