@@ -109,7 +109,8 @@ __device__ __forceinline__ bool read_ids(const DistillArgs& a, const DistillLds&
 
 // The largest logit of the row, and of its list.
 struct RowStats {
-    Above sc;
+    float top;
+    Scale sc;
     float top_listed;
     bool some, twice;  // a share is not 0; a token may be listed twice
 };
@@ -130,17 +131,17 @@ __device__ __forceinline__ RowStats row_tops(const DistillArgs& a, const Distill
     }
     float v[4] = {top, listed, some ? 1.f : 0.f, twice ? 1.f : 0.f};
     team.largest(v, 0);
-    return RowStats{above(v[0], kLog2e * a.inv_temp), v[1], v[2] > 0.f, v[3] > 0.f};
+    return RowStats{v[0], scale_of(v[0], kLog2e * a.inv_temp), v[1], v[2] > 0.f, v[3] > 0.f};
 }
 
-// A row once its sums are known: weights' scale, log2 of their sum, what a logit that is not listed has as its gradient's factor.
+// A row once its sums are known: weights' scale, the sum's inverse (0: every logit is masked), what a logit that is not listed has as
+// its gradient's factor.
 struct DistillRow {
-    Above sc;
-    float l2z, factor, amount, share;  // share: what the weights of the list are multiplied by
-    bool some;                         // a logit is not masked
-    __device__ __forceinline__ float probability(float x) const {
-        return some ? exp2_fast(__builtin_elementwise_maximum(fmaf(x - sc.top, sc.c, -l2z), kLog2Zero)) : 0.f;
-    }
+    Scale sc;
+    float inv, factor, amount, share;  // share: what the weights of the list are multiplied by
+    // f times the probability of logit x. (The weight times the sum's inverse and not by the logarithm of the sum: the
+    // rounding of the scale is in both, and cancels.)
+    __device__ __forceinline__ float times(float f, float x) const { return exp2_fast(sc.log2_weight(x)) * f; }
 };
 
 // From each lane's sums of the weights outside the list and in it: the row's, and its loss.
@@ -193,12 +194,14 @@ __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const Disti
         r.share = 1.f / v[1];
         log_sum = kLn2 * log2_fast(v[1]);
     }
-    r.some = !(z == 0.f);  // (NaN is some)
-    r.l2z = r.some ? log2_fast(z) : 0.f;
+    const bool unmasked = !(z == 0.f);  // (NaN counts)
+    r.inv = unmasked ? 1.f / z : 0.f;
+    // log z relative to the top itself: the scale's m is rounded, by what this product leaves over
+    const float log_z = unmasked ? kLn2 * (log2_fast(z) - fmaf(st.top, st.sc.c, -st.sc.m)) : 0.f;
     const float top_listed = TAIL ? 0.f : st.top_listed;
     for (int k = team.lane; k < a.K; k += Team<W>::kLanes) {
         // (not by way of the base 2: 1.44 times a finite mask of the type's lowest value overflows)
-        const float t = l.t[k] * r.share, lp = r.some ? fmaf(l.x[k] - st.sc.top, a.inv_temp, -kLn2 * r.l2z) : kNegInf;
+        const float t = l.t[k] * r.share, lp = unmasked ? fmaf(l.x[k] - st.top, a.inv_temp, -log_z) : kNegInf;
         if (!(t == 0.f)) loss = fmaf(t, (l.lt[k] - top_listed) - log_sum - lp, loss);
     }
     if constexpr (TAIL) {
@@ -232,7 +235,7 @@ __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Dist
             }
             if (!first) continue;
         }
-        g[id] = narrow(r.amount * (r.probability(l.x[k]) - t * r.share), DT{});
+        g[id] = narrow(r.amount * (r.times(r.inv, l.x[k]) - t * r.share), DT{});
     }
 }
 
@@ -253,10 +256,10 @@ __device__ __forceinline__ uint32_t vector_bits(const uint32_t* bits, int64_t i)
 
 // A vector's weights, added to what they belong to.
 template <bool TAIL, class V>
-__device__ __forceinline__ void add_weights(const V& v, const Above& sc, uint32_t bits, float& z_out, float& z_in) {
+__device__ __forceinline__ void add_weights(const V& v, const Scale& sc, uint32_t bits, float& z_out, float& z_in) {
     float e[V::K];
 #pragma unroll
-    for (int k = 0; k < V::K; ++k) e[k] = exp2_fast(__builtin_elementwise_maximum(sc.log2_weight(v.at(k)), kLog2Zero));
+    for (int k = 0; k < V::K; ++k) e[k] = exp2_fast(sc.log2_weight(v.at(k)));
     if (TAIL && bits) {
 #pragma unroll
         for (int k = 0; k < V::K; ++k) {
@@ -313,12 +316,13 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
     }
     const DistillRow r = row_loss<TAIL, W>(a, l, team, st, z_out, z_in, w, row);
     if (!g) return;
+    const float factor = r.factor * r.inv;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t i = team.lane + u * kLanes;
         float d[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) d[k] = r.factor * r.probability(v[u].at(k));
+        for (int k = 0; k < K; ++k) d[k] = r.times(factor, v[u].at(k));
         if (i * K < a.V) store_row_vec<DT>(g, i, a.V, d);
     }
     listed_gradient<DT, W>(a, l, team, st.twice, r, g);
@@ -350,12 +354,15 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
     const int64_t vecs = (a.V + K - 1) / K;
     // (sums from chunk to chunk in 64 bits: one addition after another in 32 drifts in the longest rows)
     float top = kNegInf;
+    Scale sc = scale_of(top, c);
     double out = 0., in = 0.;
     auto rebase = [&](float t) {
-        const double f = top == t ? 1. : double(exp2_fast(fmaxf((top - t) * c, kLog2Zero)));
+        const Scale to = scale_of(t, c);
+        const double f = top == kNegInf ? 0. : double(exp2_fast(scale_step(sc, to)));
         out *= f;
         in *= f;
         top = t;
+        sc = to;
     };
     const int64_t span = TAIL ? kBits / K : vecs;  // vectors whose bits are there
     for (int64_t from = 0; from < vecs; from += span) {
@@ -381,7 +388,6 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
 #pragma unroll
                 for (int k = 0; k < K; ++k) t = fmaxf(t, v[u].at(k));
             if (t > top) rebase(t);
-            const Above sc = above(top, c);
             float z_out = 0.f, z_in = 0.f;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -399,9 +405,10 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
         if (g) zero_row<DT, kLanes>(g, a.V, tid);
         return;
     }
-    if (top > kNegInf) rebase(st.sc.top);
+    if (top > kNegInf && st.top > top) rebase(st.top);
     const DistillRow r = row_loss<TAIL, W>(a, l, team, st, float(out), float(in), w, row);
     if (!g) return;
+    const float factor = r.factor * r.inv;
     // backwards: what the first pass read last is nearest in the caches
     for (int64_t i0 = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid; i0 >= 0; i0 -= U * kLanes) {
         RowVec<DT> v[U];
@@ -412,7 +419,7 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
             const int64_t i = i0 + u * kLanes;
             float d[K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) d[k] = r.factor * r.probability(v[u].at(k));
+            for (int k = 0; k < K; ++k) d[k] = r.times(factor, v[u].at(k));
             if (i < vecs) store_row_vec<DT>(g, i, a.V, d);
         }
     }

@@ -21,8 +21,9 @@ void launch_rows(const DistillArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((distill_rows_kernel<DT, TAIL, W>), row_grid(a.M), dim3(W * kWave), unsigned(distill_lds(a)), s, a);
 }
 
-// As many waves and vectors a lane as hold the row in registers; longer rows are read twice.
-constexpr int64_t kFewRows = 256, kLongRow = 200 << 10;
+// As many waves and vectors a lane as hold the row in registers; longer rows are read twice, by 16 waves where there is no more
+// than a row for each CU (128 rows of 128000 bfloat16: 23.7 us, 8 waves 27.6) and else by 8 (8192 rows: 768 us, 16 waves 773).
+constexpr int64_t kFewRows = 256;
 
 template <typename DT, bool TAIL>
 rlcs_status run_distill(const DistillArgs& a, hipStream_t s) {
@@ -35,7 +36,7 @@ rlcs_status run_distill(const DistillArgs& a, hipStream_t s) {
     else if (a.V <= 4096 * k) launch_vec<DT, TAIL, 4, 4>(a, s);
     else if (a.V <= 8192 * k) launch_vec<DT, TAIL, 4, 8>(a, s);
     else if (a.V <= 16384 * k) launch_vec<DT, TAIL, 8, 8>(a, s);
-    else if (a.M <= kFewRows || a.V * int64_t(sizeof(DT)) >= kLongRow) launch_rows<DT, TAIL, 16>(a, s);
+    else if (a.M <= kFewRows) launch_rows<DT, TAIL, 16>(a, s);
     else launch_rows<DT, TAIL, 8>(a, s);
     return hipGetLastError() == hipSuccess ? RLCS_OK : RLCS_ERR_LAUNCH;
 }
