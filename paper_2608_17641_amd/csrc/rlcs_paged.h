@@ -2,7 +2,7 @@
 //
 // A tile is up to R rows (token, query head of one key head) of one sequence, in the order of tokens; row i of a
 // sequence with T new tokens and L in all sees the first L - T + i / r + 1 keys, r query heads to a key head.
-// Sequences of up to kFewRows rows a key head are one tile, whose keys are dealt to the waves of a workgroup, each
+// Sequences of up to few_rows rows a key head are one tile, whose keys are dealt to the waves of a workgroup, each
 // with running maxima, sums and outputs of its own, which join at the end: bound by reading the keys. Longer
 // chunks are tiles of more rows, each wave with rows of its own and all with the same keys, in LDS: bound by the
 // matrix and the vector units. Long key ranges are cut into parts, which a second kernel joins; how long a part is

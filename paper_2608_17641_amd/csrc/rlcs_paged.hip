@@ -32,13 +32,18 @@ bool whole_vectors(const int64_t* s, int n, int64_t vec) {
     return true;
 }
 
-// Sequences of up to this many rows a key head are the first kernel's.
-constexpr int64_t kFewRows = 2 * kTileRows;
-// Pieces that all keys are dealt out in: as many as the GPU holds at once. Waves of the first kernel, two a SIMD with one tile of
-// rows and one with two; workgroups of the second, one a CU.
-constexpr int64_t kPiecesFew = 1024, kPiecesFew2 = 1024, kPiecesMany = 256;
-// Where no sequence can have more keys than this, all are taken whole: no second kernel.
-constexpr int64_t kWholeKeys = 512;
+// Where no sequence can have more keys than this, all are taken whole: no second kernel. (64 sequences of 1024 keys, 8 key
+// heads of 128 dimensions, 4 rows: 42 us, in pieces 51; of one to 1024 keys 29 and 35; of 2048 keys 97 and 106, but of one to 2048
+// 59 and 54.)
+constexpr int64_t kWholeKeys = 1024;
+// Tiles of sixteen rows, up to which the rows of a sequence are the first kernel's: two. One in bfloat16 where all sequences have as
+// many (64 of 4096 keys, 20 rows: 213 us with two, 198 by the second kernel; float32, 64 of 2048: 130 and 186) and keys are not taken
+// whole (8 of 512: 12 us, by the second 22; where rows differ, the second would be one more: 64 of up to 4096 keys and up to 20 rows 156
+// us, else 181). One of more than 128 dimensions, as two do not fit in a wave's registers (192 dimensions: 664 us, by the second 449).
+int few_tiles_of(int64_t D, bool bf16, bool ragged, bool whole) { return D <= 128 && (whole || ragged || !bf16) ? 2 : 1; }
+// Pieces that all keys are dealt out in: as many as the GPU holds at once. Waves of the first kernel, one a SIMD;
+// workgroups of the second, one a CU.
+constexpr int64_t kPiecesFew = 1024, kPiecesMany = 256;
 
 // Which kernels a call takes, and their parts.
 struct PagedPlan {
@@ -53,11 +58,12 @@ bool make_plan(PagedPlan& p, int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv,
                int64_t most_keys = 0) {
     const int64_t r = Hq / Hkv, most = max_chunk * r;
     p = PagedPlan{};
-    p.few = ragged || most <= kFewRows;
-    p.many = most > kFewRows;
-    p.few_tiles = most <= kTileRows ? 1 : 2;
+    const bool whole = most_keys && most_keys <= kWholeKeys;
+    p.few_tiles = most <= kTileRows ? 1 : few_tiles_of(D, bf16, ragged, whole);
+    p.few = ragged || most <= p.few_tiles * kTileRows;
+    p.many = most > p.few_tiles * kTileRows;
     p.many_rows = D > 128 || tokens * r <= 64 * B ? 64 : bf16 ? 256 : 128;
-    p.few_pieces = most_keys && most_keys <= kWholeKeys ? 0 : ceil_div(ceil_div(p.few_tiles == 1 ? kPiecesFew : kPiecesFew2, Hkv), kAttnWaves) * kAttnWaves;
+    p.few_pieces = whole ? 0 : ceil_div(ceil_div(kPiecesFew, Hkv), kAttnWaves) * kAttnWaves;
     p.many_pieces = ceil_div(kPiecesMany, Hkv);
     return B <= INT32_MAX / Hkv && tokens * r / 64 + B <= INT32_MAX / Hkv;
 }
@@ -110,8 +116,12 @@ template <typename DT, int ND>
 rlcs_status run_paged(PagedArgs a, const PagedPlan& p, void* ws, hipStream_t s) {
     if (p.few) {
         deal(a, p.few_pieces, p.few_tiles * kTileRows, ws);
-        if (p.few_tiles == 1) launch_few<DT, ND, 1>(a, s);
-        else launch_few<DT, ND, 2>(a, s);
+        if constexpr (ND <= 8) {
+            if (p.few_tiles == 2) launch_few<DT, ND, 2>(a, s);
+            else launch_few<DT, ND, 1>(a, s);
+        } else {
+            launch_few<DT, ND, 1>(a, s);
+        }
     }
     if (p.many) {
         deal(a, p.many_pieces, p.many_rows, ws);
@@ -185,12 +195,13 @@ size_t rlcs_workspace_size_paged(int64_t tokens, int64_t B, int64_t Hq, int64_t 
     if (B > INT32_MAX / 2 || Hq > INT32_MAX || tokens > (INT32_MAX - (1 << 20)) / Hq) return 0;
     if (max_chunk == 0 || max_chunk > tokens) max_chunk = tokens;
     size_t most = 0;
-    for (const bool bf16 : {false, true}) {
-        PagedPlan p;
-        if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, true, bf16)) return 0;
-        const size_t n = plan_bytes(p, Hkv, D);
-        most = n > most ? n : most;
-    }
+    for (const bool bf16 : {false, true})
+        for (const bool ragged : {false, true}) {
+            PagedPlan p;
+            if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, ragged, bf16)) return 0;
+            const size_t n = plan_bytes(p, Hkv, D);
+            most = n > most ? n : most;
+        }
     return most;
 }
 

@@ -192,7 +192,7 @@ __device__ __forceinline__ int2 chunks_before(const PagesArgs& a, int64_t c) {
     return int2{before, all};
 }
 
-// Free pages go to the sequences, in order; a sequence whose pages there are not enough for stays as it was.
+// Free pages go to the sequences, in order, each wave with chunks that follow one another; a sequence whose pages there are not enough for stays as it was.
 __device__ __forceinline__ void pages_assign(const PagesArgs& a, Lanes at, int* s_offset) {
     const int lane = threadIdx.x & 63;
     const int needed = a.total[0];
@@ -203,8 +203,9 @@ __device__ __forceinline__ void pages_assign(const PagesArgs& a, Lanes at, int* 
     }
     const int64_t chunks = (int64_t(a.pages) + kChunkPages - 1) / kChunkPages;
     int free = chunks_before(a, 0).y;
-    for (int64_t c = at.id >> 6; c < chunks; c += at.n >> 6) {
-        int rank = chunks_before(a, c).x;
+    const int64_t per = (chunks + (at.n >> 6) - 1) / (at.n >> 6), c0 = (at.id >> 6) * per, c1 = c0 + per < chunks ? c0 + per : chunks;
+    int rank = c0 < c1 ? chunks_before(a, c0).x : 0;
+    for (int64_t c = c0; c < c1; ++c) {
         for (int i = 0; i < kChunkWords && rank < needed && (c * kChunkWords + i) * kWordPages < a.pages; ++i) {
             const uint64_t word = a.bits[c * kChunkWords + i];
             const int mine = rank + __popcll(word & ((uint64_t(1) << lane) - 1));
@@ -255,8 +256,9 @@ __device__ __forceinline__ void pages_plan_moves(const PagesArgs& a, Lanes at) {
         a.total[1] = front;
         a.count[0] = int(U);
     }
-    for (int64_t c = at.id >> 6; c < chunks; c += at.n >> 6) {
-        int rank = chunks_before(a, c).x;
+    const int64_t per = (chunks + (at.n >> 6) - 1) / (at.n >> 6), c0 = (at.id >> 6) * per, c1 = c0 + per < chunks ? c0 + per : chunks;
+    int rank = c0 < c1 ? chunks_before(a, c0).x : 0;
+    for (int64_t c = c0; c < c1; ++c) {
         for (int i = 0; i < kChunkWords && c * kChunkWords + i < words; ++i) {
             const int64_t at_word = c * kChunkWords + i, p = at_word * kWordPages + lane;
             const uint64_t word = a.bits[at_word];

@@ -146,3 +146,27 @@ def test_nothing():
     assert rl.rlcs_pages_copy(cache, torch.empty((0, 2), dtype=I32, device="cuda")) is cache
     t, r, m, c = rl.rlcs_pages_compact(torch.empty((0, 5), dtype=I32, device="cuda"), ints([0, 3]))
     assert t.shape == (0, 5) and r.tolist() == [3, 0] and m.tolist() == [[1, 0]] and c.item() == 1
+
+
+def test_more_pages_than_lanes_at_once():
+    """Each wave has several chunks of pages: 2.2 million and some."""
+    pages, page, W = 2 ** 21 + 100037, 16, 700
+    g = torch.Generator().manual_seed(5)
+    refs = (torch.rand(pages, generator=g) < 0.6).int()
+    used, free = refs.nonzero().flatten(), (refs == 0).nonzero().flatten()
+    U = len(used)
+    late, holes = used[used >= U], free[free < U]
+    held = torch.cat([used[:200], late[:100], late[-400:]])
+    table = held.int()[None].cuda()
+    t, r, m, c = rl.rlcs_pages_compact(table, refs.cuda())
+    to = torch.arange(pages)
+    to[late] = holes
+    assert c.item() == U and t.cpu().tolist() == [to[held].tolist()]
+    assert torch.equal(r.cpu(), (torch.arange(pages) < U).int())
+    assert torch.equal(m[: len(late)].cpu(), torch.stack([late, holes], 1).int()) and bool((m[len(late):] == -1).all())
+    B = 2000
+    t, n, r, m = rl.rlcs_pages_resize(torch.full((B, W), -1, dtype=I32, device="cuda"), torch.zeros(B, dtype=I32, device="cuda"), refs.cuda(),
+                                      torch.full((B,), W * page, dtype=I32, device="cuda"), page=page)
+    fit = min(B, len(free) // W)
+    assert torch.equal(t[:fit].cpu().flatten(), free[: fit * W].int()) and bool((t[fit:] == -1).all())
+    assert n.tolist() == [W * page] * fit + [0] * (B - fit) and int(r.sum()) == U + fit * W
