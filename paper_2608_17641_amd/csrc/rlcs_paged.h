@@ -119,16 +119,17 @@ struct PagedSeqs {
 };
 
 // How the tiles of a kernel, R rows each, are dealt out within a key head. Tiles lie one after the other on a line, each as long
-// as its work: its keys, and kTileWork units for what a tile costs beside them. The line is cut into pieces of equal length, whole tiles and parts
-// of tiles, so that all end together however lengths differ. Where they lie follows from the lengths on the device, which
-// every wave adds up for itself. Where there are more tiles than pieces, all but the last few tiles are not cut (many rows).
-constexpr int kTileWork = 2;
+// as its work: its keys, and kTile units for what a tile costs beside them. The line is cut into pieces of equal length, whole tiles and
+// parts of tiles, so that all end together however lengths differ. Where they lie follows from the lengths on the device, which
+// every wave adds up for itself.
+// kTile was measured: of many rows, 4 sequences of 2048 to 16384 keys, the last 2048 of them new: 1366 us with 6, 1381 with 4,
+// 1490 with 2, 1380 with 10, and 1421 where tiles are cut only as far as they are no multiple of the pieces.
+constexpr int kTileWork = 2, kTileWorkMany = 6;
 constexpr int kLeastWork = 4;  // units of a piece, at least
 template <bool FEW, int R>
 struct PagedLine {
-    int origin, each;  // where the pieces begin, their length;
-    int more, pieces;  // the first `more` are longer by one
-    int uncut;         // tiles before them
+    static constexpr int kTile = FEW ? kTileWork : kTileWorkMany;
+    int each, more, pieces;  // their length; the first `more` are longer by one
 
     // Tiles of a sequence: none, if it is the other kernel's.
     static __device__ __forceinline__ int tiles(const PagedArgs& a, const PagedSeq& s) {
@@ -139,26 +140,14 @@ struct PagedLine {
     // Where tile t of a sequence begins. (A tile's keys are those before the chunk and as many tokens as its rows and the
     // ones before are.)
     static __device__ __forceinline__ int begin(const PagedArgs& a, const PagedSeq& s, int t) {
-        if (FEW) return t * (kTileWork + (s.length >> a.unit));
+        if (FEW) return t * (kTile + (s.length >> a.unit));
         const int before = s.length > s.n ? s.length - s.n : 0;
-        return t * (kTileWork + (before >> a.unit)) + int(double(int64_t(t) * (t + 1) / 2) * a.rise);
+        return t * (kTile + (before >> a.unit)) + int(double(int64_t(t) * (t + 1) / 2) * a.rise);
     }
     static __device__ __forceinline__ int work(const PagedArgs& a, const PagedSeq& s) { return begin(a, s, tiles(a, s)); }
     __device__ __forceinline__ void plan(const PagedArgs& a, const PagedSeqs& seqs) {
-        uncut = origin = pieces = each = more = 0;
-        auto count = [&](const PagedSeq& s) { return tiles(a, s); };
-        auto length = [&](const PagedSeq& s) { return work(a, s); };
-        if (!FEW) {
-            const int n = seqs.sum(a.B, count);
-            uncut = n / a.pieces * a.pieces;
-            if (uncut == n) return;
-            if (uncut > 0) {
-                int b = 0;
-                const int t = seqs.locate(uncut, b, count);
-                origin = seqs.sum(b, length) + begin(a, seqs.get(b), t);
-            }
-        }
-        const int total = seqs.sum(a.B, length) - origin, most = (total + kLeastWork - 1) / kLeastWork;
+        each = more = 0;
+        const int total = seqs.sum(a.B, [&](const PagedSeq& s) { return work(a, s); }), most = (total + kLeastWork - 1) / kLeastWork;
         pieces = most < a.pieces ? most : a.pieces;
         if (pieces <= 0) {
             pieces = 0;
@@ -167,11 +156,11 @@ struct PagedLine {
         each = int(unsigned(total) / unsigned(pieces));
         more = total - each * pieces;
     }
-    __device__ __forceinline__ int piece(int w) const { return origin + w * each + (w < more ? w : more); }
+    __device__ __forceinline__ int piece(int w) const { return w * each + (w < more ? w : more); }
     // The key, a multiple of 64 or past the last, at which a tile is cut that many units after its begin; `sees`: its keys.
     static __device__ __forceinline__ int cut(const PagedArgs& a, int at, int length, int sees) {
         if (at >= length) return sees;
-        const int64_t key = at <= kTileWork ? 0 : int64_t(at - kTileWork) << a.unit;
+        const int64_t key = at <= kTile ? 0 : int64_t(at - kTile) << a.unit;
         return key < sees ? int(key) : sees;
     }
 };
@@ -385,24 +374,19 @@ __device__ __forceinline__ void hide_scores(f32x4 (&s)[KT], int first, int sees,
             if (first + 16 * kt + i >= sees || (out >> kt & 1)) s[kt][i] = kNegInf;
 }
 
-// Share k of a key head: a tile that is not cut, or a piece of the line, tile by tile.
+// Piece w of a key head, tile by tile.
 template <bool FEW, int R, class F>
-__device__ __forceinline__ void paged_share(const PagedArgs& a, const PagedSeqs& seqs, int k, int hk, F&& tile) {
+__device__ __forceinline__ void paged_share(const PagedArgs& a, const PagedSeqs& seqs, int w, int hk, F&& tile) {
     PagedLine<FEW, R> line;
     line.plan(a, seqs);
+    if (w >= line.pieces) return;
+    int x = line.piece(w);
+    const int end = line.piece(w + 1);
     PagedItem it;
     it.hk = hk;
-    int x = 0, end = 0, w = k - line.uncut;
-    if (w < 0) {
-        if (!it.number<FEW, R>(a, seqs, k)) return;
-    } else {
-        if (w >= line.pieces) return;
-        x = line.piece(w);
-        end = line.piece(w + 1);
-        if (!it.find<FEW, R>(a, seqs, x)) return;
-    }
+    if (!it.find<FEW, R>(a, seqs, x)) return;
     for (;;) {
-        const int rest = it.length - it.at, units = w < 0 || rest < end - x ? rest : end - x;
+        const int rest = it.length - it.at, units = rest < end - x ? rest : end - x;
         if (it.take<PagedLine<FEW, R>>(a, w, units)) tile(it);
         x += units;
         if (x >= end || !it.next<FEW, R>(a, seqs)) return;

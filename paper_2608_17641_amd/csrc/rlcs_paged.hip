@@ -106,7 +106,7 @@ void launch_few(const PagedArgs& a, hipStream_t s) {
 template <typename DT, int ND, int QT, int W>
 void launch_many(const PagedArgs& a, hipStream_t s) {
     constexpr int64_t R = W * QT * kTileRows;
-    const dim3 grid = row_grid((a.tokens * a.r / R + a.B + a.pieces) * a.Hkv), block(W * kWave);
+    const dim3 grid = row_grid(int64_t(a.pieces) * a.Hkv), block(W * kWave);
     if (a.D == 16 * ND) hipLaunchKernelGGL((paged_many_kernel<DT, ND, QT, W, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((paged_many_kernel<DT, ND, QT, W, false>), grid, block, 0, s, a);
     launch_join<DT, false, R>(a, s);
@@ -145,7 +145,7 @@ int work_unit(const PagedArgs& a) {
     const double tiles = double(a.tokens) * a.r / 64 + a.B, held = double(a.W) * double(1 << a.shift);
     const double keys = held > double(a.tokens) ? held : double(a.tokens);
     int unit = 6;
-    while (unit < 30 && tiles * (kTileWork + 3 + keys / double(1 << unit)) > double(1 << 30)) ++unit;
+    while (unit < 30 && tiles * (kTileWorkMany + 3 + keys / double(1 << unit)) > double(1 << 30)) ++unit;
     return unit;
 }
 
