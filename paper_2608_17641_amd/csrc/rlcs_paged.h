@@ -374,6 +374,46 @@ __device__ __forceinline__ void hide_scores(f32x4 (&s)[KT], int first, int sees,
             if (first + 16 * kt + i >= sees || (out >> kt & 1)) s[kt][i] = kNegInf;
 }
 
+// Infinite and NaN values of keys that some of the rows do not see: their product with a weight of 0 is NaN. In blocks of such keys they
+// count as 0, and are added at the end to the rows that see them.
+template <typename DT>
+__device__ __forceinline__ bool take_odd(u32x4& w) {  // true: there were some
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(DT) == 4) {
+            const uint32_t odd = (w[i] & 0x7f800000u) == 0x7f800000u ? ~0u : 0u;
+            w[i] &= ~odd;
+            all |= odd;
+        } else {  // (the top bit of each half whose exponent is all ones)
+            const uint32_t odd = ~((~w[i] & 0x7f807f80u) + 0x7fff7fffu) & 0x80008000u;
+            w[i] &= ~((odd >> 15) * 0xffffu);
+            all |= odd;
+        }
+    }
+    return all != 0;
+}
+// Where the blocks begin that not all rows see all of; `least`: keys that all rows see.
+__device__ __forceinline__ int first_unseen(int from, int least, int keys) { return from + (least > from ? (least - from) / keys * keys : 0); }
+// The sum of such values of keys [first, sees), four dimensions at d. (Apart from the products, whose registers a loop over the
+// outputs would cost: 1727 us became 1790.)
+template <typename DT>
+__device__ __forceinline__ f32x4 odd_values(const PagedArgs& a, const PagedItem& it, int first, int sees, int d) {
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int j = first; j < sees; ++j) {
+        const int page = a.table[int64_t(it.b) * a.ld_table + (j >> a.shift)];
+        if (unsigned(page) >= unsigned(a.pages)) continue;
+        const int64_t token = j & ((1 << a.shift) - 1);
+        const DT* v = reinterpret_cast<const DT*>(reinterpret_cast<const char*>(a.v) + page * a.vs[0] + token * a.vs[1] + it.hk * a.vs[2]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float value = widen(v[d + e]);
+            if ((__float_as_uint(value) & 0x7f800000u) == 0x7f800000u) o[e] += value;
+        }
+    }
+    return o;
+}
+
 // Piece w of a key head, tile by tile.
 template <bool FEW, int R, class F>
 __device__ __forceinline__ void paged_share(const PagedArgs& a, const PagedSeqs& seqs, int w, int hk, F&& tile) {
@@ -395,16 +435,17 @@ __device__ __forceinline__ void paged_share(const PagedArgs& a, const PagedSeqs&
 
 // ------------------------------------------------------------- few rows: keys dealt to waves
 
-// Keys [from, end) of one item, blocks wave, wave + W, ..., by a wave with QT tiles of sixteen rows.
+// Keys [from, end) of one item, blocks wave, wave + W, ..., by a wave with QT tiles of sixteen rows. True: there were odd values in
+// blocks that not all rows see all of.
 template <typename DT, int ND, int QT, int W, bool EXACT>
-__device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const PagedArgs& a, const PagedItem& it, const int (&sees)[QT], int least,
+__device__ __forceinline__ bool paged_run(AttnWave<DT, ND, QT, EXACT>& w, const PagedArgs& a, const PagedItem& it, const int (&sees)[QT], int least,
                                           int D, float scale, bf16_t* lds, int wave, int lane) {
     typedef KeyBlock<DT, ND, EXACT> Block;
     constexpr bool kWide = sizeof(DT) == 4;
     constexpr int kKeys = Block::kKeys, KT = kKeys / 16, G = kKeys / kKeyGroup, kVecs = Block::kVecs;
     const int c = lane & 15, g = lane >> 4, end = it.end;
     int j = it.from + wave * kKeys;
-    if (j >= end) return;
+    if (j >= end) return false;
     PageNumbers<G> numbers;
     numbers.begin(a.table + int64_t(it.b) * a.ld_table, j, W * kKeys, end, a.shift, [](int x) { return kKeyGroup * x; });
     Block b;
@@ -466,6 +507,7 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
         for (int x = 0; x < G; ++x) m |= at[x].there ? 0u : 1u << x;
         return m;
     };
+    bool odd = false;
     aim(0, j);
     uint32_t out = missing();
     load_k();
@@ -481,6 +523,10 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
                 constexpr int kRows = kWide ? 0 : 64 / kVecs;
                 if (out_here >> (i * kRows / kKeyGroup) & 1) b.v[i] = u32x4{0, 0, 0, 0};
             }
+        }
+        if (here + kKeys > least) {
+#pragma unroll
+            for (int i = 0; i < ND; ++i) odd |= take_odd<DT>(b.v[i]);
         }
         if (more) {
             aim(n, j);
@@ -546,7 +592,7 @@ __device__ __forceinline__ void paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
                     for (int x = 0; x < QT; ++x)
                         w.acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(now[t][i]), s[x][0][i], w.acc[x][t], 0, 0, 0);
         }
-        if (!more) return;
+        if (!more) return __any(odd);
     }
 }
 
@@ -568,7 +614,9 @@ __device__ __forceinline__ void paged_few_tile(const PagedArgs& a, const PagedIt
     }
     int least = it.sees(0, a);
     if (least > it.end) least = it.end;
-    paged_run<DT, ND, QT, W, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(mem) + wave * 32 * (16 * ND + 16), wave, lane);
+    const bool odd = paged_run<DT, ND, QT, W, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(mem) + wave * 32 * (16 * ND + 16), wave, lane);
+
+    const int first = __syncthreads_or(odd) ? first_unseen(it.from, least, KeyBlock<DT, ND, EXACT>::kKeys) : it.end;
 
     // the waves join, sixteen rows at a time
     float* join = reinterpret_cast<float*>(mem);
@@ -601,6 +649,10 @@ __device__ __forceinline__ void paged_few_tile(const PagedArgs& a, const PagedIt
                 const float keep = s_m[v][i] == kNegInf ? 0.f : exp2_fast(s_m[v][i] - m);
                 z = fmaf(keep, s_l[v][i], z);
                 o += keep * *reinterpret_cast<const f32x4*>(join + (v * kTileRows + i) * kJoinRow + d);
+            }
+            if (first < it.end) {
+                const int seen = it.sees(row0 + i, a);
+                o += odd_values<DT>(a, it, first, seen < it.end ? seen : it.end, d);
             }
             it.template store<DT, R>(row0 + i, it.out_row(row0 + i, a), d, o, m, z, a);
         }
@@ -639,7 +691,8 @@ __global__ __launch_bounds__(kAttnWaves * kWave) __attribute__((amdgpu_waves_per
         }
         int least = it.sees(0, a);
         if (least > it.end) least = it.end;
-        paged_run<DT, ND, QT, 1, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(s_mem) + wave * 32 * (16 * ND + 16), 0, lane);
+        const bool odd = paged_run<DT, ND, QT, 1, EXACT>(w, a, it, sees, least, D, score_scale(a.scale2), reinterpret_cast<bf16_t*>(s_mem) + wave * 32 * (16 * ND + 16), 0, lane);
+        const int first = odd ? first_unseen(it.from, least, KeyBlock<DT, ND, EXACT>::kKeys) : it.end;
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
             float l = w.l[x];
@@ -650,7 +703,10 @@ __global__ __launch_bounds__(kAttnWaves * kWave) __attribute__((amdgpu_waves_per
             const int64_t out = it.out_row(row, a);
 #pragma unroll
             for (int t = 0; t < ND; ++t)
-                if (EXACT || 16 * t + 4 * g4 < D) it.store<DT, R>(row, out, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
+                if (EXACT || 16 * t + 4 * g4 < D) {
+                    if (first < it.end) w.acc[x][t] += odd_values<DT>(a, it, first, sees[x], 16 * t + 4 * g4);
+                    it.store<DT, R>(row, out, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
+                }
         }
     });
 }
@@ -673,12 +729,12 @@ struct PagedShared {
     static constexpr size_t kLds = size_t(2 * kHalf) * sizeof(DT);
     static constexpr int kGroups = kKeys / kKeyGroup;
 
-    static __device__ __forceinline__ void run(AttnWave<DT, ND, QT, EXACT>& w, const PagedArgs& a, const PagedItem& it, const int (&sees)[QT], int least,
-                                               int most, int D, float scale, DT* lds, uint32_t (*s_out)[4], int tid) {
+    static __device__ __forceinline__ bool run(AttnWave<DT, ND, QT, EXACT>& w, const PagedArgs& a, const PagedItem& it, const int (&sees)[QT], int least,
+                                               int least_of_all, int most, int D, float scale, DT* lds, uint32_t (*s_out)[4], int tid) {
         const int lane = tid & 63, c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         constexpr int KT = kKeys / 16;
         const int from = it.from, end = it.end;
-        if (from >= end) return;
+        if (from >= end) return false;
         // piece i of a wave's lanes: rows (64 wave + 64 W i) / kVecs ... of a block, all in one group
         auto first_row = [&](int i) { return (64 * wave + 64 * W * i) / kVecs; };
         PageNumbers<kPieces> numbers;
@@ -702,8 +758,14 @@ struct PagedShared {
                 v[i] = *reinterpret_cast<const u32x4*>(values + at.at_v + row * sv + d);
             }
         };
-        auto put = [&](int turn) {
+        bool odd = false;
+        auto put = [&](int n) {
+            const int turn = n & 1;
             DT* half = lds + turn * kHalf;
+            if (__builtin_expect(from + (n + 1) * kKeys > least_of_all, 0)) {
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) odd |= take_odd<DT>(v[i]);
+            }
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int at = tid + W * kWave * i;
@@ -723,7 +785,7 @@ struct PagedShared {
             const DT* lk = lds + turn * kHalf;
             const DT* lv = lk + kKeys * kKRow;
             __syncthreads();  // this block is there, and the one before has been read
-            if (n + 1 < blocks) put(turn ^ 1);
+            if (n + 1 < blocks) put(n + 1);
             if (n + 2 < blocks) load(n + 2);
             if (j >= most) continue;  // (none of the wave's rows sees it)
             f32x4 s[QT][KT];
@@ -817,6 +879,7 @@ struct PagedShared {
                 }
             }
         }
+        return __syncthreads_or(odd);
     }
 };
 
@@ -839,7 +902,10 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs& a, const PagedI
     }
     int least = it.sees(row0, a), most = row0 < it.rows ? it.sees(row0 + QT * kTileRows - 1, a) : 0;
     if (least > it.end) least = it.end;
-    Shared::run(w, a, it, sees, least, most, D, score_scale(a.scale2), reinterpret_cast<DT*>(mem), s_out, tid);
+    int least_of_all = it.sees(it.tile * R, a);
+    if (least_of_all > it.end) least_of_all = it.end;
+    const bool odd = Shared::run(w, a, it, sees, least, least_of_all, most, D, score_scale(a.scale2), reinterpret_cast<DT*>(mem), s_out, tid);
+    const int first = odd ? first_unseen(it.from, least_of_all, Shared::kKeys) : it.end;
     const int g4 = lane >> 4;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
@@ -851,7 +917,10 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs& a, const PagedI
         const int64_t out = it.out_row(row, a);
 #pragma unroll
         for (int t = 0; t < ND; ++t)
-            if (EXACT || 16 * t + 4 * g4 < D) it.template store<DT, R>(row, out, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
+            if (EXACT || 16 * t + 4 * g4 < D) {
+                if (first < it.end) w.acc[x][t] += odd_values<DT>(a, it, first, sees[x], 16 * t + 4 * g4);
+                it.template store<DT, R>(row, out, 16 * t + 4 * g4, w.acc[x][t], w.m[x], l, a);
+            }
     }
 }
 
@@ -859,7 +928,7 @@ template <typename DT, int ND, int QT, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(ND > 8 ? 1 : 2, ND > 8 ? 1 : 2))) void paged_many_kernel(PagedArgs a) {
     constexpr int R = W * QT * kTileRows;
     __shared__ __attribute__((aligned(16))) char s_mem[PagedShared<DT, ND, QT, W, EXACT>::kLds];
-    __shared__ uint32_t s_out[2][4];
+    __shared__ uint32_t s_out[2][4];  // groups without a page, of each half
     const int block = int(grid_row());
     const PagedSeqs seqs(a);
     paged_share<false, R>(a, seqs, block / a.Hkv, block % a.Hkv, [&](const PagedItem& it) {

@@ -153,6 +153,33 @@ def test_nan_and_infinite(T):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,r,D,page,length", [(2, 1, 64, 16, 70), (3, 4, 128, 16, 300), (6, 4, 72, 64, 1500), (30, 2, 128, 16, 300), (90, 4, 64, 128, 2000),
+                                               (300, 1, 200, 16, 300), (9, 8, 256, 64, 1200)])
+def test_values_that_some_do_not_see(T, r, D, page, length, dtype):
+    """An infinite or NaN value shows in the tokens that see it; the others are what they are without it."""
+    Hkv = 2
+    c = case([length, length - 7, 5], [T, T, min(T, 5)], r * Hkv, Hkv, D, page, dtype, T + D)
+    q, k, v, table, lengths, start = c
+    bad = {}
+    for seq, back, head, d, x in [(0, 1, 0, 0, math.nan), (0, 2, 1, D - 1, math.inf), (0, T // 2 + 1, 1, 3, -math.inf), (1, T, 0, 7, math.nan),
+                                     (1, 1, 0, 5, math.inf), (1, 2, 0, 5, -math.inf), (2, 1, 1, 6, -math.inf), (0, length, 0, D - 2, math.nan)]:
+        bad[seq, max(0, lengths[seq] - back), head, d] = x
+    clean = v.clone()
+    for (seq, t, head, d), x in bad.items():
+        at = table[seq][t // page], t % page, head, d
+        v[at], clean[at] = x, 0.0
+    o, lse = rl.rlcs_paged_attn(*to_gpu(*c))
+    want, want_lse = rl.rlcs_paged_attn(*to_gpu(q, k, clean, table, lengths, start))
+    add = torch.zeros(want.shape)
+    for (seq, t, head, d), x in bad.items():
+        first = max(start[seq], start[seq + 1] - (lengths[seq] - t))
+        add[first:start[seq + 1], head * r:(head + 1) * r, d] += x
+    assert torch.equal(lse, want_lse) and not torch.isnan(want).any() and int((add != 0).sum()) > 0
+    want = torch.where(add == 0, want.cpu().float(), add)
+    assert torch.equal(torch.nan_to_num(o.cpu().float(), 3e38, 2e38, -2e38), torch.nan_to_num(want, 3e38, 2e38, -2e38))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_layouts(dtype):
     """Heads before tokens in a page, gaps between pages and heads, strided queries and tables."""
     c = case([100, 47], [33, 2], 4, 2, 64, 16, dtype, 11)
