@@ -486,7 +486,8 @@ size_t rlcs_workspace_size_paged(int64_t tokens, int64_t B, int64_t Hq, int64_t 
 
 /* The new tokens' keys and values to their places in the cache.
  *   k, v     [tokens, Hkv, D] dtype;  k_cache, v_cache  [pages, page, Hkv, D] dtype, written at the new tokens'
- *            positions only. Positions below 0 and entries that are no page are passed over
+ *            positions only. Positions below 0 and entries that are no page are passed over. Distinct
+ *            pages, tokens and heads do not overlap
  * Two sequences whose new tokens lie in the same page write over each other: rlcs_pages_resize gives each its
  * own. Strides, alignment and D as above.                                                    */
 rlcs_status rlcs_paged_write(const void* k, const void* v, void* k_cache, void* v_cache,

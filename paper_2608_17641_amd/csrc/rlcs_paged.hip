@@ -26,6 +26,21 @@ bool reachable(std::initializer_list<int64_t> sizes, const int64_t* strides) {
     }
     return true;
 }
+// Whether distinct places are distinct memory, D elements each: each axis steps over all that the ones with smaller steps reach.
+bool apart(const int64_t (&sizes)[3], const int64_t* strides, int64_t D) {
+    int64_t reach = D;
+    bool done[3] = {};
+    for (int n = 0; n < 3; ++n) {
+        int next = -1;
+        for (int i = 0; i < 3; ++i)
+            if (!done[i] && sizes[i] > 1 && (next < 0 || strides[i] < strides[next])) next = i;
+        if (next < 0) return true;
+        if (strides[next] < reach) return false;
+        reach += (sizes[next] - 1) * strides[next];
+        done[next] = true;
+    }
+    return true;
+}
 bool whole_vectors(const int64_t* s, int n, int64_t vec) {
     for (int i = 0; i < n; ++i)
         if (s[i] % vec) return false;
@@ -231,7 +246,8 @@ rlcs_status rlcs_paged_attn(const void* q, const void* k_cache, const void* v_ca
     if (!q_start) max_chunk = tokens / B;
     PagedPlan p;
     if (!make_plan(p, tokens, B, Hq, Hkv, D, max_chunk, q_start != nullptr, bf16, W * page)) return RLCS_ERR_INVALID_ARG;
-    if (const size_t need = plan_bytes(p, Hkv, D)) {
+    // (what every call of these sizes may need, though keys taken whole need none)
+    if (const size_t need = rlcs_workspace_size_paged(tokens, B, Hq, Hkv, D, max_chunk)) {
         if (!ws || ws_bytes < need) return RLCS_ERR_WORKSPACE;
         if (!aligned(ws, 16)) return RLCS_ERR_INVALID_ARG;
     }
@@ -262,6 +278,7 @@ rlcs_status rlcs_paged_write(const void* k, const void* v, void* k_cache, void* 
     if (!k || !v || !k_cache || !v_cache) return RLCS_ERR_INVALID_ARG;
     for (const void* p : {k, v, static_cast<const void*>(k_cache), static_cast<const void*>(v_cache)})
         if (!aligned(p, 16)) return RLCS_ERR_INVALID_ARG;
+    if (!apart({pages, page, Hkv}, at.k_cache, D) || !apart({pages, page, Hkv}, at.v_cache, D)) return RLCS_ERR_INVALID_ARG;
     const int64_t vec = 16 / int64_t(dtype_size(dtype));
     if (!whole_vectors(at.k_new, 2, vec) || !whole_vectors(at.v_new, 2, vec) || !reachable({tokens, Hkv}, at.k_new) ||
         !reachable({tokens, Hkv}, at.v_new))

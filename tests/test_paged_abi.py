@@ -64,6 +64,17 @@ def test_paged_write(lib):
     assert f(n=0, k=None) == f(pages=0, kc=None) == n.RLCS_OK
 
 
+def test_paged_write_to_overlapping_places(lib):
+    for page, token, head in ((0, 128, 64), (2048, 64, 64), (1024, 128, 64), (2048, 128, 0), (64, 64 * 17, 64 * 9)):
+        at = n.PagedLayout()
+        at.k_new[:], at.v_new[:] = (128, 64), (128, 64)
+        at.k_cache[:], at.v_cache[:] = (2048, 128, 64), (page, token, head)
+        a = dict(k=A, v=A, kc=A, vc=A, t=A, len=A, start=A, n=6, B=3, W=4, ld=4, pages=9, page=16, Hkv=2, D=64, at=ctypes.addressof(at), dtype=1, s=None)
+        assert lib.rlcs_paged_write(*a.values()) == n.RLCS_ERR_INVALID_ARG, (page, token, head)
+        at.k_cache[:], at.v_cache[:] = at.v_cache[:], at.k_cache[:]
+        assert lib.rlcs_paged_write(*a.values()) == n.RLCS_ERR_INVALID_ARG, (page, token, head)
+
+
 def test_pages(lib):
     def fork(**kw):
         a = dict(t=A, len=A, refs=A, parent=A, to=B2, lo=B2, ro=B2, B=3, W=4, pages=9, page=16, ws=A, wb=1 << 30, s=None)
