@@ -5,9 +5,10 @@
 // page is found by its rank among the free ones, in the order of their numbers, so what a call does follows
 // from its inputs alone. Counts change by atomics on integers, whose order does not show.
 //
-// A call is a few phases, each of which needs all of the one before: kernels of their own, or, where pages
-// and tables are small, one workgroup that waits between them. Bound by latency: a phase is one or two
-// dependent loads (a kernel of its own some 2 us).
+// A call is a few phases, each of which needs all of the one before: kernels of their own. Bound by latency: a phase is one or two
+// dependent loads, 2.3 to 6 us (64 sequences of 64 pages, 4096 pages, replayed from a graph: fork 16 us, resize 20, compact 17). One
+// workgroup that does all of a call and fences between its phases is slower at every size: with 256 pages and 128 entries resize 30
+// us and 17 in phases, compact 23 and 16, fork alike; with 8192 of both 40 and 20, 35 and 17, 31 and 17.
 #pragma once
 
 #include "rlcs.h"
@@ -19,7 +20,7 @@ constexpr int kWordPages = 64;             // pages whose state is one word of b
 constexpr int kChunkWords = 4;             // words that a wave counts
 constexpr int kChunkPages = kWordPages * kChunkWords;
 constexpr int kOffsetsInLds = 4096;        // sequences whose offsets a workgroup keeps in LDS
-constexpr int kPagesGroup = 256, kPagesSmall = 1024;  // lanes of a workgroup, and of the only one
+constexpr int kPagesGroup = 256;           // lanes of a workgroup
 
 // What a sequence asks for: pages from rank `offset` of the free ones on, `need` of them, the first of which
 // replaces the last it holds where `copies`.
@@ -45,15 +46,6 @@ struct Lanes {
 __device__ __forceinline__ Lanes grid_lanes() {
     return Lanes{int64_t(blockIdx.x) * blockDim.x + threadIdx.x, int64_t(gridDim.x) * blockDim.x};
 }
-__device__ __forceinline__ Lanes group_lanes() { return Lanes{threadIdx.x, blockDim.x}; }
-
-// Between the phases of a single workgroup: atomics pass the CU's own cache by.
-__device__ __forceinline__ void next_phase() {
-    __threadfence();
-    __syncthreads();
-    __threadfence();
-}
-
 __device__ __forceinline__ int pages_of(int tokens, int shift) { return (tokens + (1 << shift) - 1) >> shift; }
 __device__ __forceinline__ bool is_page(const PagesArgs& a, int p) { return unsigned(p) < unsigned(a.pages); }
 __device__ __forceinline__ int held_length(const PagesArgs& a, int b) {
@@ -124,9 +116,9 @@ __device__ __forceinline__ void pages_count(const PagesArgs& a, const int32_t* r
     }
 }
 
-// What each sequence needs, and its place among the free pages: by one workgroup of T lanes.
-template <int T>
+// What each sequence needs, and its place among the free pages: by one workgroup.
 __device__ __forceinline__ void pages_needs(const PagesArgs& a, int* s_scan) {
+    constexpr int T = kPagesGroup;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += T) {
@@ -318,7 +310,7 @@ __global__ __launch_bounds__(kPagesGroup) void pages_phase_kernel(PagesArgs a) {
     if constexpr (PH == kRelease) pages_release(a, at);
     if constexpr (PH == kCountFree) {
         __shared__ int s_scan[kPagesGroup / kWave];
-        if (blockIdx.x + 1 == gridDim.x) pages_needs<kPagesGroup>(a, s_scan);
+        if (blockIdx.x + 1 == gridDim.x) pages_needs(a, s_scan);
         else pages_count<true>(a, a.refs_out, at.id >> 6, (at.n - kPagesGroup) >> 6);
     }
     if constexpr (PH == kAssign) {
@@ -328,37 +320,6 @@ __global__ __launch_bounds__(kPagesGroup) void pages_phase_kernel(PagesArgs a) {
     if constexpr (PH == kCountUsed) pages_count<false>(a, a.refs, at.id >> 6, at.n >> 6);
     if constexpr (PH == kPlanMoves) pages_plan_moves(a, at);
     if constexpr (PH == kRenumber) pages_renumber(a, at);
-}
-
-enum PagesCall { kCallFork, kCallResize, kCallCompact };
-
-// All of a call by one workgroup.
-template <PagesCall C>
-__global__ __launch_bounds__(kPagesSmall) void pages_small_kernel(PagesArgs a) {
-    const Lanes at = group_lanes();
-    if constexpr (C == kCallFork) {
-        pages_copy_refs(a, at);
-        next_phase();
-        pages_fork(a, at);
-    }
-    if constexpr (C == kCallResize) {
-        __shared__ int s_scan[kPagesSmall / kWave], s_offset[kOffsetsInLds];
-        pages_copy_refs(a, at);
-        next_phase();
-        pages_release(a, at);
-        next_phase();
-        pages_count<true>(a, a.refs_out, at.id >> 6, at.n >> 6);
-        pages_needs<kPagesSmall>(a, s_scan);
-        next_phase();
-        pages_assign(a, at, s_offset);
-    }
-    if constexpr (C == kCallCompact) {
-        pages_count<false>(a, a.refs, at.id >> 6, at.n >> 6);
-        next_phase();
-        pages_plan_moves(a, at);
-        next_phase();
-        pages_renumber(a, at);
-    }
 }
 
 struct PagesCopyArgs {

@@ -7,8 +7,6 @@ using namespace rlcs::host;
 
 namespace {
 
-// Calls of at most this many pages and table entries run as one workgroup.
-constexpr int64_t kSmallPages = 4096;
 constexpr int64_t kMaxGroups = 2048;
 
 bool good_page(int64_t page) { return page >= 16 && page <= 65536 && (page & (page - 1)) == 0; }
@@ -59,18 +57,12 @@ rlcs_status prepare(PagesArgs& a, int64_t B, int64_t W, int64_t pages, int64_t p
     return RLCS_OK;
 }
 
-bool small(const PagesArgs& a) { return int64_t(a.pages) + int64_t(a.B) * a.W <= kSmallPages && a.B <= kOffsetsInLds; }
-
 template <PagesPhase PH>
 void phase(const PagesArgs& a, int64_t lanes, hipStream_t s, int extra = 0) {
     int64_t groups = (lanes + kPagesGroup - 1) / kPagesGroup;
     if (groups > kMaxGroups) groups = kMaxGroups;
     if (groups < 1) groups = 1;
     hipLaunchKernelGGL((pages_phase_kernel<PH>), dim3(unsigned(groups + extra)), dim3(kPagesGroup), 0, s, a);
-}
-template <PagesCall C>
-void whole(const PagesArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((pages_small_kernel<C>), dim3(1), dim3(kPagesSmall), 0, s, a);
 }
 int64_t entries(const PagesArgs& a) { return int64_t(a.B) * a.W; }
 int64_t counting(const PagesArgs& a) { return (int64_t(a.pages) + kChunkPages - 1) / kChunkPages * kWave; }
@@ -110,12 +102,8 @@ rlcs_status rlcs_pages_fork(const int32_t* table, const int32_t* length, const i
     a.table = table; a.length = length; a.refs = refs; a.wanted = parent;
     a.table_out = table_out; a.length_out = length_out; a.refs_out = refs_out;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (small(a)) {
-        whole<kCallFork>(a, s);
-    } else {
-        if (refs_out != refs) phase<kCopyRefs>(a, pages, s);
-        phase<kFork>(a, entries(a), s);
-    }
+    if (refs_out != refs) phase<kCopyRefs>(a, pages, s);
+    phase<kFork>(a, entries(a), s);
     return launched();
 }
 
@@ -132,14 +120,10 @@ rlcs_status rlcs_pages_resize(const int32_t* table, const int32_t* length, const
     a.table = table; a.length = length; a.refs = refs; a.wanted = new_length;
     a.table_out = table_out; a.length_out = length_out; a.refs_out = refs_out; a.moves = moves;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (small(a)) {
-        whole<kCallResize>(a, s);
-    } else {
-        if (refs_out != refs) phase<kCopyRefs>(a, pages, s);
-        phase<kRelease>(a, entries(a), s);
-        phase<kCountFree>(a, counting(a), s, 1);
-        phase<kAssign>(a, most_of(counting(a), B), s);
-    }
+    if (refs_out != refs) phase<kCopyRefs>(a, pages, s);
+    phase<kRelease>(a, entries(a), s);
+    phase<kCountFree>(a, counting(a), s, 1);
+    phase<kAssign>(a, most_of(counting(a), B), s);
     return launched();
 }
 
@@ -158,13 +142,9 @@ rlcs_status rlcs_pages_compact(const int32_t* table, const int32_t* refs, int32_
         if (p && !aligned(p, 4)) return RLCS_ERR_INVALID_ARG;
     a.table = table; a.refs = refs; a.table_out = table_out; a.refs_out = refs_out; a.moves = moves; a.count = count;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (small(a)) {
-        whole<kCallCompact>(a, s);
-    } else {
-        phase<kCountUsed>(a, counting(a), s);
-        phase<kPlanMoves>(a, most_of(counting(a), pages / 8), s);
-        phase<kRenumber>(a, most_of(entries(a), pages), s);
-    }
+    phase<kCountUsed>(a, counting(a), s);
+    phase<kPlanMoves>(a, most_of(counting(a), pages / 8), s);
+    phase<kRenumber>(a, most_of(entries(a), pages), s);
     return launched();
 }
 

@@ -8,7 +8,8 @@ using namespace rlcs::host;
 namespace {
 
 constexpr int64_t kMaxDrafted = 1024;
-// Parts of a row: as many as give kWantItems workgroups in all, each of at least kMinPart logits.
+// Parts of a row: as many as give kWantItems workgroups in all, each of at least kMinPart logits. (64 sequences of 7 tokens, 128000
+// logits: 67 us; with 2048 workgroups 72, with 512 68. 256 of one token, 32000 logits: 33 us, 39, 34. Parts of at least 4096: alike.)
 constexpr int64_t kWantItems = 1024, kMinPart = 2048, kMostParts = 64;
 
 int64_t parts_of(int64_t rows, int64_t V) {
