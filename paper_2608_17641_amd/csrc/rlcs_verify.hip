@@ -45,7 +45,7 @@ bool sizes_fit(int64_t B, int64_t K, int64_t V) {
     return B >= 0 && K >= 0 && V >= 0 && K <= kMaxDrafted && V <= (int64_t(1) << 24) && B <= INT32_MAX / (2 * K + 1) / kMostParts;
 }
 
-// Rows of at most this many logits are a wave's.
+// Parts of at most this many logits are a wave's: a lane of four waves would have one vector or two.
 constexpr int64_t kWaveRow = 2048;
 
 template <typename DT>
