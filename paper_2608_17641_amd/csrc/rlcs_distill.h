@@ -330,14 +330,15 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
 }
 
 // Longer rows, one per workgroup of W waves: one pass for the sums, each lane relative to its own running
-// maximum, and one that writes the gradient. Both passes spend about eight vector operations a logit, one of them an exponential.
-// 8192 rows of 128000 bfloat16 logits, a third of weight 0: 768 us; the caches fetch 1.4 GB twice and write 2.1, 6.4 TB/s of that. Loads of two
-// vectors at a time: 834 us, of eight 782; all of a row in 16 waves' registers 2294 us.
+// maximum, and one backwards that writes the gradient, from the registers of the first pass's last vectors. Both passes spend about eight vector operations a logit, one of them an exponential.
+// 8192 rows of 128000 bfloat16 logits, a third of weight 0: 710 us, 8 waves with eight vectors a lane at a time; the caches
+// fetch most of 1.4 GB twice and write 2.1, 6.4 TB/s of that. Four vectors: 772 us, twelve 884, sixteen 841; eight by 4 waves 824, by 16
+// 753; all of a row in 16 waves' registers 2294 us.
 template <typename DT, bool TAIL, int W>
 __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) {
     extern __shared__ __attribute__((aligned(16))) char s_mem[];
     __shared__ float s_slots[Team<W>::kFolds * W];
-    constexpr int K = RowVec<DT>::K, U = 4, kLanes = W * kWave;
+    constexpr int K = RowVec<DT>::K, U = 8, kLanes = W * kWave;
     const int64_t row = grid_row();
     if (row >= a.M) return;
     const int tid = threadIdx.x;
@@ -368,6 +369,7 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
         sc = to;
     };
     const int64_t span = TAIL ? kBits / K : vecs;  // vectors whose bits are there
+    RowVec<DT> v[U];
     for (int64_t from = 0; from < vecs; from += span) {
         const int64_t end = from + span < vecs ? from + span : vecs;
         if (TAIL && a.V > kBits) {  // the bits of this part of the row
@@ -382,7 +384,6 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
             __syncthreads();
         }
         for (int64_t i0 = from + tid; i0 < end; i0 += U * kLanes) {
-            RowVec<DT> v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, i0 + u * kLanes < end ? a.V : 0);  // (past the end: -inf)
             float t = top;
@@ -413,10 +414,12 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
     if (!g) return;
     const float factor = r.factor * r.inv;
     // backwards: what the first pass read last is nearest in the caches
-    for (int64_t i0 = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid; i0 >= 0; i0 -= U * kLanes) {
-        RowVec<DT> v[U];
+    const int64_t last = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid;
+    for (int64_t i0 = last; i0 >= 0; i0 -= U * kLanes) {
+        if (i0 != last) {  // (which is still there)
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, a.V);
+            for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, a.V);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = i0 + u * kLanes;

@@ -22,7 +22,7 @@ void launch_rows(const DistillArgs& a, hipStream_t s) {
 }
 
 // As many waves and vectors a lane as hold the row in registers; longer rows are read twice, by 16 waves where there is no more
-// than a row for each CU (128 rows of 128000 bfloat16: 23.7 us, 8 waves 27.6) and else by 8 (8192 rows: 768 us, 16 waves 773).
+// than a row for each CU (128 rows of 128000 bfloat16: 22.7 us, 8 waves 27.6) and else by 8 (8192 rows: 710 us, 16 waves 753).
 constexpr int64_t kFewRows = 256;
 
 template <typename DT, bool TAIL>

@@ -178,8 +178,8 @@ struct PagedItem {
     int from, end, slot;  // keys of this part; slot: of the workspace, or -1: these are all
 
     template <class Line>
-    __device__ __forceinline__ void enter(const PagedArgs& a, const PagedSeqs& seqs) {
-        s = seqs.get(b);
+    __device__ __forceinline__ void enter(const PagedArgs& a, const PagedSeq& of) {
+        s = of;
         tiles = Line::tiles(a, s);
         rows = s.taken * a.r;
     }
@@ -188,15 +188,16 @@ struct PagedItem {
         length = Line::begin(a, s, tile + 1) - Line::begin(a, s, tile);
         all = sees((tile + 1) * R - 1, a);
     }
-    // Tile number k of all, to be taken whole.
-    template <bool FEW, int R>
-    __device__ __forceinline__ bool number(const PagedArgs& a, const PagedSeqs& seqs, int k) {
-        typedef PagedLine<FEW, R> Line;
-        tile = seqs.locate(k, b, [&](const PagedSeq& o) { return Line::tiles(a, o); });
-        if (tile < 0) return false;
-        enter<Line>(a, seqs);
+    // The tile of sequence `of`, where it has one at most, to be taken whole.
+    template <int R>
+    __device__ __forceinline__ bool only(const PagedArgs& a, int of) {
+        typedef PagedLine<true, R> Line;
+        b = of;
+        tile = at = 0;
+        const PagedSeq one = paged_seq(a, b);
+        enter<Line>(a, PagedSeq{agreed(one.first), agreed(one.n), agreed(one.taken), agreed(one.length)});
+        if (tiles == 0) return false;
         aim<Line, R>(a);
-        at = 0;
         return true;
     }
     // The tile at place x of the line.
@@ -205,7 +206,7 @@ struct PagedItem {
         typedef PagedLine<FEW, R> Line;
         at = seqs.locate(x, b, [&](const PagedSeq& o) { return Line::work(a, o); });
         if (at < 0) return false;
-        enter<Line>(a, seqs);
+        enter<Line>(a, seqs.get(b));
         int lo = 0, hi = tiles;  // the last tile that begins at `at` or before
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -226,7 +227,7 @@ struct PagedItem {
             tile = 0;
             do {
                 if (++b >= a.B) return false;
-                enter<Line>(a, seqs);
+                enter<Line>(a, seqs.get(b));
             } while (tiles == 0);
         }
         aim<Line, R>(a);
@@ -669,10 +670,10 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs
     __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, kAttnWaves>()];
     __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
     const int block = int(grid_row());
-    const PagedSeqs seqs(a);
     PagedItem it;
     it.hk = block % a.Hkv;
-    if (it.number<true, QT * kTileRows>(a, seqs, block / a.Hkv) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length)) paged_few_tile<DT, ND, QT, EXACT>(a, it, s_mem, s_m, s_l);
+    if (it.only<QT * kTileRows>(a, block / a.Hkv) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length))
+        paged_few_tile<DT, ND, QT, EXACT>(a, it, s_mem, s_m, s_l);
 }
 
 // The same with a wave on each piece of the line: no barrier, and nothing to join within the workgroup. One wave a SIMD, with all of
