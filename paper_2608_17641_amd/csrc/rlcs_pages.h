@@ -194,9 +194,10 @@ __device__ __forceinline__ void pages_assign(const PagesArgs& a, Lanes at, int* 
         __syncthreads();
     }
     const int64_t chunks = (int64_t(a.pages) + kChunkPages - 1) / kChunkPages;
-    int free = chunks_before(a, 0).y;
     const int64_t per = (chunks + (at.n >> 6) - 1) / (at.n >> 6), c0 = (at.id >> 6) * per, c1 = c0 + per < chunks ? c0 + per : chunks;
-    int rank = c0 < c1 ? chunks_before(a, c0).x : 0;
+    const int2 sums = chunks_before(a, c0);
+    int rank = sums.x;
+    const int free = sums.y;
     for (int64_t c = c0; c < c1; ++c) {
         for (int i = 0; i < kChunkWords && rank < needed && (c * kChunkWords + i) * kWordPages < a.pages; ++i) {
             const uint64_t word = a.bits[c * kChunkWords + i];
@@ -233,7 +234,10 @@ __device__ __forceinline__ void pages_assign(const PagesArgs& a, Lanes at, int* 
 __device__ __forceinline__ void pages_plan_moves(const PagesArgs& a, Lanes at) {
     const int lane = threadIdx.x & 63;
     const int64_t chunks = (int64_t(a.pages) + kChunkPages - 1) / kChunkPages, words = (int64_t(a.pages) + kWordPages - 1) / kWordPages;
-    const int64_t U = chunks_before(a, 0).y, cu = U / kChunkPages;
+    const int64_t per = (chunks + (at.n >> 6) - 1) / (at.n >> 6), c0 = (at.id >> 6) * per, c1 = c0 + per < chunks ? c0 + per : chunks;
+    const int2 sums = chunks_before(a, c0);
+    int rank = sums.x;
+    const int64_t U = sums.y, cu = U / kChunkPages;
     int front = 0;  // of the pages in use, those before U
     if (lane < kChunkWords && cu * kChunkWords + lane < words) {
         const int64_t left = U - (cu * kChunkWords + lane) * kWordPages;
@@ -248,8 +252,6 @@ __device__ __forceinline__ void pages_plan_moves(const PagesArgs& a, Lanes at) {
         a.total[1] = front;
         a.count[0] = int(U);
     }
-    const int64_t per = (chunks + (at.n >> 6) - 1) / (at.n >> 6), c0 = (at.id >> 6) * per, c1 = c0 + per < chunks ? c0 + per : chunks;
-    int rank = c0 < c1 ? chunks_before(a, c0).x : 0;
     for (int64_t c = c0; c < c1; ++c) {
         for (int i = 0; i < kChunkWords && c * kChunkWords + i < words; ++i) {
             const int64_t at_word = c * kChunkWords + i, p = at_word * kWordPages + lane;
