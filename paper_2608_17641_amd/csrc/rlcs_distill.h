@@ -332,7 +332,7 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
 // Longer rows, one per workgroup of W waves: one pass for the sums, each lane relative to its own running
 // maximum, and one backwards that writes the gradient, from the registers of the first pass's last vectors. Both passes spend about eight vector operations a logit, one of them an exponential.
 // 8192 rows of 128000 bfloat16 logits, a third of weight 0: 710 us, 8 waves with eight vectors a lane at a time; the caches
-// fetch most of 1.4 GB twice and write 2.1, 6.4 TB/s of that. Four vectors: 772 us, twelve 884, sixteen 841; eight by 4 waves 824, by 16
+// fetch 2.5 GB for 1.4 and write 2.1, 6.5 TB/s of that. Four vectors: 772 us, twelve 884, sixteen 841; eight by 4 waves 824, by 16
 // 753; all of a row in 16 waves' registers 2294 us.
 template <typename DT, bool TAIL, int W>
 __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) {

@@ -5,10 +5,10 @@
 // page is found by its rank among the free ones, in the order of their numbers, so what a call does follows
 // from its inputs alone. Counts change by atomics on integers, whose order does not show.
 //
-// A call is a few phases, each of which needs all of the one before: kernels of their own. Bound by latency: a phase is one or two
-// dependent loads, 2.3 to 6 us (64 sequences of 64 pages, 4096 pages, replayed from a graph: fork 16 us, resize 20, compact 17). One
-// workgroup that does all of a call and fences between its phases is slower at every size: with 256 pages and 128 entries resize 30
-// us and 17 in phases, compact 23 and 16, fork alike; with 8192 of both 40 and 20, 35 and 17, 31 and 17.
+// A call is a few phases, each of which needs all of the one before: barriers of one workgroup that has all counts in LDS, or, of
+// more pages or entries than that is good for, kernels of their own. Bound by latency: a phase is one or two dependent loads. (One workgroup with
+// its counts in memory, whose atomics pass its cache by, has to fence between phases: 30 us for a resize of 256 pages that takes 5
+// in LDS and 12 in four kernels.)
 #pragma once
 
 #include "rlcs.h"
@@ -20,7 +20,8 @@ constexpr int kWordPages = 64;             // pages whose state is one word of b
 constexpr int kChunkWords = 4;             // words that a wave counts
 constexpr int kChunkPages = kWordPages * kChunkWords;
 constexpr int kOffsetsInLds = 4096;        // sequences whose offsets a workgroup keeps in LDS
-constexpr int kPagesGroup = 256;           // lanes of a workgroup
+constexpr int kLdsPages = 8192;            // pages whose counts fit in LDS
+constexpr int kPagesGroup = 256, kPagesSmall = 1024;  // lanes of a workgroup, and of the only one
 
 // What a sequence asks for: pages from rank `offset` of the free ones on, `need` of them, the first of which
 // replaces the last it holds where `copies`.
@@ -46,6 +47,8 @@ struct Lanes {
 __device__ __forceinline__ Lanes grid_lanes() {
     return Lanes{int64_t(blockIdx.x) * blockDim.x + threadIdx.x, int64_t(gridDim.x) * blockDim.x};
 }
+__device__ __forceinline__ Lanes group_lanes() { return Lanes{threadIdx.x, blockDim.x}; }
+
 __device__ __forceinline__ int pages_of(int tokens, int shift) { return (tokens + (1 << shift) - 1) >> shift; }
 __device__ __forceinline__ bool is_page(const PagesArgs& a, int p) { return unsigned(p) < unsigned(a.pages); }
 __device__ __forceinline__ int held_length(const PagesArgs& a, int b) {
@@ -116,9 +119,9 @@ __device__ __forceinline__ void pages_count(const PagesArgs& a, const int32_t* r
     }
 }
 
-// What each sequence needs, and its place among the free pages: by one workgroup.
+// What each sequence needs, and its place among the free pages: by one workgroup of T lanes.
+template <int T>
 __device__ __forceinline__ void pages_needs(const PagesArgs& a, int* s_scan) {
-    constexpr int T = kPagesGroup;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += T) {
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(kPagesGroup) void pages_phase_kernel(PagesArgs a) {
     if constexpr (PH == kRelease) pages_release(a, at);
     if constexpr (PH == kCountFree) {
         __shared__ int s_scan[kPagesGroup / kWave];
-        if (blockIdx.x + 1 == gridDim.x) pages_needs(a, s_scan);
+        if (blockIdx.x + 1 == gridDim.x) pages_needs<kPagesGroup>(a, s_scan);
         else pages_count<true>(a, a.refs_out, at.id >> 6, (at.n - kPagesGroup) >> 6);
     }
     if constexpr (PH == kAssign) {
@@ -322,6 +325,44 @@ __global__ __launch_bounds__(kPagesGroup) void pages_phase_kernel(PagesArgs a) {
     if constexpr (PH == kCountUsed) pages_count<false>(a, a.refs, at.id >> 6, at.n >> 6);
     if constexpr (PH == kPlanMoves) pages_plan_moves(a, at);
     if constexpr (PH == kRenumber) pages_renumber(a, at);
+}
+
+enum PagesCall { kCallFork, kCallResize, kCallCompact };
+
+// All of a call by one workgroup, with the counts of all pages in LDS, where a barrier is all that lies between two phases.
+template <PagesCall C>
+__global__ __launch_bounds__(kPagesSmall) void pages_lds_kernel(PagesArgs given) {
+    __shared__ int32_t s_refs[kLdsPages], s_chunk[kLdsPages / kChunkPages], s_before[kLdsPages / kWordPages], s_total[2];
+    __shared__ uint64_t s_bits[kLdsPages / kWordPages];
+    const Lanes at = group_lanes();
+    PagesArgs a = given;
+    a.bits = s_bits;
+    a.chunk = s_chunk;
+    a.before = s_before;
+    a.total = s_total;
+    a.refs_out = s_refs;
+    for (int64_t p = at.id; p < a.pages; p += at.n) s_refs[p] = given.refs[p];
+    __syncthreads();
+    if constexpr (C == kCallFork) pages_fork(a, at);
+    if constexpr (C == kCallResize) {
+        __shared__ int s_scan[kPagesSmall / kWave], s_offset[kOffsetsInLds];
+        pages_release(a, at);
+        __syncthreads();
+        pages_count<true>(a, s_refs, at.id >> 6, at.n >> 6);
+        pages_needs<kPagesSmall>(a, s_scan);
+        __syncthreads();
+        pages_assign(a, at, s_offset);
+    }
+    if constexpr (C == kCallCompact) {
+        a.refs = s_refs;
+        pages_count<false>(a, s_refs, at.id >> 6, at.n >> 6);
+        __syncthreads();
+        pages_plan_moves(a, at);
+        __syncthreads();
+        pages_renumber(a, at);
+    }
+    __syncthreads();
+    for (int64_t p = at.id; p < a.pages; p += at.n) given.refs_out[p] = s_refs[p];
 }
 
 struct PagesCopyArgs {
