@@ -495,13 +495,15 @@ __device__ __forceinline__ bool paged_run(AttnWave<DT, ND, QT, EXACT>& w, const 
                 }
             }
         } else {
+            // (whole rows, past the caches, which keys in pieces of 64 bytes need: 64 sequences of 4096 keys, 8 key heads of 128 dimensions:
+            // 180 us, else 197; of 64 dimensions 91 and 113; but four sequences on the same pages each 103 and 91, sixteen 91 and 84)
 #pragma unroll
             for (int i = 0; i < ND; ++i) {
                 constexpr int kRows = 64 / kVecs;  // of a load
                 const KeyGroup& k = at[i * kRows / kKeyGroup];
                 const int r = (lane / kVecs + i * kRows) % kKeyGroup, piece = lane % kVecs;
                 const uint32_t o = row(r, k) * sv + 16u * (EXACT || 8 * piece < D ? piece : D / 8 - 1);
-                b.v[i] = *reinterpret_cast<const u32x4*>(values + k.at_v + o);
+                b.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(values + k.at_v + o));
             }
         }
     };
@@ -677,8 +679,8 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs
 }
 
 // The same with a wave on each piece of the line: no barrier, and nothing to join within the workgroup. One wave a SIMD, with all of
-// its registers for keys on their way. 64 sequences of 5120 keys, 8 key heads of 128 dimensions, bfloat16: 243 us for one new
-// token each (5.5 TB/s; of 20480 keys 5.8), of up to 8192 keys and 4 query heads to a key head 245 to 259 us for 1.35 GB.
+// its registers for keys on their way. 64 sequences of 5120 keys, 8 key heads of 128 dimensions, bfloat16, 4 query heads
+// to a key head: 235 us for one new token each (5.7 TB/s); of up to 8192 keys 238 us for 1.35 GB.
 template <typename DT, int ND, int QT, bool EXACT>
 __global__ __launch_bounds__(kAttnWaves * kWave) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_solo_kernel(PagedArgs a) {
     constexpr int R = QT * kTileRows;
@@ -974,7 +976,7 @@ __device__ __forceinline__ int sequence_of(const PagedArgs& a, int64_t t) {
 // Joins the parts of the tiles that are cut, o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i: a tile by the workgroups of the
 // first cut in it, each with kJoinRows of its rows, D / 4 lanes (four dimensions each) a row; where that leaves lanes, several
 // groups of them on parts in turn. Bound by latency, the plan first (with 8 rows a workgroup, and twice as many plans, 159 us where
-// it takes 156 in all, with 4 167). 64 sequences, 20 rows: 16 us of 156; 4 of 2048 tokens 36 of 1720.
+// it took 156 in all, with 4 167). 64 sequences, 20 rows: 16 us of 147; 4 of 2048 tokens 36 of 1720.
 constexpr int kJoinRows = 16;
 template <typename DT, bool FEW, int R>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {

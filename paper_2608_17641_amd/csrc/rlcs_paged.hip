@@ -48,14 +48,13 @@ bool whole_vectors(const int64_t* s, int n, int64_t vec) {
 }
 
 // Where no sequence can have more keys than this, all are taken whole: no second kernel. (64 sequences of 1024 keys, 8 key
-// heads of 128 dimensions, 4 rows: 42 us, in pieces 51; of one to 1024 keys 29 and 35; of 2048 keys 97 and 106, but of one to 2048
+// heads of 128 dimensions, 4 rows: 42 us, in pieces 51; of one to 1024 keys 29 and 35; of 2048 keys 79 and 89, but of one to 2048
 // 59 and 54.)
 constexpr int64_t kWholeKeys = 1024;
-// Tiles of sixteen rows, up to which the rows of a sequence are the first kernel's: two. One in bfloat16 where all sequences have as
-// many (64 of 4096 keys, 20 rows: 213 us with two, 198 by the second kernel; float32, 64 of 2048: 130 and 186) and keys are not taken
-// whole (8 of 512: 12 us, by the second 22; where rows differ, the second would be one more: 64 of up to 4096 keys and up to 20 rows 156
-// us, else 181). One of more than 128 dimensions, as two do not fit in a wave's registers (192 dimensions: 664 us, by the second 449).
-int few_tiles_of(int64_t D, bool bf16, bool ragged, bool whole) { return D <= 128 && (whole || ragged || !bf16) ? 2 : 1; }
+// Tiles of sixteen rows, up to which the rows of a sequence are the first kernel's: two (64 sequences of 4096 bfloat16 keys, 20 rows: 198 us,
+// by the second kernel 212; of 64 dimensions 98 and 140; float32, 64 of 2048: 130 and 186; but 8 sequences of 4096 keys, 32 rows: 66 and
+// 49). One of more than 128 dimensions, as two do not fit in a wave's registers (192 dimensions: 664 us, by the second 449).
+int few_tiles_of(int64_t D) { return D <= 128 ? 2 : 1; }
 // Pieces that all keys are dealt out in: as many as the GPU holds at once. Waves of the first kernel, one a SIMD;
 // workgroups of the second, one a CU.
 constexpr int64_t kPiecesFew = 1024, kPiecesMany = 256;
@@ -74,7 +73,7 @@ bool make_plan(PagedPlan& p, int64_t tokens, int64_t B, int64_t Hq, int64_t Hkv,
     const int64_t r = Hq / Hkv, most = max_chunk * r;
     p = PagedPlan{};
     const bool whole = most_keys && most_keys <= kWholeKeys;
-    p.few_tiles = most <= kTileRows ? 1 : few_tiles_of(D, bf16, ragged, whole);
+    p.few_tiles = most <= kTileRows ? 1 : few_tiles_of(D);
     p.few = ragged || most <= p.few_tiles * kTileRows;
     p.many = most > p.few_tiles * kTileRows;
     p.many_rows = D > 128 || tokens * r <= 64 * B ? 64 : bf16 ? 256 : 128;
