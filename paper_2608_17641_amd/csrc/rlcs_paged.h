@@ -665,16 +665,22 @@ __device__ __forceinline__ void paged_few_tile(const PagedArgs& a, const PagedIt
     }
 }
 
+// The sequence and key head of a workgroup. False: there is none, as the grid of more than 2^20 workgroups is a multiple of that many.
+__host__ __device__ __forceinline__ bool whole_tile(int64_t block, int B, int Hkv, int& b, int& hk) {
+    b = int(block / Hkv);
+    hk = int(block % Hkv);
+    return b < B;
+}
+
 // Whole tiles. 64 sequences of 1024 keys as below: 42 us (6.3 TB/s); 8 of 300 float32 keys, one head of 64 dimensions: 9.3 us, all of it
 // latency (lengths, page numbers, five blocks of keys a wave one after the other).
 template <typename DT, int ND, int QT, bool EXACT>
 __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs a) {
     __shared__ __attribute__((aligned(16))) char s_mem[attn_lds<DT, ND, kAttnWaves>()];
     __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
-    const int block = int(grid_row());
+    int b;
     PagedItem it;
-    it.hk = block % a.Hkv;
-    if (it.only<QT * kTileRows>(a, block / a.Hkv) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length))
+    if (whole_tile(grid_row(), a.B, a.Hkv, b, it.hk) && it.only<QT * kTileRows>(a, b) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length))
         paged_few_tile<DT, ND, QT, EXACT>(a, it, s_mem, s_m, s_l);
 }
 
