@@ -1236,7 +1236,7 @@ def rlcs_distill_loss(logits, top_ids, top_logp, weight=None, loss=None, dlogits
     and its gradient by the logits. top_ids int32 and top_logp float32 [..., K] (an id outside [0, V) is none), weight
     float32 of the leading shape; a row of weight 0 is left out. With tail false the listed shares are made to add up to 1 (any
     logits will do for top_logp); with tail true top_logp are log-probabilities, and what they leave of 1 is the mass of one
-    more class, everything that is not listed. `dlogits` may be `logits`.
+    more class, everything that is not listed (left out where either has nothing of it). `dlogits` may be `logits`.
 
     Nothing here is recorded by autograd, as in rlcs_policy_loss: ``logits.backward(dlogits)`` carries the gradient on."""
     done = (_fast or _load_fast()).distill_loss(logits, top_ids, top_logp, weight, loss, dlogits, temperature, tail, want_grad)

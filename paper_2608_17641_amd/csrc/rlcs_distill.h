@@ -1,8 +1,9 @@
 // Distillation from a teacher's largest logits: the loss of each row and its gradient by the logits.
 //
 // With u = (x - max x) * log2(e) / temperature and z = sum 2^u, log p_j = ln 2 (u_j - log2 z). The gradient is
-// p_j - t_j at the K listed tokens and p_j times one factor a row everywhere else: a row is written as if nothing
-// were listed, then the listed places again. What lies outside the list is summed apart, by a bit for each logit in LDS
+// S p_j - t_j at the K listed tokens, S the sum of all shares that count, and p_j times one factor a row everywhere else: a
+// row is written as if nothing were listed, then the listed places again. S is 1 but where the class of the rest is left out: then what the
+// list has, whatever it adds up to. What lies outside the list is summed apart, by a bit for each logit in LDS
 // (as the difference of two sums it would be lost where the list has almost all of the mass).
 #pragma once
 
@@ -139,6 +140,7 @@ __device__ __forceinline__ RowStats row_tops(const DistillArgs& a, const Distill
 struct DistillRow {
     Scale sc;
     float inv, factor, amount, share;  // share: what the weights of the list are multiplied by
+    float mass;                        // of all shares that count
     // f times the probability of logit x. (The weight times the sum's inverse and not by the logarithm of the sum: the
     // rounding of the scale is in both, and cancels.)
     __device__ __forceinline__ float times(float f, float x) const { return exp2_fast(sc.log2_weight(x)) * f; }
@@ -152,6 +154,7 @@ __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const Disti
     r.sc = st.sc;
     r.amount = w * a.inv_temp;
     r.factor = r.amount;
+    r.mass = 1.f;
     float rest = 0.f, log_sum = 0.f, loss = 0.f, z;
     if constexpr (TAIL) {
         // (in 64 bits: what is left of 1 may be small. Over the waves as two floats, the sum's high part and what it leaves out)
@@ -180,6 +183,7 @@ __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const Disti
         z_out = v[0];
         z = v[0] + v[1];
         rest = left < 0. ? 0.f : float(left);
+        r.mass = float(1. - left);
         r.share = 1.f;
     } else {
         float sum = 0.f;
@@ -208,7 +212,10 @@ __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const Disti
         const float p_out = z_out / z;
         if (!(rest == 0.f) && !(z_out == 0.f)) {
             if (team.lane == 0) loss = fmaf(rest, kLn2 * (log2_fast(rest) - log2_fast(p_out)), loss);
+            r.mass = 1.f;
             r.factor = r.amount * (1.f - rest / p_out);
+        } else {
+            r.factor = r.amount * r.mass;
         }
     }
     float v[1] = {loss};
@@ -235,7 +242,7 @@ __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Dist
             }
             if (!first) continue;
         }
-        g[id] = narrow(r.amount * (r.times(r.inv, l.x[k]) - t * r.share), DT{});
+        g[id] = narrow(r.amount * (r.times(r.inv * r.mass, l.x[k]) - t * r.share), DT{});
     }
 }
 

@@ -1,0 +1,225 @@
+"""rlcs_distill_loss with the rest as a class, where that class has nothing or next to nothing: everything outside the list masked or
+far below it, shares that add up to more than 1. The 64-bit form works with logarithms, and its gradient is held against
+autograd's and against differences."""
+import math
+
+import pytest
+import torch
+
+import paper_2608_17641_amd as rl
+
+EPS = 2.0 ** -24
+FAR = 110.0  # nats: what is farther below the largest of its sum adds nothing to it
+
+
+def loss_of(x, ids, lp, T):
+    """The loss of float64 rows x [M, V], by the definition, for autograd."""
+    M, V = x.shape
+    out = []
+    for m in range(M):
+        y = x[m] / T
+        here = (ids[m] >= 0) & (ids[m] < V)
+        outside = torch.ones(V, dtype=torch.bool)
+        outside[ids[m][here].long()] = False
+        outside &= y.detach() > -math.inf
+        ok = here & (lp[m] > -math.inf)
+        lt = lp[m][ok].double()
+        t = torch.exp(lt)
+        z = torch.logsumexp(y[y.detach() > -math.inf], 0) if bool((y.detach() > -math.inf).any()) else torch.tensor(0.0, dtype=torch.float64)
+        total = (t * (lt - (y[ids[m][ok].long()] - z))).sum()
+        rest = 1.0 - float(t.sum())
+        if rest > 0 and bool(outside.any()):
+            total = total + rest * (math.log(rest) - (torch.logsumexp(y[outside], 0) - z))
+        out.append(total)
+    return torch.stack(out)
+
+
+def form(x, ids, lp, w, T):
+    """(loss, gradient, sizes of the loss's and of the gradient's parts) by the formulas."""
+    M, V = x.shape
+    loss, size = torch.zeros(M, dtype=torch.float64), torch.zeros(M, dtype=torch.float64)
+    grad, parts = torch.zeros((M, V), dtype=torch.float64), torch.zeros((M, V), dtype=torch.float64)
+    for m in range(M):
+        y = x[m].double() / T
+        here = (ids[m] >= 0) & (ids[m] < V)
+        outside = torch.ones(V, dtype=torch.bool)
+        outside[ids[m][here].long()] = False
+        outside &= y > -math.inf
+        ok = here & (lp[m] > -math.inf)
+        lt, at = lp[m][ok].double(), ids[m][ok].long()
+        t = torch.exp(lt)
+        top = float(y.max())  # (taken off first: beside 10^38 a sum's logarithm is lost)
+        z = float(torch.logsumexp(y - top, 0)) if top > -math.inf else 0.0
+        ls = (y - top) - z if top > -math.inf else y
+        p = torch.exp(ls)
+        share = torch.zeros(V, dtype=torch.float64).index_add(0, at, t)
+        rest, mass = max(0.0, 1.0 - float(t.sum())), float(t.sum())
+        loss[m] = (t * (lt - ls[at])).sum()
+        size[m] = (t * (lt.abs() + ls[at].abs() + FAR)).sum()
+        spread = torch.zeros(V, dtype=torch.float64)
+        if rest > 0 and bool(outside.any()):
+            most = float(y[outside].max())
+            zo = float(torch.logsumexp(y[outside] - most, 0))
+            lo = (most - top) + (zo - z)
+            loss[m] += rest * (math.log(rest) - lo)
+            size[m] += rest * (abs(math.log(rest)) + abs(lo) + FAR)
+            spread[outside] = rest * torch.exp((y[outside] - most) - zo)
+            mass = 1.0
+        grad[m] = mass * p - share - spread
+        parts[m] = mass * p + share + spread
+    w = w.double()
+    return w * loss, w[:, None] / T * grad, w * size, w[:, None] / T * parts
+
+
+def check(x, ids, lp, w, T, got):
+    """Logarithms err by some roundings of themselves and by those of the sums they come from (V / 64 + 64 of them); an exponential by
+    its argument's, 8 FAR at most where it counts. What is 2^-66 of its sum may be left out."""
+    loss, grad = got[0].double().cpu(), got[1].double().cpu()
+    want, want_g, size, parts = form(x, ids, lp, w, T)
+    e = EPS * (8 * FAR + x.shape[1] / 64 + 64)
+    both = torch.isfinite(want)
+    assert torch.equal(both, torch.isfinite(loss)), (want, loss)
+    off = ((loss - want).abs() - e * (size + w.double()))[both]
+    assert bool((off <= 1e-30).all()), (loss, want)
+    allowed = parts * e * 8 + w.double()[:, None] / T * 2.0 ** -66
+    if x.dtype == torch.bfloat16:
+        allowed = allowed + 2.0 ** -8 * want_g.abs() + 1e-38
+    off = (grad - want_g).abs() - allowed
+    assert bool((off <= 0).all()), [(i, float(off[i].max()), int(off[i].argmax())) for i in range(x.shape[0])]
+
+
+def inputs(V, K, dtype, seed):
+    """Rows of every kind; the first K logits are not the list's, which is drawn."""
+    g = torch.Generator().manual_seed(seed)
+    M = 14
+    x = torch.randn((M, V), generator=g)
+    ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(M)]).to(torch.int32)
+    lp = torch.log_softmax(torch.randn((M, K + 3), generator=g), -1)[:, :K].contiguous()  # (three more tokens have the rest)
+    listed = torch.zeros((M, V), dtype=torch.bool).scatter_(1, ids.long(), True)
+    x[0][~listed[0]] = -math.inf                       # the class has nothing
+    lp[1] += 1.2                                       # shares above 1
+    ids[2, 1], lp[2] = ids[2, 0], lp[2] + 0.9          # twice, and above 1
+    for row, gap in zip(range(3, 10), (38.0, 45.0, 87.5, 95.0, 200.0, 700.0, 2000.0)):
+        x[row][~listed[row]] -= gap                    # the class is far below
+    far = (~listed[10]).nonzero()[:, 0]
+    x[10][far] -= 300.0                                # one of it is not so far
+    x[10, far[len(far) // 2]] += 200.0
+    x[11][~listed[11]] = torch.finfo(dtype).min        # a finite mask is a logit like any other
+    x[12] *= 3.0
+    x[13][~listed[13]] -= 120.0                        # far below, and masked in part
+    x[13][(~listed[13]).nonzero()[1::2, 0]] = -math.inf
+    w = torch.rand(M, generator=g) + 0.2
+    return x.to(dtype), ids, lp, w
+
+
+def test_form():
+    """The form's gradient is autograd's, and the differences', of the definition."""
+    x, ids, lp, w = inputs(23, 5, torch.float32, 1)
+    rows = [r for r in range(x.shape[0]) if r != 11]  # (differences of 10^38 are no numbers)
+    x, ids, lp, w = (t[rows] for t in (x, ids, lp, w))
+    for T in (1.0, 0.5):
+        loss, grad, _, _ = form(x, ids, lp, w, T)
+        z = x.double().requires_grad_()
+        value = w.double() * loss_of(z, ids, lp, T)
+        assert torch.allclose(value.detach(), loss, rtol=1e-12)
+        value.sum().backward()
+        assert torch.allclose(z.grad, grad, rtol=1e-9, atol=1e-12)
+        h = 2.0 ** -10
+        for j in range(x.shape[1]):
+            up, down = x.double().clone(), x.double().clone()
+            up[:, j] += h
+            down[:, j] -= h
+            slope = w.double() * (loss_of(up, ids, lp, T) - loss_of(down, ids, lp, T)) / (2 * h)
+            # third derivatives are below 1 / T^3 for each unit of mass, of which there are less than 4
+            assert float((slope - grad[:, j]).abs().max()) <= 4 * h * h / T ** 3 + 1e-9
+        assert float(grad.sum(1).abs().max()) < 1e-12  # (a softmax does not see what all logits have in common)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [23, 90, 700, 3000, 9001, 40000, 300001])
+@pytest.mark.parametrize("kind", ["nothing outside", "above 1"])
+def test_class_of_the_rest(kind, V, dtype):
+    x, ids, lp, w = inputs(V, 8, dtype, V)
+    rows = {"nothing outside": [0, 12], "above 1": [1, 2, 12]}[kind]
+    x, ids, lp, w = (t[rows] for t in (x, ids, lp, w))
+    dev = [t.cuda() for t in (x, ids, lp, w)]
+    for T in (1.0, 0.1, 3.0):
+        # (a finite mask over less than 1 is past float32, as the loss then is)
+        keep = [i for i, r in enumerate(rows) if r != 11 or T >= 1.0]
+        got = rl.rlcs_distill_loss(*dev, temperature=T, tail=True)
+        check(x[keep], ids[keep], lp[keep], w[keep], float(torch.tensor(T)), [t.cpu()[keep] for t in got])
+        assert torch.equal(rl.rlcs_distill_loss(*dev, temperature=T, tail=True, want_grad=False)[0], got[0])
+        own = dev[0].clone()
+        again = rl.rlcs_distill_loss(own, *dev[1:], dlogits=own, temperature=T, tail=True)
+        assert torch.equal(own, got[1]) and torch.equal(again[0], got[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["nothing outside", "above 1"])
+def test_differences(kind):
+    """The gradient by central differences of the kernel's own loss: a step of 2^-6, whose third-order term is at most 4 step^2 (as in
+    test_form), and roundings of losses and of their parts, up to 2^8 each, over the step."""
+    x, ids, lp, w = inputs(50, 6, torch.float32, 8)
+    rows = {"nothing outside": [0], "above 1": [1, 2]}[kind]
+    x, ids, lp, w = (t[rows] for t in (x, ids, lp, w))
+    M, V = x.shape
+    _, g = rl.rlcs_distill_loss(x.cuda(), ids.cuda(), lp.cuda(), w.cuda(), tail=True)
+    h = 2.0 ** -6
+    rep = lambda t: t[:, None].expand(M, V, *t.shape[1:]).contiguous().cuda()  # noqa: E731
+    f = [rl.rlcs_distill_loss((x[:, None, :] + s * h * torch.eye(V)).cuda(), rep(ids), rep(lp), rep(w), tail=True, want_grad=False)[0].double().cpu() for s in (1, -1)]
+    slope = (f[0] - f[1]) / (2 * h)
+    bound = 4 * h * h + 2 * EPS * (2.0 ** 8 + 64) / h
+    assert float((slope - g.double().cpu()).abs().max()) <= bound
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 6, 90])
+def test_all_listed(V, dtype):
+    """No token outside the list: the class has nothing, whatever the shares leave for it."""
+    g = torch.Generator().manual_seed(V)
+    M = 5
+    x = torch.randn((M, V), generator=g).to(dtype)
+    ids = torch.stack([torch.randperm(V, generator=g) for _ in range(M)]).to(torch.int32)
+    lp = torch.log_softmax(torch.randn((M, V), generator=g), -1) + torch.tensor([-0.7, 0.0, 0.7, -3.0, -0.1])[:, None]
+    w = torch.rand(M, generator=g) + 0.2
+    got = rl.rlcs_distill_loss(x.cuda(), ids.cuda(), lp.cuda(), w.cuda(), tail=True)
+    check(x, ids, lp, w, 1.0, got)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [90, 3000, 40000])
+def test_masked_and_odd_logits(V, dtype):
+    M, K = 9, 8
+    g = torch.Generator().manual_seed(5)
+    x = (torch.randn((M, V), generator=g) * 2).to(dtype)
+    ids = torch.topk(x.float(), K).indices.to(torch.int32)
+    lp = torch.log_softmax(torch.randn((M, K + 3), generator=g), -1)[:, :K].contiguous()
+    w = torch.ones(M)
+    out = [j for j in range(V) if j not in ids[1].tolist()]
+    x[0, ids[0, 2].item()] = -math.inf  # a listed token is masked: an infinite loss
+    x[1, out] = -math.inf               # everything that is not listed is masked
+    x[2] = -math.inf
+    x[3, ::3] = torch.finfo(dtype).min
+    x[4] = torch.finfo(dtype).min
+    dev = [t.cuda() for t in (x, ids, lp)]
+    got = [t.cpu() for t in rl.rlcs_distill_loss(*dev, tail=True)]
+    check(x, ids, lp, w, 1.0, got)
+    assert math.isinf(float(got[0][0])) and math.isinf(float(got[0][2]))
+    for bad in (math.nan, math.inf):
+        for at in (V // 2, ids[5, 3].item()):
+            y = x.clone()
+            y[5, at] = bad
+            l2, g2 = rl.rlcs_distill_loss(y.cuda(), *dev[1:], tail=True)
+            assert math.isnan(float(l2[5])) and bool(torch.isnan(g2[5]).all())
+            assert torch.equal(l2[6:].cpu(), got[0][6:]) and torch.equal(g2[6:].cpu(), got[1][6:])
+    lp2 = lp.clone()
+    lp2[7, 1] = math.nan
+    l2, g2 = rl.rlcs_distill_loss(dev[0], dev[1], lp2.cuda(), tail=True)
+    assert math.isnan(float(l2[7])) and bool(torch.isnan(g2[7, ids[7, 1].item()])) and torch.equal(l2[8].cpu(), got[0][8])
+    w2, y = w.clone(), x.clone()
+    w2[6], w2[8], y[8] = math.nan, 0.0, math.nan
+    l2, g2 = rl.rlcs_distill_loss(y.cuda(), *dev[1:], w2.cuda(), tail=True)
+    assert math.isnan(float(l2[6])) and float(l2[8]) == 0.0 and not bool(g2[8].any())
