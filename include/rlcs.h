@@ -577,6 +577,7 @@ size_t rlcs_workspace_size_verify(int64_t B, int64_t K, int64_t V);
  *   tail = 1:  t_k = e^{top_logp_k}, and what they leave, t' = max(0, 1 - sum_k t_k), is the mass of one more
  *            class, of all tokens that are not listed, p' in the student's: loss += weight * t' (log t' - log p'), and there
  *            dlogits_j = weight / temperature * p_j (1 - t' / p'). Left out where p' or t' is 0: S is then sum_k t_k.
+ *            (p' is 0 where no token outside the list is unmasked, and not where p' is too small for a float32)
  *   logits   [M, V] dtype, row m at m * ld; -inf masks an entry (p = 0)
  *   top_ids  [M, K] int32; one outside [0, V) is not listed (t = 0). One listed twice has both shares
  *   top_logp [M, K] float32, at the temperature of the loss; -inf: t = 0

@@ -3,8 +3,9 @@
 // With u = (x - max x) * log2(e) / temperature and z = sum 2^u, log p_j = ln 2 (u_j - log2 z). The gradient is
 // S p_j - t_j at the K listed tokens, S the sum of all shares that count, and p_j times one factor a row everywhere else: a
 // row is written as if nothing were listed, then the listed places again. S is 1 but where the class of the rest is left out: then what the
-// list has, whatever it adds up to. What lies outside the list is summed apart, by a bit for each logit in LDS
-// (as the difference of two sums it would be lost where the list has almost all of the mass).
+// list has, whatever it adds up to. What lies outside the list is summed apart, by a bit for each logit in LDS (as the difference of two
+// sums it would be lost where the list has almost all of the mass). Where it lies so far below the row's largest logit that its weights
+// underflow, it is summed again relative to its own: p' is a number however small, and the gradient there is each logit's share of it.
 #pragma once
 
 #include "rlcs_softmax.h"
@@ -44,7 +45,7 @@ inline size_t distill_lds(const DistillArgs& a) { return (size_t(a.words) * 4 + 
 // wait; `slots`: kFolds floats a wave, every fold of a row with its own (from `at` on), so that none waits for the one before.
 template <int W>
 struct Team {
-    static constexpr int kLanes = W * kWave, kFolds = 9;
+    static constexpr int kLanes = W * kWave, kFolds = 11;
     float* slots;
     int lane;
     __device__ __forceinline__ void sync() const {
@@ -141,20 +142,65 @@ struct DistillRow {
     Scale sc;
     float inv, factor, amount, share;  // share: what the weights of the list are multiplied by
     float mass;                        // of all shares that count
+    // Of a class summed apart: what its weights, relative to its largest, are multiplied by; 0: it was not.
+    float apart;
+    Scale sc_out;
     // f times the probability of logit x. (The weight times the sum's inverse and not by the logarithm of the sum: the
     // rounding of the scale is in both, and cancels.)
     __device__ __forceinline__ float times(float f, float x) const { return exp2_fast(sc.log2_weight(x)) * f; }
 };
 
-// From each lane's sums of the weights outside the list and in it: the row's, and its loss.
-template <bool TAIL, int W>
+// The largest logit outside the list and the sum of the weights relative to it; each(f): f(vector, its bits) for all of a lane's vectors.
+// (Bits of a list, a word's low ones for a vector; past the row's end -inf.)
+struct RowRest {
+    float top, sum;
+    Scale sc;
+};
+template <int W, class F>
+__device__ __forceinline__ RowRest row_rest(const Team<W>& team, float c, F&& each) {
+    float top = kNegInf;
+    double sum = 0.;
+    Scale sc = scale_of(top, c);
+    auto rebase = [&](float t) {
+        const Scale to = scale_of(t, c);
+        sum *= top == kNegInf ? 0. : double(exp2_fast(scale_step(sc, to)));
+        top = t;
+        sc = to;
+    };
+    each([&](const auto& v, uint32_t bits) {
+        constexpr int K = std::decay<decltype(v)>::type::K;
+        float t = top;
+#pragma unroll
+        for (int k = 0; k < K; ++k) t = bits >> k & 1 ? t : fmaxf(t, v.at(k));
+        if (t > top) rebase(t);
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) z += bits >> k & 1 ? 0.f : exp2_fast(sc.log2_weight(v.at(k)));
+        sum += z;
+    });
+    float v[1] = {top};
+    team.largest(v, 9);
+    if (top > kNegInf && v[0] > top) rebase(v[0]);
+    float z[1] = {float(sum)};
+    team.sums(z, 10);
+    return RowRest{v[0], z[0], scale_of(v[0], c)};
+}
+
+// Sums of weights outside the list below this are taken again by row_rest(): of larger ones, what underflowed is less than 2^-36. (Rows
+// where it is so are read once more for the sum and once for the gradient: 4096 of 32000 bfloat16 logits 178 us, else 97; 2048 of
+// 128000 343 and 222.)
+constexpr float kLeastRest = 0x1p-60f;
+
+// From each lane's sums of the weights outside the list and in it: the row's, and its loss. each: as row_rest() takes it.
+template <bool TAIL, int W, class F>
 __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const DistillLds& l, const Team<W>& team, const RowStats& st, float z_out,
-                                               float z_in, float w, int64_t row) {
+                                               float z_in, float w, int64_t row, F&& each) {
     DistillRow r;
     r.sc = st.sc;
     r.amount = w * a.inv_temp;
     r.factor = r.amount;
     r.mass = 1.f;
+    r.apart = 0.f;
     float rest = 0.f, log_sum = 0.f, loss = 0.f, z;
     if constexpr (TAIL) {
         // (in 64 bits: what is left of 1 may be small. Over the waves as two floats, the sum's high part and what it leaves out)
@@ -209,11 +255,26 @@ __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const Disti
         if (!(t == 0.f)) loss = fmaf(t, (l.lt[k] - top_listed) - log_sum - lp, loss);
     }
     if constexpr (TAIL) {
-        const float p_out = z_out / z;
-        if (!(rest == 0.f) && !(z_out == 0.f)) {
-            if (team.lane == 0) loss = fmaf(rest, kLn2 * (log2_fast(rest) - log2_fast(p_out)), loss);
+        bool some = !(rest == 0.f);
+        float log_ratio = 0.f, ratio = 0.f;  // of the class's share to its probability
+        if (some && z_out < kLeastRest) {
+            const RowRest o = row_rest(team, kLog2e * a.inv_temp, each);
+            some = unmasked && !(o.top == kNegInf);
+            if (some) {
+                const float log_p = fmaf(o.top - st.top, a.inv_temp, kLn2 * (log2_fast(o.sum) - fmaf(o.top, o.sc.c, -o.sc.m)) - log_z);
+                log_ratio = kLn2 * log2_fast(rest) - log_p;
+                r.apart = r.amount * (rest / o.sum);
+                r.sc_out = o.sc;
+            }
+        } else {
+            const float p_out = z_out / z;
+            log_ratio = kLn2 * (log2_fast(rest) - log2_fast(p_out));
+            ratio = rest / p_out;
+        }
+        if (some) {
+            if (team.lane == 0) loss = fmaf(rest, log_ratio, loss);
             r.mass = 1.f;
-            r.factor = r.amount * (1.f - rest / p_out);
+            r.factor = r.amount * (1.f - ratio);
         } else {
             r.factor = r.amount * r.mass;
         }
@@ -222,6 +283,23 @@ __device__ __forceinline__ DistillRow row_loss(const DistillArgs& a, const Disti
     team.sums(v, 8);
     if (team.lane == 0) a.loss[row] = w * v[0];
     return r;
+}
+
+// The gradient of a row whose class was summed apart, as if nothing were listed. (It reads the row again: beside vectors in registers
+// it would take half as many more of these, and rows like this are rare.)
+template <typename DT, int L>
+__device__ __forceinline__ void gradient_apart(const DT* x, DT* g, int64_t V, int lane, const DistillRow& r, float factor) {
+    constexpr int K = RowVec<DT>::K;
+    const int64_t vecs = (V + K - 1) / K;
+#pragma unroll 1
+    for (int64_t i = lane; i < vecs; i += L) {
+        RowVec<DT> v;
+        v.load(x, i, V);
+        float d[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) d[k] = r.times(factor, v.at(k)) - r.apart * exp2_fast(r.sc_out.log2_weight(v.at(k)));
+        store_row_vec<DT>(g, i, V, d);
+    }
 }
 
 // The listed places of the gradient, once everything else of the row is written.
@@ -283,8 +361,10 @@ __device__ __forceinline__ void add_weights(const V& v, const Scale& sc, uint32_
 // Rows of up to U vectors a lane of W waves, which stay in registers. Every logit is read and every gradient
 // written once. Bound by memory: 4096 rows of 32000 bfloat16 logits (8 waves of 8 vectors) 88 us for 438 MB, 5.0 TB/s; by 4 waves of
 // 16 vectors 91, by 16 of 4 128 us.
+// (Waves a SIMD as without row_rest(), beside which the compiler would hold a few registers more than these allow.)
 template <typename DT, bool TAIL, int W, int U>
-__global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(DistillArgs a, int row_lds) {
+__global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) __attribute__((amdgpu_waves_per_eu(!TAIL ? 1 : U == 8 ? 4 : sizeof(DT) == 2 ? 6 : 8)))
+void distill_vec_kernel(DistillArgs a, int row_lds) {
     extern __shared__ __attribute__((aligned(16))) char s_mem[];
     __shared__ float s_slots[Team<W>::kFolds * W];
     constexpr int K = RowVec<DT>::K, kLanes = W * kWave;
@@ -322,16 +402,27 @@ __global__ __launch_bounds__((W == 1 ? 4 : W) * kWave) void distill_vec_kernel(D
         const uint32_t bits = TAIL && i * K < a.V ? vector_bits<K>(l.bits, i) : 0u;
         add_weights<TAIL>(v[u], st.sc, bits, z_out, z_in);
     }
-    const DistillRow r = row_loss<TAIL, W>(a, l, team, st, z_out, z_in, w, row);
+    const DistillRow r = row_loss<TAIL, W>(a, l, team, st, z_out, z_in, w, row, [&](auto&& f) {
+#pragma unroll 1
+        for (int64_t i = team.lane; i * K < a.V; i += kLanes) {
+            RowVec<DT> one;
+            one.load(x, i, a.V);
+            f(one, vector_bits<K>(l.bits, i));
+        }
+    });
     if (!g) return;
     const float factor = r.factor * r.inv;
+    if (TAIL && r.apart != 0.f) {
+        gradient_apart<DT, kLanes>(x, g, a.V, team.lane, r, factor);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t i = team.lane + u * kLanes;
-        float d[K];
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = team.lane + u * kLanes;
+            float d[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) d[k] = r.times(factor, v[u].at(k));
-        if (i * K < a.V) store_row_vec<DT>(g, i, a.V, d);
+            for (int k = 0; k < K; ++k) d[k] = r.times(factor, v[u].at(k));
+            if (i * K < a.V) store_row_vec<DT>(g, i, a.V, d);
+        }
     }
     listed_gradient<DT, W>(a, l, team, st.twice, r, g);
 }
@@ -377,19 +468,21 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
     };
     const int64_t span = TAIL ? kBits / K : vecs;  // vectors whose bits are there
     RowVec<DT> v[U];
+    auto part_bits = [&](int64_t from, int64_t end) {  // the bits of this part of a longer row
+        if (!TAIL || a.V <= kBits) return;
+        __syncthreads();
+        for (int i = tid; i < a.words; i += kLanes) l.bits[i] = 0;
+        __syncthreads();
+        bool unused = false;
+        for (int k = tid; k < a.K; k += kLanes) {
+            const int64_t id = l.id[k];
+            if (id >= from * K && id < end * K) mark(l.bits, id, unused);
+        }
+        __syncthreads();
+    };
     for (int64_t from = 0; from < vecs; from += span) {
         const int64_t end = from + span < vecs ? from + span : vecs;
-        if (TAIL && a.V > kBits) {  // the bits of this part of the row
-            __syncthreads();
-            for (int i = tid; i < a.words; i += kLanes) l.bits[i] = 0;
-            __syncthreads();
-            bool unused = false;
-            for (int k = tid; k < a.K; k += kLanes) {
-                const int64_t id = l.id[k];
-                if (id >= from * K && id < end * K) mark(l.bits, id, unused);
-            }
-            __syncthreads();
-        }
+        part_bits(from, end);
         for (int64_t i0 = from + tid; i0 < end; i0 += U * kLanes) {
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u].load(x, i0 + u * kLanes, i0 + u * kLanes < end ? a.V : 0);  // (past the end: -inf)
@@ -417,9 +510,25 @@ __global__ __launch_bounds__(W * kWave) void distill_rows_kernel(DistillArgs a) 
         return;
     }
     if (top > kNegInf && st.top > top) rebase(st.top);
-    const DistillRow r = row_loss<TAIL, W>(a, l, team, st, float(out), float(in), w, row);
+    const DistillRow r = row_loss<TAIL, W>(a, l, team, st, float(out), float(in), w, row, [&](auto&& f) {
+        for (int64_t from = 0; from < vecs; from += span) {
+            const int64_t end = from + span < vecs ? from + span : vecs;
+            part_bits(from, end);
+#pragma unroll 1
+            for (int64_t i = from + tid; i < end; i += kLanes) {
+                RowVec<DT> one;
+                one.load(x, i, a.V);
+                f(one, vector_bits<K>(l.bits, i - from));
+            }
+        }
+    });
     if (!g) return;
     const float factor = r.factor * r.inv;
+    if (TAIL && r.apart != 0.f) {
+        gradient_apart<DT, kLanes>(x, g, a.V, tid, r, factor);
+        listed_gradient<DT, W>(a, l, team, st.twice, r, g);
+        return;
+    }
     // backwards: what the first pass read last is nearest in the caches
     const int64_t last = (vecs - 1) / (U * kLanes) * (U * kLanes) + tid;
     for (int64_t i0 = last; i0 >= 0; i0 -= U * kLanes) {

@@ -138,10 +138,10 @@ def test_form():
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("V", [23, 90, 700, 3000, 9001, 40000, 300001])
-@pytest.mark.parametrize("kind", ["nothing outside", "above 1"])
+@pytest.mark.parametrize("kind", ["nothing outside", "above 1", "far below"])
 def test_class_of_the_rest(kind, V, dtype):
     x, ids, lp, w = inputs(V, 8, dtype, V)
-    rows = {"nothing outside": [0, 12], "above 1": [1, 2, 12]}[kind]
+    rows = {"nothing outside": [0, 12], "above 1": [1, 2, 12], "far below": [3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13]}[kind]
     x, ids, lp, w = (t[rows] for t in (x, ids, lp, w))
     dev = [t.cuda() for t in (x, ids, lp, w)]
     for T in (1.0, 0.1, 3.0):
@@ -156,12 +156,12 @@ def test_class_of_the_rest(kind, V, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("kind", ["nothing outside", "above 1"])
+@pytest.mark.parametrize("kind", ["nothing outside", "above 1", "far below"])
 def test_differences(kind):
     """The gradient by central differences of the kernel's own loss: a step of 2^-6, whose third-order term is at most 4 step^2 (as in
     test_form), and roundings of losses and of their parts, up to 2^8 each, over the step."""
     x, ids, lp, w = inputs(50, 6, torch.float32, 8)
-    rows = {"nothing outside": [0], "above 1": [1, 2]}[kind]
+    rows = {"nothing outside": [0], "above 1": [1, 2], "far below": [4, 5, 6, 7, 10, 13]}[kind]
     x, ids, lp, w = (t[rows] for t in (x, ids, lp, w))
     M, V = x.shape
     _, g = rl.rlcs_distill_loss(x.cuda(), ids.cuda(), lp.cuda(), w.cuda(), tail=True)
