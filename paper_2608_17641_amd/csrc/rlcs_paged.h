@@ -666,10 +666,14 @@ __device__ __forceinline__ void paged_few_tile(const PagedArgs& a, const PagedIt
 }
 
 // The sequence and key head of a workgroup. False: there is none, as the grid of more than 2^20 workgroups is a multiple of that many.
-__host__ __device__ __forceinline__ bool whole_tile(int64_t block, int B, int Hkv, int& b, int& hk) {
-    b = int(block / Hkv);
-    hk = int(block % Hkv);
-    return b < B;
+// (The pairs are below 2^31, and so are the grid's workgroups: one division in 32 bits. Past the last sequence b is the last: what is read of
+// it does not wait for the comparison.)
+__host__ __device__ __forceinline__ bool whole_tile(int block, int B, int Hkv, int& b, int& hk) {
+    b = block / Hkv;
+    hk = block - b * Hkv;
+    const bool is = b < B;
+    b = is ? b : B - 1;
+    return is;
 }
 
 // Whole tiles. 64 sequences of 1024 keys as below: 42 us (6.3 TB/s); 8 of 300 float32 keys, one head of 64 dimensions: 9.3 us, all of it
@@ -680,7 +684,8 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void paged_few_kernel(PagedArgs
     __shared__ float s_m[kAttnWaves][kTileRows], s_l[kAttnWaves][kTileRows];
     int b;
     PagedItem it;
-    if (whole_tile(grid_row(), a.B, a.Hkv, b, it.hk) && it.only<QT * kTileRows>(a, b) && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length))
+    const bool is = whole_tile(int(grid_row()), a.B, a.Hkv, b, it.hk);
+    if (it.only<QT * kTileRows>(a, b) && is && it.take<PagedLine<true, QT * kTileRows>>(a, 0, it.length))
         paged_few_tile<DT, ND, QT, EXACT>(a, it, s_mem, s_m, s_l);
 }
 
